@@ -42,7 +42,12 @@ typedef enum {
 } dlf_status;
 
 typedef enum { DLF_CONV = 0, DLF_DWCONV = 1, DLF_FC = 2, DLF_MAXPOOL = 3, DLF_GLOBAL_AVGPOOL = 4 } dlf_op;
-typedef enum { DLF_ACT_NONE = 0, DLF_ACT_RELU = 1, DLF_ACT_RELU6 = 2 } dlf_act;
+/* Network layers take the first three; all are activations of the feed-forward operators below. */
+typedef enum { DLF_ACT_NONE = 0, DLF_ACT_RELU = 1, DLF_ACT_RELU6 = 2,
+               DLF_ACT_GELU = 3,       /* z * (1 + erf(z / sqrt(2))) / 2                                    */
+               DLF_ACT_GELU_TANH = 4,  /* z * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) / 2             */
+               DLF_ACT_SILU = 5,       /* z / (1 + exp(-z))                                                 */
+               DLF_ACT_SIGMOID = 6     /* 1 / (1 + exp(-z))                                                 */ } dlf_act;
 
 /* One layer.  Convolution is cross-correlation with zero padding; the operation count of a
  * layer is Eq. 1 (convolution: 2*Hout*Wout*Hk*Wk*Cin*Cout) or Eq. 2 (FC: 2*M*K*N, M = batch). */
@@ -273,6 +278,64 @@ dlf_status dlf_i8conv_info(const dlf_i8conv_t* layer, int32_t* th, int32_t* tw, 
                            uint64_t* op_count);
 /* One launch on hip_stream; asynchronous, allocates nothing.  DLF_ERR_NO_WEIGHTS on a shape-only layer. */
 dlf_status dlf_i8conv_run(const dlf_i8conv_t* layer, const void* in_dev, void* out_dev, void* hip_stream);
+
+/* ---- Feed-forward operators ------------------------------------------------------------------
+ * The feed-forward half of a transformer block as fused layers: a matrix product with bias, activation and
+ * residual in its epilogue, and a gated pair of projections -- both products, the activation and the product of the
+ * two in one kernel --, with their gradients.  Unlike a network layer's, the weights are the caller's DEVICE tensors,
+ * read where they lie (a program may change them between calls), and the number of rows is free from call to call.
+ *
+ *   dlf_linear   z[m][o] = sum over i of x[m][i] * weight[o][i] + bias[o]        y = act(z) + residual
+ *                dz = dy * act'(z);  dx = dz weight;  dweight = dz^T x;  dbias[o] = sum over m of dz[m][o]
+ *                (the gradient of the residual is dy itself)
+ *   dlf_gated    g = x w_gate^T + b_gate,  u = x w_up^T + b_up                   h = act(g) * u
+ *                dg = dh * u * act'(g),  du = dh * act(g);  dx = dg w_gate + du w_up;
+ *                dw_gate = dg^T x;  dw_up = du^T x;  db_gate, db_up: column sums of dg, du
+ *
+ * (The activation comes before the residual, as in a transformer block; a network layer applies its own after it.)
+ * Products and sums are accumulated in 32 bits and rounded once, to the tensors' type; in the backward pass dz (dg,
+ * du) is rounded to that type on its way into the products, the bias gradients are summed before that.  An activation
+ * with a step has the derivative 0 on it.  Results do not depend on timing: equal calls give equal bits.
+ *
+ * Tensors are DEVICE and row-major: x [rows][in_features], weight, w_gate, w_up [out_features][in_features], residual,
+ * y, h, dy, dh [rows][out_features], of type `dtype`, a row's elements next to each other, rows as far apart as the
+ * strides say (in elements, 0: next to each other); any 2-byte aligned address.  bias, b_gate, b_up and their
+ * gradients are fp32 [out_features].  saved: fp32, [rows][out_features] (gated: [2][rows][out_features]), the
+ * pre-activations z (g, then u) that the backward pass needs, 4-byte aligned; written by the forward call if not NULL.  The
+ * gradients dx [rows][in_features] and dweight, dw_gate, dw_up [out_features][in_features] are written with rows next to each other.
+ * y may be the residual itself (same address and stride); other outputs must not overlap anything.
+ * rows = 0 is valid: nothing to compute forward, zero weight and bias gradients backward. */
+typedef enum { DLF_F16 = 0, DLF_BF16 = 1 } dlf_dtype;
+typedef struct {
+    int32_t dtype;              /* dlf_dtype                                                              */
+    int32_t act;                /* dlf_act                                                                */
+    int64_t rows;               /* 0 .. 2^30                                                              */
+    int32_t in_features;        /* 1 .. 2^20                                                              */
+    int32_t out_features;       /* 1 .. 2^20 (gated: of either projection)                                */
+    int64_t x_stride;           /* elements from row to row, >= the row, < 2^31; 0: the row               */
+    int64_t w_stride;           /* ... of weight, of w_gate and w_up                                      */
+    int64_t y_stride;           /* ... of y or h                                                          */
+    int64_t res_stride;         /* ... of residual (dlf_linear)                                           */
+    int64_t dy_stride;          /* ... of dy or dh                                                        */
+} dlf_ff_desc;
+/* Bytes of workspace (DEVICE, 256-byte aligned, caller-owned, used by one call at a time) that a call with this description
+ * needs; 0: none, the pointer may be NULL.  SIZE_MAX for a description that the calls refuse.  Works without a GPU. */
+size_t dlf_linear_workspace_bytes(const dlf_ff_desc* d);
+size_t dlf_linear_backward_workspace_bytes(const dlf_ff_desc* d);
+size_t dlf_gated_workspace_bytes(const dlf_ff_desc* d);
+size_t dlf_gated_backward_workspace_bytes(const dlf_ff_desc* d);
+/* Asynchronous on hip_stream (NULL = default stream); they allocate nothing and record only kernel launches.  bias, residual,
+ * b_gate, b_up and saved may be NULL (none).  Backward: saved as the forward call wrote it on the same description and
+ * inputs (dlf_linear with DLF_ACT_NONE reads none: NULL); a gradient whose pointer is NULL is not computed. */
+dlf_status dlf_linear(const dlf_ff_desc* d, const void* x, const void* weight, const float* bias, const void* residual, void* y,
+                      float* saved, void* workspace, size_t workspace_bytes, void* hip_stream);
+dlf_status dlf_linear_backward(const dlf_ff_desc* d, const void* dy, const void* x, const void* weight, const float* saved, void* dx,
+                               void* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, const void* w_up, const float* b_gate, const float* b_up,
+                     void* h, float* saved, void* workspace, size_t workspace_bytes, void* hip_stream);
+dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved,
+                              void* dx, void* dw_gate, void* dw_up, float* db_gate, float* db_up, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
 
 const char* dlf_status_string(dlf_status s);
 const char* dlf_last_error(void);

@@ -14,6 +14,9 @@ LIB_PATH = os.path.join(HERE, "libdlf.so")
 
 OP = {"conv": 0, "dwconv": 1, "fc": 2, "maxpool": 3, "gavgpool": 4}
 ACT = {"none": 0, "relu": 1, "relu6": 2}
+# ... of the feed-forward operators
+FF_ACT = dict(ACT, gelu=3, gelu_tanh=4, silu=5, sigmoid=6)
+DTYPE = {"fp16": 0, "bf16": 1}
 TUNER_DP, TUNER_GREEDY, TUNER_MANUAL, TUNER_LAYERWISE, TUNER_MAXFUSE = 0, 1, 2, 3, 4
 DLF_OK = 0
 DLF_ERR_INVALID_ARG = 1
@@ -48,6 +51,13 @@ class TunerOpts(ctypes.Structure):
                 ("manual_budget", ctypes.POINTER(ctypes.c_int32)),
                 ("manual_n", ctypes.c_int32), ("max_lds_bytes", ctypes.c_int32),
                 ("fixed_budget", ctypes.c_int32)]
+
+
+class FfDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("res_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -145,6 +155,14 @@ def lib():
     L.dlf_i8conv_info.restype = i32
     L.dlf_i8conv_run.argtypes = [vp, vp, vp, vp]
     L.dlf_i8conv_run.restype = i32
+    ffp, sz = ctypes.POINTER(FfDesc), ctypes.c_size_t
+    for name, n in (("dlf_linear", 6), ("dlf_linear_backward", 7), ("dlf_gated", 7), ("dlf_gated_backward", 10)):
+        f = getattr(L, name)
+        f.argtypes = [ffp] + [vp] * (n + 1) + [sz, vp]
+        f.restype = i32
+        f = getattr(L, name + "_workspace_bytes")
+        f.argtypes = [ffp]
+        f.restype = sz
     _lib = L
     return L
 
@@ -350,6 +368,53 @@ def dlf_i8conv_info(layer):
 
 def dlf_i8conv_run(layer, in_ptr, out_ptr, stream=None):
     _check(lib().dlf_i8conv_run(layer, in_ptr, out_ptr, stream))
+
+
+def dlf_ff_desc(dtype, act, rows, in_features, out_features, x_stride=0, w_stride=0, y_stride=0, res_stride=0, dy_stride=0):
+    """The description of a feed-forward call; dtype: "fp16" or "bf16", act: a key of FF_ACT, strides in elements (0: rows next to each other)."""
+    return FfDesc(DTYPE[dtype], FF_ACT[act], rows, in_features, out_features, x_stride, w_stride, y_stride, res_stride, dy_stride)
+
+
+def _ff_workspace(name, desc):
+    n = getattr(lib(), name + "_workspace_bytes")(desc)
+    if n == ctypes.c_size_t(-1).value:
+        raise DlfError(DLF_ERR_INVALID_ARG, lib().dlf_last_error().decode())
+    return n
+
+
+def dlf_linear_workspace_bytes(desc):
+    return _ff_workspace("dlf_linear", desc)
+
+
+def dlf_linear_backward_workspace_bytes(desc):
+    return _ff_workspace("dlf_linear_backward", desc)
+
+
+def dlf_gated_workspace_bytes(desc):
+    return _ff_workspace("dlf_gated", desc)
+
+
+def dlf_gated_backward_workspace_bytes(desc):
+    return _ff_workspace("dlf_gated_backward", desc)
+
+
+def dlf_linear(desc, x, weight, bias, residual, y, saved=None, workspace=None, workspace_bytes=0, stream=None):
+    """Device addresses (int or None)."""
+    _check(lib().dlf_linear(desc, x, weight, bias, residual, y, saved, workspace, workspace_bytes, stream))
+
+
+def dlf_linear_backward(desc, dy, x, weight, saved, dx, dweight, dbias, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().dlf_linear_backward(desc, dy, x, weight, saved, dx, dweight, dbias, workspace, workspace_bytes, stream))
+
+
+def dlf_gated(desc, x, w_gate, w_up, b_gate, b_up, h, saved=None, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().dlf_gated(desc, x, w_gate, w_up, b_gate, b_up, h, saved, workspace, workspace_bytes, stream))
+
+
+def dlf_gated_backward(desc, dh, x, w_gate, w_up, saved, dx, dw_gate, dw_up, db_gate, db_up, workspace=None, workspace_bytes=0,
+                       stream=None):
+    _check(lib().dlf_gated_backward(desc, dh, x, w_gate, w_up, saved, dx, dw_gate, dw_up, db_gate, db_up, workspace, workspace_bytes,
+                                    stream))
 
 
 def dlf_cost_model_version():

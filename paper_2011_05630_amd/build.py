@@ -5,8 +5,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdlf.so")
-SOURCES = ["dlf_kernels.hip", "dlf_host.cpp"]
-HEADERS = ["dlf_internal.h", os.path.join("..", "..", "include", "dlf.h"),
+SOURCES = ["dlf_kernels.hip", "dlf_host.cpp", "dlf_ffn.hip", "dlf_ffn.cpp"]
+HEADERS = ["dlf_internal.h", "dlf_ffn.h", os.path.join("..", "..", "include", "dlf.h"),
            os.path.join("..", "..", "include", "dlf_debug.h")]
 
 

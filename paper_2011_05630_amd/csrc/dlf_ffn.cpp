@@ -1,0 +1,283 @@
+// Host side of the feed-forward operators: checks of the arguments, workspace layout, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+
+#include "dlf_ffn.h"
+
+namespace {
+
+dlf_status fail(dlf_status s, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return dlf_set_error(s, buf);
+}
+
+// A description with its strides filled in.
+struct Ff {
+    dlf_ff_desc d;
+    bool gated;
+    const char* call;
+};
+
+dlf_status check_desc(const dlf_ff_desc* d, bool gated, const char* call, Ff& f)
+{
+    if (!d) return fail(DLF_ERR_INVALID_ARG, "%s: null description", call);
+    f.d = *d;
+    f.gated = gated;
+    f.call = call;
+    if (d->dtype != DLF_F16 && d->dtype != DLF_BF16) return fail(DLF_ERR_INVALID_ARG, "%s: dtype %d", call, d->dtype);
+    if (d->act < DLF_ACT_NONE || d->act > DLF_ACT_SIGMOID) return fail(DLF_ERR_INVALID_ARG, "%s: act %d", call, d->act);
+    if (d->rows < 0 || d->rows > (int64_t)1 << 30) return fail(DLF_ERR_INVALID_ARG, "%s: %lld rows", call, (long long)d->rows);
+    if (d->in_features < 1 || d->in_features > 1 << 20 || d->out_features < 1 || d->out_features > 1 << 20)
+        return fail(DLF_ERR_INVALID_ARG, "%s: %d -> %d features", call, d->in_features, d->out_features);
+    struct { int64_t* s; int64_t row; const char* name; } strides[] = {
+        {&f.d.x_stride, d->in_features, "x"}, {&f.d.w_stride, d->in_features, "weight"}, {&f.d.y_stride, d->out_features, "y"},
+        {&f.d.res_stride, d->out_features, "residual"}, {&f.d.dy_stride, d->out_features, "dy"}};
+    for (auto& q : strides) {
+        if (*q.s == 0) *q.s = q.row;
+        if (*q.s < q.row || *q.s >= (int64_t)1 << 31)
+            return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %lld elements, %lld apart", call, q.name, (long long)q.row, (long long)*q.s);
+    }
+    // the products of the forward pass and of the gradients by the tiles of their grids
+    const int64_t t = DLF_FF_ANY_TILE, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
+    if (std::max({m * o, m * i, 2 * i * o}) >= (int64_t)1 << 24)
+        return fail(DLF_ERR_UNSUPPORTED, "%s: %lld rows, %d -> %d features are more tiles than a launch holds", call, (long long)d->rows,
+                    d->in_features, d->out_features);
+    return DLF_OK;
+}
+
+dlf_status check_ptr(const Ff& f, const void* p, const char* name, bool wanted, uintptr_t align)
+{
+    if (!p && wanted) return fail(DLF_ERR_INVALID_ARG, "%s: null %s", f.call, name);
+    if (((uintptr_t)p & (align - 1)) != 0) return fail(DLF_ERR_INVALID_ARG, "%s: %s is not aligned to %d bytes", f.call, name, (int)align);
+    return DLF_OK;
+}
+
+// The workspace of a backward call.
+struct BackLayout {
+    size_t dz = 0, lddz = 0, part = 0, bytes = 0;   // offsets; elements per row of dz
+    int chunk = 0, chunks = 0;
+};
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+bool needs_dz(const Ff& f) { return f.gated || f.d.act != DLF_ACT_NONE; }
+BackLayout back_layout(const Ff& f)
+{
+    BackLayout l;
+    const size_t nz = f.gated ? 2 : 1;
+    l.lddz = ((size_t)f.d.out_features + 7) / 8 * 8;
+    // rows of one partial sum: enough of them that the sums are few, few enough that the grid is not
+    l.chunk = (int)std::max<int64_t>(32, (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS);
+    l.chunks = f.d.rows > 0 ? (int)((f.d.rows + l.chunk - 1) / l.chunk) : 1;
+    if (needs_dz(f)) l.bytes = nz * align256((size_t)f.d.rows * l.lddz * 2);
+    l.part = l.bytes;
+    l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
+    return l;
+}
+
+dlf_status check_ws(const Ff& f, const void* ws, size_t have, size_t need)
+{
+    if (need == 0) return DLF_OK;
+    if (have < need) return fail(DLF_ERR_OOM, "%s: workspace too small: %zu < %zu", f.call, have, need);
+    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(DLF_ERR_INVALID_ARG, "%s: workspace must be a 256-byte aligned device pointer", f.call);
+    return DLF_OK;
+}
+
+#define TRY(X)                             \
+    do {                                   \
+        const dlf_status try_s = (X);      \
+        if (try_s != DLF_OK) return try_s; \
+    } while (0)
+
+dlf_status launched(const Ff& f, int e)
+{
+    if (e != 0) return fail(DLF_ERR_HIP, "%s: launch failed: %s", f.call, hipGetErrorString((hipError_t)e));
+    return DLF_OK;
+}
+
+// One product of the operators.
+dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stream)
+{
+    a.tiles_r = (a.nr + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
+    a.tiles_c = (a.nc + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
+    return launched(f, dlf_ff_start_any(&a, f.d.dtype, layout, gated, stream));
+}
+
+dlf_status forward(const Ff& f, const void* x, const void* const w[2], const float* const bias[2], const void* res, void* y, float* saved,
+                   void* stream)
+{
+    if (f.d.rows == 0) return DLF_OK;
+    DlfFfArgs a;
+    memset(&a, 0, sizeof a);
+    a.p[0] = w[0]; a.p[1] = w[1];
+    a.q[0] = x;
+    a.ldp = f.d.w_stride; a.ldq = f.d.x_stride;
+    a.nr = (int)f.d.rows; a.nc = f.d.out_features; a.nk = f.d.in_features;
+    a.segments = a.problems = 1;
+    a.bias[0] = bias[0]; a.bias[1] = bias[1];
+    a.res = res; a.ldres = f.d.res_stride;
+    a.out[0] = y; a.ldo = f.d.y_stride;
+    a.saved = saved; a.act = f.d.act;
+    return product(f, a, DLF_FF_NN, f.gated, stream);
+}
+
+dlf_status backward(const Ff& f, const void* dy, const void* x, const void* const w[2], const float* saved, void* dx, void* const dw[2],
+                    float* const db[2], char* ws, void* stream)
+{
+    const BackLayout l = back_layout(f);
+    const int nz = f.gated ? 2 : 1;
+    const bool sums = db[0] || db[1], products = dx || dw[0] || dw[1];
+    const void* dz[2] = {dy, nullptr};
+    int64_t lddz = f.d.dy_stride;
+    if (sums || (products && needs_dz(f))) {
+        DlfFfDzArgs z;
+        memset(&z, 0, sizeof z);
+        z.dy = dy; z.lddy = f.d.dy_stride;
+        z.rows = (int)f.d.rows; z.n = f.d.out_features; z.act = f.d.act; z.chunk = l.chunk;
+        if (sums) z.part = (float*)(ws + l.part);
+        if (needs_dz(f)) {
+            z.saved = saved;
+            z.lddz = lddz = (int64_t)l.lddz;
+            for (int i = 0; i < nz; ++i) dz[i] = z.dz[i] = ws + i * align256((size_t)f.d.rows * l.lddz * 2);
+        }
+        TRY(launched(f, dlf_ff_start_dz(&z, f.d.dtype, f.gated, stream)));
+        if (sums) {
+            DlfFfSumArgs s = {z.part, {db[0], db[1]}, z.n, l.chunks};
+            TRY(launched(f, dlf_ff_start_sum(&s, f.gated, stream)));
+        }
+    }
+    DlfFfArgs a;
+    if (dx && f.d.rows > 0) {
+        memset(&a, 0, sizeof a);
+        for (int i = 0; i < nz; ++i) { a.p[i] = w[i]; a.q[i] = dz[i]; }
+        a.ldp = f.d.w_stride; a.ldq = lddz;
+        a.nr = (int)f.d.rows; a.nc = f.d.in_features; a.nk = f.d.out_features;
+        a.segments = nz; a.problems = 1;
+        a.out[0] = dx; a.ldo = f.d.in_features;
+        TRY(product(f, a, DLF_FF_TN, false, stream));
+    }
+    memset(&a, 0, sizeof a);
+    a.segments = 1;
+    for (int i = 0; i < nz; ++i)
+        if (dw[i]) {
+            a.p[a.problems] = x; a.q[a.problems] = dz[i]; a.out[a.problems] = dw[i];
+            ++a.problems;
+        }
+    if (a.problems > 0) {
+        a.ldp = f.d.x_stride; a.ldq = lddz;
+        a.nr = f.d.out_features; a.nc = f.d.in_features; a.nk = (int)f.d.rows;
+        a.ldo = f.d.in_features;
+        TRY(product(f, a, DLF_FF_TT, false, stream));
+    }
+    return DLF_OK;
+}
+
+size_t forward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
+{
+    Ff f;
+    return check_desc(d, gated, call, f) == DLF_OK ? 0 : SIZE_MAX;
+}
+size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
+{
+    Ff f;
+    return check_desc(d, gated, call, f) == DLF_OK ? back_layout(f).bytes : SIZE_MAX;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dlf_linear_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, false, "dlf_linear_workspace_bytes"); }
+size_t dlf_gated_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, true, "dlf_gated_workspace_bytes"); }
+size_t dlf_linear_backward_workspace_bytes(const dlf_ff_desc* d) { return backward_bytes(d, false, "dlf_linear_backward_workspace_bytes"); }
+size_t dlf_gated_backward_workspace_bytes(const dlf_ff_desc* d) { return backward_bytes(d, true, "dlf_gated_backward_workspace_bytes"); }
+
+dlf_status dlf_linear(const dlf_ff_desc* d, const void* x, const void* weight, const float* bias, const void* residual, void* y,
+                      float* saved, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    Ff f;
+    TRY(check_desc(d, false, "dlf_linear", f));
+    const bool some = f.d.rows > 0;
+    TRY(check_ptr(f, x, "x", some, 2));
+    TRY(check_ptr(f, weight, "weight", some, 2));
+    TRY(check_ptr(f, bias, "bias", false, 4));
+    TRY(check_ptr(f, residual, "residual", false, 2));
+    TRY(check_ptr(f, y, "y", some, 2));
+    TRY(check_ptr(f, saved, "saved", false, 4));
+    TRY(check_ws(f, workspace, workspace_bytes, 0));
+    const void* w[2] = {weight, nullptr};
+    const float* b[2] = {bias, nullptr};
+    return forward(f, x, w, b, residual, y, saved, hip_stream);
+}
+
+dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, const void* w_up, const float* b_gate, const float* b_up,
+                     void* h, float* saved, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    Ff f;
+    TRY(check_desc(d, true, "dlf_gated", f));
+    const bool some = f.d.rows > 0;
+    TRY(check_ptr(f, x, "x", some, 2));
+    TRY(check_ptr(f, w_gate, "w_gate", some, 2));
+    TRY(check_ptr(f, w_up, "w_up", some, 2));
+    TRY(check_ptr(f, b_gate, "b_gate", false, 4));
+    TRY(check_ptr(f, b_up, "b_up", false, 4));
+    TRY(check_ptr(f, h, "h", some, 2));
+    TRY(check_ptr(f, saved, "saved", false, 4));
+    TRY(check_ws(f, workspace, workspace_bytes, 0));
+    const void* w[2] = {w_gate, w_up};
+    const float* b[2] = {b_gate, b_up};
+    return forward(f, x, w, b, nullptr, h, saved, hip_stream);
+}
+
+dlf_status dlf_linear_backward(const dlf_ff_desc* d, const void* dy, const void* x, const void* weight, const float* saved, void* dx,
+                               void* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    Ff f;
+    TRY(check_desc(d, false, "dlf_linear_backward", f));
+    const bool some = f.d.rows > 0;
+    TRY(check_ptr(f, dy, "dy", some, 2));
+    TRY(check_ptr(f, x, "x", some && dweight, 2));
+    TRY(check_ptr(f, weight, "weight", some && dx, 2));
+    TRY(check_ptr(f, saved, "saved", some && needs_dz(f), 4));
+    TRY(check_ptr(f, dx, "dx", false, 2));
+    TRY(check_ptr(f, dweight, "dweight", false, 2));
+    TRY(check_ptr(f, dbias, "dbias", false, 4));
+    TRY(check_ws(f, workspace, workspace_bytes, back_layout(f).bytes));
+    const void* w[2] = {weight, nullptr};
+    void* dw[2] = {dweight, nullptr};
+    float* db[2] = {dbias, nullptr};
+    return backward(f, dy, x, w, saved, dx, dw, db, (char*)workspace, hip_stream);
+}
+
+dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved,
+                              void* dx, void* dw_gate, void* dw_up, float* db_gate, float* db_up, void* workspace, size_t workspace_bytes,
+                              void* hip_stream)
+{
+    Ff f;
+    TRY(check_desc(d, true, "dlf_gated_backward", f));
+    const bool some = f.d.rows > 0;
+    TRY(check_ptr(f, dh, "dh", some, 2));
+    TRY(check_ptr(f, x, "x", some && (dw_gate || dw_up), 2));
+    TRY(check_ptr(f, w_gate, "w_gate", some && dx, 2));
+    TRY(check_ptr(f, w_up, "w_up", some && dx, 2));
+    TRY(check_ptr(f, saved, "saved", some, 4));
+    TRY(check_ptr(f, dx, "dx", false, 2));
+    TRY(check_ptr(f, dw_gate, "dw_gate", false, 2));
+    TRY(check_ptr(f, dw_up, "dw_up", false, 2));
+    TRY(check_ptr(f, db_gate, "db_gate", false, 4));
+    TRY(check_ptr(f, db_up, "db_up", false, 4));
+    TRY(check_ws(f, workspace, workspace_bytes, back_layout(f).bytes));
+    const void* w[2] = {w_gate, w_up};
+    void* dw[2] = {dw_gate, dw_up};
+    float* db[2] = {db_gate, db_up};
+    return backward(f, dh, x, w, saved, dx, dw, db, (char*)workspace, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,62 @@
+// Shared between the host side of the feed-forward operators (dlf_ffn.cpp) and their kernels (dlf_ffn.hip).
+//
+// Every product of the operators is C[r][c] = sum over k of Q[r][k] * P[c][k], c running along the rows of C in memory:
+//   forward            r = token, c = output feature, k = input feature:   Q = x,  P = weight   both with k along the row
+//   gradient of x      r = token, c = input feature,  k = output feature:  Q = dz, P = weight   P with k across the rows ("T")
+//   gradient of weight r = output feature, c = input feature, k = token:   Q = dz, P = x        both with k across the rows
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/dlf.h"
+
+// The layouts the products come in: P with k across its rows, Q with k across its rows.
+enum { DLF_FF_NN = 0, DLF_FF_TN = 1, DLF_FF_TT = 2 };
+
+struct DlfFfArgs {
+    const void* p[2];       // two of them: gate and up (gated), or the operands of the second segment / problem
+    const void* q[2];
+    int64_t ldp, ldq;       // elements between the rows of P and Q as they lie in memory
+    int32_t nr, nc, nk;
+    int32_t segments;       // 2: the sum runs over (p[0], q[0]) and then over (p[1], q[1])
+    int32_t problems;       // 2: two products of one shape, (p[0], q[0]) -> out[0] and (p[1], q[1]) -> out[1]
+    int32_t tiles_r, tiles_c;
+    // epilogue
+    const float* bias[2];
+    const void* res;
+    int64_t ldres;
+    void* out[2];
+    int64_t ldo;
+    float* saved;           // pre-activations, [1 or 2][nr][nc], or null
+    int32_t act;
+};
+
+// dz = dy * act'(z), gated: dg = dh * u * act'(g), du = dh * act(g); and the column sums of either in 32 bits.
+struct DlfFfDzArgs {
+    const void* dy;
+    int64_t lddy;
+    const float* saved;     // null: dz = dy, only the sums are wanted
+    void* dz[2];            // rows of lddz elements, zeros behind column n
+    int64_t lddz;
+    int32_t rows, n, act;
+    int32_t chunk;          // rows of one partial sum
+    float* part;            // [1 or 2][chunks][n], or null
+};
+struct DlfFfSumArgs {
+    const float* part;      // [1 or 2][chunks][n]
+    float* out[2];
+    int32_t n, chunks;
+};
+
+// Largest column count of partial sums, workgroup tile of the general kernel.
+#define DLF_FF_MAX_CHUNKS 128
+#define DLF_FF_ANY_TILE 64
+
+extern "C" {
+int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream);
+int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
+int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);
+}
+
+// Sets the message of dlf_last_error and returns the status (dlf_host.cpp).
+__attribute__((visibility("hidden"))) dlf_status dlf_set_error(dlf_status s, const char* msg);

@@ -20,6 +20,7 @@
 #include "../../include/dlf.h"
 #include "../../include/dlf_debug.h"
 #include "dlf_internal.h"
+#include "dlf_ffn.h"
 
 // Workspace of dlf_run_noalloc: a file-scope device array, one copy per GPU the library runs on, held
 // until the process ends.  In host code the array's name is only a handle for
@@ -2769,6 +2770,8 @@ void algorithm1(const dlf_net_s& net, int batch, double crit, double alpha, doub
 }
 
 }  // namespace
+
+dlf_status dlf_set_error(dlf_status s, const char* msg) { return fail(s, "%s", msg); }
 
 extern "C" {
 
