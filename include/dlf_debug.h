@@ -83,6 +83,10 @@ void dlf_debug_small_pair_mode(int32_t mode, int32_t shape, int32_t waves);
  * refuses its arguments.  Needs neither a GPU nor weights. */
 dlf_status dlf_debug_check_launches(const dlf_plan_t* plan);
 
+/* Testing hook: the kernel of the feed-forward operators' products: 0 = by the library's rule (default), 1 = the general
+ * kernel, 2 = tiles of 256 x 256, 3 = tiles of 128 x 128, wherever the operands' alignment allows them.  Process-wide, not thread-safe. */
+void dlf_debug_ff_kernel(int32_t kernel);
+
 #ifdef __cplusplus
 }
 #endif

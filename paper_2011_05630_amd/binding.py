@@ -155,6 +155,8 @@ def lib():
     L.dlf_i8conv_info.restype = i32
     L.dlf_i8conv_run.argtypes = [vp, vp, vp, vp]
     L.dlf_i8conv_run.restype = i32
+    L.dlf_debug_ff_kernel.argtypes = [i32]
+    L.dlf_debug_ff_kernel.restype = None
     ffp, sz = ctypes.POINTER(FfDesc), ctypes.c_size_t
     for name, n in (("dlf_linear", 6), ("dlf_linear_backward", 7), ("dlf_gated", 7), ("dlf_gated_backward", 10)):
         f = getattr(L, name)
@@ -473,6 +475,12 @@ def dlf_debug_small_mode(mode=0, shape=-1, waves=0):
 def dlf_debug_small_pair_mode(mode=0, shape=-1, waves=0):
     """Testing hook: as dlf_debug_small_mode, for a depthwise layer with the 1x1 layer behind it (shape 0, 1)."""
     lib().dlf_debug_small_pair_mode(mode, shape, waves)
+
+
+def dlf_debug_ff_kernel(kernel=0):
+    """Testing hook: 0 = the feed-forward operators' kernels by the library's rule, 1 = the general kernel, 2 / 3 = tiles of
+    256 x 256 / 128 x 128 wherever they apply."""
+    lib().dlf_debug_ff_kernel(kernel)
 
 
 def dlf_debug_check_launches(plan):

@@ -5,7 +5,9 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 
+#include "../../include/dlf_debug.h"
 #include "dlf_ffn.h"
 
 namespace {
@@ -102,9 +104,42 @@ dlf_status launched(const Ff& f, int e)
     return DLF_OK;
 }
 
+std::once_flag g_once;
+int g_once_rc = 0;
+
+// Whether the tile kernel takes an operand: rows in whole 16-byte lines, offsets inside a tile that fit 31 bits.
+bool lines(const void* p, int64_t ld, int64_t row)
+{
+    return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (row & 7) == 0 && ld < (int64_t)1 << 21;
+}
+
+// Testing hook: 0 = by rule, 1 = the general kernel, 2 + shape = a tile kernel wherever it applies.
+int g_force = 0;
+
 // One product of the operators.
 dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stream)
 {
+    bool whole = true;
+    const int n = gated ? 2 : std::max(a.segments, a.problems);
+    for (int i = 0; i < n; ++i) {
+        whole = whole && lines(a.p[i], a.ldp, layout == DLF_FF_NN ? a.nk : a.nc);
+        if (!gated) whole = whole && lines(a.q[i], a.ldq, layout == DLF_FF_TT ? a.nr : a.nk);
+    }
+    if (gated) whole = whole && lines(a.q[0], a.ldq, a.nk);
+    if (whole && g_force != 1) {
+        int shape = DLF_FF_SHAPE_256;
+        auto tiles = [&](int s) {
+            a.tiles_r = (a.nr + DLF_FF_SHAPES[s].br - 1) / DLF_FF_SHAPES[s].br;
+            const int cols = DLF_FF_SHAPES[s].bc / (gated ? 2 : 1);
+            a.tiles_c = (a.nc + cols - 1) / cols;
+            return a.tiles_r * a.tiles_c * a.problems;
+        };
+        if (tiles(shape) < 160) tiles(shape = DLF_FF_SHAPE_128);
+        if (g_force > 1) tiles(shape = g_force - 2);
+        std::call_once(g_once, [] { g_once_rc = dlf_ff_kernels_init(); });
+        if (g_once_rc != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc));
+        return launched(f, dlf_ff_start_tile(&a, shape, f.d.dtype, layout, gated, stream));
+    }
     a.tiles_r = (a.nr + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
     a.tiles_c = (a.nc + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
     return launched(f, dlf_ff_start_any(&a, f.d.dtype, layout, gated, stream));
@@ -193,6 +228,8 @@ size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 }  // namespace
 
 extern "C" {
+
+void dlf_debug_ff_kernel(int32_t kernel) { g_force = kernel >= 0 && kernel < 2 + DLF_FF_NUM_SHAPES ? kernel : 0; }
 
 size_t dlf_linear_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, false, "dlf_linear_workspace_bytes"); }
 size_t dlf_gated_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, true, "dlf_gated_workspace_bytes"); }

@@ -52,7 +52,14 @@ struct DlfFfSumArgs {
 #define DLF_FF_MAX_CHUNKS 128
 #define DLF_FF_ANY_TILE 64
 
+// Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and its waves.
+struct DlfFfShape { int bc, br, wc, wr; };
+enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_NUM_SHAPES = 2 };
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 4, 2}, {128, 128, 2, 2}};
+
 extern "C" {
+int dlf_ff_kernels_init(void);
+int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
 int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);

@@ -268,6 +268,261 @@ __global__ __launch_bounds__(256) void k_ff_any(const DlfFfArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------
+// k_ff_tile: the product for operands whose rows are whole 16-byte lines.  A workgroup of WC x WR waves computes BC x BR of C (gated: BC / 2
+// features of both projections), a wave FC x FR blocks of 32 x 32; 64 k at a time ("stage") pass through LDS, two stages in turn.
+//   Global -> LDS: 16-byte direct loads, 1 KiB per instruction, lane l's 16 bytes at 16 l.  Rows, columns and k that do not exist
+//     are read from an offset behind the resource's end, which brings zeros and no traffic.
+//   An operand with k along its rows lies in LDS as [row][64 k], 128 bytes a row, its 16-byte part c at position c ^ (row / 2) % 8: the 16
+//     lanes that LDS serves at a time, 16 rows of one part, fall into 16 different 16-byte groups of the 256 bytes of banks.
+//   An operand with k across its rows lies as [k][row] as it comes, and is turned on its way into registers: one transposing
+//     read gives a lane four k of its row, the 16 lanes of a group reading 4 k x 16 rows.  The 64-byte part b of line k is kept at b ^ f(k),
+//     f(k) = k % 4 + 4 * (k / 8 % 2) (modulo the parts of a line): the eight lines of a read fall into different banks.
+//   The multiplications of 16 k run while the operands of the next 16 are read.  Behind the third of a stage's four steps a wave has all of the
+//     stage in registers: there it waits for its part of the next stage (requested a whole stage ago) and for the other waves, and
+//     requests the stage after that into the LDS just read, so that the fourth step's multiplications cover the first reads
+//     of the next stage and the barrier.
+//   The epilogue goes through LDS in passes of 32 rows per wave, so that stores are whole lines and the activations unrolled once.
+// Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, in bands of four rows of tiles, and its workgroups share operands
+// in its L2.
+// ------------------------------------------------------------------------------------------------
+#define OOB ((int)0x80000000)
+typedef int i4v __attribute__((ext_vector_type(4)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef short s8v __attribute__((ext_vector_type(8)));
+extern __shared__ __attribute__((aligned(16))) char ff_lds[];
+typedef __attribute__((address_space(3))) char lds_char;
+
+__device__ __forceinline__ i4v resource(const void* p)
+{
+    const unsigned long long v = (unsigned long long)p;
+    i4v r;
+    r.x = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
+    r.y = __builtin_amdgcn_readfirstlane((int)((unsigned)(v >> 32) & 0xffffu));
+    r.z = 0x7fffffff;
+    r.w = 0x00020000;
+    return r;
+}
+// Lane l's 16 bytes at base + off into LDS at dst + 16 l.  Written as an instruction: the compiler would wait for such loads
+// wherever it waits for an LDS read.
+__device__ __forceinline__ void line_to_lds(const i4v& base, int off, unsigned dst)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(base), "s"(dst) : "memory");
+}
+#define WAIT_ALL 0x0070          // s_waitcnt vmcnt(0) lgkmcnt(0); known to the compiler, unlike an instruction in assembly
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// One operand's way from memory into LDS: a wave's N instructions of a stage.  ROWS of the operand per tile; TR: k across the rows.
+template <int N, int ROWS, bool TR> struct Loader {
+    static constexpr int CPL = TR ? ROWS / 8 : 8;      // 16-byte parts of a line in LDS
+    int off[N];
+    // first: the wave's first instruction; avail: rows of the operand from the tile's first on; half: gated P, see below
+    __device__ __forceinline__ static int line(int first, int i) { return (first + i) * (64 / CPL) + (threadIdx.x & 63) / CPL; }
+    __device__ __forceinline__ static int part(int first, int i)
+    {
+        const int l = line(first, i), p = (threadIdx.x & 63) % CPL;
+        if (!TR) return p ^ ((l >> 1) & 7);
+        return p ^ ((((l & 3) | ((l >> 3) & 1) << 2) & (ROWS / 32 - 1)) << 2);
+    }
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int l = line(first, i), p = part(first, i);
+            // a gated tile's lines: for every 32 features 32 lines of the gate projection and 32 of the other
+            const int row = GATED ? (l >> 6) * 32 + (l & 31) : l;
+            if (!TR) off[i] = row < avail ? (int)(row * ld + p * 8) * 2 : OOB;
+            else off[i] = p * 8 < avail ? (int)(l * ld + p * 8) * 2 : OOB;
+        }
+    }
+    template <bool TAIL> __device__ __forceinline__ void issue(const i4v& base, int first, unsigned dst, int k_left) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            line_to_lds(base, !TAIL || (TR ? line(first, i) : part(first, i) * 8) < k_left ? off[i] : OOB, dst + (unsigned)(first + i) * 1024);
+    }
+};
+// ... and from LDS into registers: the fragment of 32 rows and 16 k as the matrix instruction takes it (lane l: row l % 32, k = 8 (l / 32) + 0 .. 7).
+template <typename T, int ROWS, bool TR> struct Reader {
+    unsigned at[4];         // byte offsets, by step of 16 k (k along the rows) or by block of 32 rows (across)
+    __device__ __forceinline__ void setup(int row0)
+    {
+        const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!TR) at[i] = (row0 + l32) * 128 + (((2 * i + lhi) ^ ((l32 >> 1) & 7)) << 4);
+            else {
+                const int f = ((lane >> 2 & 3) | lhi << 2) & (ROWS / 32 - 1);
+                at[i] = (lhi * 8 + (lane >> 2 & 3)) * (ROWS * 2) + (((row0 / 32 + i) ^ f) << 6) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+            }
+        }
+    }
+    __device__ __forceinline__ typename T::v8 get(unsigned stage, int step, int block) const
+    {
+        if constexpr (!TR) {
+            return *(const __attribute__((address_space(3))) typename T::v8*)((const lds_char*)ff_lds + (stage + at[step] + block * 4096));
+        } else {
+            const unsigned a = stage + at[block] + step * (16 * ROWS * 2);
+            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)((lds_char*)ff_lds + a));
+            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)((lds_char*)ff_lds + (a + 4 * ROWS * 2)));
+            return __builtin_bit_cast(typename T::v8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+template <int I, int N, typename F> __device__ __forceinline__ void static_for(F&& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        static_for<I + 1, N>(f);
+    }
+}
+
+template <typename T, int BC, int BR, int WC, int WR, bool PT, bool QT, bool GATED>
+__global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
+{
+    typedef typename T::v8 v8;
+    constexpr int NW = WC * WR, FC = BC / WC / 32, FR = BR / WR / 32, LP = BC / 8 / NW, LQ = BR / 8 / NW;
+    constexpr unsigned QOFF = BC * 128, STAGE = (BC + BR) * 128;
+    constexpr int READS = FC * (PT ? 2 : 1) + FR * (QT ? 2 : 1), RPM = (READS + FC * FR - 2) / (FC * FR - 1);   // reads of a step; per multiplication
+    static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1, "");
+    static_assert(!GATED || (LP == 4 && FC == 2 && !PT), "a wave's loads of a gated tile belong to one projection, its two blocks to both");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
+    const int wc = wave % WC, wr = wave / WC;
+    // tile
+    const int per = a.tiles_r * a.tiles_c, all = per * a.problems, each = (all + 7) >> 3;
+    int t = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= each || t >= all) return;
+    const int prob = t / per;
+    t -= prob * per;
+    const int band = t / (4 * a.tiles_c), rows = min(4, a.tiles_r - band * 4), in = t - band * 4 * a.tiles_c;
+    constexpr int CF = GATED ? BC / 2 : BC;            // columns of C per tile
+    const int r0 = (band * 4 + in % rows) * BR, c0 = in / rows * CF;
+
+    Loader<LP, BC, PT> lp;
+    Loader<LQ, BR, QT> lq;
+    lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
+    lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
+    Reader<T, BC, PT> rp;
+    Reader<T, BR, QT> rq;
+    rp.setup(wc * FC * 32);
+    rq.setup(wr * FR * 32);
+    const int64_t p0 = PT ? (int64_t)c0 : (int64_t)c0 * a.ldp, q0 = QT ? (int64_t)r0 : (int64_t)r0 * a.ldq;
+    const int64_t pstep = PT ? 128 * a.ldp : 128, qstep = QT ? 128 * a.ldq : 128;   // bytes
+    const char *pb, *qb;
+    int k_left;
+    auto segment = [&](int w) __attribute__((always_inline)) {
+        pb = (const char*)a.p[GATED ? wave & 1 : w] + p0 * 2;
+        qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2;
+        k_left = a.nk;
+    };
+    segment(a.problems == 2 ? prob : 0);
+    const unsigned lds0 = (unsigned)(size_t)(lds_char*)ff_lds;
+    auto issue = [&](unsigned stage) __attribute__((always_inline)) {
+        if (k_left <= 0) segment(1);
+        if (k_left >= 64) {
+            lp.template issue<false>(resource(pb), wave * LP, lds0 + stage, 64);
+            lq.template issue<false>(resource(qb), wave * LQ, lds0 + stage + QOFF, 64);
+        } else {                            // k beyond the operands' last are zeros
+            lp.template issue<true>(resource(pb), wave * LP, lds0 + stage, k_left);
+            lq.template issue<true>(resource(qb), wave * LQ, lds0 + stage + QOFF, k_left);
+        }
+        pb += pstep;
+        qb += qstep;
+        k_left -= 64;
+    };
+    const int total = (a.nk + 63) / 64 * a.segments;
+    f16v acc[FC][FR];
+#pragma unroll
+    for (int i = 0; i < FC; ++i)
+#pragma unroll
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    v8 fp[2][FC], fq[2][FR];
+    auto read = [&](unsigned stage, int step, int set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FC; ++i) fp[set][i] = rp.get(stage, step, i);
+#pragma unroll
+        for (int j = 0; j < FR; ++j) fq[set][j] = rq.get(stage + QOFF, step, j);
+    };
+    // the reads of the next step's operands go out between the first multiplications of this one
+    auto interleave = [&]() __attribute__((always_inline)) {
+        static_for<0, FC * FR>([](auto i) __attribute__((always_inline)) {
+            if constexpr (decltype(i)::value * RPM < READS) __builtin_amdgcn_sched_group_barrier(0x100, RPM, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        });
+    };
+    auto multiply = [&](int set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FC; ++i)
+#pragma unroll
+            for (int j = 0; j < FR; ++j) acc[i][j] = T::mma(fp[set][i], fq[set][j], acc[i][j]);
+    };
+    auto steps012 = [&](unsigned stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int step = 0; step < 3; ++step) {
+            read(stage, step + 1, (step + 1) & 1);
+            multiply(step & 1);
+            interleave();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (total > 0) {
+        issue(0);
+        if (total > 1) {
+            issue(STAGE);
+            wait_loads<LP + LQ>();
+        } else {
+            wait_loads<0>();
+        }
+        asm volatile("s_barrier" ::: "memory");
+        unsigned cur = 0;
+        read(cur, 0, 0);
+        for (int s = 0; s < total - 1; ++s) {
+            steps012(cur);
+            // this wave's reads of the stage have arrived, and so has its part of the next one
+            __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+            asm volatile("s_barrier" ::: "memory");
+            if (s + 2 < total) issue(cur);
+            cur = STAGE - cur;
+            read(cur, 0, 0);
+            multiply(1);
+            interleave();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        steps012(cur);
+        multiply(1);
+    }
+    // ---- epilogue: 32 rows of every wave at a time through LDS ----
+    constexpr int CROW = BC + 4;                        // floats
+    float* const lf = (float*)ff_lds;                   // [WR * 32][CROW]
+#pragma unroll
+    for (int j = 0; j < FR; ++j) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < FC; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f4v*)(lf + (wr * 32 + l32) * CROW + (wc * FC + i) * 32 + q * 8 + lhi * 4) =
+                    f4v{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+        __syncthreads();
+#pragma unroll 1
+        for (int i = threadIdx.x; i < WR * 32 * CF / 8; i += NW * 64) {
+            const int lr = i / (CF / 8), c = i % (CF / 8) * 8, r = r0 + (lr >> 5) * (FR * 32) + j * 32 + (lr & 31);
+            if (r >= a.nr || c0 + c >= a.nc) continue;
+            float v[8], u[8];
+            const float* const src = lf + lr * CROW + (GATED ? (c >> 5) * 64 + (c & 31) : c);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                *(f4v*)(v + e * 4) = *(const f4v*)(src + e * 4);
+                if (GATED) *(f4v*)(u + e * 4) = *(const f4v*)(src + 32 + e * 4);
+            }
+            finish8<T, GATED>(a, prob, r, c0 + c, a.nc - c0 - c, v, u);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
 // k_ff_dz: the gradient behind the activation, and partial column sums of it in 32 bits (before it is rounded).  A workgroup takes
 // `chunk` rows of 256 columns: 32 threads by eight columns, 8 rows at a time; the sums of the 8 meet in LDS in a fixed order.
 // ------------------------------------------------------------------------------------------------
@@ -366,6 +621,45 @@ extern "C" int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int g
 {
     hipLaunchKernelGGL(dtype == DLF_F16 ? any_kernel<F16>(layout, gated) : any_kernel<BF16>(layout, gated),
                        dim3((unsigned)(a->tiles_r * a->tiles_c * a->problems)), dim3(256), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+// The tile kernels by shape (DLF_FF_SHAPE_*).
+template <typename T, int BC, int BR, int WC, int WR> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
+{
+    if (gated) return k_ff_tile<T, BC, BR, WC, WR, false, false, true>;
+    switch (layout) {
+    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, false, false, false>;
+    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, true, false, false>;
+    default: return k_ff_tile<T, BC, BR, WC, WR, true, true, false>;
+    }
+}
+template <typename T> static void (*tile_kernel(int shape, int layout, int gated))(const DlfFfArgs)
+{
+    return shape == DLF_FF_SHAPE_256 ? tile_of<T, 256, 256, 4, 2>(layout, gated) : tile_of<T, 128, 128, 2, 2>(layout, gated);
+}
+static size_t tile_lds(int shape)
+{
+    const DlfFfShape& s = DLF_FF_SHAPES[shape];
+    const size_t ring = 2 * (s.bc + s.br) * 128, out = (size_t)s.wr * 32 * (s.bc + 4) * 4;
+    return ring > out ? ring : out;
+}
+extern "C" int dlf_ff_kernels_init(void)
+{
+    for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
+        for (int k = 0; k < 8; ++k) {
+            const int layout = k >> 1 & 3, gated = layout == 3;
+            auto f = (k & 1) ? tile_kernel<BF16>(shape, gated ? 0 : layout, gated) : tile_kernel<F16>(shape, gated ? 0 : layout, gated);
+            const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
+            if (e != hipSuccess) return (int)e;
+        }
+    return 0;
+}
+extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream)
+{
+    const unsigned tiles = (unsigned)(a->tiles_r * a->tiles_c * a->problems);
+    const DlfFfShape& s = DLF_FF_SHAPES[shape];
+    hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, layout, gated) : tile_kernel<BF16>(shape, layout, gated),
+                       dim3((tiles + 7) / 8 * 8), dim3((unsigned)(s.wc * s.wr * 64)), tile_lds(shape), (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream)
