@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <mutex>
 
@@ -107,6 +108,13 @@ dlf_status launched(const Ff& f, int e)
 std::once_flag g_once;
 int g_once_rc = 0;
 
+dlf_status kernels_ready()
+{
+    std::call_once(g_once, [] { g_once_rc = dlf_ff_kernels_init(); });
+    if (g_once_rc != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc));
+    return DLF_OK;
+}
+
 // Whether the tile kernel takes an operand: rows in whole 16-byte lines, offsets inside a tile that fit 31 bits.
 bool lines(const void* p, int64_t ld, int64_t row)
 {
@@ -119,6 +127,17 @@ int g_force = 0;
 // One product of the operators.
 dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stream)
 {
+    TRY(kernels_ready());
+    // few rows
+    int few = a.nr <= 64, nf = gated || a.nc < 16 * 1024 ? 1 : 2, mr = a.nr <= 16 ? 1 : a.nr <= 32 ? 2 : 4, waves;
+    {
+        const int64_t groups = (a.nc + 16 * nf - 1) / (16 * nf);
+        waves = 8;
+        while (waves > 4 && (groups * waves > 4096 || waves * 64 > a.nk)) waves >>= 1;
+    }
+    if (const char* e = getenv("FF_FEW")) sscanf(e, "%d,%d,%d,%d", &few, &nf, &mr, &waves);
+    if (layout == DLF_FF_NN && few && (g_force == 0 || g_force == 2 + DLF_FF_NUM_SHAPES))
+        return launched(f, dlf_ff_start_few(&a, f.d.dtype, gated, gated ? 1 : nf, mr, waves, stream));
     bool whole = true;
     const int n = gated ? 2 : std::max(a.segments, a.problems);
     for (int i = 0; i < n; ++i) {
@@ -136,8 +155,6 @@ dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stre
         };
         if (tiles(shape) < 160) tiles(shape = DLF_FF_SHAPE_128);
         if (g_force > 1) tiles(shape = g_force - 2);
-        std::call_once(g_once, [] { g_once_rc = dlf_ff_kernels_init(); });
-        if (g_once_rc != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc));
         return launched(f, dlf_ff_start_tile(&a, shape, f.d.dtype, layout, gated, stream));
     }
     a.tiles_r = (a.nr + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
@@ -229,7 +246,7 @@ size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 
 extern "C" {
 
-void dlf_debug_ff_kernel(int32_t kernel) { g_force = kernel >= 0 && kernel < 2 + DLF_FF_NUM_SHAPES ? kernel : 0; }
+void dlf_debug_ff_kernel(int32_t kernel) { g_force = kernel >= 0 && kernel <= 2 + DLF_FF_NUM_SHAPES ? kernel : 0; }
 
 size_t dlf_linear_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, false, "dlf_linear_workspace_bytes"); }
 size_t dlf_gated_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, true, "dlf_gated_workspace_bytes"); }

@@ -60,6 +60,7 @@ static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 4, 2}
 extern "C" {
 int dlf_ff_kernels_init(void);
 int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
+int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream);
 int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
 int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);

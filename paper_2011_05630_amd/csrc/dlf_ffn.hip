@@ -11,16 +11,18 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef unsigned u4v __attribute__((ext_vector_type(4)));
 
-// The two element types and their 32x32x16 matrix instruction.
+// The two element types and their matrix instructions, 32x32x16 and 16x16x32.
 struct F16 {
     typedef _Float16 e;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ f16v mma(v8 a, v8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f4v mma16(v8 a, v8 b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 struct BF16 {
     typedef __bf16 e;
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ f16v mma(v8 a, v8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f4v mma16(v8 a, v8 b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
 // ------------------------------------------------------------------------------------------------
@@ -94,91 +96,96 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F&& f)
 }
 
 // ------------------------------------------------------------------------------------------------
-// Eight consecutive elements, of which n exist (n may be anything; nothing outside them is touched).
+// V consecutive elements, of which n exist (n may be anything; nothing outside them is touched).
 // Rows start where they like: a 16-byte access of any 2-byte alignment is one instruction here.
 // ------------------------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ typename T::v8 load8(const void* base, int64_t at, int n)
+template <typename T, int V> struct Some { typedef typename T::e v __attribute__((ext_vector_type(V))); };
+template <typename T, int V> __device__ __forceinline__ typename Some<T, V>::v load_some(const void* base, int64_t at, int n)
 {
     const typename T::e* p = (const typename T::e*)base + at;
-    typename T::v8 v;
-    if (n >= 8) {
-        __builtin_memcpy(&v, p, 16);
+    typename Some<T, V>::v v;
+    if (n >= V) {
+        __builtin_memcpy(&v, p, 2 * V);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (typename T::e)0.0f;
+        for (int i = 0; i < V; ++i) v[i] = i < n ? p[i] : (typename T::e)0.0f;
     }
     return v;
 }
-template <typename T> __device__ __forceinline__ void store8(void* base, int64_t at, int n, const float (&f)[8])
+template <typename T> __device__ __forceinline__ typename T::v8 load8(const void* base, int64_t at, int n)
+{
+    return __builtin_bit_cast(typename T::v8, load_some<T, 8>(base, at, n));
+}
+template <typename T, int V> __device__ __forceinline__ void store_some(void* base, int64_t at, int n, const float (&f)[V])
 {
     typename T::e* p = (typename T::e*)base + at;
-    typename T::v8 v;
+    typename Some<T, V>::v v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (typename T::e)f[i];
-    if (n >= 8) {
-        __builtin_memcpy(p, &v, 16);
+    for (int i = 0; i < V; ++i) v[i] = (typename T::e)f[i];
+    if (n >= V) {
+        __builtin_memcpy(p, &v, 2 * V);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < V; ++i)
             if (i < n) p[i] = v[i];
     }
 }
-__device__ __forceinline__ void load8f(const float* p, int n, float (&f)[8])
+template <int V> __device__ __forceinline__ void load_floats(const float* p, int n, float (&f)[V])
 {
-    if (n >= 8) {
-        __builtin_memcpy(f, p, 32);
+    if (n >= V) {
+        __builtin_memcpy(f, p, 4 * V);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.0f;
+        for (int i = 0; i < V; ++i) f[i] = i < n ? p[i] : 0.0f;
     }
 }
-__device__ __forceinline__ void store8f(float* p, int n, const float (&f)[8])
+template <int V> __device__ __forceinline__ void store_floats(float* p, int n, const float (&f)[V])
 {
-    if (n >= 8) {
-        __builtin_memcpy(p, f, 32);
+    if (n >= V) {
+        __builtin_memcpy(p, f, 4 * V);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < V; ++i)
             if (i < n) p[i] = f[i];
     }
 }
 
-// The epilogue of eight outputs C[r][c .. c + n): bias, pre-activations kept, activation, product with the second projection,
+// The epilogue of V outputs C[r][c .. c + n): bias, pre-activations kept, activation, product with the second projection,
 // residual, one rounding.
-template <typename T, bool GATED>
-__device__ __forceinline__ void finish8(const DlfFfArgs& a, int prob, int r, int c, int n, float (&v)[8], float (&u)[8])
+template <typename T, bool GATED, int V>
+__device__ __forceinline__ void finish(const DlfFfArgs& a, int prob, int r, int c, int n, float (&v)[V], float (&u)[V])
 {
     if (a.bias[0] != nullptr) {
-        float b[8];
-        load8f(a.bias[0] + c, n, b);
+        float b[V];
+        load_floats(a.bias[0] + c, n, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += b[i];
+        for (int i = 0; i < V; ++i) v[i] += b[i];
     }
     if (GATED && a.bias[1] != nullptr) {
-        float b[8];
-        load8f(a.bias[1] + c, n, b);
+        float b[V];
+        load_floats(a.bias[1] + c, n, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] += b[i];
+        for (int i = 0; i < V; ++i) u[i] += b[i];
     }
     if (a.saved != nullptr) {
-        store8f(a.saved + (int64_t)r * a.nc + c, n, v);
-        if (GATED) store8f(a.saved + ((int64_t)a.nr + r) * a.nc + c, n, u);
+        store_floats(a.saved + (int64_t)r * a.nc + c, n, v);
+        if (GATED) store_floats(a.saved + ((int64_t)a.nr + r) * a.nc + c, n, u);
     }
     if (a.act != DLF_ACT_NONE)
         with_act(a.act, [&](auto k) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = act_of<decltype(k)::value>(v[i]);
+            for (int i = 0; i < V; ++i) v[i] = act_of<decltype(k)::value>(v[i]);
         });
     if (GATED) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= u[i];
+        for (int i = 0; i < V; ++i) v[i] *= u[i];
     }
     if (a.res != nullptr) {
-        const typename T::v8 q = load8<T>(a.res, (int64_t)r * a.ldres + c, n);
+        const typename Some<T, V>::v q = load_some<T, V>(a.res, (int64_t)r * a.ldres + c, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += (float)q[i];
+        for (int i = 0; i < V; ++i) v[i] += (float)q[i];
     }
-    store8<T>(a.out[prob], (int64_t)r * a.ldo + c, n, v);
+    store_some<T, V>(a.out[prob], (int64_t)r * a.ldo + c, n, v);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -261,9 +268,9 @@ __global__ __launch_bounds__(256) void k_ff_any(const DlfFfArgs a)
         const int r = i >> 3, c = (i & 7) * 8;
         if (r0 + r >= a.nr || c0 + c >= a.nc) continue;
         float v[8], u[8];
-        load8f(lf + r * CROW + c, 8, v);
-        if (GATED) load8f(lf + (TILE + r) * CROW + c, 8, u);
-        finish8<T, GATED>(a, prob, r0 + r, c0 + c, a.nc - c0 - c, v, u);
+        load_floats(lf + r * CROW + c, 8, v);
+        if (GATED) load_floats(lf + (TILE + r) * CROW + c, 8, u);
+        finish<T, GATED, 8>(a, prob, r0 + r, c0 + c, a.nc - c0 - c, v, u);
     }
 }
 
@@ -517,7 +524,107 @@ __global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
                 *(f4v*)(v + e * 4) = *(const f4v*)(src + e * 4);
                 if (GATED) *(f4v*)(u + e * 4) = *(const f4v*)(src + 32 + e * 4);
             }
-            finish8<T, GATED>(a, prob, r, c0 + c, a.nc - c0 - c, v, u);
+            finish<T, GATED, 8>(a, prob, r, c0 + c, a.nc - c0 - c, v, u);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_ff_few: the forward product of few rows: one token, a handful of requests.  Bound by the weights' bytes, or for small layers by the
+// launch and one round trip to memory: nothing is staged, every wave reads its operands from memory straight into the registers
+// that v_mfma_f32_16x16x32 takes them from.  A workgroup computes 16 NF features (gated: 16 of both projections) for 16 MR rows, its waves
+// share k in equal runs of 32-wide steps and meet in LDS, in a fixed order.  A wave requests U steps while it multiplies the U before.
+// Steps beyond a wave's run are requested again at its last one and not multiplied; rows that do not exist are read as the last that does and not stored; a last
+// step that is not whole is the last wave's, requested first.
+// ------------------------------------------------------------------------------------------------
+template <typename T, int NF, int MR, bool GATED>
+__global__ __launch_bounds__(512) void k_ff_few(const DlfFfArgs a)
+{
+    typedef typename T::e e;
+    typedef typename T::v8 v8;
+    constexpr int U = MR == 4 ? 2 : 4, NP = GATED ? 2 : NF;       // W fragments per step
+    static_assert(!GATED || NF == 1, "");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int l16 = lane & 15, kg = (lane >> 4) * 8;
+    const int c0 = blockIdx.x * (16 * NF), r0 = blockIdx.y * (16 * MR);
+    const int steps = a.nk >> 5, s0 = (int)((int64_t)steps * wave / waves), s1 = (int)((int64_t)steps * (wave + 1) / waves);
+    const e *wp[NP], *xp[MR];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+        wp[i] = (const e*)a.p[GATED ? i : 0] + (int64_t)min(c0 + (GATED ? 0 : i * 16) + l16, a.nc - 1) * a.ldp + kg;
+#pragma unroll
+    for (int j = 0; j < MR; ++j) xp[j] = (const e*)a.q[0] + (int64_t)min(r0 + j * 16 + l16, a.nr - 1) * a.ldq + kg;
+    f4v acc[NP][MR];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < MR; ++j) acc[i][j] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+    const bool last = wave == waves - 1 && (a.nk & 31) != 0;
+    v8 tw[NP], tx[MR];
+    if (last) {
+        const int k = steps * 32, n = a.nk - k - kg;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) tw[i] = load8<T>(wp[i], k, n);
+#pragma unroll
+        for (int j = 0; j < MR; ++j) tx[j] = load8<T>(xp[j], k, n);
+    }
+    if (s0 < s1) {
+        v8 w[2][U][NP], x[2][U][MR];
+        auto request = [&](int s, int set) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t k = (int64_t)min(s + u, s1 - 1) * 32;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) __builtin_memcpy(&w[set][u][i], wp[i] + k, 16);
+#pragma unroll
+                for (int j = 0; j < MR; ++j) __builtin_memcpy(&x[set][u][j], xp[j] + k, 16);
+            }
+        };
+        auto multiply = [&](int s, int set) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u < s1) {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i)
+#pragma unroll
+                        for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(w[set][u][i], x[set][u][j], acc[i][j]);
+                }
+        };
+        request(s0, 0);
+        for (int s = s0; s < s1; s += 2 * U) {
+            if (s + U < s1) request(s + U, 1);
+            multiply(s, 0);
+            if (s + U < s1) {
+                if (s + 2 * U < s1) request(s + 2 * U, 0);
+                multiply(s + U, 1);
+            }
+        }
+    }
+    if (last) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(tw[i], tx[j], acc[i][j]);
+    }
+    // [wave][block][lane] four consecutive c of row lane % 16
+    f4v* const part = (f4v*)ff_lds;
+    constexpr int NB = NP * MR;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < MR; ++j) part[(wave * NB + i * MR + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int b = wave; b < NF * MR; b += waves) {
+        const int i = b / MR, j = b - i * MR;
+        f4v v = f4v{0.0f, 0.0f, 0.0f, 0.0f}, u = v;
+        for (int w = 0; w < waves; ++w) {
+            v += part[(w * NB + i * MR + j) * 64 + lane];
+            if (GATED) u += part[(w * NB + MR + j) * 64 + lane];
+        }
+        const int r = r0 + j * 16 + l16, c = c0 + i * 16 + (lane >> 4) * 4;
+        if (r < a.nr && c < a.nc) {
+            float fv[4] = {v.x, v.y, v.z, v.w}, fu[4] = {u.x, u.y, u.z, u.w};
+            finish<T, GATED, 4>(a, 0, r, c, a.nc - c, fv, fu);
         }
     }
 }
@@ -547,8 +654,8 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
             for (int i = 0; i < 8; ++i) d[0][i] = (float)dy[i];
             if (a.saved != nullptr) {
                 float z[8], u[8];
-                load8f(a.saved + (int64_t)r * a.n + c, n, z);
-                if (GATED) load8f(a.saved + ((int64_t)a.rows + r) * a.n + c, n, u);
+                load_floats(a.saved + (int64_t)r * a.n + c, n, z);
+                if (GATED) load_floats(a.saved + ((int64_t)a.rows + r) * a.n + c, n, u);
                 with_act(a.act, [&](auto k) __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -569,7 +676,7 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) d[z2][i] = i < n ? d[z2][i] : 0.0f;
                     }
-                    store8<T>(a.dz[z2], (int64_t)r * a.lddz + c, 8, d[z2]);
+                    store_some<T, 8>(a.dz[z2], (int64_t)r * a.lddz + c, 8, d[z2]);
                 }
             }
 #pragma unroll
@@ -643,8 +750,27 @@ static size_t tile_lds(int shape)
     const size_t ring = 2 * (s.bc + s.br) * 128, out = (size_t)s.wr * 32 * (s.bc + 4) * 4;
     return ring > out ? ring : out;
 }
+template <typename T> static void (*few_kernel(int nf, int mr, int gated))(const DlfFfArgs)
+{
+    if (gated) return mr == 1 ? k_ff_few<T, 1, 1, true> : mr == 2 ? k_ff_few<T, 1, 2, true> : k_ff_few<T, 1, 4, true>;
+    if (nf == 1) return mr == 1 ? k_ff_few<T, 1, 1, false> : mr == 2 ? k_ff_few<T, 1, 2, false> : k_ff_few<T, 1, 4, false>;
+    return mr == 1 ? k_ff_few<T, 2, 1, false> : mr == 2 ? k_ff_few<T, 2, 2, false> : k_ff_few<T, 2, 4, false>;
+}
+extern "C" int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream)
+{
+    hipLaunchKernelGGL(dtype == DLF_F16 ? few_kernel<F16>(nf, mr, gated) : few_kernel<BF16>(nf, mr, gated),
+                       dim3((unsigned)((a->nc + 16 * nf - 1) / (16 * nf)), (unsigned)((a->nr + 16 * mr - 1) / (16 * mr))), dim3((unsigned)waves * 64),
+                       (size_t)waves * nf * mr * (gated ? 2 : 1) * 1024, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
 extern "C" int dlf_ff_kernels_init(void)
 {
+    for (int k = 0; k < 18; ++k) {
+        const int mr = 1 << k / 6, nf = k / 2 % 3 == 1 ? 2 : 1, gated = k / 2 % 3 == 2;
+        auto f = (k & 1) ? few_kernel<BF16>(nf, mr, gated) : few_kernel<F16>(nf, mr, gated);
+        const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * 2 * mr * 1024);
+        if (e != hipSuccess) return (int)e;
+    }
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
         for (int k = 0; k < 8; ++k) {
             const int layout = k >> 1 & 3, gated = layout == 3;

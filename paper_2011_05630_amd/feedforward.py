@@ -46,37 +46,64 @@ class _Operator:
     """What the operators share: the weights' type, device and sizes, views of the operands as rows, the call itself."""
 
     def _setup(self, w, act):
-        _need(act in B.FF_ACT, "act: one of %s expected", ", ".join(sorted(B.FF_ACT)))
-        B.lib()
+        if act not in B.FF_ACT:
+            raise ValueError("act: one of %s expected" % ", ".join(sorted(B.FF_ACT)))
         self.act, self.dtype, self.device = act, w.dtype, w.device
         self.out_features, self.in_features = w.shape
+        self._index, self._w_stride = w.get_device(), _stride(w, "weight")
+        self._calls = {}        # descriptions by call, rows and strides, with the workspace they ask for
 
     def _rows(self, t, width, name, rows=None):
-        _need(isinstance(t, torch.Tensor) and t.dtype == self.dtype and t.device == self.device and t.dim() >= 1 and t.shape[-1] == width,
-              "%s: a %s tensor [..., %d] on %s expected", name, self.dtype, width, self.device)
+        """t as rows, and their distance."""
+        if not isinstance(t, torch.Tensor) or t.dtype is not self.dtype or t.get_device() != self._index or t.dim() < 1 or t.shape[-1] != width:
+            raise ValueError("%s: a %s tensor [..., %d] on %s expected" % (name, self.dtype, width, self.device))
         if t.dim() != 2:
             try:
                 t = t.view(-1, width)
             except RuntimeError:
                 raise ValueError("%s: its rows do not lie at one distance" % name) from None
-        _need(rows is None or t.shape[0] == rows, "%s: %s rows expected", name, rows)
-        return t, _stride(t, name)
+        m, (s, one) = t.shape[0], t.stride()
+        if rows is not None and m != rows:
+            raise ValueError("%s: %d rows expected" % (name, rows))
+        if one != 1 and width != 1:
+            raise ValueError("%s: a row's elements have to lie next to each other" % name)
+        if m <= 1:
+            s = width
+        elif s < width:
+            raise ValueError("%s: rows overlap" % name)
+        return t, s
+
+    def _out(self, out, shape, rows):
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            return out, out, self.out_features
+        _need(out.shape == shape, "out: shape %s expected", tuple(shape))
+        return (out,) + self._rows(out, self.out_features, "out", rows)
 
     def _saved(self, saved, shape):
         _need(isinstance(saved, torch.Tensor) and saved.dtype == torch.float32 and saved.device == self.device and tuple(saved.shape) == shape and
               saved.is_contiguous(), "saved: the tensor that the forward call returned, fp32 %s, expected", shape)
         return saved
 
-    def _call(self, name, desc, *tensors):
-        need = B._ff_workspace(name, desc)
+    def _call(self, name, rows, strides, *tensors):
+        """strides: of x, y, residual and dy."""
+        key = (name, rows, strides)
+        call = self._calls.get(key)
+        if call is None:
+            xs, ys, rs, ds = strides
+            desc = B.dlf_ff_desc(_TYPE[self.dtype], self.act, rows, self.in_features, self.out_features, xs, self._w_stride, ys, rs, ds)
+            if len(self._calls) >= 1024:
+                self._calls.clear()
+            call = self._calls[key] = (getattr(B, name), desc, B._ff_workspace(name, desc))
+        f, desc, need = call
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         ptr = [None if t is None else t.data_ptr() for t in tensors]
-        with torch.cuda.device(self.device):
-            stream = torch.cuda.current_stream(self.device).cuda_stream
-            getattr(B, name)(desc, *ptr, None if ws is None else ws.data_ptr(), need, stream)
-
-    def _desc(self, rows, **strides):
-        return B.dlf_ff_desc(_TYPE[self.dtype], self.act, rows, self.in_features, self.out_features, **strides)
+        ptr.append(None if ws is None else ws.data_ptr())
+        if torch.cuda.current_device() == self._index:
+            f(desc, *ptr, need, torch._C._cuda_getCurrentRawStream(self._index))
+        else:
+            with torch.cuda.device(self._index):
+                f(desc, *ptr, need, torch._C._cuda_getCurrentRawStream(self._index))
 
 
 class Linear(_Operator):
@@ -90,18 +117,14 @@ class Linear(_Operator):
     def _forward(self, x, residual, out, save):
         x2, xs = self._rows(x, self.in_features, "x")
         rows = x2.shape[0]
-        shape = tuple(x.shape[:-1]) + (self.out_features,)
+        shape = x.shape[:-1] + (self.out_features,)
         rs = 0
         if residual is not None:
-            _need(tuple(residual.shape) == shape, "residual: shape %s expected", shape)
+            _need(residual.shape == shape, "residual: shape %s expected", tuple(shape))
             residual, rs = self._rows(residual, self.out_features, "residual", rows)
-        if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        _need(tuple(out.shape) == shape, "out: shape %s expected", shape)
-        o2, ys = self._rows(out, self.out_features, "out", rows)
+        out, o2, ys = self._out(out, shape, rows)
         saved = torch.empty((rows, self.out_features), dtype=torch.float32, device=self.device) if save and self.act != "none" else None
-        desc = self._desc(rows, x_stride=xs, w_stride=_stride(self.weight, "weight"), y_stride=ys, res_stride=rs)
-        self._call("dlf_linear", desc, x2, self.weight, self.bias, residual, o2, saved)
+        self._call("dlf_linear", rows, (xs, ys, rs, 0), x2, self.weight, self.bias, residual, o2, saved)
         return out, saved
 
     def run(self, x, residual=None, out=None):
@@ -125,8 +148,7 @@ class Linear(_Operator):
         dx = new(tuple(x.shape), self.dtype) if "x" in need else None
         dw = new((self.out_features, self.in_features), self.dtype) if "weight" in need else None
         db = new((self.out_features,), torch.float32) if "bias" in need and self.bias is not None else None
-        desc = self._desc(rows, x_stride=xs, w_stride=_stride(self.weight, "weight"), dy_stride=ds)
-        self._call("dlf_linear_backward", desc, d2, x2, self.weight, saved if self.act != "none" else None, dx, dw, db)
+        self._call("dlf_linear_backward", rows, (xs, 0, 0, ds), d2, x2, self.weight, saved if self.act != "none" else None, dx, dw, db)
         return dx, dw, db
 
 
@@ -144,14 +166,9 @@ class GatedLinear(_Operator):
     def _forward(self, x, out, save):
         x2, xs = self._rows(x, self.in_features, "x")
         rows = x2.shape[0]
-        shape = tuple(x.shape[:-1]) + (self.out_features,)
-        if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        _need(tuple(out.shape) == shape, "out: shape %s expected", shape)
-        o2, ys = self._rows(out, self.out_features, "out", rows)
+        out, o2, ys = self._out(out, x.shape[:-1] + (self.out_features,), rows)
         saved = torch.empty((2, rows, self.out_features), dtype=torch.float32, device=self.device) if save else None
-        desc = self._desc(rows, x_stride=xs, w_stride=_stride(self.w_gate, "w_gate"), y_stride=ys)
-        self._call("dlf_gated", desc, x2, self.w_gate, self.w_up, self.b_gate, self.b_up, o2, saved)
+        self._call("dlf_gated", rows, (xs, ys, 0, 0), x2, self.w_gate, self.w_up, self.b_gate, self.b_up, o2, saved)
         return out, saved
 
     def run(self, x, out=None):
@@ -174,8 +191,7 @@ class GatedLinear(_Operator):
         dx = new(tuple(x.shape), self.dtype) if "x" in need else None
         dw = [new((self.out_features, self.in_features), self.dtype) if "weight" in need else None for _ in range(2)]
         db = [new((self.out_features,), torch.float32) if "bias" in need and b is not None else None for b in (self.b_gate, self.b_up)]
-        desc = self._desc(rows, x_stride=xs, w_stride=_stride(self.w_gate, "w_gate"), dy_stride=ds)
-        self._call("dlf_gated_backward", desc, d2, x2, self.w_gate, self.w_up, saved, dx, *dw, *db)
+        self._call("dlf_gated_backward", rows, (xs, 0, 0, ds), d2, x2, self.w_gate, self.w_up, saved, dx, *dw, *db)
         return (dx, *dw, *db)
 
 
