@@ -137,7 +137,15 @@ dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stre
     }
     if (const char* e = getenv("FF_FEW")) sscanf(e, "%d,%d,%d,%d", &few, &nf, &mr, &waves);
     if (layout == DLF_FF_NN && few && (g_force == 0 || g_force == 2 + DLF_FF_NUM_SHAPES))
+    {
+        bool al = lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+        if (getenv("FF_NOROWS")) al = false;
+        if (al) {
+            while (DLF_FF_ROWS_LDS(waves, nf, mr, gated) > 160 * 1024) waves >>= 1;
+            return launched(f, dlf_ff_start_rows(&a, f.d.dtype, gated, gated ? 1 : nf, mr, waves, stream));
+        }
         return launched(f, dlf_ff_start_few(&a, f.d.dtype, gated, gated ? 1 : nf, mr, waves, stream));
+    }
     bool whole = true;
     const int n = gated ? 2 : std::max(a.segments, a.problems);
     for (int i = 0; i < n; ++i) {

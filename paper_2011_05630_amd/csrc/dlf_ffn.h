@@ -57,7 +57,12 @@ struct DlfFfShape { int bc, br, wc, wr; };
 enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_NUM_SHAPES = 2 };
 static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 4, 2}, {128, 128, 2, 2}};
 
+// k_ff_rows: stages of 64 k that a wave holds in LDS; LDS of a workgroup.
+#define DLF_FF_ROWS_RING 4
+#define DLF_FF_ROWS_LDS(WAVES, NF, MR, GATED) ((WAVES) * DLF_FF_ROWS_RING * (((GATED) ? 2 : (NF)) + (MR)) * 2048)
+
 extern "C" {
+int dlf_ff_start_rows(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream);
 int dlf_ff_kernels_init(void);
 int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream);

@@ -315,6 +315,7 @@ __device__ __forceinline__ void line_to_lds(const i4v& base, int off, unsigned d
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(base), "s"(dst) : "memory");
 }
+#define WAIT_LDS 0xc07f          // s_waitcnt lgkmcnt(0)
 #define WAIT_ALL 0x0070          // s_waitcnt vmcnt(0) lgkmcnt(0); known to the compiler, unlike an instruction in assembly
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -529,20 +530,48 @@ __global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
     }
 }
 
+// The waves' partial sums of a workgroup's 16 NF features x 16 MR rows meet in LDS, in the order of the waves.
+template <typename T, int NF, int MR, bool GATED>
+__device__ __forceinline__ void few_finish(const DlfFfArgs& a, const f4v (&acc)[GATED ? 2 : NF][MR], int c0, int r0, int wave, int waves)
+{
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    __syncthreads();
+    // [wave][block][lane] four consecutive c of row lane % 16
+    f4v* const part = (f4v*)ff_lds;
+    constexpr int NP = GATED ? 2 : NF, NB = NP * MR;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < MR; ++j) part[(wave * NB + i * MR + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int b = wave; b < NF * MR; b += waves) {
+        const int i = b / MR, j = b - i * MR;
+        f4v v = f4v{0.0f, 0.0f, 0.0f, 0.0f}, u = v;
+        for (int w = 0; w < waves; ++w) {
+            v += part[(w * NB + i * MR + j) * 64 + lane];
+            if (GATED) u += part[(w * NB + MR + j) * 64 + lane];
+        }
+        const int r = r0 + j * 16 + l16, c = c0 + i * 16 + (lane >> 4) * 4;
+        if (r < a.nr && c < a.nc) {
+            float fv[4] = {v.x, v.y, v.z, v.w}, fu[4] = {u.x, u.y, u.z, u.w};
+            finish<T, GATED, 4>(a, 0, r, c, a.nc - c, fv, fu);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------
 // k_ff_few: the forward product of few rows: one token, a handful of requests.  Bound by the weights' bytes, or for small layers by the
 // launch and one round trip to memory: nothing is staged, every wave reads its operands from memory straight into the registers
 // that v_mfma_f32_16x16x32 takes them from.  A workgroup computes 16 NF features (gated: 16 of both projections) for 16 MR rows, its waves
-// share k in equal runs of 32-wide steps and meet in LDS, in a fixed order.  A wave requests U steps while it multiplies the U before.
-// Steps beyond a wave's run are requested again at its last one and not multiplied; rows that do not exist are read as the last that does and not stored; a last
-// step that is not whole is the last wave's, requested first.
+// share k in equal runs of 32-wide steps and meet in LDS, in a fixed order.  A wave keeps D steps requested.  Rows that do not exist are
+// read as the last that does and not stored; a last step that is not whole is the last wave's, requested first.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int NF, int MR, bool GATED>
-__global__ __launch_bounds__(512) void k_ff_few(const DlfFfArgs a)
+__global__ __launch_bounds__(512, (GATED ? 2 : NF) + MR <= 3 ? 4 : 2) void k_ff_few(const DlfFfArgs a)
 {
     typedef typename T::e e;
     typedef typename T::v8 v8;
-    constexpr int U = MR == 4 ? 2 : 4, NP = GATED ? 2 : NF;       // W fragments per step
+    constexpr int NP = GATED ? 2 : NF, D = NP + MR == 2 ? 8 : NP + MR == 3 ? 6 : 4;     // W fragments of a step; steps requested ahead
     static_assert(!GATED || NF == 1, "");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int l16 = lane & 15, kg = (lane >> 4) * 8;
@@ -569,36 +598,39 @@ __global__ __launch_bounds__(512) void k_ff_few(const DlfFfArgs a)
         for (int j = 0; j < MR; ++j) tx[j] = load8<T>(xp[j], k, n);
     }
     if (s0 < s1) {
-        v8 w[2][U][NP], x[2][U][MR];
-        auto request = [&](int s, int set) __attribute__((always_inline)) {
+        v8 w[D][NP], x[D][MR];
+        auto request = [&](int s, int slot) __attribute__((always_inline)) {
+            const int64_t k = (int64_t)s * 32;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t k = (int64_t)min(s + u, s1 - 1) * 32;
+            for (int i = 0; i < NP; ++i) __builtin_memcpy(&w[slot][i], wp[i] + k, 16);
 #pragma unroll
-                for (int i = 0; i < NP; ++i) __builtin_memcpy(&w[set][u][i], wp[i] + k, 16);
-#pragma unroll
-                for (int j = 0; j < MR; ++j) __builtin_memcpy(&x[set][u][j], xp[j] + k, 16);
-            }
+            for (int j = 0; j < MR; ++j) __builtin_memcpy(&x[slot][j], xp[j] + k, 16);
         };
-        auto multiply = [&](int s, int set) __attribute__((always_inline)) {
+        auto multiply = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (s + u < s1) {
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-                    for (int i = 0; i < NP; ++i)
-#pragma unroll
-                        for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(w[set][u][i], x[set][u][j], acc[i][j]);
-                }
+                for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(w[slot][i], x[slot][j], acc[i][j]);
         };
-        request(s0, 0);
-        for (int s = s0; s < s1; s += 2 * U) {
-            if (s + U < s1) request(s + U, 1);
-            multiply(s, 0);
-            if (s + U < s1) {
-                if (s + 2 * U < s1) request(s + 2 * U, 0);
-                multiply(s + U, 1);
+#pragma unroll
+        for (int d = 0; d < D; ++d) request(min(s0 + d, s1 - 1), d);
+        int s = s0;
+        for (; s + 2 * D <= s1; s += D) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                multiply(d);
+                request(s + D + d, d);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            if (s + d < s1) multiply(d);
+            if (s + D + d < s1) request(s + D + d, d);
+        }
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+            if (s + D + d < s1) multiply(d);
     }
     if (last) {
 #pragma unroll
@@ -606,27 +638,82 @@ __global__ __launch_bounds__(512) void k_ff_few(const DlfFfArgs a)
 #pragma unroll
             for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(tw[i], tx[j], acc[i][j]);
     }
-    // [wave][block][lane] four consecutive c of row lane % 16
-    f4v* const part = (f4v*)ff_lds;
-    constexpr int NB = NP * MR;
+    few_finish<T, NF, MR, GATED>(a, acc, c0, r0, wave, waves);
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_ff_rows: k_ff_few for operands whose rows are whole 16-byte lines.  There a wave's load takes 64 bytes of each of 16 rows, and pieces
+// of many lines cost a compute unit several times their size; here the operands come as whole 128-byte lines, eight rows per
+// instruction, into a ring in LDS that belongs to the wave alone: 64 k ("stage") of its features and rows at a time, D stages
+// requested ahead, no barrier before the waves meet.  LDS holds a stage as k_ff_tile does.
+// ------------------------------------------------------------------------------------------------
+template <typename T, int NF, int MR, bool GATED>
+__global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
+{
+    typedef typename T::v8 v8;
+    constexpr int NP = GATED ? 2 : NF, D = DLF_FF_ROWS_RING, LW = GATED ? 2 : 2 * NF, L = 2 * (NP + MR);
+    constexpr unsigned STAGE = L * 1024, XOFF = 2 * NP * 1024;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int l16 = lane & 15;
+    const int c0 = blockIdx.x * (16 * NF), r0 = blockIdx.y * (16 * MR);
+    const int stages = (a.nk + 63) >> 6, s0 = (int)((int64_t)stages * wave / waves), s1 = (int)((int64_t)stages * (wave + 1) / waves);
+    Loader<LW, 64, false> lw;
+    Loader<2 * MR, 64, false> lx;
+    lw.template setup<false>(0, a.nc - c0, a.ldp);
+    lx.template setup<false>(0, a.nr - r0, a.ldq);
+    const char* wb[2] = {(const char*)a.p[0] + (int64_t)c0 * a.ldp * 2, GATED ? (const char*)a.p[1] + (int64_t)c0 * a.ldp * 2 : nullptr};
+    const char* xb = (const char*)a.q[0] + (int64_t)r0 * a.ldq * 2;
+    const unsigned ring = (unsigned)wave * (D * STAGE), lds0 = (unsigned)(size_t)(lds_char*)ff_lds + ring;
+    auto issue = [&](int s) __attribute__((always_inline)) {
+        const unsigned slot = lds0 + (unsigned)(s % D) * STAGE;
+        const int left = a.nk - s * 64;
+        const int64_t at = (int64_t)s * 128;
+        if (left >= 64) {
+            lw.template issue<false>(resource(wb[0] + at), 0, slot, 64);
+            if (GATED) lw.template issue<false>(resource(wb[1] + at), 0, slot + 2048, 64);
+            lx.template issue<false>(resource(xb + at), 0, slot + XOFF, 64);
+        } else {
+            lw.template issue<true>(resource(wb[0] + at), 0, slot, left);
+            if (GATED) lw.template issue<true>(resource(wb[1] + at), 0, slot + 2048, left);
+            lx.template issue<true>(resource(xb + at), 0, slot + XOFF, left);
+        }
+    };
+    f4v acc[NP][MR];
 #pragma unroll
     for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int j = 0; j < MR; ++j) part[(wave * NB + i * MR + j) * 64 + lane] = acc[i][j];
-    __syncthreads();
-    for (int b = wave; b < NF * MR; b += waves) {
-        const int i = b / MR, j = b - i * MR;
-        f4v v = f4v{0.0f, 0.0f, 0.0f, 0.0f}, u = v;
-        for (int w = 0; w < waves; ++w) {
-            v += part[(w * NB + i * MR + j) * 64 + lane];
-            if (GATED) u += part[(w * NB + MR + j) * 64 + lane];
+        for (int j = 0; j < MR; ++j) acc[i][j] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (s0 + d < s1) issue(s0 + d);
+    unsigned at[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) at[k] = ring + l16 * 128 + (((k * 4 + (lane >> 4)) ^ (l16 >> 1)) << 4);
+    for (int s = s0; s < s1; ++s) {
+        if (s + D <= s1) wait_loads<(D - 1) * L>();
+        else wait_loads<0>();
+        const unsigned slot = (unsigned)(s % D) * STAGE;
+        v8 w[2][NP], x[2][MR];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) w[k][i] = *(const __attribute__((address_space(3))) v8*)((const lds_char*)ff_lds + (slot + at[k] + i * 2048));
+#pragma unroll
+            for (int j = 0; j < MR; ++j) x[k][j] = *(const __attribute__((address_space(3))) v8*)((const lds_char*)ff_lds + (slot + at[k] + XOFF + j * 2048));
         }
-        const int r = r0 + j * 16 + l16, c = c0 + i * 16 + (lane >> 4) * 4;
-        if (r < a.nr && c < a.nc) {
-            float fv[4] = {v.x, v.y, v.z, v.w}, fu[4] = {u.x, u.y, u.z, u.w};
-            finish<T, GATED, 4>(a, 0, r, c, a.nc - c, fv, fu);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < MR; ++j) acc[i][j] = T::mma16(w[k][i], x[k][j], acc[i][j]);
+        if (s + D < s1) {
+            __builtin_amdgcn_s_waitcnt(WAIT_LDS);             // the slot has been read
+            __builtin_amdgcn_sched_barrier(0);
+            issue(s + D);
         }
     }
+    few_finish<T, NF, MR, GATED>(a, acc, c0, r0, wave, waves);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -756,6 +843,19 @@ template <typename T> static void (*few_kernel(int nf, int mr, int gated))(const
     if (nf == 1) return mr == 1 ? k_ff_few<T, 1, 1, false> : mr == 2 ? k_ff_few<T, 1, 2, false> : k_ff_few<T, 1, 4, false>;
     return mr == 1 ? k_ff_few<T, 2, 1, false> : mr == 2 ? k_ff_few<T, 2, 2, false> : k_ff_few<T, 2, 4, false>;
 }
+template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
+{
+    if (gated) return mr == 1 ? k_ff_rows<T, 1, 1, true> : mr == 2 ? k_ff_rows<T, 1, 2, true> : k_ff_rows<T, 1, 4, true>;
+    if (nf == 1) return mr == 1 ? k_ff_rows<T, 1, 1, false> : mr == 2 ? k_ff_rows<T, 1, 2, false> : k_ff_rows<T, 1, 4, false>;
+    return mr == 1 ? k_ff_rows<T, 2, 1, false> : mr == 2 ? k_ff_rows<T, 2, 2, false> : k_ff_rows<T, 2, 4, false>;
+}
+extern "C" int dlf_ff_start_rows(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream)
+{
+    hipLaunchKernelGGL(dtype == DLF_F16 ? rows_kernel<F16>(nf, mr, gated) : rows_kernel<BF16>(nf, mr, gated),
+                       dim3((unsigned)((a->nc + 16 * nf - 1) / (16 * nf)), (unsigned)((a->nr + 16 * mr - 1) / (16 * mr))), dim3((unsigned)waves * 64),
+                       (size_t)DLF_FF_ROWS_LDS(waves, nf, mr, gated), (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
 extern "C" int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream)
 {
     hipLaunchKernelGGL(dtype == DLF_F16 ? few_kernel<F16>(nf, mr, gated) : few_kernel<BF16>(nf, mr, gated),
@@ -770,6 +870,9 @@ extern "C" int dlf_ff_kernels_init(void)
         auto f = (k & 1) ? few_kernel<BF16>(nf, mr, gated) : few_kernel<F16>(nf, mr, gated);
         const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * 2 * mr * 1024);
         if (e != hipSuccess) return (int)e;
+        auto g = (k & 1) ? rows_kernel<BF16>(nf, mr, gated) : rows_kernel<F16>(nf, mr, gated);
+        const hipError_t e2 = hipFuncSetAttribute((const void*)g, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e2 != hipSuccess) return (int)e2;
     }
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
         for (int k = 0; k < 8; ++k) {
