@@ -4,7 +4,6 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 #include <cstring>
 #include <mutex>
 
@@ -124,28 +123,28 @@ bool lines(const void* p, int64_t ld, int64_t row)
 // Testing hook: 0 = by rule, 1 = the general kernel, 2 + shape = a tile kernel wherever it applies.
 int g_force = 0;
 
+// The forward product of few rows, straight from memory.
+dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
+{
+    DlfFfFew c;
+    c.rows = lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+    // Rows per workgroup: 32 rather than 64 of them even where 64 exist (gated 64 x 2048 -> 2 x 5632: 16.6 against 18.4 us), there with
+    // 32 features for the reads of x (64 x 4096 -> 4096: 12.1 against 14.8 us; fewer workgroups lose below 33 rows).
+    c.mr = a.nr <= 16 ? 1 : 2;
+    c.nf = gated || a.nr <= 32 ? 1 : 2;
+    // Waves that share k: eight while every workgroup has a compute unit to itself, else four (2001 of them: 24.3 against 24.7 us, 680
+    // gated: 31.8 against 35.9), and no more than there are stages of 64 k.
+    const int64_t groups = (int64_t)((a.nc + 16 * c.nf - 1) / (16 * c.nf)) * ((a.nr + 16 * c.mr - 1) / (16 * c.mr));
+    c.waves = groups <= 256 ? 8 : 4;
+    while (c.waves > 1 && c.waves * 64 >= 2 * a.nk) c.waves >>= 1;
+    return launched(f, dlf_ff_start_few(&a, &c, f.d.dtype, gated, stream));
+}
+
 // One product of the operators.
 dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stream)
 {
     TRY(kernels_ready());
-    // few rows
-    int few = a.nr <= 64, nf = gated || a.nc < 16 * 1024 ? 1 : 2, mr = a.nr <= 16 ? 1 : a.nr <= 32 ? 2 : 4, waves;
-    {
-        const int64_t groups = (a.nc + 16 * nf - 1) / (16 * nf);
-        waves = 8;
-        while (waves > 4 && (groups * waves > 4096 || waves * 64 > a.nk)) waves >>= 1;
-    }
-    if (const char* e = getenv("FF_FEW")) sscanf(e, "%d,%d,%d,%d", &few, &nf, &mr, &waves);
-    if (layout == DLF_FF_NN && few && (g_force == 0 || g_force == 2 + DLF_FF_NUM_SHAPES))
-    {
-        bool al = lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
-        if (getenv("FF_NOROWS")) al = false;
-        if (al) {
-            while (DLF_FF_ROWS_LDS(waves, nf, mr, gated) > 160 * 1024) waves >>= 1;
-            return launched(f, dlf_ff_start_rows(&a, f.d.dtype, gated, gated ? 1 : nf, mr, waves, stream));
-        }
-        return launched(f, dlf_ff_start_few(&a, f.d.dtype, gated, gated ? 1 : nf, mr, waves, stream));
-    }
+    if (layout == DLF_FF_NN && a.nr <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 2 + DLF_FF_NUM_SHAPES)) return few_rows(f, a, gated, stream);
     bool whole = true;
     const int n = gated ? 2 : std::max(a.segments, a.problems);
     for (int i = 0; i < n; ++i) {

@@ -57,15 +57,18 @@ struct DlfFfShape { int bc, br, wc, wr; };
 enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_NUM_SHAPES = 2 };
 static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 4, 2}, {128, 128, 2, 2}};
 
-// k_ff_rows: stages of 64 k that a wave holds in LDS; LDS of a workgroup.
-#define DLF_FF_ROWS_RING 4
+// Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
+#define DLF_FF_FEW_ROWS 64
+struct DlfFfFew { int rows, nf, mr, waves; };
+// k_ff_rows: stages of 64 k that a wave holds in LDS (2: 16 x 5632 -> 2048 takes 10.4 us with 2, 3 and 4, 1 x 4096 -> 2 x 10880 gated 31.8, 31.3 and
+// 34.8 us, 16 x 2048 -> 2 x 5632 gated 12.5, 12.6 and 15.1: with more, fewer workgroups share a compute unit); LDS of a workgroup.
+#define DLF_FF_ROWS_RING 2
 #define DLF_FF_ROWS_LDS(WAVES, NF, MR, GATED) ((WAVES) * DLF_FF_ROWS_RING * (((GATED) ? 2 : (NF)) + (MR)) * 2048)
 
 extern "C" {
-int dlf_ff_start_rows(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream);
 int dlf_ff_kernels_init(void);
 int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
-int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream);
+int dlf_ff_start_few(const DlfFfArgs* a, const DlfFfFew* c, int dtype, int gated, void* stream);
 int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
 int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);

@@ -571,11 +571,13 @@ __global__ __launch_bounds__(512, (GATED ? 2 : NF) + MR <= 3 ? 4 : 2) void k_ff_
 {
     typedef typename T::e e;
     typedef typename T::v8 v8;
-    constexpr int NP = GATED ? 2 : NF, D = NP + MR == 2 ? 8 : NP + MR == 3 ? 6 : 4;     // W fragments of a step; steps requested ahead
+    constexpr int NP = GATED ? 2 : NF, D = NP + MR == 2 ? 8 : 6;     // W fragments of a step; steps requested ahead
     static_assert(!GATED || NF == 1, "");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int l16 = lane & 15, kg = (lane >> 4) * 8;
-    const int c0 = blockIdx.x * (16 * NF), r0 = blockIdx.y * (16 * MR);
+    const int bc = (blockIdx.x >> 3) / a.tiles_r * 8 + (blockIdx.x & 7);   // all rows of a feature group on one XCD: they share its weights
+    if (bc >= a.tiles_c) return;
+    const int c0 = bc * (16 * NF), r0 = (blockIdx.x >> 3) % a.tiles_r * (16 * MR);
     const int steps = a.nk >> 5, s0 = (int)((int64_t)steps * wave / waves), s1 = (int)((int64_t)steps * (wave + 1) / waves);
     const e *wp[NP], *xp[MR];
 #pragma unroll
@@ -655,7 +657,9 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
     constexpr unsigned STAGE = L * 1024, XOFF = 2 * NP * 1024;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int l16 = lane & 15;
-    const int c0 = blockIdx.x * (16 * NF), r0 = blockIdx.y * (16 * MR);
+    const int bc = (blockIdx.x >> 3) / a.tiles_r * 8 + (blockIdx.x & 7);   // all rows of a feature group on one XCD: they share its weights
+    if (bc >= a.tiles_c) return;
+    const int c0 = bc * (16 * NF), r0 = (blockIdx.x >> 3) % a.tiles_r * (16 * MR);
     const int stages = (a.nk + 63) >> 6, s0 = (int)((int64_t)stages * wave / waves), s1 = (int)((int64_t)stages * (wave + 1) / waves);
     Loader<LW, 64, false> lw;
     Loader<2 * MR, 64, false> lx;
@@ -837,42 +841,38 @@ static size_t tile_lds(int shape)
     const size_t ring = 2 * (s.bc + s.br) * 128, out = (size_t)s.wr * 32 * (s.bc + 4) * 4;
     return ring > out ? ring : out;
 }
-template <typename T> static void (*few_kernel(int nf, int mr, int gated))(const DlfFfArgs)
-{
-    if (gated) return mr == 1 ? k_ff_few<T, 1, 1, true> : mr == 2 ? k_ff_few<T, 1, 2, true> : k_ff_few<T, 1, 4, true>;
-    if (nf == 1) return mr == 1 ? k_ff_few<T, 1, 1, false> : mr == 2 ? k_ff_few<T, 1, 2, false> : k_ff_few<T, 1, 4, false>;
-    return mr == 1 ? k_ff_few<T, 2, 1, false> : mr == 2 ? k_ff_few<T, 2, 2, false> : k_ff_few<T, 2, 4, false>;
-}
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
 {
-    if (gated) return mr == 1 ? k_ff_rows<T, 1, 1, true> : mr == 2 ? k_ff_rows<T, 1, 2, true> : k_ff_rows<T, 1, 4, true>;
-    if (nf == 1) return mr == 1 ? k_ff_rows<T, 1, 1, false> : mr == 2 ? k_ff_rows<T, 1, 2, false> : k_ff_rows<T, 1, 4, false>;
-    return mr == 1 ? k_ff_rows<T, 2, 1, false> : mr == 2 ? k_ff_rows<T, 2, 2, false> : k_ff_rows<T, 2, 4, false>;
+    if (gated) return mr == 1 ? k_ff_rows<T, 1, 1, true> : k_ff_rows<T, 1, 2, true>;
+    return nf == 1 ? mr == 1 ? k_ff_rows<T, 1, 1, false> : k_ff_rows<T, 1, 2, false> : k_ff_rows<T, 2, 2, false>;
 }
-extern "C" int dlf_ff_start_rows(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream)
+template <typename T> static void (*few_kernel(int nf, int mr, int gated))(const DlfFfArgs)
 {
-    hipLaunchKernelGGL(dtype == DLF_F16 ? rows_kernel<F16>(nf, mr, gated) : rows_kernel<BF16>(nf, mr, gated),
-                       dim3((unsigned)((a->nc + 16 * nf - 1) / (16 * nf)), (unsigned)((a->nr + 16 * mr - 1) / (16 * mr))), dim3((unsigned)waves * 64),
-                       (size_t)DLF_FF_ROWS_LDS(waves, nf, mr, gated), (hipStream_t)stream, *a);
-    return (int)hipGetLastError();
+    if (gated) return mr == 1 ? k_ff_few<T, 1, 1, true> : k_ff_few<T, 1, 2, true>;
+    return nf == 1 ? mr == 1 ? k_ff_few<T, 1, 1, false> : k_ff_few<T, 1, 2, false> : k_ff_few<T, 2, 2, false>;
 }
-extern "C" int dlf_ff_start_few(const DlfFfArgs* a, int dtype, int gated, int nf, int mr, int waves, void* stream)
+extern "C" int dlf_ff_start_few(const DlfFfArgs* a, const DlfFfFew* c, int dtype, int gated, void* stream)
 {
-    hipLaunchKernelGGL(dtype == DLF_F16 ? few_kernel<F16>(nf, mr, gated) : few_kernel<BF16>(nf, mr, gated),
-                       dim3((unsigned)((a->nc + 16 * nf - 1) / (16 * nf)), (unsigned)((a->nr + 16 * mr - 1) / (16 * mr))), dim3((unsigned)waves * 64),
-                       (size_t)waves * nf * mr * (gated ? 2 : 1) * 1024, (hipStream_t)stream, *a);
+    const int nf = c->nf, mr = c->mr;
+    DlfFfArgs b = *a;
+    b.tiles_r = (a->nr + 16 * mr - 1) / (16 * mr);
+    b.tiles_c = (a->nc + 16 * nf - 1) / (16 * nf);
+    const dim3 grid((unsigned)((b.tiles_c + 7) / 8 * 8 * b.tiles_r)), block((unsigned)c->waves * 64);
+    if (c->rows)
+        hipLaunchKernelGGL(dtype == DLF_F16 ? rows_kernel<F16>(nf, mr, gated) : rows_kernel<BF16>(nf, mr, gated), grid, block,
+                           (size_t)DLF_FF_ROWS_LDS(c->waves, nf, mr, gated), (hipStream_t)stream, b);
+    else
+        hipLaunchKernelGGL(dtype == DLF_F16 ? few_kernel<F16>(nf, mr, gated) : few_kernel<BF16>(nf, mr, gated), grid, block,
+                           (size_t)c->waves * nf * mr * (gated ? 2 : 1) * 1024, (hipStream_t)stream, b);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ff_kernels_init(void)
 {
-    for (int k = 0; k < 18; ++k) {
-        const int mr = 1 << k / 6, nf = k / 2 % 3 == 1 ? 2 : 1, gated = k / 2 % 3 == 2;
-        auto f = (k & 1) ? few_kernel<BF16>(nf, mr, gated) : few_kernel<F16>(nf, mr, gated);
-        const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * 2 * mr * 1024);
+    for (int k = 0; k < 10; ++k) {
+        const int gated = k / 2 < 2, nf = k / 2 == 4 ? 2 : 1, mr = k / 2 == 0 || k / 2 == 2 ? 1 : 2;
+        auto f = (k & 1) ? rows_kernel<BF16>(nf, mr, gated) : rows_kernel<F16>(nf, mr, gated);
+        const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, DLF_FF_ROWS_LDS(8, nf, mr, gated));
         if (e != hipSuccess) return (int)e;
-        auto g = (k & 1) ? rows_kernel<BF16>(nf, mr, gated) : rows_kernel<F16>(nf, mr, gated);
-        const hipError_t e2 = hipFuncSetAttribute((const void*)g, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e2 != hipSuccess) return (int)e2;
     }
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
         for (int k = 0; k < 8; ++k) {
