@@ -55,7 +55,7 @@ struct DlfFfSumArgs {
 // Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and its waves.
 struct DlfFfShape { int bc, br, wc, wr; };
 enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_NUM_SHAPES = 2 };
-static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 4, 2}, {128, 128, 2, 2}};
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2}, {128, 128, 2, 2}};
 
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64

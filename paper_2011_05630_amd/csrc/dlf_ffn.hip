@@ -42,16 +42,35 @@ __device__ __forceinline__ float sigmoid(float x)
     const float p = __builtin_amdgcn_exp2f(t);
     return __builtin_amdgcn_rcpf(1.0f + p * __builtin_fmaf(d, 0.693147182f, 1.0f));   // p may be infinite: the factor is not 0
 }
+// The normal distribution's density (without its factor 1 / sqrt(2 pi)) and distribution function: Phi(-|z|) = exp(-z^2 / 2) erfcx(a) / 2 with
+// a = |z| / sqrt(2) and erfcx(a) = exp(a^2) erfc(a), which is t times a polynomial in t = 1 / (1 + 0.4 a) to 1.3e-7 of its value (a
+// least-squares fit of degree 8 at Chebyshev nodes), so the far tail keeps its relative precision.  The library's erff costs a 4096 x 4096 tile
+// product 25 us, this 9.
+__device__ __forceinline__ float normal_cdf(float z, float& density)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(z), 0.282842712f, 1.0f));
+    float p = 0.0501872883f;
+    p = __builtin_fmaf(p, t, -0.182615347f);
+    p = __builtin_fmaf(p, t, 0.168643858f);
+    p = __builtin_fmaf(p, t, -0.00525540996f);
+    p = __builtin_fmaf(p, t, 0.141277341f);
+    p = __builtin_fmaf(p, t, 0.168578172f);
+    p = __builtin_fmaf(p, t, 0.207838584f);
+    p = __builtin_fmaf(p, t, 0.225669773f);
+    p = __builtin_fmaf(p, t, 0.225675861f);
+    density = __builtin_amdgcn_exp2f(z * z * -0.721347520f);
+    const float tail = 0.5f * t * p * density;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
 #define GELU_2C 1.59576912f       // 2 sqrt(2 / pi): 0.5 (1 + tanh(y)) = 1 / (1 + exp(-2 y))
 #define GELU_A 0.044715f
-#define SQRT_HALF 0.707106769f
 #define INV_SQRT_2PI 0.398942280f
 
 template <int ACT> __device__ __forceinline__ float act_of(float z)
 {
     if constexpr (ACT == DLF_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if constexpr (ACT == DLF_ACT_RELU6) return z < 0.0f ? 0.0f : z > 6.0f ? 6.0f : z;
-    if constexpr (ACT == DLF_ACT_GELU) return 0.5f * z * (1.0f + erff(z * SQRT_HALF));
+    if constexpr (ACT == DLF_ACT_GELU) { float density; return z * normal_cdf(z, density); }
     if constexpr (ACT == DLF_ACT_GELU_TANH) return z * sigmoid(GELU_2C * (z + GELU_A * z * z * z));
     if constexpr (ACT == DLF_ACT_SILU) return z * sigmoid(z);
     if constexpr (ACT == DLF_ACT_SIGMOID) return sigmoid(z);
@@ -67,9 +86,10 @@ template <int ACT> __device__ __forceinline__ void act_grad_of(float z, float& a
         d = z <= 0.0f || z >= 6.0f ? 0.0f : z == z ? 1.0f : z;
     }
     if constexpr (ACT == DLF_ACT_GELU) {
-        const float c = 0.5f * (1.0f + erff(z * SQRT_HALF));
+        float density;
+        const float c = normal_cdf(z, density);
         a = z * c;
-        d = __builtin_fmaf(z, INV_SQRT_2PI * expf(-0.5f * z * z), c);
+        d = __builtin_fmaf(z, INV_SQRT_2PI * density, c);
     }
     if constexpr (ACT == DLF_ACT_GELU_TANH) {
         const float s = sigmoid(GELU_2C * (z + GELU_A * z * z * z));
@@ -188,6 +208,59 @@ __device__ __forceinline__ void finish(const DlfFfArgs& a, int prob, int r, int 
     store_some<T, V>(a.out[prob], (int64_t)r * a.ldo + c, n, v);
 }
 
+// ... of N units of eight outputs that all exist, `step` rows apart: their loads share a wait.
+template <typename T, bool GATED, int N>
+__device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r, int step, int c, float (&v)[N][8], float (&u)[N][8])
+{
+    typename T::v8 q[N];
+    if (a.res != nullptr) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = load8<T>(a.res, (int64_t)(r + k * step) * a.ldres + c, 8);
+    }
+    if (a.bias[0] != nullptr) {
+        float b[8];
+        load_floats(a.bias[0] + c, 8, b);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] += b[i];
+    }
+    if (GATED && a.bias[1] != nullptr) {
+        float b[8];
+        load_floats(a.bias[1] + c, 8, b);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[k][i] += b[i];
+    }
+    if (a.saved != nullptr) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            store_floats(a.saved + (int64_t)(r + k * step) * a.nc + c, 8, v[k]);
+            if (GATED) store_floats(a.saved + ((int64_t)a.nr + r + k * step) * a.nc + c, 8, u[k]);
+        }
+    }
+    if (a.act != DLF_ACT_NONE)
+        with_act(a.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[k][i] = act_of<decltype(act)::value>(v[k][i]);
+        });
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (GATED) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] *= u[k][i];
+        }
+        if (a.res != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] += (float)q[k][i];
+        }
+        store_some<T, 8>(a.out[prob], (int64_t)(r + k * step) * a.ldo + c, 8, v[k]);
+    }
+}
+
 // ------------------------------------------------------------------------------------------------
 // k_ff_any: the product for operands of any alignment, stride and size.  A workgroup of four waves computes 64 x 64 of C (gated: of
 // both projections); 32 k at a time pass through registers into LDS, where every operand lies with k along the row, the next 32 being
@@ -288,7 +361,8 @@ __global__ __launch_bounds__(256) void k_ff_any(const DlfFfArgs a)
 //     stage in registers: there it waits for its part of the next stage (requested a whole stage ago) and for the other waves, and
 //     requests the stage after that into the LDS just read, so that the fourth step's multiplications cover the first reads
 //     of the next stage and the barrier.
-//   The epilogue goes through LDS in passes of 32 rows per wave, so that stores are whole lines and the activations unrolled once.
+//   The epilogue goes through LDS, 32 rows of a wave at a time, so that stores are whole lines and the code of the activations is there
+//     once; a lane's loads for several rows go out together (one after the other they made the epilogue of 256 x 256 take 16 us).
 // Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, in bands of four rows of tiles, and its workgroups share operands
 // in its L2.
 // ------------------------------------------------------------------------------------------------
@@ -299,13 +373,13 @@ typedef short s8v __attribute__((ext_vector_type(8)));
 extern __shared__ __attribute__((aligned(16))) char ff_lds[];
 typedef __attribute__((address_space(3))) char lds_char;
 
-__device__ __forceinline__ i4v resource(const void* p)
+__device__ __forceinline__ i4v resource(const void* p, int bytes = 0x7fffffff)
 {
     const unsigned long long v = (unsigned long long)p;
     i4v r;
     r.x = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
     r.y = __builtin_amdgcn_readfirstlane((int)((unsigned)(v >> 32) & 0xffffu));
-    r.z = 0x7fffffff;
+    r.z = bytes;
     r.w = 0x00020000;
     return r;
 }
@@ -316,19 +390,22 @@ __device__ __forceinline__ void line_to_lds(const i4v& base, int off, unsigned d
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(base), "s"(dst) : "memory");
 }
 #define WAIT_LDS 0xc07f          // s_waitcnt lgkmcnt(0)
-#define WAIT_ALL 0x0070          // s_waitcnt vmcnt(0) lgkmcnt(0); known to the compiler, unlike an instruction in assembly
+// s_waitcnt vmcnt(N) lgkmcnt(0); known to the compiler, unlike an instruction in assembly
+#define WAIT_LOADS_AND_LDS(N) (0x0070 | ((N) & 15) | ((N) >> 4) << 14)
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
+// What the 16-byte parts of row `row` are kept at, of KB k a row (32 or 64): position c ^ swizzle.
+template <int KB> __device__ __forceinline__ int swizzle(int row) { return KB == 64 ? row >> 1 & 7 : row >> 2 & 3; }
 // One operand's way from memory into LDS: a wave's N instructions of a stage.  ROWS of the operand per tile; TR: k across the rows.
-template <int N, int ROWS, bool TR> struct Loader {
-    static constexpr int CPL = TR ? ROWS / 8 : 8;      // 16-byte parts of a line in LDS
+template <int N, int ROWS, bool TR, int KB> struct Loader {
+    static constexpr int CPL = TR ? ROWS / 8 : KB / 8;      // 16-byte parts of a line in LDS
     int off[N];
     // first: the wave's first instruction; avail: rows of the operand from the tile's first on; half: gated P, see below
     __device__ __forceinline__ static int line(int first, int i) { return (first + i) * (64 / CPL) + (threadIdx.x & 63) / CPL; }
     __device__ __forceinline__ static int part(int first, int i)
     {
         const int l = line(first, i), p = (threadIdx.x & 63) % CPL;
-        if (!TR) return p ^ ((l >> 1) & 7);
+        if (!TR) return p ^ swizzle<KB>(l);
         return p ^ ((((l & 3) | ((l >> 3) & 1) << 2) & (ROWS / 32 - 1)) << 2);
     }
     template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
@@ -342,6 +419,12 @@ template <int N, int ROWS, bool TR> struct Loader {
             else off[i] = p * 8 < avail ? (int)(l * ld + p * 8) * 2 : OOB;
         }
     }
+    // zeros for what lies behind the operand's last k_left k of a stage
+    __device__ __forceinline__ void mask(int first, int k_left)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) off[i] = (TR ? line(first, i) : part(first, i) * 8) < k_left ? off[i] : OOB;
+    }
     template <bool TAIL> __device__ __forceinline__ void issue(const i4v& base, int first, unsigned dst, int k_left) const
     {
 #pragma unroll
@@ -350,14 +433,14 @@ template <int N, int ROWS, bool TR> struct Loader {
     }
 };
 // ... and from LDS into registers: the fragment of 32 rows and 16 k as the matrix instruction takes it (lane l: row l % 32, k = 8 (l / 32) + 0 .. 7).
-template <typename T, int ROWS, bool TR> struct Reader {
+template <typename T, int ROWS, bool TR, int KB> struct Reader {
     unsigned at[4];         // byte offsets, by step of 16 k (k along the rows) or by block of 32 rows (across)
     __device__ __forceinline__ void setup(int row0)
     {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (!TR) at[i] = (row0 + l32) * 128 + (((2 * i + lhi) ^ ((l32 >> 1) & 7)) << 4);
+            if (!TR) at[i] = (row0 + l32) * (KB * 2) + (((2 * i + lhi) ^ swizzle<KB>(l32)) << 4);
             else {
                 const int f = ((lane >> 2 & 3) | lhi << 2) & (ROWS / 32 - 1);
                 at[i] = (lhi * 8 + (lane >> 2 & 3)) * (ROWS * 2) + (((row0 / 32 + i) ^ f) << 6) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
@@ -367,7 +450,7 @@ template <typename T, int ROWS, bool TR> struct Reader {
     __device__ __forceinline__ typename T::v8 get(unsigned stage, int step, int block) const
     {
         if constexpr (!TR) {
-            return *(const __attribute__((address_space(3))) typename T::v8*)((const lds_char*)ff_lds + (stage + at[step] + block * 4096));
+            return *(const __attribute__((address_space(3))) typename T::v8*)((const lds_char*)ff_lds + (stage + at[step] + block * (KB * 64)));
         } else {
             const unsigned a = stage + at[block] + step * (16 * ROWS * 2);
             const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)((lds_char*)ff_lds + a));
@@ -385,15 +468,16 @@ template <int I, int N, typename F> __device__ __forceinline__ void static_for(F
     }
 }
 
-template <typename T, int BC, int BR, int WC, int WR, bool PT, bool QT, bool GATED>
-__global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool PT, bool QT, bool GATED>
+__global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) void k_ff_tile(const DlfFfArgs a)
 {
     typedef typename T::v8 v8;
-    constexpr int NW = WC * WR, FC = BC / WC / 32, FR = BR / WR / 32, LP = BC / 8 / NW, LQ = BR / 8 / NW;
-    constexpr unsigned QOFF = BC * 128, STAGE = (BC + BR) * 128;
-    constexpr int READS = FC * (PT ? 2 : 1) + FR * (QT ? 2 : 1), RPM = (READS + FC * FR - 2) / (FC * FR - 1);   // reads of a step; per multiplication
-    static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1, "");
-    static_assert(!GATED || (LP == 4 && FC == 2 && !PT), "a wave's loads of a gated tile belong to one projection, its two blocks to both");
+    constexpr int NW = WC * WR, FC = BC / WC / 32, FR = BR / WR / 32, KS = KB / 16;
+    constexpr unsigned QOFF = BC * KB * 2, STAGE = (BC + BR) * KB * 2;
+    constexpr int LP = BC * KB / 512 / NW, LQ = BR * KB / 512 / NW;
+    static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1 && KS % 2 == 0, "");
+    constexpr bool TWO = GATED && LP * 512 / KB == 64;     // a wave's loads of a gated tile: 32 lines of either projection, or of both
+    static_assert(!GATED || ((TWO || LP * 512 / KB == 32) && FC % 2 == 0 && !PT), "");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
     const int wc = wave % WC, wr = wave / WC;
     // tile
@@ -406,39 +490,60 @@ __global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
     constexpr int CF = GATED ? BC / 2 : BC;            // columns of C per tile
     const int r0 = (band * 4 + in % rows) * BR, c0 = in / rows * CF;
 
-    Loader<LP, BC, PT> lp;
-    Loader<LQ, BR, QT> lq;
-    lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
-    lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
-    Reader<T, BC, PT> rp;
-    Reader<T, BR, QT> rq;
+    Loader<LP, BC, PT, KB> lp;
+    Loader<LQ, BR, QT, KB> lq;
+    Reader<T, BC, PT, KB> rp;
+    Reader<T, BR, QT, KB> rq;
     rp.setup(wc * FC * 32);
     rq.setup(wr * FR * 32);
     const int64_t p0 = PT ? (int64_t)c0 : (int64_t)c0 * a.ldp, q0 = QT ? (int64_t)r0 : (int64_t)r0 * a.ldq;
-    const int64_t pstep = PT ? 128 * a.ldp : 128, qstep = QT ? 128 * a.ldq : 128;   // bytes
-    const char *pb, *qb;
+    const int64_t pstep = (PT ? a.ldp : 1) * (KB * 2), qstep = (QT ? a.ldq : 1) * (KB * 2);   // bytes
+    const char *pb, *qb, *ub = nullptr;
     int k_left;
     auto segment = [&](int w) __attribute__((always_inline)) {
-        pb = (const char*)a.p[GATED ? wave & 1 : w] + p0 * 2;
-        qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2;
-        k_left = a.nk;
+        pb = (const char*)a.p[GATED ? TWO ? 0 : wave & 1 : w] + p0 * 2 - pstep;
+        if (TWO) ub = (const char*)a.p[1] + p0 * 2 - pstep;
+        qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2 - qstep;
+        k_left = a.nk + KB;
+        lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
+        lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
     };
     segment(a.problems == 2 ? prob : 0);
     const unsigned lds0 = (unsigned)(size_t)(lds_char*)ff_lds;
-    auto issue = [&](unsigned stage) __attribute__((always_inline)) {
-        if (k_left <= 0) segment(1);
-        if (k_left >= 64) {
-            lp.template issue<false>(resource(pb), wave * LP, lds0 + stage, 64);
-            lq.template issue<false>(resource(qb), wave * LQ, lds0 + stage + QOFF, 64);
-        } else {                            // k beyond the operands' last are zeros
-            lp.template issue<true>(resource(pb), wave * LP, lds0 + stage, k_left);
-            lq.template issue<true>(resource(qb), wave * LQ, lds0 + stage + QOFF, k_left);
+    // The next stage's requests: first where they start, then one after the other, load 0 .. LP + LQ - 1.  Behind the last stage they
+    // go on with resources of no bytes (zeros into LDS that nobody reads), so that the loop below has one form.
+    i4v pres, qres, ures;
+    int limit = 0x7fffffff, segments = a.segments;
+    auto next = [&]() __attribute__((always_inline)) {
+        k_left -= KB;
+        if (k_left < KB) {
+            if (k_left <= 0) {
+                if (--segments > 0) {
+                    segment(1);
+                    k_left -= KB;
+                } else {
+                    limit = 0;
+                }
+            }
+            if (k_left < KB) {
+                lp.mask(wave * LP, k_left);
+                lq.mask(wave * LQ, k_left);
+            }
         }
         pb += pstep;
         qb += qstep;
-        k_left -= 64;
+        pres = resource(pb, limit);
+        if (TWO) {
+            ub += pstep;
+            ures = resource(ub, limit);
+        }
+        qres = resource(qb, limit);
     };
-    const int total = (a.nk + 63) / 64 * a.segments;
+    auto load = [&](unsigned stage, int i) __attribute__((always_inline)) {
+        if (i < LP) line_to_lds(TWO && i >= LP / 2 ? ures : pres, lp.off[i], lds0 + stage + (unsigned)(wave * LP + i) * 1024);
+        else line_to_lds(qres, lq.off[i - LP], lds0 + stage + QOFF + (unsigned)(wave * LQ + i - LP) * 1024);
+    };
+    const int total = (a.nk + KB - 1) / KB * a.segments;
     f16v acc[FC][FR];
 #pragma unroll
     for (int i = 0; i < FC; ++i)
@@ -447,86 +552,111 @@ __global__ __launch_bounds__(WC * WR * 64, 2) void k_ff_tile(const DlfFfArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     v8 fp[2][FC], fq[2][FR];
-    auto read = [&](unsigned stage, int step, int set) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < FC; ++i) fp[set][i] = rp.get(stage, step, i);
-#pragma unroll
-        for (int j = 0; j < FR; ++j) fq[set][j] = rq.get(stage + QOFF, step, j);
+    auto read = [&](unsigned stage, int step, int set, int i) __attribute__((always_inline)) {
+        if (i < FC) fp[set][i] = rp.get(stage, step, i);
+        else fq[set][i - FC] = rq.get(stage + QOFF, step, i - FC);
     };
-    // the reads of the next step's operands go out between the first multiplications of this one
-    auto interleave = [&]() __attribute__((always_inline)) {
-        static_for<0, FC * FR>([](auto i) __attribute__((always_inline)) {
-            if constexpr (decltype(i)::value * RPM < READS) __builtin_amdgcn_sched_group_barrier(0x100, RPM, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    // A step's multiplications, between them the reads of the step after it (rstep of the stage at rstage) and the requests [l0, l1)
+    // for the stage at lstage: a wave that sent them all at once would wait for the memory pipe, and its multiplications with it.
+    constexpr int M = FC * FR;
+    auto step = [&](int set, bool reads, unsigned rstage, int rstep, unsigned lstage, int l0, int l1) __attribute__((always_inline)) {
+        constexpr int RPM = (FC + FR + M - 2) / (M - 1);     // reads in front of a multiplication
+        static_for<0, M>([&](auto mc) __attribute__((always_inline)) {
+            constexpr int m = decltype(mc)::value, i = m / FR, j = m % FR;
+            if (reads) {
+#pragma unroll
+                for (int r = m * RPM; r < (m + 1) * RPM; ++r)
+                    if (r < FC + FR) read(rstage, rstep, set ^ 1, r);
+            }
+            acc[i][j] = T::mma(fp[set][i], fq[set][j], acc[i][j]);
+#pragma unroll
+            for (int l = l0 + m * (l1 - l0) / M; l < l0 + (m + 1) * (l1 - l0) / M; ++l) load(lstage, l);
+            __builtin_amdgcn_sched_barrier(0);
         });
     };
-    auto multiply = [&](int set) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < FC; ++i)
-#pragma unroll
-            for (int j = 0; j < FR; ++j) acc[i][j] = T::mma(fp[set][i], fq[set][j], acc[i][j]);
-    };
-    auto steps012 = [&](unsigned stage) __attribute__((always_inline)) {
-#pragma unroll
-        for (int step = 0; step < 3; ++step) {
-            read(stage, step + 1, (step + 1) & 1);
-            multiply(step & 1);
-            interleave();
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
+    // A stage's requests by the step that they go out in: the last of the stage that makes room for them, and the first of the next.
+    constexpr int NL = LP + LQ, L0 = KS == 2 ? (NL + 1) / 2 : (3 * NL + 7) / 8, L1 = KS == 2 ? NL : (6 * NL + 7) / 8;
     if (total > 0) {
-        issue(0);
-        if (total > 1) {
-            issue(STAGE);
-            wait_loads<LP + LQ>();
-        } else {
-            wait_loads<0>();
+#pragma unroll
+        for (int i = 0; i < RING; ++i) {
+            next();
+#pragma unroll
+            for (int l = 0; l < (i < RING - 1 ? NL : L0); ++l) load(i * STAGE, l);
         }
+        wait_loads<(RING - 2) * NL + L0>();
         asm volatile("s_barrier" ::: "memory");
-        unsigned cur = 0;
-        read(cur, 0, 0);
+        unsigned cur = 0, last = (RING - 1) * STAGE;
+#pragma unroll
+        for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
         for (int s = 0; s < total - 1; ++s) {
-            steps012(cur);
-            // this wave's reads of the stage have arrived, and so has its part of the next one
-            __builtin_amdgcn_s_waitcnt(WAIT_ALL);
-            asm volatile("s_barrier" ::: "memory");
-            if (s + 2 < total) issue(cur);
-            cur = STAGE - cur;
-            read(cur, 0, 0);
-            multiply(1);
-            interleave();
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        steps012(cur);
-        multiply(1);
-    }
-    // ---- epilogue: 32 rows of every wave at a time through LDS ----
-    constexpr int CROW = BC + 4;                        // floats
-    float* const lf = (float*)ff_lds;                   // [WR * 32][CROW]
-#pragma unroll
-    for (int j = 0; j < FR; ++j) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < FC; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *(f4v*)(lf + (wr * 32 + l32) * CROW + (wc * FC + i) * 32 + q * 8 + lhi * 4) =
-                    f4v{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-        __syncthreads();
-#pragma unroll 1
-        for (int i = threadIdx.x; i < WR * 32 * CF / 8; i += NW * 64) {
-            const int lr = i / (CF / 8), c = i % (CF / 8) * 8, r = r0 + (lr >> 5) * (FR * 32) + j * 32 + (lr & 31);
-            if (r >= a.nr || c0 + c >= a.nc) continue;
-            float v[8], u[8];
-            const float* const src = lf + lr * CROW + (GATED ? (c >> 5) * 64 + (c & 31) : c);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                *(f4v*)(v + e * 4) = *(const f4v*)(src + e * 4);
-                if (GATED) *(f4v*)(u + e * 4) = *(const f4v*)(src + 32 + e * 4);
+            step(0, true, cur, 1, last, L0, L1);
+            if constexpr (KS == 4) {
+                step(1, true, cur, 2, last, L1, NL);
+                step(0, true, cur, 3, 0, 0, 0);
             }
-            finish<T, GATED, 8>(a, prob, r, c0 + c, a.nc - c0 - c, v, u);
+            // this wave's reads of the stage have arrived, and so has its part of the next one
+            __builtin_amdgcn_s_waitcnt(WAIT_LOADS_AND_LDS((RING - 2) * NL));
+            asm volatile("s_barrier" ::: "memory");
+            next();
+            last = cur;
+            cur = cur == (RING - 1) * STAGE ? 0 : cur + STAGE;
+            step(1, true, cur, 0, last, 0, L0);
         }
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+        step(1, false, 0, 0, 0, 0, 0);
+        wait_loads<0>();
+    }
+    // ---- epilogue: 32 rows at a time through an area of LDS that is the wave's own ----
+    constexpr int CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;       // columns of the wave, floats of an LDS row, columns of C
+    constexpr int LPR = CO / 8, RPU = 64 / LPR, UNITS = 32 / RPU;              // lanes to a row, rows that they cover at a time
+    float* const lf = (float*)ff_lds + wave * (32 * CROW);
+    const int cw = lane % LPR * 8, c = c0 + wc * CO + cw, rw = lane / LPR;
+    const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
+    const bool whole = r0 + BR <= a.nr && c0 + CF <= a.nc;                     // uniform over the workgroup
+    __syncthreads();
+#pragma unroll 1
+    for (int j = 0; j < FR; ++j) {
+        static_for<0, FR>([&](auto jc) __attribute__((always_inline)) {        // (accumulators have no index at run time)
+            constexpr int J = decltype(jc)::value;
+            if (j == J) {
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *(f4v*)(lf + l32 * CROW + i * 32 + q * 8 + lhi * 4) =
+                            f4v{acc[i][J][q * 4], acc[i][J][q * 4 + 1], acc[i][J][q * 4 + 2], acc[i][J][q * 4 + 3]};
+            }
+        });
+        __builtin_amdgcn_wave_barrier();
+        const int r = r0 + (wr * FR + j) * 32 + rw;
+        if (whole) {
+            constexpr int AT = UNITS < 4 ? UNITS : 4;                          // units whose waits are shared
+#pragma unroll 1
+            for (int u = 0; u < UNITS; u += AT) {
+                float v[AT][8], w[AT][8];
+#pragma unroll
+                for (int k = 0; k < AT; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        *(f4v*)(v[k] + e * 4) = *(const f4v*)(src + (u + k) * RPU * CROW + e * 4);
+                        if (GATED) *(f4v*)(w[k] + e * 4) = *(const f4v*)(src + (u + k) * RPU * CROW + 32 + e * 4);
+                    }
+                finish_many<T, GATED, AT>(a, prob, r + u * RPU, RPU, c, v, w);
+            }
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < UNITS; ++u) {
+                float v[8], w[8];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    *(f4v*)(v + e * 4) = *(const f4v*)(src + u * RPU * CROW + e * 4);
+                    if (GATED) *(f4v*)(w + e * 4) = *(const f4v*)(src + u * RPU * CROW + 32 + e * 4);
+                }
+                if (r + u * RPU < a.nr && c < a.nc) finish<T, GATED, 8>(a, prob, r + u * RPU, c, a.nc - c, v, w);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -661,8 +791,8 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
     if (bc >= a.tiles_c) return;
     const int c0 = bc * (16 * NF), r0 = (blockIdx.x >> 3) % a.tiles_r * (16 * MR);
     const int stages = (a.nk + 63) >> 6, s0 = (int)((int64_t)stages * wave / waves), s1 = (int)((int64_t)stages * (wave + 1) / waves);
-    Loader<LW, 64, false> lw;
-    Loader<2 * MR, 64, false> lx;
+    Loader<LW, 64, false, 64> lw;
+    Loader<2 * MR, 64, false, 64> lx;
     lw.template setup<false>(0, a.nc - c0, a.ldp);
     lx.template setup<false>(0, a.nr - r0, a.ldq);
     const char* wb[2] = {(const char*)a.p[0] + (int64_t)c0 * a.ldp * 2, GATED ? (const char*)a.p[1] + (int64_t)c0 * a.ldp * 2 : nullptr};
@@ -821,24 +951,32 @@ extern "C" int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int g
                        dim3((unsigned)(a->tiles_r * a->tiles_c * a->problems)), dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
+#define K256 64
+#define R256 2
+#define K128 64
+#define R128 2
+#define W128 2, 2
+#ifndef W256
+#define W256 2, 2
+#endif
 // The tile kernels by shape (DLF_FF_SHAPE_*).
-template <typename T, int BC, int BR, int WC, int WR> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
 {
-    if (gated) return k_ff_tile<T, BC, BR, WC, WR, false, false, true>;
+    if (gated) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, false, false, true>;
     switch (layout) {
-    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, false, false, false>;
-    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, true, false, false>;
-    default: return k_ff_tile<T, BC, BR, WC, WR, true, true, false>;
+    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, false, false, false>;
+    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, true, false, false>;
+    default: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, true, true, false>;
     }
 }
 template <typename T> static void (*tile_kernel(int shape, int layout, int gated))(const DlfFfArgs)
 {
-    return shape == DLF_FF_SHAPE_256 ? tile_of<T, 256, 256, 4, 2>(layout, gated) : tile_of<T, 128, 128, 2, 2>(layout, gated);
+    return shape == DLF_FF_SHAPE_256 ? tile_of<T, 256, 256, W256, K256, R256>(layout, gated) : tile_of<T, 128, 128, W128, K128, R128>(layout, gated);
 }
 static size_t tile_lds(int shape)
 {
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
-    const size_t ring = 2 * (s.bc + s.br) * 128, out = (size_t)s.wr * 32 * (s.bc + 4) * 4;
+    const size_t ring = (size_t)(shape == 0 ? K256 * R256 : K128 * R128) * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 32 * (s.bc / s.wc + 4) * 4;
     return ring > out ? ring : out;
 }
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
