@@ -29,18 +29,12 @@ struct BF16 {
 // Activations, in 32 bits.
 // ------------------------------------------------------------------------------------------------
 
-// 1 / (1 + exp(-x)).  exp(-x) = 2^t with t = -x * log2(e): the instruction gives 2^t to one unit in the last place, but a t of
-// magnitude 100 has lost seven bits of the exponent's fraction, so what the product rounds off (its low part and that of log2(e))
-// is put back as a factor 1 + d * ln(2).  The bounds keep infinities out of that correction and let NaN through.
+// 1 / (1 + exp(-x)), exp(-x) = 2^t with t = -x log2(e).  t is rounded once, which costs the exponential |t| * 2^-24 of its value: below
+// 1e-6 where the result is not within 1e-6 of 0 or 1 anyway.  (A matrix tile's epilogue is bound by vector instructions: what the
+// product rounds off, put back as a factor, took twice as many.)
 __device__ __forceinline__ float sigmoid(float x)
 {
-    float n = -x;
-    n = n > 126.0f ? 126.0f : n;
-    n = n < -126.0f ? -126.0f : n;
-    const float t = n * 1.44269502f;
-    const float d = __builtin_fmaf(n, 1.92596299e-8f, __builtin_fmaf(n, 1.44269502f, -t));
-    const float p = __builtin_amdgcn_exp2f(t);
-    return __builtin_amdgcn_rcpf(1.0f + p * __builtin_fmaf(d, 0.693147182f, 1.0f));   // p may be infinite: the factor is not 0
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269502f));
 }
 // The normal distribution's density (without its factor 1 / sqrt(2 pi)) and distribution function: Phi(-|z|) = exp(-z^2 / 2) erfcx(a) / 2 with
 // a = |z| / sqrt(2) and erfcx(a) = exp(a^2) erfc(a), which is t times a polynomial in t = 1 / (1 + 0.4 a) to 1.3e-7 of its value (a
@@ -71,7 +65,7 @@ template <int ACT> __device__ __forceinline__ float act_of(float z)
     if constexpr (ACT == DLF_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if constexpr (ACT == DLF_ACT_RELU6) return z < 0.0f ? 0.0f : z > 6.0f ? 6.0f : z;
     if constexpr (ACT == DLF_ACT_GELU) { float density; return z * normal_cdf(z, density); }
-    if constexpr (ACT == DLF_ACT_GELU_TANH) return z * sigmoid(GELU_2C * (z + GELU_A * z * z * z));
+    if constexpr (ACT == DLF_ACT_GELU_TANH) return z * sigmoid(z * __builtin_fmaf(z * z, GELU_2C * GELU_A, GELU_2C));
     if constexpr (ACT == DLF_ACT_SILU) return z * sigmoid(z);
     if constexpr (ACT == DLF_ACT_SIGMOID) return sigmoid(z);
     return z;
@@ -92,7 +86,7 @@ template <int ACT> __device__ __forceinline__ void act_grad_of(float z, float& a
         d = __builtin_fmaf(z, INV_SQRT_2PI * density, c);
     }
     if constexpr (ACT == DLF_ACT_GELU_TANH) {
-        const float s = sigmoid(GELU_2C * (z + GELU_A * z * z * z));
+        const float s = sigmoid(z * __builtin_fmaf(z * z, GELU_2C * GELU_A, GELU_2C));
         a = z * s;
         // s (1 - s) underflows to zero before the cubic's derivative overflows (|z| > 1e19: keep 0 * inf out)
         const float t = s * (1.0f - s);
@@ -361,7 +355,7 @@ __global__ __launch_bounds__(256) void k_ff_any(const DlfFfArgs a)
 //     stage in registers: there it waits for its part of the next stage (requested a whole stage ago) and for the other waves, and
 //     requests the stage after that into the LDS just read, so that the fourth step's multiplications cover the first reads
 //     of the next stage and the barrier.
-//   The epilogue goes through LDS, 32 rows of a wave at a time, so that stores are whole lines and the code of the activations is there
+//   The epilogue goes through LDS, 64 rows of a wave at a time, so that stores are whole lines and the code of the activations is there
 //     once; a lane's loads for several rows go out together (one after the other they made the epilogue of 256 x 256 take 16 us).
 // Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, in bands of four rows of tiles, and its workgroups share operands
 // in its L2.
@@ -607,27 +601,25 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
         step(1, false, 0, 0, 0, 0, 0);
         wait_loads<0>();
     }
-    // ---- epilogue: 32 rows at a time through an area of LDS that is the wave's own ----
-    constexpr int CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;       // columns of the wave, floats of an LDS row, columns of C
-    constexpr int LPR = CO / 8, RPU = 64 / LPR, UNITS = 32 / RPU;              // lanes to a row, rows that they cover at a time
-    float* const lf = (float*)ff_lds + wave * (32 * CROW);
+    // ---- epilogue: JB * 32 rows at a time through an area of LDS that is the wave's own ----
+    constexpr int JB = 2, CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;   // columns of the wave, floats of an LDS row, columns of C
+    constexpr int LPR = CO / 8, RPU = 64 / LPR, UNITS = JB * 32 / RPU;         // lanes to a row, rows that they cover at a time
+    static_assert(FR % JB == 0, "");
+    float* const lf = (float*)ff_lds + wave * (JB * 32 * CROW);
     const int cw = lane % LPR * 8, c = c0 + wc * CO + cw, rw = lane / LPR;
     const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
     const bool whole = r0 + BR <= a.nr && c0 + CF <= a.nc;                     // uniform over the workgroup
     __syncthreads();
-#pragma unroll 1
-    for (int j = 0; j < FR; ++j) {
-        static_for<0, FR>([&](auto jc) __attribute__((always_inline)) {        // (accumulators have no index at run time)
-            constexpr int J = decltype(jc)::value;
-            if (j == J) {
 #pragma unroll
-                for (int i = 0; i < FC; ++i)
+    for (int j = 0; j < FR; j += JB) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        *(f4v*)(lf + l32 * CROW + i * 32 + q * 8 + lhi * 4) =
-                            f4v{acc[i][J][q * 4], acc[i][J][q * 4 + 1], acc[i][J][q * 4 + 2], acc[i][J][q * 4 + 3]};
-            }
-        });
+        for (int b = 0; b < JB; ++b)
+#pragma unroll
+            for (int i = 0; i < FC; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(f4v*)(lf + (b * 32 + l32) * CROW + i * 32 + q * 8 + lhi * 4) =
+                        f4v{acc[i][j + b][q * 4], acc[i][j + b][q * 4 + 1], acc[i][j + b][q * 4 + 2], acc[i][j + b][q * 4 + 3]};
         __builtin_amdgcn_wave_barrier();
         const int r = r0 + (wr * FR + j) * 32 + rw;
         if (whole) {
@@ -976,7 +968,7 @@ template <typename T> static void (*tile_kernel(int shape, int layout, int gated
 static size_t tile_lds(int shape)
 {
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
-    const size_t ring = (size_t)(shape == 0 ? K256 * R256 : K128 * R128) * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 32 * (s.bc / s.wc + 4) * 4;
+    const size_t ring = (size_t)(shape == 0 ? K256 * R256 : K128 * R128) * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
     return ring > out ? ring : out;
 }
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
