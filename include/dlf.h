@@ -312,7 +312,7 @@ typedef struct {
     int64_t rows;               /* 0 .. 2^30                                                              */
     int32_t in_features;        /* 1 .. 2^20                                                              */
     int32_t out_features;       /* 1 .. 2^20 (gated: of either projection)                                */
-    int64_t x_stride;           /* elements from row to row, >= the row, < 2^31; 0: the row               */
+    int64_t x_stride;           /* elements from row to row, >= the row, < 2^24; 0: the row               */
     int64_t w_stride;           /* ... of weight, of w_gate and w_up                                      */
     int64_t y_stride;           /* ... of y or h                                                          */
     int64_t res_stride;         /* ... of residual (dlf_linear)                                           */

@@ -83,9 +83,11 @@ void dlf_debug_small_pair_mode(int32_t mode, int32_t shape, int32_t waves);
  * refuses its arguments.  Needs neither a GPU nor weights. */
 dlf_status dlf_debug_check_launches(const dlf_plan_t* plan);
 
-/* Testing hook: the kernel of the feed-forward operators' products: 0 = by the library's rule (default), 1 = the general
- * kernel, 2 = tiles of 256 x 256, 3 = tiles of 128 x 128, wherever the operands' alignment allows them.  Process-wide, not thread-safe. */
-void dlf_debug_ff_kernel(int32_t kernel);
+/* Testing hook: the kernels of the feed-forward operators' products: kernel 0 = by the library's rule (default), 1 = few rows always on the
+ * kernel for rows that start anywhere, 2 / 3 = tiles of 256 x 256 / 128 x 128 wherever the operands' alignment allows them, 4 = tiles of 128 x
+ * 128 through registers; splits > 0: that many workgroups share every tile's k, as far as it goes (0: by rule).  It changes the
+ * workspace that a call needs.  Process-wide, not thread-safe. */
+void dlf_debug_ff_kernel(int32_t kernel, int32_t splits);
 
 #ifdef __cplusplus
 }

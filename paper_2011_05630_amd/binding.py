@@ -155,7 +155,7 @@ def lib():
     L.dlf_i8conv_info.restype = i32
     L.dlf_i8conv_run.argtypes = [vp, vp, vp, vp]
     L.dlf_i8conv_run.restype = i32
-    L.dlf_debug_ff_kernel.argtypes = [i32]
+    L.dlf_debug_ff_kernel.argtypes = [i32, i32]
     L.dlf_debug_ff_kernel.restype = None
     ffp, sz = ctypes.POINTER(FfDesc), ctypes.c_size_t
     for name, n in (("dlf_linear", 6), ("dlf_linear_backward", 7), ("dlf_gated", 7), ("dlf_gated_backward", 10)):
@@ -477,10 +477,10 @@ def dlf_debug_small_pair_mode(mode=0, shape=-1, waves=0):
     lib().dlf_debug_small_pair_mode(mode, shape, waves)
 
 
-def dlf_debug_ff_kernel(kernel=0):
-    """Testing hook: 0 = the feed-forward operators' kernels by the library's rule, 1 = the general kernel, 2 / 3 = tiles of
-    256 x 256 / 128 x 128 wherever they apply."""
-    lib().dlf_debug_ff_kernel(kernel)
+def dlf_debug_ff_kernel(kernel=0, splits=0):
+    """Testing hook: 0 = the feed-forward operators' kernels by the library's rule, 1 = few rows on the kernel for rows that start
+    anywhere, 2 / 3 / 4 = tiles of 256 x 256 / 128 x 128 / 128 x 128 through registers; splits > 0: so many workgroups share a tile's k."""
+    lib().dlf_debug_ff_kernel(kernel, splits)
 
 
 def dlf_debug_check_launches(plan):

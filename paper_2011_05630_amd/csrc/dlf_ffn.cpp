@@ -45,12 +45,12 @@ dlf_status check_desc(const dlf_ff_desc* d, bool gated, const char* call, Ff& f)
         {&f.d.res_stride, d->out_features, "residual"}, {&f.d.dy_stride, d->out_features, "dy"}};
     for (auto& q : strides) {
         if (*q.s == 0) *q.s = q.row;
-        if (*q.s < q.row || *q.s >= (int64_t)1 << 31)
+        if (*q.s < q.row || *q.s >= (int64_t)1 << 24)
             return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %lld elements, %lld apart", call, q.name, (long long)q.row, (long long)*q.s);
     }
     // the products of the forward pass and of the gradients by the tiles of their grids
-    const int64_t t = DLF_FF_ANY_TILE, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
-    if (std::max({m * o, m * i, 2 * i * o}) >= (int64_t)1 << 24)
+    const int64_t t = 128, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
+    if (std::max({m * o * 2, m * i, 2 * i * o}) >= (int64_t)1 << 23)
         return fail(DLF_ERR_UNSUPPORTED, "%s: %lld rows, %d -> %d features are more tiles than a launch holds", call, (long long)d->rows,
                     d->in_features, d->out_features);
     return DLF_OK;
@@ -61,27 +61,6 @@ dlf_status check_ptr(const Ff& f, const void* p, const char* name, bool wanted, 
     if (!p && wanted) return fail(DLF_ERR_INVALID_ARG, "%s: null %s", f.call, name);
     if (((uintptr_t)p & (align - 1)) != 0) return fail(DLF_ERR_INVALID_ARG, "%s: %s is not aligned to %d bytes", f.call, name, (int)align);
     return DLF_OK;
-}
-
-// The workspace of a backward call.
-struct BackLayout {
-    size_t dz = 0, lddz = 0, part = 0, bytes = 0;   // offsets; elements per row of dz
-    int chunk = 0, chunks = 0;
-};
-size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
-bool needs_dz(const Ff& f) { return f.gated || f.d.act != DLF_ACT_NONE; }
-BackLayout back_layout(const Ff& f)
-{
-    BackLayout l;
-    const size_t nz = f.gated ? 2 : 1;
-    l.lddz = ((size_t)f.d.out_features + 7) / 8 * 8;
-    // rows of one partial sum: enough of them that the sums are few, few enough that the grid is not
-    l.chunk = (int)std::max<int64_t>(32, (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS);
-    l.chunks = f.d.rows > 0 ? (int)((f.d.rows + l.chunk - 1) / l.chunk) : 1;
-    if (needs_dz(f)) l.bytes = nz * align256((size_t)f.d.rows * l.lddz * 2);
-    l.part = l.bytes;
-    l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
-    return l;
 }
 
 dlf_status check_ws(const Ff& f, const void* ws, size_t have, size_t need)
@@ -104,6 +83,9 @@ dlf_status launched(const Ff& f, int e)
     return DLF_OK;
 }
 
+// Testing hook: 0 = by rule, 1 = k_ff_few wherever a few-rows kernel applies, 2 + shape = a tile kernel wherever it applies.
+int g_force = 0;
+
 std::once_flag g_once;
 int g_once_rc = 0;
 
@@ -117,17 +99,16 @@ dlf_status kernels_ready()
 // Whether the tile kernel takes an operand: rows in whole 16-byte lines, offsets inside a tile that fit 31 bits.
 bool lines(const void* p, int64_t ld, int64_t row)
 {
-    return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (row & 7) == 0 && ld < (int64_t)1 << 21;
+    return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (row & 7) == 0 && ld < (int64_t)1 << 22;
 }
 
-// Testing hook: 0 = by rule, 1 = the general kernel, 2 + shape = a tile kernel wherever it applies.
-int g_force = 0;
+
 
 // The forward product of few rows, straight from memory.
 dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
 {
     DlfFfFew c;
-    c.rows = lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+    c.rows = g_force != 1 && lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
     // Rows per workgroup: 32 rather than 64 of them even where 64 exist (gated 64 x 2048 -> 2 x 5632: 16.6 against 18.4 us), there with
     // 32 features for the reads of x (64 x 4096 -> 4096: 12.1 against 14.8 us; fewer workgroups lose below 33 rows).
     c.mr = a.nr <= 16 ? 1 : 2;
@@ -140,37 +121,119 @@ dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
     return launched(f, dlf_ff_start_few(&a, &c, f.d.dtype, gated, stream));
 }
 
-// One product of the operators.
-dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, void* stream)
+// How a product of these sizes is cut: a tile shape and the workgroups that share a tile's k.
+struct Cut {
+    int shape = DLF_FF_SHAPE_128, splits = 1, tiles_r = 0, tiles_c = 0;
+    size_t part_bytes = 0;
+};
+int g_force_splits = 0;
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+Cut cut_as(int shape, int splits, int64_t nr, int64_t nc, int problems, bool gated)
+{
+    Cut c;
+    c.shape = shape;
+    c.splits = splits;
+    c.tiles_r = ceil_div(nr, DLF_FF_SHAPES[shape].br);
+    c.tiles_c = ceil_div(nc, DLF_FF_SHAPES[shape].bc / (gated ? 2 : 1));
+    if (splits > 1) c.part_bytes = (size_t)splits * (gated ? 2 : problems) * nr * nc * 4;
+    return c;
+}
+
+// Modelled time of a cut in ns, from measurements at 4096^3 and around: a stage of 64 k takes a 256 x 256 tile 1450 ns; two 128 x 128
+// tiles that share a compute unit 900 ns, one that has it to itself 550; the first loads and the epilogue of a tile 7 and 4 us;
+// joining, a launch and the partial sums' bytes twice.
+double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+{
+    const int64_t wgs = (int64_t)c.tiles_r * c.tiles_c * problems * c.splits;
+    const double stages = (double)ceil_div(nk, 64) * segments / c.splits;
+    double t;
+    if (c.shape == DLF_FF_SHAPE_256) {
+        t = (double)ceil_div(wgs, 256) * (stages * 1450 + 7000);
+    } else {
+        t = (double)(wgs / 512) * (stages * 900 + 4000);
+        if (wgs % 512 > 256) t += stages * 900 + 4000;
+        else if (wgs % 512 > 0) t += stages * 550 + 4000;
+    }
+    if (c.splits > 1) t += 3500 + (double)c.part_bytes * 2 / 4000;
+    return t;
+}
+
+Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+{
+    Cut best;
+    double least = 0;
+    const int64_t stages = (int64_t)ceil_div(nk, 64) * segments;
+    for (int shape = DLF_FF_SHAPE_256; shape <= DLF_FF_SHAPE_128; ++shape) {
+        if (g_force >= 2 && g_force < 2 + DLF_FF_NUM_SHAPES && shape != (g_force == 2 ? DLF_FF_SHAPE_256 : DLF_FF_SHAPE_128)) continue;
+        for (int splits = 1; splits <= 16; ++splits) {
+            if (splits > 1 && stages / splits < 4) break;
+            if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;
+            const Cut c = cut_as(shape, splits, nr, nc, problems, gated);
+            const double t = cut_ns(c, nr, nc, nk, segments, problems, gated);
+            if (least == 0 || t < least) { least = t; best = c; }
+        }
+    }
+    return best;
+}
+
+bool is_few(int64_t rows) { return rows <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 1); }
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+// One product of the operators; part: the workspace of its cut.
+dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, char* part, void* stream)
 {
     TRY(kernels_ready());
-    if (layout == DLF_FF_NN && a.nr <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 2 + DLF_FF_NUM_SHAPES)) return few_rows(f, a, gated, stream);
-    bool whole = true;
+    if (layout == DLF_FF_NN && is_few(a.nr)) return few_rows(f, a, gated, stream);
+    Cut c = choose(a.nr, a.nc, a.nk, a.segments, a.problems, gated);
+    bool whole = g_force != 2 + DLF_FF_SHAPE_ANY;
     const int n = gated ? 2 : std::max(a.segments, a.problems);
     for (int i = 0; i < n; ++i) {
         whole = whole && lines(a.p[i], a.ldp, layout == DLF_FF_NN ? a.nk : a.nc);
         if (!gated) whole = whole && lines(a.q[i], a.ldq, layout == DLF_FF_TT ? a.nr : a.nk);
     }
     if (gated) whole = whole && lines(a.q[0], a.ldq, a.nk);
-    if (whole && g_force != 1) {
-        int shape = DLF_FF_SHAPE_256;
-        auto tiles = [&](int s) {
-            a.tiles_r = (a.nr + DLF_FF_SHAPES[s].br - 1) / DLF_FF_SHAPES[s].br;
-            const int cols = DLF_FF_SHAPES[s].bc / (gated ? 2 : 1);
-            a.tiles_c = (a.nc + cols - 1) / cols;
-            return a.tiles_r * a.tiles_c * a.problems;
-        };
-        if (tiles(shape) < 160) tiles(shape = DLF_FF_SHAPE_128);
-        if (g_force > 1) tiles(shape = g_force - 2);
-        return launched(f, dlf_ff_start_tile(&a, shape, f.d.dtype, layout, gated, stream));
-    }
-    a.tiles_r = (a.nr + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
-    a.tiles_c = (a.nc + DLF_FF_ANY_TILE - 1) / DLF_FF_ANY_TILE;
-    return launched(f, dlf_ff_start_any(&a, f.d.dtype, layout, gated, stream));
+    if (!whole) c = cut_as(DLF_FF_SHAPE_ANY, c.splits, a.nr, a.nc, a.problems, gated);
+    a.tiles_r = c.tiles_r;
+    a.tiles_c = c.tiles_c;
+    a.splits = c.splits;
+    a.part = (float*)part;
+    return launched(f, dlf_ff_start_tile(&a, c.shape, f.d.dtype, layout, gated, stream));
+}
+
+// The workspace of a backward call.
+struct BackLayout {
+    size_t lddz = 0, part = 0, join = 0, bytes = 0;   // elements per row of dz; offsets of the column sums and of the products' partial sums
+    int chunk = 0, chunks = 0;
+};
+bool needs_dz(const Ff& f) { return f.gated || f.d.act != DLF_ACT_NONE; }
+BackLayout back_layout(const Ff& f)
+{
+    BackLayout l;
+    const size_t nz = f.gated ? 2 : 1;
+    l.lddz = ((size_t)f.d.out_features + 7) / 8 * 8;
+    // rows of one partial sum: enough of them that the sums are few, few enough that the grid is not
+    l.chunk = (int)std::max<int64_t>(32, (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS);
+    l.chunks = f.d.rows > 0 ? (int)((f.d.rows + l.chunk - 1) / l.chunk) : 1;
+    if (needs_dz(f)) l.bytes = nz * align256((size_t)f.d.rows * l.lddz * 2);
+    l.part = l.bytes;
+    l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
+    l.join = l.bytes;
+    const int problems = f.gated ? 2 : 1;
+    l.bytes += align256(std::max(choose(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, problems, 1, false).part_bytes,
+                                 choose(f.d.out_features, f.d.in_features, f.d.rows, 1, problems, false).part_bytes));
+    return l;
+}
+
+size_t forward_ws(const Ff& f)
+{
+    if (f.d.rows == 0 || is_few(f.d.rows)) return 0;
+    return align256(choose(f.d.rows, f.d.out_features, f.d.in_features, 1, 1, f.gated).part_bytes);
 }
 
 dlf_status forward(const Ff& f, const void* x, const void* const w[2], const float* const bias[2], const void* res, void* y, float* saved,
-                   void* stream)
+                   char* ws, void* stream)
 {
     if (f.d.rows == 0) return DLF_OK;
     DlfFfArgs a;
@@ -184,7 +247,7 @@ dlf_status forward(const Ff& f, const void* x, const void* const w[2], const flo
     a.res = res; a.ldres = f.d.res_stride;
     a.out[0] = y; a.ldo = f.d.y_stride;
     a.saved = saved; a.act = f.d.act;
-    return product(f, a, DLF_FF_NN, f.gated, stream);
+    return product(f, a, DLF_FF_NN, f.gated, ws, stream);
 }
 
 dlf_status backward(const Ff& f, const void* dy, const void* x, const void* const w[2], const float* saved, void* dx, void* const dw[2],
@@ -220,7 +283,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         a.nr = (int)f.d.rows; a.nc = f.d.in_features; a.nk = f.d.out_features;
         a.segments = nz; a.problems = 1;
         a.out[0] = dx; a.ldo = f.d.in_features;
-        TRY(product(f, a, DLF_FF_TN, false, stream));
+        TRY(product(f, a, DLF_FF_TN, false, ws + l.join, stream));
     }
     memset(&a, 0, sizeof a);
     a.segments = 1;
@@ -233,7 +296,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         a.ldp = f.d.x_stride; a.ldq = lddz;
         a.nr = f.d.out_features; a.nc = f.d.in_features; a.nk = (int)f.d.rows;
         a.ldo = f.d.in_features;
-        TRY(product(f, a, DLF_FF_TT, false, stream));
+        TRY(product(f, a, DLF_FF_TT, false, ws + l.join, stream));
     }
     return DLF_OK;
 }
@@ -241,7 +304,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
 size_t forward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 {
     Ff f;
-    return check_desc(d, gated, call, f) == DLF_OK ? 0 : SIZE_MAX;
+    return check_desc(d, gated, call, f) == DLF_OK ? forward_ws(f) : SIZE_MAX;
 }
 size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 {
@@ -253,7 +316,11 @@ size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 
 extern "C" {
 
-void dlf_debug_ff_kernel(int32_t kernel) { g_force = kernel >= 0 && kernel <= 2 + DLF_FF_NUM_SHAPES ? kernel : 0; }
+void dlf_debug_ff_kernel(int32_t kernel, int32_t splits)
+{
+    g_force = kernel >= 0 && kernel < 2 + DLF_FF_NUM_SHAPES ? kernel : 0;
+    g_force_splits = splits > 0 ? splits : 0;
+}
 
 size_t dlf_linear_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, false, "dlf_linear_workspace_bytes"); }
 size_t dlf_gated_workspace_bytes(const dlf_ff_desc* d) { return forward_bytes(d, true, "dlf_gated_workspace_bytes"); }
@@ -272,10 +339,10 @@ dlf_status dlf_linear(const dlf_ff_desc* d, const void* x, const void* weight, c
     TRY(check_ptr(f, residual, "residual", false, 2));
     TRY(check_ptr(f, y, "y", some, 2));
     TRY(check_ptr(f, saved, "saved", false, 4));
-    TRY(check_ws(f, workspace, workspace_bytes, 0));
+    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     const void* w[2] = {weight, nullptr};
     const float* b[2] = {bias, nullptr};
-    return forward(f, x, w, b, residual, y, saved, hip_stream);
+    return forward(f, x, w, b, residual, y, saved, (char*)workspace, hip_stream);
 }
 
 dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, const void* w_up, const float* b_gate, const float* b_up,
@@ -291,10 +358,10 @@ dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, co
     TRY(check_ptr(f, b_up, "b_up", false, 4));
     TRY(check_ptr(f, h, "h", some, 2));
     TRY(check_ptr(f, saved, "saved", false, 4));
-    TRY(check_ws(f, workspace, workspace_bytes, 0));
+    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     const void* w[2] = {w_gate, w_up};
     const float* b[2] = {b_gate, b_up};
-    return forward(f, x, w, b, nullptr, h, saved, hip_stream);
+    return forward(f, x, w, b, nullptr, h, saved, (char*)workspace, hip_stream);
 }
 
 dlf_status dlf_linear_backward(const dlf_ff_desc* d, const void* dy, const void* x, const void* weight, const float* saved, void* dx,

@@ -21,6 +21,8 @@ struct DlfFfArgs {
     int32_t segments;       // 2: the sum runs over (p[0], q[0]) and then over (p[1], q[1])
     int32_t problems;       // 2: two products of one shape, (p[0], q[0]) -> out[0] and (p[1], q[1]) -> out[1]
     int32_t tiles_r, tiles_c;
+    int32_t splits;         // > 1: as many workgroups share a tile's k and leave their sums in part, which a second launch adds up
+    float* part;            // [splits][planes][nr][nc], planes: gate and up, or problems
     // epilogue
     const float* bias[2];
     const void* res;
@@ -48,14 +50,13 @@ struct DlfFfSumArgs {
     int32_t n, chunks;
 };
 
-// Largest column count of partial sums, workgroup tile of the general kernel.
+// Largest number of partial column sums.
 #define DLF_FF_MAX_CHUNKS 128
-#define DLF_FF_ANY_TILE 64
 
 // Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and its waves.
 struct DlfFfShape { int bc, br, wc, wr; };
-enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_NUM_SHAPES = 2 };
-static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2}, {128, 128, 2, 2}};
+enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_NUM_SHAPES = 3 };   // ANY: rows that start anywhere
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2}, {128, 128, 2, 2}, {128, 128, 2, 2}};
 
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64
@@ -69,7 +70,6 @@ extern "C" {
 int dlf_ff_kernels_init(void);
 int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_few(const DlfFfArgs* a, const DlfFfFew* c, int dtype, int gated, void* stream);
-int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream);
 int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
 int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);
 }

@@ -256,92 +256,6 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ff_any: the product for operands of any alignment, stride and size.  A workgroup of four waves computes 64 x 64 of C (gated: of
-// both projections); 32 k at a time pass through registers into LDS, where every operand lies with k along the row, the next 32 being
-// on their way meanwhile.
-// ------------------------------------------------------------------------------------------------
-template <typename T, bool PT, bool QT, bool GATED>
-__global__ __launch_bounds__(256) void k_ff_any(const DlfFfArgs a)
-{
-    typedef typename T::e e;
-    typedef typename T::v8 v8;
-    constexpr int TILE = DLF_FF_ANY_TILE, KS = 32, ROW = KS + 8, NP = GATED ? 2 : 1, CROW = TILE + 4;
-    constexpr int OPS = (NP + 1) * TILE * ROW * 2, OUT = NP * TILE * CROW * 4;
-    __shared__ __attribute__((aligned(16))) char mem[OPS > OUT ? OPS : OUT];
-    e* const ls = (e*)mem;                     // P (, second P), Q: [64][ROW]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lhi = lane >> 5;
-    int t = blockIdx.x;
-    const int per = a.tiles_r * a.tiles_c;
-    const int prob = t / per;
-    t -= prob * per;
-    const int r0 = t / a.tiles_c * TILE, c0 = t % a.tiles_c * TILE;
-    const int steps = (a.nk + KS - 1) / KS, total = steps * a.segments;
-
-    // 64 rows of 32 k, or 32 rows of 64: one chunk of eight per thread
-    const int nrow = tid >> 2, nch = (tid & 3) * 8, trow = tid >> 3, tch = (tid & 7) * 8;
-    auto chunk = [&](const void* base, int64_t ld, bool tr, int i0, int ni, int k0) __attribute__((always_inline)) -> v8 {
-        const int row = tr ? k0 + trow : i0 + nrow, col = tr ? i0 + tch : k0 + nch;
-        const int rows = tr ? a.nk : ni, cols = tr ? ni : a.nk;
-        return load8<T>(base, (int64_t)row * ld + col, row < rows ? cols - col : 0);
-    };
-    auto put = [&](e* to, bool tr, v8 v) __attribute__((always_inline)) {
-        if (!tr) {
-            *(v8*)(to + nrow * ROW + nch) = v;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) to[(tch + i) * ROW + trow] = v[i];
-        }
-    };
-    v8 np[NP], nq;
-    auto request = [&](int s) __attribute__((always_inline)) {
-        const int seg = s >= steps ? 1 : 0, k0 = (s - seg * steps) * KS, w = a.problems == 2 ? prob : seg;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) np[i] = chunk(a.p[GATED ? i : w], a.ldp, PT, c0, a.nc, k0);
-        nq = chunk(a.q[GATED ? 0 : w], a.ldq, QT, r0, a.nr, k0);
-    };
-    f16v acc[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
-    const int wc = (wave & 1) * 32, wr = (wave >> 1) * 32;
-    if (total > 0) request(0);
-    for (int s = 0; s < total; ++s) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NP; ++i) put(ls + i * TILE * ROW, PT, np[i]);
-        put(ls + NP * TILE * ROW, QT, nq);
-        __syncthreads();
-        if (s + 1 < total) request(s + 1);
-#pragma unroll
-        for (int k = 0; k < KS; k += 16) {
-            const v8 q = *(const v8*)(ls + (NP * TILE + wr + l32) * ROW + k + lhi * 8);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) acc[i] = T::mma(*(const v8*)(ls + (i * TILE + wc + l32) * ROW + k + lhi * 8), q, acc[i]);
-        }
-    }
-    // through LDS, so that a thread finishes eight consecutive c and the activations are unrolled once
-    __syncthreads();
-    float* const lf = (float*)mem;             // [NP][64 r][CROW]
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *(f4v*)(lf + (i * TILE + wr + l32) * CROW + wc + q * 8 + lhi * 4) =
-                f4v{acc[i][q * 4], acc[i][q * 4 + 1], acc[i][q * 4 + 2], acc[i][q * 4 + 3]};
-    __syncthreads();
-#pragma unroll 1
-    for (int i = tid; i < TILE * TILE / 8; i += 256) {
-        const int r = i >> 3, c = (i & 7) * 8;
-        if (r0 + r >= a.nr || c0 + c >= a.nc) continue;
-        float v[8], u[8];
-        load_floats(lf + r * CROW + c, 8, v);
-        if (GATED) load_floats(lf + (TILE + r) * CROW + c, 8, u);
-        finish<T, GATED, 8>(a, prob, r0 + r, c0 + c, a.nc - c0 - c, v, u);
-    }
-}
-
-// ------------------------------------------------------------------------------------------------
 // k_ff_tile: the product for operands whose rows are whole 16-byte lines.  A workgroup of WC x WR waves computes BC x BR of C (gated: BC / 2
 // features of both projections), a wave FC x FR blocks of 32 x 32; 64 k at a time ("stage") pass through LDS, two stages in turn.
 //   Global -> LDS: 16-byte direct loads, 1 KiB per instruction, lane l's 16 bytes at 16 l.  Rows, columns and k that do not exist
@@ -426,6 +340,44 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
             line_to_lds(base, !TAIL || (TR ? line(first, i) : part(first, i) * 8) < k_left ? off[i] : OOB, dst + (unsigned)(first + i) * 1024);
     }
 };
+// ... of rows that start anywhere: through registers, by a load and, a stage later, a write to LDS.  Rows and columns that do not exist
+// are read as others and not stored; k behind the last are zeros.
+template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
+    typedef Loader<N, ROWS, TR, KB> Map;
+    unsigned off[N];
+    typename T::v8 v[N];
+    int edge;               // columns of a tile that ends inside a part of eight, else 0
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
+    {
+        edge = TR && avail < ROWS && (avail & 7) != 0 ? avail : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int l = Map::line(first, i), p = Map::part(first, i), row = GATED ? (l >> 6) * 32 + (l & 31) : l;
+            if (!TR) off[i] = (unsigned)(min(row, avail - 1) * ld + p * 8) * 2;
+            else off[i] = (unsigned)(l * ld + (p * 8 < avail ? p * 8 : 0)) * 2;
+        }
+    }
+    __device__ __forceinline__ void load(const char* base, int first, int k_left)
+    {
+        if (k_left >= KB && edge == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base + off[i], 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int p = Map::part(first, i) * 8;
+                const int n = !TR ? k_left - p : Map::line(first, i) >= k_left ? 0 : edge > 0 ? edge - p : 8;
+                v[i] = load8<T>(base + off[i], 0, n);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(unsigned dst, int first) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            *(__attribute__((address_space(3))) typename T::v8*)((lds_char*)ff_lds + (dst + (unsigned)(first + i) * 1024 + (threadIdx.x & 63) * 16)) = v[i];
+    }
+};
 // ... and from LDS into registers: the fragment of 32 rows and 16 k as the matrix instruction takes it (lane l: row l % 32, k = 8 (l / 32) + 0 .. 7).
 template <typename T, int ROWS, bool TR, int KB> struct Reader {
     unsigned at[4];         // byte offsets, by step of 16 k (k along the rows) or by block of 32 rows (across)
@@ -462,7 +414,7 @@ template <int I, int N, typename F> __device__ __forceinline__ void static_for(F
     }
 }
 
-template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool PT, bool QT, bool GATED>
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT, bool PT, bool QT, bool GATED>
 __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) void k_ff_tile(const DlfFfArgs a)
 {
     typedef typename T::v8 v8;
@@ -475,17 +427,19 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
     const int wc = wave % WC, wr = wave / WC;
     // tile
-    const int per = a.tiles_r * a.tiles_c, all = per * a.problems, each = (all + 7) >> 3;
+    const int per = a.tiles_r * a.tiles_c, all = per * a.problems * a.splits, each = (all + 7) >> 3;
     int t = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= each || t >= all) return;
+    const int split = t / (per * a.problems);
+    t -= split * (per * a.problems);
     const int prob = t / per;
     t -= prob * per;
     const int band = t / (4 * a.tiles_c), rows = min(4, a.tiles_r - band * 4), in = t - band * 4 * a.tiles_c;
     constexpr int CF = GATED ? BC / 2 : BC;            // columns of C per tile
     const int r0 = (band * 4 + in % rows) * BR, c0 = in / rows * CF;
 
-    Loader<LP, BC, PT, KB> lp;
-    Loader<LQ, BR, QT, KB> lq;
+    typename std::conditional<DIRECT, Loader<LP, BC, PT, KB>, Stager<T, LP, BC, PT, KB>>::type lp;
+    typename std::conditional<DIRECT, Loader<LQ, BR, QT, KB>, Stager<T, LQ, BR, QT, KB>>::type lq;
     Reader<T, BC, PT, KB> rp;
     Reader<T, BR, QT, KB> rq;
     rp.setup(wc * FC * 32);
@@ -494,50 +448,58 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     const int64_t pstep = (PT ? a.ldp : 1) * (KB * 2), qstep = (QT ? a.ldq : 1) * (KB * 2);   // bytes
     const char *pb, *qb, *ub = nullptr;
     int k_left;
-    auto segment = [&](int w) __attribute__((always_inline)) {
-        pb = (const char*)a.p[GATED ? TWO ? 0 : wave & 1 : w] + p0 * 2 - pstep;
-        if (TWO) ub = (const char*)a.p[1] + p0 * 2 - pstep;
-        qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2 - qstep;
-        k_left = a.nk + KB;
+    // Requests go on with stage `at` of segment w (operand pair) at the next call of next().
+    auto segment = [&](int w, int at) __attribute__((always_inline)) {
+        pb = (const char*)a.p[GATED ? TWO ? 0 : wave & 1 : w] + p0 * 2 + (at - 1) * pstep;
+        if (TWO) ub = (const char*)a.p[1] + p0 * 2 + (at - 1) * pstep;
+        qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2 + (at - 1) * qstep;
+        k_left = a.nk - (at - 1) * KB;
         lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
         lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
     };
-    segment(a.problems == 2 ? prob : 0);
+    // this workgroup's stages, of one segment or two
+    const int per_seg = (a.nk + KB - 1) / KB, stages = per_seg * a.segments;
+    const int first = (int)((int64_t)stages * split / a.splits), total = (int)((int64_t)stages * (split + 1) / a.splits) - first;
+    int segments = a.segments - (first >= per_seg ? 1 : 0);              // this one and those behind it
+    if (total > 0) segment(a.problems == 2 ? prob : a.segments - segments, first - (a.segments - segments) * per_seg);
     const unsigned lds0 = (unsigned)(size_t)(lds_char*)ff_lds;
-    // The next stage's requests: first where they start, then one after the other, load 0 .. LP + LQ - 1.  Behind the last stage they
-    // go on with resources of no bytes (zeros into LDS that nobody reads), so that the loop below has one form.
+    // The next stage's requests: first where they start, then one after the other, load 0 .. LP + LQ - 1.  Behind the operands' last stage direct
+    // loads go on with resources of no bytes (zeros into LDS that nobody reads), so that the loop below has one form.
     i4v pres, qres, ures;
-    int limit = 0x7fffffff, segments = a.segments;
+    int limit = 0x7fffffff;
     auto next = [&]() __attribute__((always_inline)) {
         k_left -= KB;
         if (k_left < KB) {
             if (k_left <= 0) {
                 if (--segments > 0) {
-                    segment(1);
+                    segment(1, 0);
                     k_left -= KB;
                 } else {
                     limit = 0;
                 }
             }
-            if (k_left < KB) {
-                lp.mask(wave * LP, k_left);
-                lq.mask(wave * LQ, k_left);
+            if constexpr (DIRECT) {
+                if (k_left < KB) {
+                    lp.mask(wave * LP, k_left);
+                    lq.mask(wave * LQ, k_left);
+                }
             }
         }
         pb += pstep;
         qb += qstep;
-        pres = resource(pb, limit);
-        if (TWO) {
-            ub += pstep;
-            ures = resource(ub, limit);
+        if (TWO) ub += pstep;
+        if constexpr (DIRECT) {
+            pres = resource(pb, limit);
+            if (TWO) ures = resource(ub, limit);
+            qres = resource(qb, limit);
         }
-        qres = resource(qb, limit);
     };
     auto load = [&](unsigned stage, int i) __attribute__((always_inline)) {
-        if (i < LP) line_to_lds(TWO && i >= LP / 2 ? ures : pres, lp.off[i], lds0 + stage + (unsigned)(wave * LP + i) * 1024);
-        else line_to_lds(qres, lq.off[i - LP], lds0 + stage + QOFF + (unsigned)(wave * LQ + i - LP) * 1024);
+        if constexpr (DIRECT) {
+            if (i < LP) line_to_lds(TWO && i >= LP / 2 ? ures : pres, lp.off[i], lds0 + stage + (unsigned)(wave * LP + i) * 1024);
+            else line_to_lds(qres, lq.off[i - LP], lds0 + stage + QOFF + (unsigned)(wave * LQ + i - LP) * 1024);
+        }
     };
-    const int total = (a.nk + KB - 1) / KB * a.segments;
     f16v acc[FC][FR];
 #pragma unroll
     for (int i = 0; i < FC; ++i)
@@ -571,35 +533,70 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     // A stage's requests by the step that they go out in: the last of the stage that makes room for them, and the first of the next.
     constexpr int NL = LP + LQ, L0 = KS == 2 ? (NL + 1) / 2 : (3 * NL + 7) / 8, L1 = KS == 2 ? NL : (6 * NL + 7) / 8;
     if (total > 0) {
+        if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < RING; ++i) {
-            next();
+            for (int i = 0; i < RING; ++i) {
+                next();
 #pragma unroll
-            for (int l = 0; l < (i < RING - 1 ? NL : L0); ++l) load(i * STAGE, l);
-        }
-        wait_loads<(RING - 2) * NL + L0>();
-        asm volatile("s_barrier" ::: "memory");
-        unsigned cur = 0, last = (RING - 1) * STAGE;
-#pragma unroll
-        for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
-        for (int s = 0; s < total - 1; ++s) {
-            step(0, true, cur, 1, last, L0, L1);
-            if constexpr (KS == 4) {
-                step(1, true, cur, 2, last, L1, NL);
-                step(0, true, cur, 3, 0, 0, 0);
+                for (int l = 0; l < (i < RING - 1 ? NL : L0); ++l) load(i * STAGE, l);
             }
-            // this wave's reads of the stage have arrived, and so has its part of the next one
-            __builtin_amdgcn_s_waitcnt(WAIT_LOADS_AND_LDS((RING - 2) * NL));
+            wait_loads<(RING - 2) * NL + L0>();
             asm volatile("s_barrier" ::: "memory");
-            next();
-            last = cur;
-            cur = cur == (RING - 1) * STAGE ? 0 : cur + STAGE;
-            step(1, true, cur, 0, last, 0, L0);
-        }
+            unsigned cur = 0, last = (RING - 1) * STAGE;
 #pragma unroll
-        for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
-        step(1, false, 0, 0, 0, 0, 0);
-        wait_loads<0>();
+            for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
+            for (int s = 0; s < total - 1; ++s) {
+                step(0, true, cur, 1, last, L0, L1);
+                if constexpr (KS == 4) {
+                    step(1, true, cur, 2, last, L1, NL);
+                    step(0, true, cur, 3, 0, 0, 0);
+                }
+                // this wave's reads of the stage have arrived, and so has its part of the next one
+                __builtin_amdgcn_s_waitcnt(WAIT_LOADS_AND_LDS((RING - 2) * NL));
+                asm volatile("s_barrier" ::: "memory");
+                next();
+                last = cur;
+                cur = cur == (RING - 1) * STAGE ? 0 : cur + STAGE;
+                step(1, true, cur, 0, last, 0, L0);
+            }
+#pragma unroll
+            for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+            step(1, false, 0, 0, 0, 0, 0);
+            wait_loads<0>();
+        } else {
+            auto fetch = [&]() __attribute__((always_inline)) {
+                next();
+                lp.load(pb, wave * LP, k_left);
+                lq.load(qb, wave * LQ, k_left);
+            };
+            auto put = [&](unsigned stage) __attribute__((always_inline)) {
+                lp.put(stage, wave * LP);
+                lq.put(stage + QOFF, wave * LQ);
+            };
+            fetch();
+            put(0);
+            if (total > 1) fetch();
+            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+            asm volatile("s_barrier" ::: "memory");
+            unsigned cur = 0;
+#pragma unroll
+            for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
+            for (int s = 0; s < total - 1; ++s) {
+                step(0, true, cur, 1, 0, 0, 0);
+                put(STAGE - cur);                               // the next stage, of which everybody has read what was there before
+                if (s + 2 < total) fetch();
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 1; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+                __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+                asm volatile("s_barrier" ::: "memory");
+                cur = STAGE - cur;
+                step(1, true, cur, 0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+            step(1, false, 0, 0, 0, 0, 0);
+        }
     }
     // ---- epilogue: JB * 32 rows at a time through an area of LDS that is the wave's own ----
     constexpr int JB = 2, CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;   // columns of the wave, floats of an LDS row, columns of C
@@ -609,6 +606,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     const int cw = lane % LPR * 8, c = c0 + wc * CO + cw, rw = lane / LPR;
     const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
     const bool whole = r0 + BR <= a.nr && c0 + CF <= a.nc;                     // uniform over the workgroup
+    float* const part = a.part + (int64_t)(split * (GATED ? 2 : a.problems) + prob) * a.nr * a.nc;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < FR; j += JB) {
@@ -634,7 +632,15 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                         *(f4v*)(v[k] + e * 4) = *(const f4v*)(src + (u + k) * RPU * CROW + e * 4);
                         if (GATED) *(f4v*)(w[k] + e * 4) = *(const f4v*)(src + (u + k) * RPU * CROW + 32 + e * 4);
                     }
-                finish_many<T, GATED, AT>(a, prob, r + u * RPU, RPU, c, v, w);
+                if (a.splits > 1) {
+#pragma unroll
+                    for (int k = 0; k < AT; ++k) {
+                        store_floats(part + (int64_t)(r + (u + k) * RPU) * a.nc + c, 8, v[k]);
+                        if (GATED) store_floats(part + ((int64_t)a.nr + r + (u + k) * RPU) * a.nc + c, 8, w[k]);
+                    }
+                } else {
+                    finish_many<T, GATED, AT>(a, prob, r + u * RPU, RPU, c, v, w);
+                }
             }
         } else {
 #pragma unroll 1
@@ -645,11 +651,46 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                     *(f4v*)(v + e * 4) = *(const f4v*)(src + u * RPU * CROW + e * 4);
                     if (GATED) *(f4v*)(w + e * 4) = *(const f4v*)(src + u * RPU * CROW + 32 + e * 4);
                 }
-                if (r + u * RPU < a.nr && c < a.nc) finish<T, GATED, 8>(a, prob, r + u * RPU, c, a.nc - c, v, w);
+                const int ru = r + u * RPU;
+                if (ru >= a.nr || c >= a.nc) continue;
+                if (a.splits > 1) {
+                    store_floats(part + (int64_t)ru * a.nc + c, a.nc - c, v);
+                    if (GATED) store_floats(part + ((int64_t)a.nr + ru) * a.nc + c, a.nc - c, w);
+                } else {
+                    finish<T, GATED, 8>(a, prob, ru, c, a.nc - c, v, w);
+                }
             }
         }
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// k_ff_join: the sums over the splits of k, in order, and the epilogue.
+template <typename T, bool GATED> __global__ __launch_bounds__(256) void k_ff_join(const DlfFfArgs a)
+{
+    const int cols = (a.nc + 7) >> 3;
+    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)a.nr * a.nc;
+    const int64_t row = unit / cols;
+    const int c = (int)(unit - row * cols) * 8, n = a.nc - c;
+    const int prob = row >= a.nr ? 1 : 0, r = (int)(row - (prob ? a.nr : 0));
+    if (prob >= a.problems || r >= a.nr) return;
+    const int planes = GATED ? 2 : a.problems;
+    const float* p = a.part + prob * plane + (int64_t)r * a.nc + c;
+    float v[8], u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = u[i] = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        float x[8], y[8];
+        load_floats(p + s * planes * plane, n, x);
+        if (GATED) load_floats(p + (s * 2 + 1) * plane, n, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] += x[i];
+            if (GATED) u[i] += y[i];
+        }
+    }
+    finish<T, GATED, 8>(a, prob, r, c, n, v, u);
 }
 
 // The waves' partial sums of a workgroup's 16 NF features x 16 MR rows meet in LDS, in the order of the waves.
@@ -928,47 +969,28 @@ __global__ __launch_bounds__(256) void k_ff_sum(const DlfFfSumArgs a)
 // ------------------------------------------------------------------------------------------------
 // Launches
 // ------------------------------------------------------------------------------------------------
-template <typename T> static void (*any_kernel(int layout, int gated))(const DlfFfArgs)
+// The tile kernels by shape (DLF_FF_SHAPE_*): waves across c and r, k of a stage, stages in LDS, direct loads.
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
 {
-    if (gated) return k_ff_any<T, false, false, true>;
+    if (gated) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, true>;
     switch (layout) {
-    case DLF_FF_NN: return k_ff_any<T, false, false, false>;
-    case DLF_FF_TN: return k_ff_any<T, true, false, false>;
-    default: return k_ff_any<T, true, true, false>;
-    }
-}
-extern "C" int dlf_ff_start_any(const DlfFfArgs* a, int dtype, int layout, int gated, void* stream)
-{
-    hipLaunchKernelGGL(dtype == DLF_F16 ? any_kernel<F16>(layout, gated) : any_kernel<BF16>(layout, gated),
-                       dim3((unsigned)(a->tiles_r * a->tiles_c * a->problems)), dim3(256), 0, (hipStream_t)stream, *a);
-    return (int)hipGetLastError();
-}
-#define K256 64
-#define R256 2
-#define K128 64
-#define R128 2
-#define W128 2, 2
-#ifndef W256
-#define W256 2, 2
-#endif
-// The tile kernels by shape (DLF_FF_SHAPE_*).
-template <typename T, int BC, int BR, int WC, int WR, int KB, int RING> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
-{
-    if (gated) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, false, false, true>;
-    switch (layout) {
-    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, false, false, false>;
-    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, true, false, false>;
-    default: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, true, true, false>;
+    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, false>;
+    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>;
+    default: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>;
     }
 }
 template <typename T> static void (*tile_kernel(int shape, int layout, int gated))(const DlfFfArgs)
 {
-    return shape == DLF_FF_SHAPE_256 ? tile_of<T, 256, 256, W256, K256, R256>(layout, gated) : tile_of<T, 128, 128, W128, K128, R128>(layout, gated);
+    switch (shape) {
+    case DLF_FF_SHAPE_256: return tile_of<T, 256, 256, 2, 2, 64, 2, true>(layout, gated);
+    case DLF_FF_SHAPE_128: return tile_of<T, 128, 128, 2, 2, 64, 2, true>(layout, gated);
+    default: return tile_of<T, 128, 128, 2, 2, 64, 2, false>(layout, gated);
+    }
 }
 static size_t tile_lds(int shape)
 {
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
-    const size_t ring = (size_t)(shape == 0 ? K256 * R256 : K128 * R128) * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
+    const size_t ring = (size_t)2 * 64 * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
     return ring > out ? ring : out;
 }
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
@@ -1015,10 +1037,15 @@ extern "C" int dlf_ff_kernels_init(void)
 }
 extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream)
 {
-    const unsigned tiles = (unsigned)(a->tiles_r * a->tiles_c * a->problems);
+    const unsigned tiles = (unsigned)(a->tiles_r * a->tiles_c * a->problems * a->splits);
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
     hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, layout, gated) : tile_kernel<BF16>(shape, layout, gated),
                        dim3((tiles + 7) / 8 * 8), dim3((unsigned)(s.wc * s.wr * 64)), tile_lds(shape), (hipStream_t)stream, *a);
+    if (a->splits > 1) {
+        const int64_t units = (int64_t)a->nr * a->problems * ((a->nc + 7) / 8);
+        hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? k_ff_join<F16, true> : k_ff_join<F16, false>) : (gated ? k_ff_join<BF16, true> : k_ff_join<BF16, false>),
+                           dim3((unsigned)((units + 255) / 256)), dim3(256), 0, (hipStream_t)stream, *a);
+    }
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream)

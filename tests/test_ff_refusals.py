@@ -24,7 +24,7 @@ def status(f, *a):
 
 BAD_DESCS = [dict(rows=-1), dict(rows=(1 << 30) + 1), dict(in_features=0), dict(out_features=0), dict(in_features=(1 << 20) + 1),
              dict(out_features=-5), dict(x_stride=15), dict(w_stride=-16), dict(y_stride=23), dict(dy_stride=23), dict(res_stride=1),
-             dict(x_stride=1 << 31)]
+             dict(x_stride=1 << 24), dict(dy_stride=1 << 40)]
 
 
 @pytest.mark.parametrize("kw", BAD_DESCS)

@@ -8,9 +8,11 @@ from gpu_util import announce
 
 pytestmark = pytest.mark.gpu
 
-KERNELS = {"any": 1, "tile256": 2, "tile128": 3}
-# (rows, in, out): rows in whole lines
-SIZES = [(8, 8, 8), (128, 64, 128), (136, 72, 120), (256, 128, 256), (264, 192, 264), (504, 200, 520), (1288, 64, 776), (700, 1032, 1304)]
+# (kernel, workgroups that share a tile's k)
+KERNELS = {"few": (1, 0), "tile256": (2, 1), "tile256_split3": (2, 3), "tile128": (3, 1), "tile128_split5": (3, 5), "any": (4, 1), "any_split2": (4, 2)}
+# (rows, in, out)
+SIZES = [(8, 8, 8), (64, 72, 40), (128, 64, 128), (136, 72, 120), (256, 128, 256), (264, 192, 264), (504, 840, 520), (1288, 64, 776), (700, 1032, 1304),
+         (1, 5, 1), (131, 77, 67), (259, 1031, 517)]
 
 
 @pytest.fixture
@@ -26,7 +28,7 @@ def force():
 def test_linear(kernel, t, size, force):
     from paper_2011_05630_amd import feedforward as F
     announce("linear", kernel, t, size)
-    force(KERNELS[kernel])
+    force(*KERNELS[kernel])
     m, k, n = size
     ty = TYPES[t]
     x, w, b, r, dy = whole(m, k, 1), whole(n, k, 2), whole(1, n, 3, 9)[0], whole(m, n, 4, 9), whole(m, n, 5)
@@ -50,7 +52,7 @@ def test_linear(kernel, t, size, force):
 def test_gated(kernel, t, size, force):
     from paper_2011_05630_amd import feedforward as F
     announce("gated", kernel, t, size)
-    force(KERNELS[kernel])
+    force(*KERNELS[kernel])
     m, k, n = size
     ty = TYPES[t]
     x, wg, wu, dh = whole(m, k, 1, 1), whole(n, k, 2, 1), whole(n, k, 3, 1), whole(m, n, 4, 1)
