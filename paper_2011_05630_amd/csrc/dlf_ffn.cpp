@@ -142,8 +142,8 @@ Cut cut_as(int shape, int splits, int64_t nr, int64_t nc, int problems, bool gat
 }
 
 // Modelled time of a cut in ns, from measurements at 4096^3 and around: a stage of 64 k takes a 256 x 256 tile 1450 ns; two 128 x 128
-// tiles that share a compute unit 900 ns, one that has it to itself 550; the first loads and the epilogue of a tile 7 and 4 us;
-// joining, a launch and the partial sums' bytes twice.
+// tiles that share a compute unit 900 ns, one that has it to itself waits for memory, 900 ns a stage, unless four stages are on their way: 500;
+// through registers 1250 and 950; the first loads and the epilogue of a tile 7, 4 and 5 us; joining, a launch and the partial sums' bytes twice.
 double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
 {
     const int64_t wgs = (int64_t)c.tiles_r * c.tiles_c * problems * c.splits;
@@ -151,22 +151,30 @@ double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, in
     double t;
     if (c.shape == DLF_FF_SHAPE_256) {
         t = (double)ceil_div(wgs, 256) * (stages * 1450 + 7000);
+    } else if (c.shape == DLF_FF_SHAPE_ANY) {
+        t = (double)(wgs / 512) * (stages * 1250 + 5000);
+        if (wgs % 512 > 256) t += stages * 1250 + 5000;
+        else if (wgs % 512 > 0) t += stages * 950 + 5000;
+    } else if (c.shape == DLF_FF_SHAPE_128_DEEP) {
+        t = (double)ceil_div(wgs, 256) * (stages * 500 + 5000);
     } else {
         t = (double)(wgs / 512) * (stages * 900 + 4000);
         if (wgs % 512 > 256) t += stages * 900 + 4000;
-        else if (wgs % 512 > 0) t += stages * 550 + 4000;
+        else if (wgs % 512 > 0) t += stages * 900 + 4000;
     }
     if (c.splits > 1) t += 3500 + (double)c.part_bytes * 2 / 4000;
     return t;
 }
 
-Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+// any: the operands' rows start anywhere.
+Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
 {
     Cut best;
     double least = 0;
     const int64_t stages = (int64_t)ceil_div(nk, 64) * segments;
-    for (int shape = DLF_FF_SHAPE_256; shape <= DLF_FF_SHAPE_128; ++shape) {
-        if (g_force >= 2 && g_force < 2 + DLF_FF_NUM_SHAPES && shape != (g_force == 2 ? DLF_FF_SHAPE_256 : DLF_FF_SHAPE_128)) continue;
+    if (g_force == 2 + DLF_FF_SHAPE_ANY) any = true;
+    for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape) {
+        if (any != (shape == DLF_FF_SHAPE_ANY) || (g_force >= 2 && !any && shape != g_force - 2)) continue;
         for (int splits = 1; splits <= 16; ++splits) {
             if (splits > 1 && stages / splits < 4) break;
             if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;
@@ -178,6 +186,12 @@ Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool 
     return best;
 }
 
+// Workspace of a product: what its addresses are is not known yet.
+size_t part_bytes(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+{
+    return std::max(choose(nr, nc, nk, segments, problems, gated, false).part_bytes, choose(nr, nc, nk, segments, problems, gated, true).part_bytes);
+}
+
 bool is_few(int64_t rows) { return rows <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 1); }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
@@ -186,15 +200,14 @@ dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, char* part
 {
     TRY(kernels_ready());
     if (layout == DLF_FF_NN && is_few(a.nr)) return few_rows(f, a, gated, stream);
-    Cut c = choose(a.nr, a.nc, a.nk, a.segments, a.problems, gated);
-    bool whole = g_force != 2 + DLF_FF_SHAPE_ANY;
+    bool whole = true;
     const int n = gated ? 2 : std::max(a.segments, a.problems);
     for (int i = 0; i < n; ++i) {
         whole = whole && lines(a.p[i], a.ldp, layout == DLF_FF_NN ? a.nk : a.nc);
         if (!gated) whole = whole && lines(a.q[i], a.ldq, layout == DLF_FF_TT ? a.nr : a.nk);
     }
     if (gated) whole = whole && lines(a.q[0], a.ldq, a.nk);
-    if (!whole) c = cut_as(DLF_FF_SHAPE_ANY, c.splits, a.nr, a.nc, a.problems, gated);
+    const Cut c = choose(a.nr, a.nc, a.nk, a.segments, a.problems, gated, !whole);
     a.tiles_r = c.tiles_r;
     a.tiles_c = c.tiles_c;
     a.splits = c.splits;
@@ -213,23 +226,22 @@ BackLayout back_layout(const Ff& f)
     BackLayout l;
     const size_t nz = f.gated ? 2 : 1;
     l.lddz = ((size_t)f.d.out_features + 7) / 8 * 8;
-    // rows of one partial sum: enough of them that the sums are few, few enough that the grid is not
-    l.chunk = (int)std::max<int64_t>(32, (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS);
+    l.chunk = f.d.rows <= DLF_FF_SUM_ROWS ? DLF_FF_SUM_ROWS : (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS;
     l.chunks = f.d.rows > 0 ? (int)((f.d.rows + l.chunk - 1) / l.chunk) : 1;
     if (needs_dz(f)) l.bytes = nz * align256((size_t)f.d.rows * l.lddz * 2);
     l.part = l.bytes;
-    l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
+    if (l.chunks > 1) l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
     l.join = l.bytes;
     const int problems = f.gated ? 2 : 1;
-    l.bytes += align256(std::max(choose(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, problems, 1, false).part_bytes,
-                                 choose(f.d.out_features, f.d.in_features, f.d.rows, 1, problems, false).part_bytes));
+    l.bytes += align256(std::max(part_bytes(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, problems, 1, false),
+                                 part_bytes(f.d.out_features, f.d.in_features, f.d.rows, 1, problems, false)));
     return l;
 }
 
 size_t forward_ws(const Ff& f)
 {
     if (f.d.rows == 0 || is_few(f.d.rows)) return 0;
-    return align256(choose(f.d.rows, f.d.out_features, f.d.in_features, 1, 1, f.gated).part_bytes);
+    return align256(part_bytes(f.d.rows, f.d.out_features, f.d.in_features, 1, 1, f.gated));
 }
 
 dlf_status forward(const Ff& f, const void* x, const void* const w[2], const float* const bias[2], const void* res, void* y, float* saved,
@@ -263,15 +275,17 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         memset(&z, 0, sizeof z);
         z.dy = dy; z.lddy = f.d.dy_stride;
         z.rows = (int)f.d.rows; z.n = f.d.out_features; z.act = f.d.act; z.chunk = l.chunk;
-        if (sums) z.part = (float*)(ws + l.part);
+        float* const part = (float*)(ws + l.part);
+        for (int i = 0; i < nz; ++i)
+            if (db[i]) z.sums[i] = l.chunks > 1 ? part + (size_t)i * l.chunks * f.d.out_features : db[i];
         if (needs_dz(f)) {
             z.saved = saved;
             z.lddz = lddz = (int64_t)l.lddz;
             for (int i = 0; i < nz; ++i) dz[i] = z.dz[i] = ws + i * align256((size_t)f.d.rows * l.lddz * 2);
         }
         TRY(launched(f, dlf_ff_start_dz(&z, f.d.dtype, f.gated, stream)));
-        if (sums) {
-            DlfFfSumArgs s = {z.part, {db[0], db[1]}, z.n, l.chunks};
+        if (sums && l.chunks > 1) {
+            DlfFfSumArgs s = {part, {db[0], db[1]}, z.n, l.chunks};
             TRY(launched(f, dlf_ff_start_sum(&s, f.gated, stream)));
         }
     }

@@ -41,8 +41,8 @@ struct DlfFfDzArgs {
     void* dz[2];            // rows of lddz elements, zeros behind column n
     int64_t lddz;
     int32_t rows, n, act;
-    int32_t chunk;          // rows of one partial sum
-    float* part;            // [1 or 2][chunks][n], or null
+    int32_t chunk;          // rows of one sum: all of them, or those of a partial sum
+    float* sums[2];         // [chunks][n], or null
 };
 struct DlfFfSumArgs {
     const float* part;      // [1 or 2][chunks][n]
@@ -50,13 +50,15 @@ struct DlfFfSumArgs {
     int32_t n, chunks;
 };
 
-// Largest number of partial column sums.
-#define DLF_FF_MAX_CHUNKS 128
+// Rows whose column sums one workgroup forms; largest number of partial sums of more rows.
+#define DLF_FF_SUM_ROWS 1024
+#define DLF_FF_MAX_CHUNKS 64
 
-// Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and its waves.
-struct DlfFfShape { int bc, br, wc, wr; };
-enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_NUM_SHAPES = 3 };   // ANY: rows that start anywhere
-static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2}, {128, 128, 2, 2}, {128, 128, 2, 2}};
+// Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections), its waves and
+// the stages of 64 k that LDS holds.
+struct DlfFfShape { int bc, br, wc, wr, ring; };
+enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_SHAPE_128_DEEP = 3, DLF_FF_NUM_SHAPES = 4 };   // ANY: rows that start anywhere
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2, 2}, {128, 128, 2, 2, 2}, {128, 128, 2, 2, 2}, {128, 128, 2, 2, 4}};
 
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64

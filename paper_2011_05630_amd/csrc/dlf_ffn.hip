@@ -564,34 +564,47 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
             step(1, false, 0, 0, 0, 0, 0);
             wait_loads<0>();
         } else {
-            auto fetch = [&]() __attribute__((always_inline)) {
+            // two stages on their way in registers, each with half of them
+            auto lp2 = lp;
+            auto lq2 = lq;
+            auto fetch = [&](auto& p, auto& q) __attribute__((always_inline)) {
                 next();
-                lp.load(pb, wave * LP, k_left);
-                lq.load(qb, wave * LQ, k_left);
+                p.load(pb, wave * LP, k_left);
+                q.load(qb, wave * LQ, k_left);
             };
-            auto put = [&](unsigned stage) __attribute__((always_inline)) {
-                lp.put(stage, wave * LP);
-                lq.put(stage + QOFF, wave * LQ);
+            auto put = [&](unsigned stage, auto& p, auto& q) __attribute__((always_inline)) {
+                p.put(stage, wave * LP);
+                q.put(stage + QOFF, wave * LQ);
             };
-            fetch();
-            put(0);
-            if (total > 1) fetch();
+            fetch(lp, lq);
+            put(0, lp, lq);
+            if (total > 1) fetch(lp, lq);
+            if (total > 2) fetch(lp2, lq2);
             __builtin_amdgcn_s_waitcnt(WAIT_LDS);
             asm volatile("s_barrier" ::: "memory");
-            unsigned cur = 0;
 #pragma unroll
-            for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
-            for (int s = 0; s < total - 1; ++s) {
+            for (int r = 0; r < FC + FR; ++r) read(0, 0, 0, r);
+            // stage s, of the slot at cur; p and q hold stage s + 1, the other set s + 2
+            auto turn = [&](int s, unsigned cur, auto& p, auto& q) __attribute__((always_inline)) {
                 step(0, true, cur, 1, 0, 0, 0);
-                put(STAGE - cur);                               // the next stage, of which everybody has read what was there before
-                if (s + 2 < total) fetch();
+                put(STAGE - cur, p, q);                     // everybody has read what was there before
+                if (s + 3 < total) fetch(p, q);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int k = 1; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
                 __builtin_amdgcn_s_waitcnt(WAIT_LDS);
                 asm volatile("s_barrier" ::: "memory");
-                cur = STAGE - cur;
-                step(1, true, cur, 0, 0, 0, 0);
+                step(1, true, STAGE - cur, 0, 0, 0, 0);
+            };
+            int s = 0;
+            for (; s + 2 < total; s += 2) {
+                turn(s, 0, lp, lq);
+                turn(s + 1, STAGE, lp2, lq2);
+            }
+            unsigned cur = 0;
+            if (s + 1 < total) {
+                turn(s, 0, lp, lq);
+                cur = STAGE;
             }
 #pragma unroll
             for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
@@ -884,16 +897,18 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ff_dz: the gradient behind the activation, and partial column sums of it in 32 bits (before it is rounded).  A workgroup takes
-// `chunk` rows of 256 columns: 32 threads by eight columns, 8 rows at a time; the sums of the 8 meet in LDS in a fixed order.
+// k_ff_dz: the gradient behind the activation, and column sums of it in 32 bits (before it is rounded).  Bound by memory: 14 bytes an
+// element, gated 14 and twice the saved ones.  A workgroup takes `chunk` rows of 8 TC columns: TC threads by eight columns, blockDim / TC rows
+// at a time; their sums meet in LDS, in a fixed order.  With few rows a workgroup takes all of them, few columns wide, and its sums are the result;
+// with many it takes whole 512-byte lines, and k_ff_sum adds up what the chunks leave.
 // ------------------------------------------------------------------------------------------------
-template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
+template <typename T, bool GATED, int TC>
+__global__ __launch_bounds__(TC == 32 ? 256 : 1024) void k_ff_dz(const DlfFfDzArgs a)
 {
-    constexpr int NZ = GATED ? 2 : 1;
-    __shared__ float sums[NZ][8][256];
-    const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
-    const int c = (blockIdx.x * 32 + tc) * 8, n = a.n - c;
+    constexpr int NZ = GATED ? 2 : 1, THREADS = TC == 32 ? 256 : 1024, RT = THREADS / TC;
+    __shared__ __attribute__((aligned(16))) float sums[RT][NZ][8 * TC];
+    const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
+    const int c = (blockIdx.x * TC + tc) * 8, n = a.n - c;
     const int r0 = blockIdx.y * a.chunk, r1 = min(a.rows, r0 + a.chunk);
     float sum[NZ][8];
 #pragma unroll
@@ -901,15 +916,15 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[z][i] = 0.0f;
     if (n > 0) {
-        for (int r = r0 + tr; r < r1; r += 8) {
+        for (int r = r0 + tr; r < r1; r += RT) {
             const typename T::v8 dy = load8<T>(a.dy, (int64_t)r * a.lddy + c, n);
             float d[NZ][8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[0][i] = (float)dy[i];
             if (a.saved != nullptr) {
                 float z[8], u[8];
                 load_floats(a.saved + (int64_t)r * a.n + c, n, z);
                 if (GATED) load_floats(a.saved + ((int64_t)a.rows + r) * a.n + c, n, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[0][i] = (float)dy[i];
                 with_act(a.act, [&](auto k) __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -932,6 +947,9 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
                     }
                     store_some<T, 8>(a.dz[z2], (int64_t)r * a.lddz + c, 8, d[z2]);
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[0][i] = (float)dy[i];
             }
 #pragma unroll
             for (int z2 = 0; z2 < NZ; ++z2)
@@ -939,31 +957,36 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
                 for (int i = 0; i < 8; ++i) sum[z2][i] += d[z2][i];
         }
     }
-    if (a.part == nullptr) return;
+    if (a.sums[0] == nullptr && a.sums[1] == nullptr) return;
 #pragma unroll
     for (int z = 0; z < NZ; ++z)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[z][tr][tc * 8 + i] = sum[z][i];
+        for (int i = 0; i < 8; ++i) sums[tr][z][tc * 8 + i] = sum[z][i];
+    // pairs of rows, then pairs of pairs ...
+    for (int h = RT / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < h * NZ * 8 * TC; i += THREADS) (&sums[0][0][0])[i] += (&sums[h][0][0])[i];
+    }
     __syncthreads();
-    const int col = blockIdx.x * 256 + threadIdx.x;
-    if (col < a.n) {
-#pragma unroll
-        for (int z = 0; z < NZ; ++z) {
-            float t = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) t += sums[z][k][threadIdx.x];
-            a.part[((int64_t)z * gridDim.y + blockIdx.y) * a.n + col] = t;
-        }
+    for (int i = threadIdx.x; i < NZ * 8 * TC; i += THREADS) {
+        const int z = i / (8 * TC), col = blockIdx.x * 8 * TC + i % (8 * TC);
+        if (col < a.n && a.sums[z] != nullptr) a.sums[z][(int64_t)blockIdx.y * a.n + col] = sums[0][z][i % (8 * TC)];
     }
 }
-// The partial sums of a column added in order: the result does not depend on which workgroup came first.
+// The partial sums of a column added in order: the result does not depend on which workgroup came first.  Four threads to a column.
 __global__ __launch_bounds__(256) void k_ff_sum(const DlfFfSumArgs a)
 {
-    const int col = blockIdx.x * 256 + threadIdx.x, z = blockIdx.y;
-    if (col >= a.n || a.out[z] == nullptr) return;
+    __shared__ float part[4][64];
+    const int l = threadIdx.x & 63, g = threadIdx.x >> 6, col = blockIdx.x * 64 + l, z = blockIdx.y;
+    if (a.out[z] == nullptr) return;
     float t = 0.0f;
-    for (int k = 0; k < a.chunks; ++k) t += a.part[((int64_t)z * a.chunks + k) * a.n + col];
-    a.out[z][col] = t;
+    if (col < a.n) {
+#pragma unroll 8
+        for (int k = g; k < a.chunks; k += 4) t += a.part[((int64_t)z * a.chunks + k) * a.n + col];
+    }
+    part[g][l] = t;
+    __syncthreads();
+    if (g == 0 && col < a.n) a.out[z][col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -984,13 +1007,14 @@ template <typename T> static void (*tile_kernel(int shape, int layout, int gated
     switch (shape) {
     case DLF_FF_SHAPE_256: return tile_of<T, 256, 256, 2, 2, 64, 2, true>(layout, gated);
     case DLF_FF_SHAPE_128: return tile_of<T, 128, 128, 2, 2, 64, 2, true>(layout, gated);
+    case DLF_FF_SHAPE_128_DEEP: return tile_of<T, 128, 128, 2, 2, 64, 4, true>(layout, gated);
     default: return tile_of<T, 128, 128, 2, 2, 64, 2, false>(layout, gated);
     }
 }
 static size_t tile_lds(int shape)
 {
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
-    const size_t ring = (size_t)2 * 64 * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
+    const size_t ring = (size_t)s.ring * 64 * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
     return ring > out ? ring : out;
 }
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
@@ -1048,15 +1072,18 @@ extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int l
     }
     return (int)hipGetLastError();
 }
+template <typename T, bool GATED> static void (*dz_kernel(int wide))(const DlfFfDzArgs) { return wide ? k_ff_dz<T, GATED, 32> : k_ff_dz<T, GATED, 4>; }
 extern "C" int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream)
 {
-    const dim3 grid((unsigned)((a->n + 255) / 256), (unsigned)(a->rows > 0 ? (a->rows + a->chunk - 1) / a->chunk : 1));
-    hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? k_ff_dz<F16, true> : k_ff_dz<F16, false>) : (gated ? k_ff_dz<BF16, true> : k_ff_dz<BF16, false>),
-                       grid, dim3(256), 0, (hipStream_t)stream, *a);
+    const int wide = a->chunk < a->rows, cols = wide ? 256 : 32;
+    const dim3 grid((unsigned)((a->n + cols - 1) / cols), (unsigned)(a->rows > 0 ? (a->rows + a->chunk - 1) / a->chunk : 1));
+    hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? dz_kernel<F16, true>(wide) : dz_kernel<F16, false>(wide))
+                                        : (gated ? dz_kernel<BF16, true>(wide) : dz_kernel<BF16, false>(wide)),
+                       grid, dim3(wide ? 256 : 1024), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream)
 {
-    hipLaunchKernelGGL(k_ff_sum, dim3((unsigned)((a->n + 255) / 256), gated ? 2 : 1), dim3(256), 0, (hipStream_t)stream, *a);
+    hipLaunchKernelGGL(k_ff_sum, dim3((unsigned)((a->n + 63) / 64), gated ? 2 : 1), dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
