@@ -202,14 +202,14 @@ __device__ __forceinline__ void finish(const DlfFfArgs& a, int prob, int r, int 
     store_some<T, V>(a.out[prob], (int64_t)r * a.ldo + c, n, v);
 }
 
-// ... of N units of eight outputs that all exist, `step` rows apart: their loads share a wait.
+// ... of N units of eight outputs, `step` rows apart, of columns that all exist: their loads share a wait.
 template <typename T, bool GATED, int N>
 __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r, int step, int c, float (&v)[N][8], float (&u)[N][8])
 {
     typename T::v8 q[N];
     if (a.res != nullptr) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) q[k] = load8<T>(a.res, (int64_t)(r + k * step) * a.ldres + c, 8);
+        for (int k = 0; k < N; ++k) q[k] = load8<T>(a.res, (int64_t)min(r + k * step, a.nr - 1) * a.ldres + c, 8);
     }
     if (a.bias[0] != nullptr) {
         float b[8];
@@ -230,6 +230,7 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
     if (a.saved != nullptr) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
+            if (r + k * step >= a.nr) continue;
             store_floats(a.saved + (int64_t)(r + k * step) * a.nc + c, 8, v[k]);
             if (GATED) store_floats(a.saved + ((int64_t)a.nr + r + k * step) * a.nc + c, 8, u[k]);
         }
@@ -251,7 +252,7 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[k][i] += (float)q[k][i];
         }
-        store_some<T, 8>(a.out[prob], (int64_t)(r + k * step) * a.ldo + c, 8, v[k]);
+        if (r + k * step < a.nr) store_some<T, 8>(a.out[prob], (int64_t)(r + k * step) * a.ldo + c, 8, v[k]);
     }
 }
 
@@ -316,7 +317,7 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
         if (!TR) return p ^ swizzle<KB>(l);
         return p ^ ((((l & 3) | ((l >> 3) & 1) << 2) & (ROWS / 32 - 1)) << 2);
     }
-    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int = 0)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -341,38 +342,62 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
     }
 };
 // ... of rows that start anywhere: through registers, by a load and, a stage later, a write to LDS.  Rows and columns that do not exist
-// are read as others and not stored; k behind the last are zeros.
+// are read as others and not stored.  A part of eight that ends behind the operand's last k (or column) is read as the last eight there
+// are and shifted, zeros moving in: a 16-byte load never leaves the operand.  Only operands of less than eight are read one by one.
 template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
     typedef Loader<N, ROWS, TR, KB> Map;
-    unsigned off[N];
+    int off[N];
     typename T::v8 v[N];
-    int edge;               // columns of a tile that ends inside a part of eight, else 0
-    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
+    int64_t line_bytes;
+    int edge;               // across: columns of a tile that ends inside a part of eight, else 0
+    int tail;               // k of the stage in v if they are not whole, else 0
+    bool tiny;              // less than eight k (along) or columns (across) in all
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int extent)
     {
+        line_bytes = ld * 2;
+        tiny = extent < 8;
+        tail = 0;
         edge = TR && avail < ROWS && (avail & 7) != 0 ? avail : 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int l = Map::line(first, i), p = Map::part(first, i), row = GATED ? (l >> 6) * 32 + (l & 31) : l;
-            if (!TR) off[i] = (unsigned)(min(row, avail - 1) * ld + p * 8) * 2;
-            else off[i] = (unsigned)(l * ld + (p * 8 < avail ? p * 8 : 0)) * 2;
+            const int l = Map::line(first, i), p = Map::part(first, i) * 8, row = GATED ? (l >> 6) * 32 + (l & 31) : l;
+            if (!TR) off[i] = (int)(min(row, avail - 1) * ld + p) * 2;
+            else off[i] = (int)(l * ld + (edge > 0 && !tiny ? min(p, avail - 8) : p < avail ? p : 0)) * 2;
         }
+    }
+    // elements of part i that exist, in a stage of `left` k
+    __device__ __forceinline__ int count(int first, int i, int left) const
+    {
+        const int p = Map::part(first, i) * 8;
+        return !TR ? left - p : Map::line(first, i) >= left ? 0 : edge > 0 ? edge - p : 8;
     }
     __device__ __forceinline__ void load(const char* base, int first, int k_left)
     {
-        if (k_left >= KB && edge == 0) {
+        tail = k_left < KB ? k_left : 0;
+        if (tiny) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = load8<T>(base + off[i], 0, count(first, i, k_left));
+        } else if (tail == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base + off[i], 16);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int p = Map::part(first, i) * 8;
-                const int n = !TR ? k_left - p : Map::line(first, i) >= k_left ? 0 : edge > 0 ? edge - p : 8;
-                v[i] = load8<T>(base + off[i], 0, n);
+                const int64_t back = !TR ? max(0, 8 - count(first, i, k_left)) * 2 : max(0, Map::line(first, i) - (k_left - 1)) * line_bytes;
+                __builtin_memcpy(&v[i], base + (off[i] - back), 16);
             }
         }
     }
-    __device__ __forceinline__ void put(unsigned dst, int first) const
+    __device__ __forceinline__ void put(unsigned dst, int first)
     {
+        if (!tiny && (tail > 0 || edge > 0)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int gone = 8 - min(8, max(0, count(first, i, tail > 0 ? tail : KB)));
+                const unsigned __int128 x = __builtin_bit_cast(unsigned __int128, v[i]);
+                v[i] = __builtin_bit_cast(typename T::v8, gone > 7 ? (unsigned __int128)0 : x >> (gone * 16));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i)
             *(__attribute__((address_space(3))) typename T::v8*)((lds_char*)ff_lds + (dst + (unsigned)(first + i) * 1024 + (threadIdx.x & 63) * 16)) = v[i];
@@ -448,14 +473,18 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     const int64_t pstep = (PT ? a.ldp : 1) * (KB * 2), qstep = (QT ? a.ldq : 1) * (KB * 2);   // bytes
     const char *pb, *qb, *ub = nullptr;
     int k_left;
+    auto offsets = [&]() __attribute__((always_inline)) {
+        lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp, PT ? a.nc : a.nk);
+        lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq, QT ? a.nr : a.nk);
+    };
+    if constexpr (!DIRECT) offsets();
     // Requests go on with stage `at` of segment w (operand pair) at the next call of next().
     auto segment = [&](int w, int at) __attribute__((always_inline)) {
         pb = (const char*)a.p[GATED ? TWO ? 0 : wave & 1 : w] + p0 * 2 + (at - 1) * pstep;
         if (TWO) ub = (const char*)a.p[1] + p0 * 2 + (at - 1) * pstep;
         qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2 + (at - 1) * qstep;
         k_left = a.nk - (at - 1) * KB;
-        lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
-        lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
+        if constexpr (DIRECT) offsets();                    // (the last stage of a segment masks them)
     };
     // this workgroup's stages, of one segment or two
     const int per_seg = (a.nk + KB - 1) / KB, stages = per_seg * a.segments;
@@ -618,7 +647,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     float* const lf = (float*)ff_lds + wave * (JB * 32 * CROW);
     const int cw = lane % LPR * 8, c = c0 + wc * CO + cw, rw = lane / LPR;
     const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
-    const bool whole = r0 + BR <= a.nr && c0 + CF <= a.nc;                     // uniform over the workgroup
+    const bool whole = c0 + CF <= a.nc;                                        // uniform over the workgroup
     float* const part = a.part + (int64_t)(split * (GATED ? 2 : a.problems) + prob) * a.nr * a.nc;
     __syncthreads();
 #pragma unroll
@@ -633,7 +662,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                         f4v{acc[i][j + b][q * 4], acc[i][j + b][q * 4 + 1], acc[i][j + b][q * 4 + 2], acc[i][j + b][q * 4 + 3]};
         __builtin_amdgcn_wave_barrier();
         const int r = r0 + (wr * FR + j) * 32 + rw;
-        if (whole) {
+        if (whole || a.nc - c >= 8) {
             constexpr int AT = UNITS < 4 ? UNITS : 4;                          // units whose waits are shared
 #pragma unroll 1
             for (int u = 0; u < UNITS; u += AT) {
@@ -648,14 +677,16 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                 if (a.splits > 1) {
 #pragma unroll
                     for (int k = 0; k < AT; ++k) {
-                        store_floats(part + (int64_t)(r + (u + k) * RPU) * a.nc + c, 8, v[k]);
-                        if (GATED) store_floats(part + ((int64_t)a.nr + r + (u + k) * RPU) * a.nc + c, 8, w[k]);
+                        const int ru = r + (u + k) * RPU;
+                        if (ru >= a.nr) continue;
+                        store_floats(part + (int64_t)ru * a.nc + c, 8, v[k]);
+                        if (GATED) store_floats(part + ((int64_t)a.nr + ru) * a.nc + c, 8, w[k]);
                     }
                 } else {
                     finish_many<T, GATED, AT>(a, prob, r + u * RPU, RPU, c, v, w);
                 }
             }
-        } else {
+        } else if (c < a.nc) {
 #pragma unroll 1
             for (int u = 0; u < UNITS; ++u) {
                 float v[8], w[8];
@@ -665,7 +696,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                     if (GATED) *(f4v*)(w + e * 4) = *(const f4v*)(src + u * RPU * CROW + 32 + e * 4);
                 }
                 const int ru = r + u * RPU;
-                if (ru >= a.nr || c >= a.nc) continue;
+                if (ru >= a.nr) continue;
                 if (a.splits > 1) {
                     store_floats(part + (int64_t)ru * a.nc + c, a.nc - c, v);
                     if (GATED) store_floats(part + ((int64_t)a.nr + ru) * a.nc + c, a.nc - c, w);
