@@ -49,8 +49,8 @@ dlf_status check_desc(const dlf_ff_desc* d, bool gated, const char* call, Ff& f)
             return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %lld elements, %lld apart", call, q.name, (long long)q.row, (long long)*q.s);
     }
     // the products of the forward pass and of the gradients by the tiles of their grids
-    const int64_t t = 128, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
-    if (std::max({m * o * 2, m * i, 2 * i * o}) >= (int64_t)1 << 23)
+    const int64_t t = 64, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
+    if (std::max({m * o * 2, m * i, 2 * i * o}) >= (int64_t)1 << 24)
         return fail(DLF_ERR_UNSUPPORTED, "%s: %lld rows, %d -> %d features are more tiles than a launch holds", call, (long long)d->rows,
                     d->in_features, d->out_features);
     return DLF_OK;
@@ -151,6 +151,9 @@ double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, in
     double t;
     if (c.shape == DLF_FF_SHAPE_256) {
         t = (double)ceil_div(wgs, 256) * (stages * 1450 + 7000);
+    } else if (c.shape == DLF_FF_SHAPE_ANY64) {
+        t = (double)(wgs / 768) * (stages * 760 + 4000);
+        if (wgs % 768 > 0) t += stages * (wgs % 768 > 512 ? 760 : wgs % 768 > 256 ? 620 : 530) + 4000;
     } else if (c.shape == DLF_FF_SHAPE_ANY) {
         t = (double)(wgs / 512) * (stages * 1250 + 5000);
         if (wgs % 512 > 256) t += stages * 1250 + 5000;
@@ -172,9 +175,12 @@ Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool 
     Cut best;
     double least = 0;
     const int64_t stages = (int64_t)ceil_div(nk, 64) * segments;
-    if (g_force == 2 + DLF_FF_SHAPE_ANY) any = true;
+    auto takes = [&](int shape) {
+        if (shape == DLF_FF_SHAPE_ANY64) return !gated;
+        return shape == DLF_FF_SHAPE_ANY ? any || g_force == 2 + shape : !any;
+    };
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape) {
-        if (any != (shape == DLF_FF_SHAPE_ANY) || (g_force >= 2 && !any && shape != g_force - 2)) continue;
+        if (!takes(shape) || (g_force >= 2 && takes(g_force - 2) && shape != g_force - 2)) continue;
         for (int splits = 1; splits <= 16; ++splits) {
             if (splits > 1 && stages / splits < 4) break;
             if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;

@@ -54,11 +54,11 @@ struct DlfFfSumArgs {
 #define DLF_FF_SUM_ROWS 1024
 #define DLF_FF_MAX_CHUNKS 64
 
-// Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections), its waves and
-// the stages of 64 k that LDS holds.
-struct DlfFfShape { int bc, br, wc, wr, ring; };
-enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_SHAPE_128_DEEP = 3, DLF_FF_NUM_SHAPES = 4 };   // ANY: rows that start anywhere
-static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2, 2, 2}, {128, 128, 2, 2, 2}, {128, 128, 2, 2, 2}, {128, 128, 2, 2, 4}};
+// Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and the stages of
+// 64 k that LDS holds.  ANY: for rows that start anywhere.
+struct DlfFfShape { int bc, br, stages; };
+enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_SHAPE_128_DEEP = 3, DLF_FF_SHAPE_ANY64 = 4, DLF_FF_NUM_SHAPES = 5 };
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2}, {128, 128, 2}, {128, 128, 2}, {128, 128, 4}, {64, 64, 2}};
 
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64

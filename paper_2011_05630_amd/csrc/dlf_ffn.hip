@@ -346,7 +346,7 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
 // are and shifted, zeros moving in: a 16-byte load never leaves the operand.  Only operands of less than eight are read one by one.
 template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
     typedef Loader<N, ROWS, TR, KB> Map;
-    int off[N];
+    unsigned off[N];
     typename T::v8 v[N];
     int64_t line_bytes;
     int edge;               // across: columns of a tile that ends inside a part of eight, else 0
@@ -361,8 +361,8 @@ template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int l = Map::line(first, i), p = Map::part(first, i) * 8, row = GATED ? (l >> 6) * 32 + (l & 31) : l;
-            if (!TR) off[i] = (int)(min(row, avail - 1) * ld + p) * 2;
-            else off[i] = (int)(l * ld + (edge > 0 && !tiny ? min(p, avail - 8) : p < avail ? p : 0)) * 2;
+            if (!TR) off[i] = (unsigned)(min(row, avail - 1) * ld + p) * 2;
+            else off[i] = (unsigned)(l * ld + (edge > 0 && !tiny ? min(p, avail - 8) + 8 : p < avail ? p : 0)) * 2;   // (+ 8: see load)
         }
     }
     // elements of part i that exist, in a stage of `left` k
@@ -374,6 +374,7 @@ template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
     __device__ __forceinline__ void load(const char* base, int first, int k_left)
     {
         tail = k_left < KB ? k_left : 0;
+        if (edge > 0 && !tiny) base -= 16;                  // the last eight columns may begin in front of the tile
         if (tiny) {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = load8<T>(base + off[i], 0, count(first, i, k_left));
@@ -384,7 +385,7 @@ template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int64_t back = !TR ? max(0, 8 - count(first, i, k_left)) * 2 : max(0, Map::line(first, i) - (k_left - 1)) * line_bytes;
-                __builtin_memcpy(&v[i], base + (off[i] - back), 16);
+                __builtin_memcpy(&v[i], base + ((int64_t)off[i] - back), 16);
             }
         }
     }
@@ -545,7 +546,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     // for the stage at lstage: a wave that sent them all at once would wait for the memory pipe, and its multiplications with it.
     constexpr int M = FC * FR;
     auto step = [&](int set, bool reads, unsigned rstage, int rstep, unsigned lstage, int l0, int l1) __attribute__((always_inline)) {
-        constexpr int RPM = (FC + FR + M - 2) / (M - 1);     // reads in front of a multiplication
+        constexpr int RPM = M == 1 ? FC + FR : (FC + FR + M - 2) / (M - 1);     // reads in front of a multiplication
         static_for<0, M>([&](auto mc) __attribute__((always_inline)) {
             constexpr int m = decltype(mc)::value, i = m / FR, j = m % FR;
             if (reads) {
@@ -593,31 +594,37 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
             step(1, false, 0, 0, 0, 0, 0);
             wait_loads<0>();
         } else {
-            // two stages on their way in registers, each with half of them
-            auto lp2 = lp;
-            auto lq2 = lq;
-            auto fetch = [&](auto& p, auto& q) __attribute__((always_inline)) {
+            // RING stages on their way in registers: stage s + 1 in set s % RING when stage s is multiplied
+            decltype(lp) ps[RING];
+            decltype(lq) qs[RING];
+#pragma unroll
+            for (int d = 0; d < RING; ++d) {
+                ps[d] = lp;
+                qs[d] = lq;
+            }
+            auto fetch = [&](int d) __attribute__((always_inline)) {
                 next();
-                p.load(pb, wave * LP, k_left);
-                q.load(qb, wave * LQ, k_left);
+                ps[d].load(pb, wave * LP, k_left);
+                qs[d].load(qb, wave * LQ, k_left);
             };
-            auto put = [&](unsigned stage, auto& p, auto& q) __attribute__((always_inline)) {
-                p.put(stage, wave * LP);
-                q.put(stage + QOFF, wave * LQ);
+            auto put = [&](unsigned stage, int d) __attribute__((always_inline)) {
+                ps[d].put(stage, wave * LP);
+                qs[d].put(stage + QOFF, wave * LQ);
             };
-            fetch(lp, lq);
-            put(0, lp, lq);
-            if (total > 1) fetch(lp, lq);
-            if (total > 2) fetch(lp2, lq2);
+            fetch(0);
+            put(0, 0);
+#pragma unroll
+            for (int d = 0; d < RING; ++d)
+                if (d + 1 < total) fetch(d);
             __builtin_amdgcn_s_waitcnt(WAIT_LDS);
             asm volatile("s_barrier" ::: "memory");
 #pragma unroll
             for (int r = 0; r < FC + FR; ++r) read(0, 0, 0, r);
-            // stage s, of the slot at cur; p and q hold stage s + 1, the other set s + 2
-            auto turn = [&](int s, unsigned cur, auto& p, auto& q) __attribute__((always_inline)) {
+            auto turn = [&](int s, int d) __attribute__((always_inline)) {
+                const unsigned cur = (d & 1) * STAGE;
                 step(0, true, cur, 1, 0, 0, 0);
-                put(STAGE - cur, p, q);                     // everybody has read what was there before
-                if (s + 3 < total) fetch(p, q);
+                put(STAGE - cur, d);                        // everybody has read what was there before
+                if (s + 1 + RING < total) fetch(d);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int k = 1; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
@@ -625,29 +632,28 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                 asm volatile("s_barrier" ::: "memory");
                 step(1, true, STAGE - cur, 0, 0, 0, 0);
             };
+            static_assert(RING % 2 == 0, "two slots of LDS in turn");
             int s = 0;
-            for (; s + 2 < total; s += 2) {
-                turn(s, 0, lp, lq);
-                turn(s + 1, STAGE, lp2, lq2);
-            }
+            for (; s + RING < total; s += RING) static_for<0, RING>([&](auto d) __attribute__((always_inline)) { turn(s + decltype(d)::value, decltype(d)::value); });
             unsigned cur = 0;
-            if (s + 1 < total) {
-                turn(s, 0, lp, lq);
-                cur = STAGE;
-            }
+            static_for<0, RING - 1>([&](auto d) __attribute__((always_inline)) {
+                if (s + decltype(d)::value + 1 < total) {
+                    turn(s + decltype(d)::value, decltype(d)::value);
+                    cur = STAGE - cur;
+                }
+            });
 #pragma unroll
             for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
             step(1, false, 0, 0, 0, 0, 0);
         }
     }
     // ---- epilogue: JB * 32 rows at a time through an area of LDS that is the wave's own ----
-    constexpr int JB = 2, CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;   // columns of the wave, floats of an LDS row, columns of C
+    constexpr int JB = FR == 1 ? 1 : 2, CW = FC * 32, CROW = CW + 4, CO = GATED ? CW / 2 : CW;   // columns of the wave, floats of an LDS row, columns of C
     constexpr int LPR = CO / 8, RPU = 64 / LPR, UNITS = JB * 32 / RPU;         // lanes to a row, rows that they cover at a time
     static_assert(FR % JB == 0, "");
     float* const lf = (float*)ff_lds + wave * (JB * 32 * CROW);
     const int cw = lane % LPR * 8, c = c0 + wc * CO + cw, rw = lane / LPR;
     const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
-    const bool whole = c0 + CF <= a.nc;                                        // uniform over the workgroup
     float* const part = a.part + (int64_t)(split * (GATED ? 2 : a.problems) + prob) * a.nr * a.nc;
     __syncthreads();
 #pragma unroll
@@ -662,7 +668,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                         f4v{acc[i][j + b][q * 4], acc[i][j + b][q * 4 + 1], acc[i][j + b][q * 4 + 2], acc[i][j + b][q * 4 + 3]};
         __builtin_amdgcn_wave_barrier();
         const int r = r0 + (wr * FR + j) * 32 + rw;
-        if (whole || a.nc - c >= 8) {
+        if (a.nc - c >= 8) {
             constexpr int AT = UNITS < 4 ? UNITS : 4;                          // units whose waits are shared
 #pragma unroll 1
             for (int u = 0; u < UNITS; u += AT) {
@@ -686,23 +692,23 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
                     finish_many<T, GATED, AT>(a, prob, r + u * RPU, RPU, c, v, w);
                 }
             }
-        } else if (c < a.nc) {
-#pragma unroll 1
-            for (int u = 0; u < UNITS; ++u) {
-                float v[8], w[8];
+        }
+        // columns behind the last eight: a lane to a row
+        const int cols = a.nc - c0 - wc * CO, ct = cols & ~7, rt = r0 + (wr * FR + j) * 32 + lane;
+        if (cols < CO && (cols & 7) != 0 && cols > 0 && lane < JB * 32 && rt < a.nr) {
+            float v[8], w[8];
+            const float* const st = lf + lane * CROW + (GATED ? (ct >> 5) * 64 + (ct & 31) : ct);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    *(f4v*)(v + e * 4) = *(const f4v*)(src + u * RPU * CROW + e * 4);
-                    if (GATED) *(f4v*)(w + e * 4) = *(const f4v*)(src + u * RPU * CROW + 32 + e * 4);
-                }
-                const int ru = r + u * RPU;
-                if (ru >= a.nr) continue;
-                if (a.splits > 1) {
-                    store_floats(part + (int64_t)ru * a.nc + c, a.nc - c, v);
-                    if (GATED) store_floats(part + ((int64_t)a.nr + ru) * a.nc + c, a.nc - c, w);
-                } else {
-                    finish<T, GATED, 8>(a, prob, ru, c, a.nc - c, v, w);
-                }
+            for (int e = 0; e < 2; ++e) {
+                *(f4v*)(v + e * 4) = *(const f4v*)(st + e * 4);
+                if (GATED) *(f4v*)(w + e * 4) = *(const f4v*)(st + 32 + e * 4);
+            }
+            const int ca = c0 + wc * CO + ct, n = cols & 7;
+            if (a.splits > 1) {
+                store_floats(part + (int64_t)rt * a.nc + ca, n, v);
+                if (GATED) store_floats(part + ((int64_t)a.nr + rt) * a.nc + ca, n, w);
+            } else {
+                finish<T, GATED, 8>(a, prob, rt, ca, n, v, w);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -1026,7 +1032,10 @@ __global__ __launch_bounds__(256) void k_ff_sum(const DlfFfSumArgs a)
 // The tile kernels by shape (DLF_FF_SHAPE_*): waves across c and r, k of a stage, stages in LDS, direct loads.
 template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
 {
-    if (gated) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, true>;
+    if (gated) {
+        if constexpr (BC >= 128) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, true>;
+        return nullptr;                     // (two projections of 64 x 64 with four stages in registers do not fit them)
+    }
     switch (layout) {
     case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, false>;
     case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>;
@@ -1039,13 +1048,14 @@ template <typename T> static void (*tile_kernel(int shape, int layout, int gated
     case DLF_FF_SHAPE_256: return tile_of<T, 256, 256, 2, 2, 64, 2, true>(layout, gated);
     case DLF_FF_SHAPE_128: return tile_of<T, 128, 128, 2, 2, 64, 2, true>(layout, gated);
     case DLF_FF_SHAPE_128_DEEP: return tile_of<T, 128, 128, 2, 2, 64, 4, true>(layout, gated);
+    case DLF_FF_SHAPE_ANY64: return tile_of<T, 64, 64, 2, 2, 64, 4, false>(layout, gated);
     default: return tile_of<T, 128, 128, 2, 2, 64, 2, false>(layout, gated);
     }
 }
 static size_t tile_lds(int shape)
 {
     const DlfFfShape& s = DLF_FF_SHAPES[shape];
-    const size_t ring = (size_t)s.ring * 64 * (s.bc + s.br) * 2, out = (size_t)s.wc * s.wr * 64 * (s.bc / s.wc + 4) * 4;
+    const size_t ring = (size_t)s.stages * 64 * (s.bc + s.br) * 2, out = (size_t)4 * (s.br < 128 ? 32 : 64) * (s.bc / 2 + 4) * 4;
     return ring > out ? ring : out;
 }
 template <typename T> static void (*rows_kernel(int nf, int mr, int gated))(const DlfFfArgs)
@@ -1085,6 +1095,7 @@ extern "C" int dlf_ff_kernels_init(void)
         for (int k = 0; k < 8; ++k) {
             const int layout = k >> 1 & 3, gated = layout == 3;
             auto f = (k & 1) ? tile_kernel<BF16>(shape, gated ? 0 : layout, gated) : tile_kernel<F16>(shape, gated ? 0 : layout, gated);
+            if (f == nullptr) continue;
             const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
             if (e != hipSuccess) return (int)e;
         }
@@ -1093,9 +1104,8 @@ extern "C" int dlf_ff_kernels_init(void)
 extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream)
 {
     const unsigned tiles = (unsigned)(a->tiles_r * a->tiles_c * a->problems * a->splits);
-    const DlfFfShape& s = DLF_FF_SHAPES[shape];
     hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, layout, gated) : tile_kernel<BF16>(shape, layout, gated),
-                       dim3((tiles + 7) / 8 * 8), dim3((unsigned)(s.wc * s.wr * 64)), tile_lds(shape), (hipStream_t)stream, *a);
+                       dim3((tiles + 7) / 8 * 8), dim3(256), tile_lds(shape), (hipStream_t)stream, *a);
     if (a->splits > 1) {
         const int64_t units = (int64_t)a->nr * a->problems * ((a->nc + 7) / 8);
         hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? k_ff_join<F16, true> : k_ff_join<F16, false>) : (gated ? k_ff_join<BF16, true> : k_ff_join<BF16, false>),
