@@ -10,31 +10,54 @@ HEADERS = ["dlf_internal.h", "dlf_ffn.h", os.path.join("..", "..", "include", "d
            os.path.join("..", "..", "include", "dlf_debug.h")]
 
 
+# The feed-forward operators on PyTorch's tensors; links against libdlf.so beside it and the libraries of the PyTorch it is built with.
+TORCH_SOURCE = "dlf_torch.cpp"
+TORCH_LIB = os.path.join(HERE, "_dlf_torch.so")
+
+
 def needs_build():
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(TORCH_LIB)):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_LIB))
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS + [TORCH_SOURCE])
+
+
+def _run(cmd, target, tmp):
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed:\n%s" % (cmd[0], out))
+    if out.strip():
+        print(out)
+    os.replace(tmp, target)
+
+
+def build_torch():
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension as ext
+    tmp = TORCH_LIB + ".tmp.%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    cmd += ["-I" + p for p in ext.include_paths() + [sysconfig.get_paths()["include"]]]
+    cmd += ["-o", tmp, os.path.join(CSRC, TORCH_SOURCE), "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+    for p in ext.library_paths():
+        cmd += ["-L" + p, "-Wl,-rpath," + p]
+    _run(cmd + ["-lc10", "-ltorch_cpu", "-ltorch_python"], TORCH_LIB, tmp)
 
 
 def build(force=True, verbose=False):
     if not force and not needs_build():
         return LIB
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = ["hipcc", "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    cmd = ["hipcc", "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared", "-Wl,-soname," + os.path.basename(LIB),
            "-x", "hip",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Wno-unused-command-line-argument",
            "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-save-temps=obj")
-    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if out.strip():
-        print(out)
-    os.replace(tmp, LIB)
+    _run(cmd, LIB, tmp)
+    build_torch()
     return LIB
 
 

@@ -170,7 +170,7 @@ double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, in
 }
 
 // any: the operands' rows start anywhere.
-Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
+Cut least_cut(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
 {
     Cut best;
     double least = 0;
@@ -190,6 +190,26 @@ Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool 
         }
     }
     return best;
+}
+
+// A call asks for its products' cuts several times (sizes of workspaces, launches), a program for the same ones again and again: the last
+// ones are kept by their sizes.
+Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
+{
+    struct Kept {
+        int64_t key[6];
+        Cut cut;
+    };
+    static thread_local Kept kept[64] = {};
+    const int64_t key[6] = {nr, nc, nk, segments * 16 + problems * 4 + (gated ? 2 : 0) + (any ? 1 : 0), g_force, g_force_splits};
+    uint64_t h = 0;
+    for (int64_t k : key) h = (h ^ (uint64_t)k) * 0x9e3779b97f4a7c15ull;
+    Kept& e = kept[h >> 58];
+    if (memcmp(e.key, key, sizeof key) != 0) {
+        e.cut = least_cut(nr, nc, nk, segments, problems, gated, any);
+        memcpy(e.key, key, sizeof key);
+    }
+    return e.cut;
 }
 
 // Workspace of a product: what its addresses are is not known yet.

@@ -13,7 +13,17 @@ import torch
 
 from . import binding as B
 
-_TYPE = {torch.float16: "fp16", torch.bfloat16: "bf16"}
+_TYPES = (torch.float16, torch.bfloat16)
+
+
+def _native():
+    B.lib()                     # a missing library says so itself
+    from . import _dlf_torch
+    return _dlf_torch
+
+
+def _stream(index):
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _need(ok, msg, *a):
@@ -22,7 +32,7 @@ def _need(ok, msg, *a):
 
 
 def _weight(t, name):
-    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPE, "%s: a 2-dimensional fp16 or bf16 tensor on the GPU expected", name)
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES, "%s: a 2-dimensional fp16 or bf16 tensor on the GPU expected", name)
     _need(t.shape[0] > 0 and t.shape[1] > 0, "%s: empty", name)
     _stride(t, name)
     return t
@@ -43,67 +53,17 @@ def _stride(t, name):
 
 
 class _Operator:
-    """What the operators share: the weights' type, device and sizes, views of the operands as rows, the call itself."""
+    """What the operators share: the weights' type, device and sizes, and the native operator that holds them."""
 
-    def _setup(self, w, act):
+    def _setup(self, gated, act, weights, biases):
         if act not in B.FF_ACT:
             raise ValueError("act: one of %s expected" % ", ".join(sorted(B.FF_ACT)))
+        w = weights[0]
         self.act, self.dtype, self.device = act, w.dtype, w.device
         self.out_features, self.in_features = w.shape
-        self._index, self._w_stride = w.get_device(), _stride(w, "weight")
-        self._calls = {}        # descriptions by call, rows and strides, with the workspace they ask for
-
-    def _rows(self, t, width, name, rows=None):
-        """t as rows, and their distance."""
-        if not isinstance(t, torch.Tensor) or t.dtype is not self.dtype or t.get_device() != self._index or t.dim() < 1 or t.shape[-1] != width:
-            raise ValueError("%s: a %s tensor [..., %d] on %s expected" % (name, self.dtype, width, self.device))
-        if t.dim() != 2:
-            try:
-                t = t.view(-1, width)
-            except RuntimeError:
-                raise ValueError("%s: its rows do not lie at one distance" % name) from None
-        m, (s, one) = t.shape[0], t.stride()
-        if rows is not None and m != rows:
-            raise ValueError("%s: %d rows expected" % (name, rows))
-        if one != 1 and width != 1:
-            raise ValueError("%s: a row's elements have to lie next to each other" % name)
-        if m <= 1:
-            s = width
-        elif s < width:
-            raise ValueError("%s: rows overlap" % name)
-        return t, s
-
-    def _out(self, out, shape, rows):
-        if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-            return out, out, self.out_features
-        _need(out.shape == shape, "out: shape %s expected", tuple(shape))
-        return (out,) + self._rows(out, self.out_features, "out", rows)
-
-    def _saved(self, saved, shape):
-        _need(isinstance(saved, torch.Tensor) and saved.dtype == torch.float32 and saved.device == self.device and tuple(saved.shape) == shape and
-              saved.is_contiguous(), "saved: the tensor that the forward call returned, fp32 %s, expected", shape)
-        return saved
-
-    def _call(self, name, rows, strides, *tensors):
-        """strides: of x, y, residual and dy."""
-        key = (name, rows, strides)
-        call = self._calls.get(key)
-        if call is None:
-            xs, ys, rs, ds = strides
-            desc = B.dlf_ff_desc(_TYPE[self.dtype], self.act, rows, self.in_features, self.out_features, xs, self._w_stride, ys, rs, ds)
-            if len(self._calls) >= 1024:
-                self._calls.clear()
-            call = self._calls[key] = (getattr(B, name), desc, B._ff_workspace(name, desc))
-        f, desc, need = call
-        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        ptr = [None if t is None else t.data_ptr() for t in tensors]
-        ptr.append(None if ws is None else ws.data_ptr())
-        if torch.cuda.current_device() == self._index:
-            f(desc, *ptr, need, torch._C._cuda_getCurrentRawStream(self._index))
-        else:
-            with torch.cuda.device(self._index):
-                f(desc, *ptr, need, torch._C._cuda_getCurrentRawStream(self._index))
+        self._index = w.get_device()
+        op = _native().Op(gated, B.FF_ACT[act], *weights, *biases, _stride(w, "weight"))
+        self._forward, self._backward = op.forward, op.backward
 
 
 class Linear(_Operator):
@@ -111,45 +71,21 @@ class Linear(_Operator):
 
     def __init__(self, weight, bias=None, act="none"):
         self.weight = _weight(weight, "weight")
-        self._setup(weight, act)
-        self.bias = _bias(bias, self.out_features, weight, "bias")
-
-    def _forward(self, x, residual, out, save):
-        x2, xs = self._rows(x, self.in_features, "x")
-        rows = x2.shape[0]
-        shape = x.shape[:-1] + (self.out_features,)
-        rs = 0
-        if residual is not None:
-            _need(residual.shape == shape, "residual: shape %s expected", tuple(shape))
-            residual, rs = self._rows(residual, self.out_features, "residual", rows)
-        out, o2, ys = self._out(out, shape, rows)
-        saved = torch.empty((rows, self.out_features), dtype=torch.float32, device=self.device) if save and self.act != "none" else None
-        self._call("dlf_linear", rows, (xs, ys, rs, 0), x2, self.weight, self.bias, residual, o2, saved)
-        return out, saved
+        self.bias = _bias(bias, weight.shape[0], weight, "bias")
+        self._setup(False, act, (weight, None), (bias, None))
 
     def run(self, x, residual=None, out=None):
         """-> y [..., out]; written to `out` if given (which may be the residual)."""
-        return self._forward(x, residual, out, False)[0]
+        return self._forward(x, residual, out, False, _stream(self._index))
 
     def run_saved(self, x, residual=None, out=None):
         """-> (y, saved): the pre-activations that `backward` needs, fp32 [rows, out]; None without an activation."""
-        return self._forward(x, residual, out, True)
+        return self._forward(x, residual, out, True, _stream(self._index))
 
     def backward(self, dy, x, saved, need=("x", "weight", "bias")):
         """Gradients for dy, the gradient of y: -> (dx, dweight, dbias), None for what `need` leaves out or the layer lacks.
         x and saved are those of the forward call.  The gradient of its residual is dy."""
-        x2, xs = self._rows(x, self.in_features, "x")
-        rows = x2.shape[0]
-        _need(tuple(dy.shape) == tuple(x.shape[:-1]) + (self.out_features,), "dy: the shape of y expected")
-        d2, ds = self._rows(dy, self.out_features, "dy", rows)
-        if self.act != "none":
-            self._saved(saved, (rows, self.out_features))
-        new = lambda shape, t: torch.empty(shape, dtype=t, device=self.device)  # noqa: E731
-        dx = new(tuple(x.shape), self.dtype) if "x" in need else None
-        dw = new((self.out_features, self.in_features), self.dtype) if "weight" in need else None
-        db = new((self.out_features,), torch.float32) if "bias" in need and self.bias is not None else None
-        self._call("dlf_linear_backward", rows, (xs, 0, 0, ds), d2, x2, self.weight, saved if self.act != "none" else None, dx, dw, db)
-        return dx, dw, db
+        return self._backward(dy, x, saved, "x" in need, "weight" in need, "bias" in need, _stream(self._index))
 
 
 class GatedLinear(_Operator):
@@ -160,39 +96,21 @@ class GatedLinear(_Operator):
         self.w_gate, self.w_up = _weight(w_gate, "w_gate"), _weight(w_up, "w_up")
         _need(w_up.shape == w_gate.shape and w_up.dtype == w_gate.dtype and w_up.device == w_gate.device and
               _stride(w_up, "w_up") == _stride(w_gate, "w_gate"), "w_up: shape, type, device and row distance of w_gate expected")
-        self._setup(w_gate, act)
-        self.b_gate, self.b_up = (_bias(b, self.out_features, w_gate, n) for b, n in ((b_gate, "b_gate"), (b_up, "b_up")))
-
-    def _forward(self, x, out, save):
-        x2, xs = self._rows(x, self.in_features, "x")
-        rows = x2.shape[0]
-        out, o2, ys = self._out(out, x.shape[:-1] + (self.out_features,), rows)
-        saved = torch.empty((2, rows, self.out_features), dtype=torch.float32, device=self.device) if save else None
-        self._call("dlf_gated", rows, (xs, ys, 0, 0), x2, self.w_gate, self.w_up, self.b_gate, self.b_up, o2, saved)
-        return out, saved
+        self.b_gate, self.b_up = (_bias(b, w_gate.shape[0], w_gate, n) for b, n in ((b_gate, "b_gate"), (b_up, "b_up")))
+        self._setup(True, act, (w_gate, w_up), (b_gate, b_up))
 
     def run(self, x, out=None):
         """-> h [..., out]; written to `out` if given."""
-        return self._forward(x, out, False)[0]
+        return self._forward(x, None, out, False, _stream(self._index))
 
     def run_saved(self, x, out=None):
         """-> (h, saved): both projections' results, which `backward` needs, fp32 [2, rows, out]."""
-        return self._forward(x, out, True)
+        return self._forward(x, None, out, True, _stream(self._index))
 
     def backward(self, dh, x, saved, need=("x", "weight", "bias")):
         """Gradients for dh, the gradient of h: -> (dx, dw_gate, dw_up, db_gate, db_up), None for what `need` leaves out or the
         layer lacks.  x and saved are those of the forward call."""
-        x2, xs = self._rows(x, self.in_features, "x")
-        rows = x2.shape[0]
-        _need(tuple(dh.shape) == tuple(x.shape[:-1]) + (self.out_features,), "dh: the shape of h expected")
-        d2, ds = self._rows(dh, self.out_features, "dh", rows)
-        self._saved(saved, (2, rows, self.out_features))
-        new = lambda shape, t: torch.empty(shape, dtype=t, device=self.device)  # noqa: E731
-        dx = new(tuple(x.shape), self.dtype) if "x" in need else None
-        dw = [new((self.out_features, self.in_features), self.dtype) if "weight" in need else None for _ in range(2)]
-        db = [new((self.out_features,), torch.float32) if "bias" in need and b is not None else None for b in (self.b_gate, self.b_up)]
-        self._call("dlf_gated_backward", rows, (xs, 0, 0, ds), d2, x2, self.w_gate, self.w_up, saved, dx, *dw, *db)
-        return (dx, *dw, *db)
+        return self._backward(dh, x, saved, "x" in need, "weight" in need, "bias" in need, _stream(self._index))
 
 
 class FeedForward:
