@@ -86,7 +86,7 @@ dlf_status dlf_debug_check_launches(const dlf_plan_t* plan);
 /* Testing hook: the kernels of the feed-forward operators' products: kernel 0 = by the library's rule (default), 1 = few rows always on the
  * kernel for rows that start anywhere, 2 / 3 = tiles of 256 x 256 / 128 x 128 wherever the operands' alignment allows them, 4 = tiles of 128 x
  * 128 through registers, 5 = tiles of 128 x 128 with four stages in LDS, 6 =
- * tiles of 64 x 64 through registers; splits > 0: that many workgroups share every tile's k, as far as it goes (0: by rule).  It changes the
+ * tiles of 64 x 64 through registers, 7 = gated products on tiles of 2 x 32 x 128 through registers; splits > 0: that many workgroups share every tile's k, as far as it goes (0: by rule).  It changes the
  * workspace that a call needs.  Process-wide, not thread-safe. */
 void dlf_debug_ff_kernel(int32_t kernel, int32_t splits);
 

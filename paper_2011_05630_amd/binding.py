@@ -479,8 +479,8 @@ def dlf_debug_small_pair_mode(mode=0, shape=-1, waves=0):
 
 def dlf_debug_ff_kernel(kernel=0, splits=0):
     """Testing hook: 0 = the feed-forward operators' kernels by the library's rule, 1 = few rows on the kernel for rows that start
-    anywhere, 2 / 3 / 4 / 5 / 6 = tiles of 256 x 256 / 128 x 128 / 128 x 128 through
-    registers / 128 x 128 with four stages in LDS / 64 x 64 through registers; splits > 0: so many workgroups share a tile's k."""
+    anywhere, 2 / 3 / 4 / 5 / 6 / 7 = tiles of 256 x 256 / 128 x 128 / 128 x 128 through
+    registers / 128 x 128 with four stages in LDS / 64 x 64 through registers / 2 x 32 x 128 (gated) through registers; splits > 0: so many workgroups share a tile's k."""
     lib().dlf_debug_ff_kernel(kernel, splits)
 
 

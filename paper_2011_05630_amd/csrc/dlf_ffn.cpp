@@ -48,9 +48,9 @@ dlf_status check_desc(const dlf_ff_desc* d, bool gated, const char* call, Ff& f)
         if (*q.s < q.row || *q.s >= (int64_t)1 << 24)
             return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %lld elements, %lld apart", call, q.name, (long long)q.row, (long long)*q.s);
     }
-    // the products of the forward pass and of the gradients by the tiles of their grids
+    // the products of the forward pass and of the gradients, with the column sums, by the workgroups of their launches
     const int64_t t = 64, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
-    if (std::max({m * o * 2, m * i, 2 * i * o}) >= (int64_t)1 << 24)
+    if (std::max(m * o * 2, m * i + 2 * i * o + 2 * o) >= (int64_t)1 << 24)
         return fail(DLF_ERR_UNSUPPORTED, "%s: %lld rows, %d -> %d features are more tiles than a launch holds", call, (long long)d->rows,
                     d->in_features, d->out_features);
     return DLF_OK;
@@ -141,109 +141,147 @@ Cut cut_as(int shape, int splits, int64_t nr, int64_t nc, int problems, bool gat
     return c;
 }
 
-// Modelled time of a cut in ns, from measurements at 4096^3 and around: a stage of 64 k takes a 256 x 256 tile 1450 ns; two 128 x 128
-// tiles that share a compute unit 900 ns, one that has it to itself waits for memory, 900 ns a stage, unless four stages are on their way: 500;
-// through registers 1250 and 950; the first loads and the epilogue of a tile 7, 4 and 5 us; joining, a launch and the partial sums' bytes twice.
-double cut_ns(const Cut& c, int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+// Modelled times in ns, from measurements at 4096^3 and around.  A stage of 64 k takes a 256 x 256 tile 1450; two 128 x 128 tiles that share
+// a compute unit 900, and one that has it to itself waits for memory as long, unless four stages are on their way: 500.  Through registers
+// tiles share a compute unit by two (128 x 128) or three.  The first loads and the epilogue of a tile come on top.
+struct Rate {
+    int share;              // workgroups of a compute unit
+    double stage[3], rest;  // by how many share it
+};
+const Rate& rate(int shape)
 {
-    const int64_t wgs = (int64_t)c.tiles_r * c.tiles_c * problems * c.splits;
-    const double stages = (double)ceil_div(nk, 64) * segments / c.splits;
-    double t;
-    if (c.shape == DLF_FF_SHAPE_256) {
-        t = (double)ceil_div(wgs, 256) * (stages * 1450 + 7000);
-    } else if (c.shape == DLF_FF_SHAPE_ANY64) {
-        t = (double)(wgs / 768) * (stages * 760 + 4000);
-        if (wgs % 768 > 0) t += stages * (wgs % 768 > 512 ? 760 : wgs % 768 > 256 ? 620 : 530) + 4000;
-    } else if (c.shape == DLF_FF_SHAPE_ANY) {
-        t = (double)(wgs / 512) * (stages * 1250 + 5000);
-        if (wgs % 512 > 256) t += stages * 1250 + 5000;
-        else if (wgs % 512 > 0) t += stages * 950 + 5000;
-    } else if (c.shape == DLF_FF_SHAPE_128_DEEP) {
-        t = (double)ceil_div(wgs, 256) * (stages * 500 + 5000);
-    } else {
-        t = (double)(wgs / 512) * (stages * 900 + 4000);
-        if (wgs % 512 > 256) t += stages * 900 + 4000;
-        else if (wgs % 512 > 0) t += stages * 900 + 4000;
+    static const Rate rates[DLF_FF_NUM_SHAPES] = {{1, {1450}, 7000}, {2, {900, 900}, 4000}, {2, {950, 1250}, 5000}, {1, {500}, 5000},
+                                                  {3, {530, 620, 760}, 4000}, {2, {640, 850}, 4000}};
+    return rates[shape];
+}
+// Tiles of two lengths, the first kind's started first, as they fill the compute units.
+double fill_ns(int shape, int64_t n0, double stages0, int64_t n1, double stages1)
+{
+    const Rate& r = rate(shape);
+    const int level = (int)std::min<int64_t>(r.share, std::max<int64_t>(1, ceil_div(n0 + n1, 256))) - 1;
+    const int64_t slots = 256 * (level + 1);
+    const double t0 = stages0 * r.stage[level] + r.rest, t1 = stages1 * r.stage[level] + r.rest, a = (double)(n0 / slots) * t0;
+    const int64_t late = n0 % slots;                          // slots that are free t0 later than the others
+    double end = late > 0 ? a + t0 : a;
+    if (n1 > 0) {
+        double last = 0;
+        for (int64_t k = std::max<int64_t>(0, n1 / slots - (int64_t)(t0 / t1) - 2);; ++k) {     // rounds of the slots that are free first
+            const double at = a + (double)(k + 1) * t1, second = late > 0 ? std::max(0.0, at - a - t0) / t1 : 0;
+            last = at;
+            if ((slots - late) * (k + 1) + late * (int64_t)(second + 1e-9) >= n1) break;
+            if (late > 0) {                                   // the late ones' round that ends before the next
+                const int64_t q = (int64_t)(second + 1e-9) + 1;
+                const double at2 = a + t0 + (double)q * t1;
+                last = at2;
+                if (at2 < at + t1 && (slots - late) * (k + 1) + late * q >= n1) break;
+            }
+        }
+        end = std::max(end, last);
     }
-    if (c.splits > 1) t += 3500 + (double)c.part_bytes * 2 / 4000;
-    return t;
+    return end;
+}
+double join_ns(size_t part_bytes) { return part_bytes > 0 ? 3500 + (double)part_bytes * 2 / 4000 : 0; }
+
+// The splits that a product may have: at least four stages each.
+template <typename F> void each_split(int64_t stages, F&& f)
+{
+    for (int splits = 1; splits <= 16; ++splits) {
+        if (splits > 1 && stages / splits < 4) break;
+        if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;
+        f(splits);
+    }
+}
+// any: the operands' rows start anywhere.  (Tiles through registers take all operands; the larger ones lose where direct loads apply.)
+bool takes(int shape, bool gated, bool any)
+{
+    if (shape == DLF_FF_SHAPE_ANY64) return !gated;
+    if (shape == DLF_FF_SHAPE_ANY64G) return gated;
+    return shape == DLF_FF_SHAPE_ANY ? any || g_force == 2 + shape : !any;
+}
+template <typename F> void each_shape(bool gated, bool any, F&& f)
+{
+    const bool forced = g_force >= 2 && takes(g_force - 2, gated, any);
+    for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
+        if (takes(shape, gated, any) && (!forced || shape == g_force - 2)) f(shape);
 }
 
-// any: the operands' rows start anywhere.
-Cut least_cut(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
+Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
 {
     Cut best;
     double least = 0;
-    const int64_t stages = (int64_t)ceil_div(nk, 64) * segments;
-    auto takes = [&](int shape) {
-        if (shape == DLF_FF_SHAPE_ANY64) return !gated;
-        return shape == DLF_FF_SHAPE_ANY ? any || g_force == 2 + shape : !any;
-    };
-    for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape) {
-        if (!takes(shape) || (g_force >= 2 && takes(g_force - 2) && shape != g_force - 2)) continue;
-        for (int splits = 1; splits <= 16; ++splits) {
-            if (splits > 1 && stages / splits < 4) break;
-            if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;
-            const Cut c = cut_as(shape, splits, nr, nc, problems, gated);
-            const double t = cut_ns(c, nr, nc, nk, segments, problems, gated);
+    each_shape(gated, any, [&](int shape) {
+        each_split(ceil_div(nk, 64), [&](int splits) {
+            const Cut c = cut_as(shape, splits, nr, nc, 1, gated);
+            const double t = fill_ns(shape, (int64_t)c.tiles_r * c.tiles_c * splits, (double)ceil_div(nk, 64) / splits, 0, 0) + join_ns(c.part_bytes);
             if (least == 0 || t < least) { least = t; best = c; }
-        }
-    }
+        });
+    });
     return best;
 }
 
-// A call asks for its products' cuts several times (sizes of workspaces, launches), a program for the same ones again and again: the last
-// ones are kept by their sizes.
-Cut choose(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated, bool any)
+// The two products of a backward pass in one launch: both in tiles of one shape.
+struct BackCut {
+    Cut w, x;
+};
+// rows, in, out as of the layer; problems: 2 for the gated pair
+BackCut least_back(int64_t rows, int64_t in, int64_t out, int problems, bool any, bool want_w, bool want_x)
+{
+    BackCut best;
+    double least = 0;
+    const int64_t stages_w = ceil_div(rows, 64), stages_x = (int64_t)ceil_div(out, 64) * problems;
+    each_shape(false, any, [&](int shape) {
+        each_split(want_w ? stages_w : 1, [&](int sw) {
+            const Cut w = cut_as(shape, sw, out, in, problems, false);
+            each_split(want_x ? stages_x : 1, [&](int sx) {
+                const Cut x = cut_as(shape, sx, rows, in, 1, false);
+                const double t = fill_ns(shape, want_w ? (int64_t)w.tiles_r * w.tiles_c * problems * sw : 0, (double)stages_w / sw,
+                                         want_x ? (int64_t)x.tiles_r * x.tiles_c * sx : 0, (double)stages_x / sx) +
+                                 join_ns((want_w ? w.part_bytes : 0) + (want_x ? x.part_bytes : 0));
+                if (least == 0 || t < least) { least = t; best = {w, x}; }
+            });
+        });
+    });
+    if (!want_w) best.w.part_bytes = 0;
+    if (!want_x) best.x.part_bytes = 0;
+    return best;
+}
+
+// A call asks for its cuts several times (sizes of workspaces, launches), a program for the same ones again and again: the last ones are
+// kept by their sizes.
+template <typename C, typename F> C kept_cut(const int64_t (&sizes)[4], F&& make)
 {
     struct Kept {
         int64_t key[6];
-        Cut cut;
+        C cut;
     };
     static thread_local Kept kept[64] = {};
-    const int64_t key[6] = {nr, nc, nk, segments * 16 + problems * 4 + (gated ? 2 : 0) + (any ? 1 : 0), g_force, g_force_splits};
+    const int64_t key[6] = {sizes[0], sizes[1], sizes[2], sizes[3], g_force, g_force_splits};
     uint64_t h = 0;
     for (int64_t k : key) h = (h ^ (uint64_t)k) * 0x9e3779b97f4a7c15ull;
     Kept& e = kept[h >> 58];
     if (memcmp(e.key, key, sizeof key) != 0) {
-        e.cut = least_cut(nr, nc, nk, segments, problems, gated, any);
+        e.cut = make();
         memcpy(e.key, key, sizeof key);
     }
     return e.cut;
 }
-
-// Workspace of a product: what its addresses are is not known yet.
-size_t part_bytes(int64_t nr, int64_t nc, int64_t nk, int segments, int problems, bool gated)
+Cut choose(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
 {
-    return std::max(choose(nr, nc, nk, segments, problems, gated, false).part_bytes, choose(nr, nc, nk, segments, problems, gated, true).part_bytes);
+    return kept_cut<Cut>({nr, nc, nk, (gated ? 2 : 0) + (any ? 1 : 0)}, [&] { return least_forward(nr, nc, nk, gated, any); });
+}
+BackCut choose_back(int64_t rows, int64_t in, int64_t out, int problems, bool any, bool want_w, bool want_x)
+{
+    return kept_cut<BackCut>({rows, in, out, problems * 8 + (any ? 4 : 0) + (want_w ? 2 : 0) + (want_x ? 1 : 0)},
+                             [&] { return least_back(rows, in, out, problems, any, want_w, want_x); });
 }
 
 bool is_few(int64_t rows) { return rows <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 1); }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// One product of the operators; part: the workspace of its cut.
-dlf_status product(const Ff& f, DlfFfArgs& a, int layout, bool gated, char* part, void* stream)
-{
-    TRY(kernels_ready());
-    if (layout == DLF_FF_NN && is_few(a.nr)) return few_rows(f, a, gated, stream);
-    bool whole = true;
-    const int n = gated ? 2 : std::max(a.segments, a.problems);
-    for (int i = 0; i < n; ++i) {
-        whole = whole && lines(a.p[i], a.ldp, layout == DLF_FF_NN ? a.nk : a.nc);
-        if (!gated) whole = whole && lines(a.q[i], a.ldq, layout == DLF_FF_TT ? a.nr : a.nk);
-    }
-    if (gated) whole = whole && lines(a.q[0], a.ldq, a.nk);
-    const Cut c = choose(a.nr, a.nc, a.nk, a.segments, a.problems, gated, !whole);
-    a.tiles_r = c.tiles_r;
-    a.tiles_c = c.tiles_c;
-    a.splits = c.splits;
-    a.part = (float*)part;
-    return launched(f, dlf_ff_start_tile(&a, c.shape, f.d.dtype, layout, gated, stream));
-}
-
-// The workspace of a backward call.
+// The workspace of a backward call: dz, partial column sums, partial sums of the products.  What the addresses are, and which gradients are
+// wanted, is not known where its size is asked for.
 struct BackLayout {
-    size_t lddz = 0, part = 0, join = 0, bytes = 0;   // elements per row of dz; offsets of the column sums and of the products' partial sums
+    size_t lddz = 0, part = 0, join = 0, bytes = 0;   // elements per row of dz; offsets
     int chunk = 0, chunks = 0;
 };
 bool needs_dz(const Ff& f) { return f.gated || f.d.act != DLF_ACT_NONE; }
@@ -252,22 +290,37 @@ BackLayout back_layout(const Ff& f)
     BackLayout l;
     const size_t nz = f.gated ? 2 : 1;
     l.lddz = ((size_t)f.d.out_features + 7) / 8 * 8;
-    l.chunk = f.d.rows <= DLF_FF_SUM_ROWS ? DLF_FF_SUM_ROWS : (f.d.rows + DLF_FF_MAX_CHUNKS - 1) / DLF_FF_MAX_CHUNKS;
-    l.chunks = f.d.rows > 0 ? (int)((f.d.rows + l.chunk - 1) / l.chunk) : 1;
+    l.chunk = std::max(1, ceil_div(f.d.rows, (int64_t)DLF_FF_MAX_CHUNKS * DLF_FF_CHUNK_ROWS)) * DLF_FF_CHUNK_ROWS;
+    l.chunks = std::max(1, ceil_div(f.d.rows, l.chunk));
     if (needs_dz(f)) l.bytes = nz * align256((size_t)f.d.rows * l.lddz * 2);
     l.part = l.bytes;
     if (l.chunks > 1) l.bytes += align256(nz * l.chunks * (size_t)f.d.out_features * 4);
     l.join = l.bytes;
-    const int problems = f.gated ? 2 : 1;
-    l.bytes += align256(std::max(part_bytes(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, problems, 1, false),
-                                 part_bytes(f.d.out_features, f.d.in_features, f.d.rows, 1, problems, false)));
+    size_t most = 0;
+    if (f.d.rows > 0)
+        for (int k = 0; k < 8; ++k) {
+            const bool want_w = k & 1, want_x = k & 2;
+            if (!want_w && !want_x) continue;
+            const BackCut c = choose_back(f.d.rows, f.d.in_features, f.d.out_features, (int)nz, k & 4, want_w, want_x);
+            most = std::max(most, align256(c.w.part_bytes) + c.x.part_bytes);
+        }
+    l.bytes += align256(most);
     return l;
 }
 
 size_t forward_ws(const Ff& f)
 {
     if (f.d.rows == 0 || is_few(f.d.rows)) return 0;
-    return align256(part_bytes(f.d.rows, f.d.out_features, f.d.in_features, 1, 1, f.gated));
+    const int64_t nr = f.d.rows, nc = f.d.out_features, nk = f.d.in_features;
+    return align256(std::max(choose(nr, nc, nk, f.gated, false).part_bytes, choose(nr, nc, nk, f.gated, true).part_bytes));
+}
+
+void set_cut(DlfFfArgs& a, const Cut& c, char* part)
+{
+    a.tiles_r = c.tiles_r;
+    a.tiles_c = c.tiles_c;
+    a.splits = c.splits;
+    a.part = (float*)part;
 }
 
 dlf_status forward(const Ff& f, const void* x, const void* const w[2], const float* const bias[2], const void* res, void* y, float* saved,
@@ -285,7 +338,12 @@ dlf_status forward(const Ff& f, const void* x, const void* const w[2], const flo
     a.res = res; a.ldres = f.d.res_stride;
     a.out[0] = y; a.ldo = f.d.y_stride;
     a.saved = saved; a.act = f.d.act;
-    return product(f, a, DLF_FF_NN, f.gated, ws, stream);
+    TRY(kernels_ready());
+    if (is_few(a.nr)) return few_rows(f, a, f.gated, stream);
+    const bool whole = lines(a.p[0], a.ldp, a.nk) && (!f.gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+    const Cut c = choose(a.nr, a.nc, a.nk, f.gated, !whole);
+    set_cut(a, c, ws);
+    return launched(f, dlf_ff_start_tile(&a, c.shape, f.d.dtype, f.gated, stream));
 }
 
 dlf_status backward(const Ff& f, const void* dy, const void* x, const void* const w[2], const float* saved, void* dx, void* const dw[2],
@@ -293,17 +351,25 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
 {
     const BackLayout l = back_layout(f);
     const int nz = f.gated ? 2 : 1;
-    const bool sums = db[0] || db[1], products = dx || dw[0] || dw[1];
+    const bool sums = db[0] || db[1], want_w = dw[0] || dw[1], want_x = dx && f.d.rows > 0;
     const void* dz[2] = {dy, nullptr};
     int64_t lddz = f.d.dy_stride;
-    if (sums || (products && needs_dz(f))) {
+    TRY(kernels_ready());
+    DlfFfBackArgs b;
+    memset(&b, 0, sizeof b);
+    b.w.splits = b.x.splits = 1;
+    if (sums || ((want_w || want_x) && needs_dz(f))) {
         DlfFfDzArgs z;
         memset(&z, 0, sizeof z);
         z.dy = dy; z.lddy = f.d.dy_stride;
         z.rows = (int)f.d.rows; z.n = f.d.out_features; z.act = f.d.act; z.chunk = l.chunk;
         float* const part = (float*)(ws + l.part);
-        for (int i = 0; i < nz; ++i)
-            if (db[i]) z.sums[i] = l.chunks > 1 ? part + (size_t)i * l.chunks * f.d.out_features : db[i];
+        for (int i = 0; i < nz; ++i) {
+            if (!db[i]) continue;
+            z.sums[i] = l.chunks > 1 ? part + (size_t)i * l.chunks * f.d.out_features : db[i];
+            b.sum.part[i] = z.sums[i];
+            b.sum.out[i] = db[i];
+        }
         if (needs_dz(f)) {
             z.saved = saved;
             z.lddz = lddz = (int64_t)l.lddz;
@@ -311,32 +377,49 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         }
         TRY(launched(f, dlf_ff_start_dz(&z, f.d.dtype, f.gated, stream)));
         if (sums && l.chunks > 1) {
-            DlfFfSumArgs s = {part, {db[0], db[1]}, z.n, l.chunks};
-            TRY(launched(f, dlf_ff_start_sum(&s, f.gated, stream)));
+            b.sum.n = z.n;
+            b.sum.chunks = l.chunks;
+            b.sum.blocks = nz * ceil_div(z.n, 64);
         }
     }
-    DlfFfArgs a;
-    if (dx && f.d.rows > 0) {
-        memset(&a, 0, sizeof a);
-        for (int i = 0; i < nz; ++i) { a.p[i] = w[i]; a.q[i] = dz[i]; }
+    bool whole_x = want_x, whole_w = want_w;
+    if (want_x) {
+        DlfFfArgs& a = b.x;
+        for (int i = 0; i < nz; ++i) {
+            a.p[i] = w[i]; a.q[i] = dz[i];
+            whole_x = whole_x && lines(w[i], f.d.w_stride, f.d.in_features) && lines(dz[i], lddz, f.d.out_features);
+        }
         a.ldp = f.d.w_stride; a.ldq = lddz;
         a.nr = (int)f.d.rows; a.nc = f.d.in_features; a.nk = f.d.out_features;
         a.segments = nz; a.problems = 1;
         a.out[0] = dx; a.ldo = f.d.in_features;
-        TRY(product(f, a, DLF_FF_TN, false, ws + l.join, stream));
     }
-    memset(&a, 0, sizeof a);
-    a.segments = 1;
-    for (int i = 0; i < nz; ++i)
-        if (dw[i]) {
-            a.p[a.problems] = x; a.q[a.problems] = dz[i]; a.out[a.problems] = dw[i];
-            ++a.problems;
-        }
-    if (a.problems > 0) {
+    if (want_w) {
+        DlfFfArgs& a = b.w;
+        a.segments = 1;
+        for (int i = 0; i < nz; ++i)
+            if (dw[i]) {
+                a.p[a.problems] = x; a.q[a.problems] = dz[i]; a.out[a.problems] = dw[i];
+                ++a.problems;
+                whole_w = whole_w && lines(x, f.d.x_stride, f.d.in_features) && lines(dz[i], lddz, f.d.out_features);
+            }
         a.ldp = f.d.x_stride; a.ldq = lddz;
         a.nr = f.d.out_features; a.nc = f.d.in_features; a.nk = (int)f.d.rows;
         a.ldo = f.d.in_features;
-        TRY(product(f, a, DLF_FF_TT, false, ws + l.join, stream));
+    }
+    if (!want_x && !want_w && b.sum.blocks == 0) return DLF_OK;
+    // operands of different alignment: a launch each
+    const bool apart = want_x && want_w && whole_x != whole_w;
+    for (int part = 0; part < (apart ? 2 : 1); ++part) {
+        DlfFfBackArgs c = b;
+        const bool cw = want_w && !(apart && part == 1), cx = want_x && !(apart && part == 0), any = !(cw ? whole_w : whole_x);
+        if (!cw) c.w.problems = 0;
+        if (!cx) c.x.problems = 0;
+        if (part == 1) c.sum.blocks = 0;
+        const BackCut k = choose_back(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, nz, cw || cx ? any : false, cw, cx);
+        set_cut(c.w, k.w, ws + l.join);
+        set_cut(c.x, k.x, ws + l.join + align256(k.w.part_bytes));
+        TRY(launched(f, dlf_ff_start_back(&c, k.w.shape, f.d.dtype, stream)));
     }
     return DLF_OK;
 }

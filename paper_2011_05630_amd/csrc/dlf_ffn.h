@@ -10,9 +10,6 @@
 
 #include "../../include/dlf.h"
 
-// The layouts the products come in: P with k across its rows, Q with k across its rows.
-enum { DLF_FF_NN = 0, DLF_FF_TN = 1, DLF_FF_TT = 2 };
-
 struct DlfFfArgs {
     const void* p[2];       // two of them: gate and up (gated), or the operands of the second segment / problem
     const void* q[2];
@@ -41,24 +38,32 @@ struct DlfFfDzArgs {
     void* dz[2];            // rows of lddz elements, zeros behind column n
     int64_t lddz;
     int32_t rows, n, act;
-    int32_t chunk;          // rows of one sum: all of them, or those of a partial sum
+    int32_t chunk;          // rows of one partial sum
     float* sums[2];         // [chunks][n], or null
 };
+// The partial sums of the columns added up.
 struct DlfFfSumArgs {
-    const float* part;      // [1 or 2][chunks][n]
+    const float* part[2];   // [chunks][n]; null: none
     float* out[2];
-    int32_t n, chunks;
+    int32_t n, chunks, blocks;   // blocks: workgroups of 64 columns, over both
+};
+// What one launch of the backward pass does: tiles of the weights' gradients, of the input's, column sums; each may be none (no tiles).
+struct DlfFfBackArgs {
+    DlfFfArgs w, x;
+    DlfFfSumArgs sum;
+    int32_t blocks_w, blocks_x;  // workgroups: w's first, x's behind them, then the sums'
 };
 
-// Rows whose column sums one workgroup forms; largest number of partial sums of more rows.
-#define DLF_FF_SUM_ROWS 1024
+// Partial column sums: of at most this many parts, of at least so many rows (those that a workgroup of k_ff_dz takes at a time).
 #define DLF_FF_MAX_CHUNKS 64
+#define DLF_FF_CHUNK_ROWS 8
 
 // Shapes of the tile kernel: a workgroup's part of C (columns x rows; gated: half as many columns of both projections) and the stages of
 // 64 k that LDS holds.  ANY: for rows that start anywhere.
 struct DlfFfShape { int bc, br, stages; };
-enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_SHAPE_128_DEEP = 3, DLF_FF_SHAPE_ANY64 = 4, DLF_FF_NUM_SHAPES = 5 };
-static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2}, {128, 128, 2}, {128, 128, 2}, {128, 128, 4}, {64, 64, 2}};
+enum { DLF_FF_SHAPE_256 = 0, DLF_FF_SHAPE_128 = 1, DLF_FF_SHAPE_ANY = 2, DLF_FF_SHAPE_128_DEEP = 3, DLF_FF_SHAPE_ANY64 = 4, DLF_FF_SHAPE_ANY64G = 5,
+       DLF_FF_NUM_SHAPES = 6 };      // ANY64G: gated products only, ANY64: all others
+static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2}, {128, 128, 2}, {128, 128, 2}, {128, 128, 4}, {64, 64, 2}, {64, 128, 2}};
 
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64
@@ -70,10 +75,10 @@ struct DlfFfFew { int rows, nf, mr, waves; };
 
 extern "C" {
 int dlf_ff_kernels_init(void);
-int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream);
+int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int gated, void* stream);
+int dlf_ff_start_back(const DlfFfBackArgs* a, int shape, int dtype, void* stream);
 int dlf_ff_start_few(const DlfFfArgs* a, const DlfFfFew* c, int dtype, int gated, void* stream);
 int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream);
-int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream);
 }
 
 // Sets the message of dlf_last_error and returns the status (dlf_host.cpp).

@@ -441,21 +441,22 @@ template <int I, int N, typename F> __device__ __forceinline__ void static_for(F
 }
 
 template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT, bool PT, bool QT, bool GATED>
-__global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) void k_ff_tile(const DlfFfArgs a)
+__device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
 {
     typedef typename T::v8 v8;
     constexpr int NW = WC * WR, FC = BC / WC / 32, FR = BR / WR / 32, KS = KB / 16;
     constexpr unsigned QOFF = BC * KB * 2, STAGE = (BC + BR) * KB * 2;
     constexpr int LP = BC * KB / 512 / NW, LQ = BR * KB / 512 / NW;
     static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1 && KS % 2 == 0, "");
-    constexpr bool TWO = GATED && LP * 512 / KB == 64;     // a wave's loads of a gated tile: 32 lines of either projection, or of both
-    static_assert(!GATED || ((TWO || LP * 512 / KB == 32) && FC % 2 == 0 && !PT), "");
+    constexpr int LINES = LP * 512 / KB;                    // a wave's lines of P: of both projections of a gated tile, or of one
+    constexpr bool TWO = GATED && LINES == 64;
+    static_assert(!GATED || ((TWO || LINES == 32 || LINES == 16) && FC % 2 == 0 && !PT), "");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
     const int wc = wave % WC, wr = wave / WC;
     // tile
     const int per = a.tiles_r * a.tiles_c, all = per * a.problems * a.splits, each = (all + 7) >> 3;
-    int t = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= each || t >= all) return;
+    int t = (block & 7) * each + (block >> 3);
+    if ((block >> 3) >= each || t >= all) return;
     const int split = t / (per * a.problems);
     t -= split * (per * a.problems);
     const int prob = t / per;
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     if constexpr (!DIRECT) offsets();
     // Requests go on with stage `at` of segment w (operand pair) at the next call of next().
     auto segment = [&](int w, int at) __attribute__((always_inline)) {
-        pb = (const char*)a.p[GATED ? TWO ? 0 : wave & 1 : w] + p0 * 2 + (at - 1) * pstep;
+        pb = (const char*)a.p[GATED ? TWO ? 0 : wave * LINES / 32 & 1 : w] + p0 * 2 + (at - 1) * pstep;
         if (TWO) ub = (const char*)a.p[1] + p0 * 2 + (at - 1) * pstep;
         qb = (const char*)a.q[GATED ? 0 : w] + q0 * 2 + (at - 1) * qstep;
         k_left = a.nk - (at - 1) * KB;
@@ -715,11 +716,56 @@ __global__ __launch_bounds__(WC * WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2) v
     }
 }
 
+// A workgroup's waves per SIMD that the registers have to allow: one of 128 x 128 blocks per wave, else two.
+#define FF_TILE_BOUNDS __launch_bounds__(WC* WR * 64, BC * BR / (WC * WR) > 8192 ? 1 : 2)
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT, bool GATED>
+__global__ FF_TILE_BOUNDS void k_ff_tile(const DlfFfArgs a)
+{
+    tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, GATED>(a, blockIdx.x);
+}
+
+// Column sums: the partial sums of 64 columns added in order, four threads to a column: the result does not depend on which workgroup came
+// first.
+__device__ __forceinline__ void add_sums(const DlfFfSumArgs& a, int block)
+{
+    const int l = threadIdx.x & 63, g = threadIdx.x >> 6, per = (a.n + 63) >> 6, z = block / per, col = (block - z * per) * 64 + l;
+    float* const part = (float*)ff_lds;
+    const float* const p = a.part[z];
+    float t = 0.0f;
+    if (p != nullptr && col < a.n) {
+#pragma unroll 8
+        for (int k = g; k < a.chunks; k += 4) t += p[(int64_t)k * a.n + col];
+    }
+    part[threadIdx.x] = t;
+    __syncthreads();
+    if (p != nullptr && g == 0 && col < a.n) a.out[z][col] = (part[l] + part[l + 64]) + (part[l + 128] + part[l + 192]);
+}
+
+// k_ff_back: both products of a backward pass and the column sums in one launch: their tiles fill the chip together (each alone leaves compute
+// units idle in its last round), and small layers, bound by launches, need one instead of three.  The weights' gradients go first:
+// they are the longer sums in training, and what is short fills the gaps.
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT>
+__global__ FF_TILE_BOUNDS void k_ff_back(const DlfFfBackArgs a)
+{
+    int b = blockIdx.x;
+    if (b < a.blocks_w) {
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, b);
+        return;
+    }
+    b -= a.blocks_w;
+    if (b < a.blocks_x) {
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, b);
+        return;
+    }
+    b -= a.blocks_x;
+    if (b < a.sum.blocks) add_sums(a.sum, b);
+}
+
 // k_ff_join: the sums over the splits of k, in order, and the epilogue.
-template <typename T, bool GATED> __global__ __launch_bounds__(256) void k_ff_join(const DlfFfArgs a)
+template <typename T, bool GATED> __device__ __forceinline__ void join(const DlfFfArgs& a, int64_t unit)
 {
     const int cols = (a.nc + 7) >> 3;
-    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)a.nr * a.nc;
+    const int64_t plane = (int64_t)a.nr * a.nc;
     const int64_t row = unit / cols;
     const int c = (int)(unit - row * cols) * 8, n = a.nc - c;
     const int prob = row >= a.nr ? 1 : 0, r = (int)(row - (prob ? a.nr : 0));
@@ -741,6 +787,17 @@ template <typename T, bool GATED> __global__ __launch_bounds__(256) void k_ff_jo
         }
     }
     finish<T, GATED, 8>(a, prob, r, c, n, v, u);
+}
+
+template <typename T, bool GATED> __global__ __launch_bounds__(256) void k_ff_join(const DlfFfArgs a)
+{
+    join<T, GATED>(a, (int64_t)blockIdx.x * 256 + threadIdx.x);
+}
+// ... of the two products of a backward pass: workgroups [0, blocks_w) and the others.
+template <typename T> __global__ __launch_bounds__(256) void k_ff_join_back(const DlfFfBackArgs a)
+{
+    const bool w = (int)blockIdx.x < a.blocks_w;
+    join<T, false>(w ? a.w : a.x, (int64_t)(w ? blockIdx.x : blockIdx.x - a.blocks_w) * 256 + threadIdx.x);
 }
 
 // The waves' partial sums of a workgroup's 16 NF features x 16 MR rows meet in LDS, in the order of the waves.
@@ -934,15 +991,15 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ff_dz: the gradient behind the activation, and column sums of it in 32 bits (before it is rounded).  Bound by memory: 14 bytes an
-// element, gated 14 and twice the saved ones.  A workgroup takes `chunk` rows of 8 TC columns: TC threads by eight columns, blockDim / TC rows
-// at a time; their sums meet in LDS, in a fixed order.  With few rows a workgroup takes all of them, few columns wide, and its sums are the result;
-// with many it takes whole 512-byte lines, and k_ff_sum adds up what the chunks leave.
+// k_ff_dz: the gradient behind the activation, and column sums of it in 32 bits (before it is rounded).  Bound by memory: 8 bytes an
+// element, gated 14.  A workgroup takes `chunk` rows of 256 columns: 32 threads by eight columns, eight rows at a time; their
+// sums meet in LDS, in a fixed order, and k_ff_back adds up what the chunks leave.
 // ------------------------------------------------------------------------------------------------
-template <typename T, bool GATED, int TC>
-__global__ __launch_bounds__(TC == 32 ? 256 : 1024) void k_ff_dz(const DlfFfDzArgs a)
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
 {
-    constexpr int NZ = GATED ? 2 : 1, THREADS = TC == 32 ? 256 : 1024, RT = THREADS / TC;
+    constexpr int NZ = GATED ? 2 : 1, TC = 32, THREADS = 256, RT = DLF_FF_CHUNK_ROWS;
+    static_assert(RT * TC == THREADS, "");
     __shared__ __attribute__((aligned(16))) float sums[RT][NZ][8 * TC];
     const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
     const int c = (blockIdx.x * TC + tc) * 8, n = a.n - c;
@@ -1010,46 +1067,32 @@ __global__ __launch_bounds__(TC == 32 ? 256 : 1024) void k_ff_dz(const DlfFfDzAr
         if (col < a.n && a.sums[z] != nullptr) a.sums[z][(int64_t)blockIdx.y * a.n + col] = sums[0][z][i % (8 * TC)];
     }
 }
-// The partial sums of a column added in order: the result does not depend on which workgroup came first.  Four threads to a column.
-__global__ __launch_bounds__(256) void k_ff_sum(const DlfFfSumArgs a)
-{
-    __shared__ float part[4][64];
-    const int l = threadIdx.x & 63, g = threadIdx.x >> 6, col = blockIdx.x * 64 + l, z = blockIdx.y;
-    if (a.out[z] == nullptr) return;
-    float t = 0.0f;
-    if (col < a.n) {
-#pragma unroll 8
-        for (int k = g; k < a.chunks; k += 4) t += a.part[((int64_t)z * a.chunks + k) * a.n + col];
-    }
-    part[g][l] = t;
-    __syncthreads();
-    if (g == 0 && col < a.n) a.out[z][col] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
-}
-
 // ------------------------------------------------------------------------------------------------
 // Launches
 // ------------------------------------------------------------------------------------------------
-// The tile kernels by shape (DLF_FF_SHAPE_*): waves across c and r, k of a stage, stages in LDS, direct loads.
-template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT> static void (*tile_of(int layout, int gated))(const DlfFfArgs)
-{
-    if (gated) {
-        if constexpr (BC >= 128) return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, true>;
-        return nullptr;                     // (two projections of 64 x 64 with four stages in registers do not fit them)
-    }
-    switch (layout) {
-    case DLF_FF_NN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, false>;
-    case DLF_FF_TN: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>;
-    default: return k_ff_tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>;
-    }
-}
-template <typename T> static void (*tile_kernel(int shape, int layout, int gated))(const DlfFfArgs)
+// The tile kernels by shape (DLF_FF_SHAPE_*): waves across c and r, k of a stage, stages on their way, direct loads.
+typedef void (*TileKernel)(const DlfFfArgs);
+typedef void (*BackKernel)(const DlfFfBackArgs);
+template <typename T> static TileKernel tile_kernel(int shape, int gated)
 {
     switch (shape) {
-    case DLF_FF_SHAPE_256: return tile_of<T, 256, 256, 2, 2, 64, 2, true>(layout, gated);
-    case DLF_FF_SHAPE_128: return tile_of<T, 128, 128, 2, 2, 64, 2, true>(layout, gated);
-    case DLF_FF_SHAPE_128_DEEP: return tile_of<T, 128, 128, 2, 2, 64, 4, true>(layout, gated);
-    case DLF_FF_SHAPE_ANY64: return tile_of<T, 64, 64, 2, 2, 64, 4, false>(layout, gated);
-    default: return tile_of<T, 128, 128, 2, 2, 64, 2, false>(layout, gated);
+    case DLF_FF_SHAPE_256: return gated ? k_ff_tile<T, 256, 256, 2, 2, 64, 2, true, true> : k_ff_tile<T, 256, 256, 2, 2, 64, 2, true, false>;
+    case DLF_FF_SHAPE_128: return gated ? k_ff_tile<T, 128, 128, 2, 2, 64, 2, true, true> : k_ff_tile<T, 128, 128, 2, 2, 64, 2, true, false>;
+    case DLF_FF_SHAPE_128_DEEP: return gated ? k_ff_tile<T, 128, 128, 2, 2, 64, 4, true, true> : k_ff_tile<T, 128, 128, 2, 2, 64, 4, true, false>;
+    case DLF_FF_SHAPE_ANY64: return gated ? nullptr : k_ff_tile<T, 64, 64, 2, 2, 64, 4, false, false>;
+    case DLF_FF_SHAPE_ANY64G: return gated ? k_ff_tile<T, 64, 128, 1, 4, 64, 4, false, true> : nullptr;
+    default: return gated ? k_ff_tile<T, 128, 128, 2, 2, 64, 2, false, true> : k_ff_tile<T, 128, 128, 2, 2, 64, 2, false, false>;
+    }
+}
+template <typename T> static BackKernel back_kernel(int shape)
+{
+    switch (shape) {
+    case DLF_FF_SHAPE_256: return k_ff_back<T, 256, 256, 2, 2, 64, 2, true>;
+    case DLF_FF_SHAPE_128: return k_ff_back<T, 128, 128, 2, 2, 64, 2, true>;
+    case DLF_FF_SHAPE_128_DEEP: return k_ff_back<T, 128, 128, 2, 2, 64, 4, true>;
+    case DLF_FF_SHAPE_ANY64: return k_ff_back<T, 64, 64, 2, 2, 64, 4, false>;
+    case DLF_FF_SHAPE_ANY64G: return nullptr;
+    default: return k_ff_back<T, 128, 128, 2, 2, 64, 2, false>;
     }
 }
 static size_t tile_lds(int shape)
@@ -1092,39 +1135,44 @@ extern "C" int dlf_ff_kernels_init(void)
         if (e != hipSuccess) return (int)e;
     }
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
-        for (int k = 0; k < 8; ++k) {
-            const int layout = k >> 1 & 3, gated = layout == 3;
-            auto f = (k & 1) ? tile_kernel<BF16>(shape, gated ? 0 : layout, gated) : tile_kernel<F16>(shape, gated ? 0 : layout, gated);
+        for (int k = 0; k < 6; ++k) {
+            const void* f = k < 4 ? (const void*)((k & 1) ? tile_kernel<BF16>(shape, k >> 1) : tile_kernel<F16>(shape, k >> 1))
+                                  : (const void*)((k & 1) ? back_kernel<BF16>(shape) : back_kernel<F16>(shape));
             if (f == nullptr) continue;
-            const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
+            const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
             if (e != hipSuccess) return (int)e;
         }
     return 0;
 }
-extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int layout, int gated, void* stream)
+static unsigned tile_blocks(const DlfFfArgs& a) { return (unsigned)((a.tiles_r * a.tiles_c * a.problems * a.splits + 7) / 8 * 8); }
+static unsigned join_blocks(const DlfFfArgs& a) { return (unsigned)(((int64_t)a.nr * a.problems * ((a.nc + 7) / 8) + 255) / 256); }
+extern "C" int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int dtype, int gated, void* stream)
 {
-    const unsigned tiles = (unsigned)(a->tiles_r * a->tiles_c * a->problems * a->splits);
-    hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, layout, gated) : tile_kernel<BF16>(shape, layout, gated),
-                       dim3((tiles + 7) / 8 * 8), dim3(256), tile_lds(shape), (hipStream_t)stream, *a);
-    if (a->splits > 1) {
-        const int64_t units = (int64_t)a->nr * a->problems * ((a->nc + 7) / 8);
+    hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, gated) : tile_kernel<BF16>(shape, gated), dim3(tile_blocks(*a)), dim3(256), tile_lds(shape),
+                       (hipStream_t)stream, *a);
+    if (a->splits > 1)
         hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? k_ff_join<F16, true> : k_ff_join<F16, false>) : (gated ? k_ff_join<BF16, true> : k_ff_join<BF16, false>),
-                           dim3((unsigned)((units + 255) / 256)), dim3(256), 0, (hipStream_t)stream, *a);
-    }
+                           dim3(join_blocks(*a)), dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
-template <typename T, bool GATED> static void (*dz_kernel(int wide))(const DlfFfDzArgs) { return wide ? k_ff_dz<T, GATED, 32> : k_ff_dz<T, GATED, 4>; }
+extern "C" int dlf_ff_start_back(const DlfFfBackArgs* a, int shape, int dtype, void* stream)
+{
+    DlfFfBackArgs b = *a;
+    b.blocks_w = (int)tile_blocks(b.w);
+    b.blocks_x = (int)tile_blocks(b.x);
+    hipLaunchKernelGGL(dtype == DLF_F16 ? back_kernel<F16>(shape) : back_kernel<BF16>(shape), dim3((unsigned)(b.blocks_w + b.blocks_x + b.sum.blocks)),
+                       dim3(256), tile_lds(shape), (hipStream_t)stream, b);
+    b.blocks_w = b.w.splits > 1 ? (int)join_blocks(b.w) : 0;
+    b.blocks_x = b.x.splits > 1 ? (int)join_blocks(b.x) : 0;
+    if (b.blocks_w + b.blocks_x > 0)
+        hipLaunchKernelGGL(dtype == DLF_F16 ? k_ff_join_back<F16> : k_ff_join_back<BF16>, dim3((unsigned)(b.blocks_w + b.blocks_x)), dim3(256), 0,
+                           (hipStream_t)stream, b);
+    return (int)hipGetLastError();
+}
 extern "C" int dlf_ff_start_dz(const DlfFfDzArgs* a, int dtype, int gated, void* stream)
 {
-    const int wide = a->chunk < a->rows, cols = wide ? 256 : 32;
-    const dim3 grid((unsigned)((a->n + cols - 1) / cols), (unsigned)(a->rows > 0 ? (a->rows + a->chunk - 1) / a->chunk : 1));
-    hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? dz_kernel<F16, true>(wide) : dz_kernel<F16, false>(wide))
-                                        : (gated ? dz_kernel<BF16, true>(wide) : dz_kernel<BF16, false>(wide)),
-                       grid, dim3(wide ? 256 : 1024), 0, (hipStream_t)stream, *a);
-    return (int)hipGetLastError();
-}
-extern "C" int dlf_ff_start_sum(const DlfFfSumArgs* a, int gated, void* stream)
-{
-    hipLaunchKernelGGL(k_ff_sum, dim3((unsigned)((a->n + 63) / 64), gated ? 2 : 1), dim3(256), 0, (hipStream_t)stream, *a);
+    const dim3 grid((unsigned)((a->n + 255) / 256), (unsigned)(a->rows > 0 ? (a->rows + a->chunk - 1) / a->chunk : 1));
+    hipLaunchKernelGGL(dtype == DLF_F16 ? (gated ? k_ff_dz<F16, true> : k_ff_dz<F16, false>) : (gated ? k_ff_dz<BF16, true> : k_ff_dz<BF16, false>), grid,
+                       dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }

@@ -9,7 +9,8 @@ from gpu_util import announce
 pytestmark = pytest.mark.gpu
 
 # (kernel, workgroups that share a tile's k)
-KERNELS = {"few": (1, 0), "tile256": (2, 1), "tile256_split3": (2, 3), "tile128": (3, 1), "tile128_split5": (3, 5), "any": (4, 1), "any_split2": (4, 2), "deep": (5, 1), "deep_split4": (5, 4), "any64": (6, 1), "any64_split3": (6, 3)}
+KERNELS = {"few": (1, 0), "tile256": (2, 1), "tile256_split3": (2, 3), "tile128": (3, 1), "tile128_split5": (3, 5), "any": (4, 1), "any_split2": (4, 2), "deep": (5, 1), "deep_split4": (5, 4), "any64": (6, 1), "any64_split3": (6, 3),
+           "any64_gated": (7, 1), "any64_gated_split3": (7, 3)}
 # (rows, in, out)
 SIZES = [(8, 8, 8), (64, 72, 40), (128, 64, 128), (136, 72, 120), (256, 128, 256), (264, 192, 264), (504, 840, 520), (1288, 64, 776), (700, 1032, 1304),
          (1, 5, 1), (131, 77, 67), (259, 1031, 517)]
