@@ -491,23 +491,24 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     // this workgroup's stages, of one segment or two
     const int per_seg = (a.nk + KB - 1) / KB, stages = per_seg * a.segments;
     const int first = (int)((int64_t)stages * split / a.splits), total = (int)((int64_t)stages * (split + 1) / a.splits) - first;
-    int segments = a.segments - (first >= per_seg ? 1 : 0);              // this one and those behind it
-    if (total > 0) segment(a.problems == 2 ? prob : a.segments - segments, first - (a.segments - segments) * per_seg);
+    // All of k: each XCD starts an eighth of it behind the last and comes round to where it started.  Workgroups of an XCD share operands in its L2
+    // and stay together; if all of them read the same k at a time, rows a power of two apart would keep few channels of the memory busy.
+    const int start = a.splits > 1 ? first : (int)((int64_t)total * (block & 7) >> 3);
+    int seg = start >= per_seg && total > 0 ? 1 : 0, requests = total;   // segment; stages to request
+    if (total > 0) segment(a.problems == 2 ? prob : seg, start - seg * per_seg);
     const unsigned lds0 = (unsigned)(size_t)(lds_char*)ff_lds;
-    // The next stage's requests: first where they start, then one after the other, load 0 .. LP + LQ - 1.  Behind the operands' last stage direct
+    // The next stage's requests: first where they start, then one after the other, load 0 .. LP + LQ - 1.  Behind this workgroup's last stage direct
     // loads go on with resources of no bytes (zeros into LDS that nobody reads), so that the loop below has one form.
     i4v pres, qres, ures;
     int limit = 0x7fffffff;
     auto next = [&]() __attribute__((always_inline)) {
         k_left -= KB;
+        if (--requests < 0) limit = 0;
         if (k_left < KB) {
-            if (k_left <= 0) {
-                if (--segments > 0) {
-                    segment(1, 0);
-                    k_left -= KB;
-                } else {
-                    limit = 0;
-                }
+            if (k_left <= 0 && requests >= 0) {
+                seg = seg + 1 < a.segments ? seg + 1 : 0;
+                segment(a.problems == 2 ? prob : seg, 0);
+                k_left -= KB;
             }
             if constexpr (DIRECT) {
                 if (k_left < KB) {
@@ -562,7 +563,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
         });
     };
     // A stage's requests by the step that they go out in: the last of the stage that makes room for them, and the first of the next.
-    constexpr int NL = LP + LQ, L0 = KS == 2 ? (NL + 1) / 2 : (3 * NL + 7) / 8, L1 = KS == 2 ? NL : (6 * NL + 7) / 8;
+    constexpr int NL = LP + LQ, L0 = NL / 2, L1 = NL;
     if (total > 0) {
         if constexpr (DIRECT) {
 #pragma unroll
