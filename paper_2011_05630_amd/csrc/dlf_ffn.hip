@@ -447,7 +447,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     constexpr int NW = WC * WR, FC = BC / WC / 32, FR = BR / WR / 32, KS = KB / 16;
     constexpr unsigned QOFF = BC * KB * 2, STAGE = (BC + BR) * KB * 2;
     constexpr int LP = BC * KB / 512 / NW, LQ = BR * KB / 512 / NW;
-    static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1 && KS % 2 == 0, "");
+    static_assert(FC <= 4 && FR <= 4 && LP >= 1 && LQ >= 1 && KS == 4, "");
     constexpr int LINES = LP * 512 / KB;                    // a wave's lines of P: of both projections of a gated tile, or of one
     constexpr bool TWO = GATED && LINES == 64;
     static_assert(!GATED || ((TWO || LINES == 32 || LINES == 16) && FC % 2 == 0 && !PT), "");
@@ -501,10 +501,12 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     // loads go on with resources of no bytes (zeros into LDS that nobody reads), so that the loop below has one form.
     i4v pres, qres, ures;
     int limit = 0x7fffffff;
+    int plain = 0;                                          // further stages that need nothing but the next address
     auto next = [&]() __attribute__((always_inline)) {
         k_left -= KB;
-        if (--requests < 0) limit = 0;
-        if (k_left < KB) {
+        --requests;
+        if (__builtin_expect(--plain < 0, 0)) {
+            if (requests < 0) limit = 0;
             if (k_left <= 0 && requests >= 0) {
                 seg = seg + 1 < a.segments ? seg + 1 : 0;
                 segment(a.problems == 2 ? prob : seg, 0);
@@ -516,6 +518,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
                     lq.mask(wave * LQ, k_left);
                 }
             }
+            plain = max(0, min(requests, k_left / KB - 1));
         }
         pb += pstep;
         qb += qstep;
@@ -563,7 +566,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
         });
     };
     // A stage's requests by the step that they go out in: the last of the stage that makes room for them, and the first of the next.
-    constexpr int NL = LP + LQ, L0 = NL / 2, L1 = NL;
+    constexpr int NL = LP + LQ, L0 = NL / 2;
     if (total > 0) {
         if constexpr (DIRECT) {
 #pragma unroll
@@ -578,15 +581,13 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
 #pragma unroll
             for (int r = 0; r < FC + FR; ++r) read(cur, 0, 0, r);
             for (int s = 0; s < total - 1; ++s) {
-                step(0, true, cur, 1, last, L0, L1);
-                if constexpr (KS == 4) {
-                    step(1, true, cur, 2, last, L1, NL);
-                    step(0, true, cur, 3, 0, 0, 0);
-                }
+                step(0, true, cur, 1, last, L0, NL);
+                next();                                     // (here, where multiplications cover it, not behind the barrier)
+                step(1, true, cur, 2, 0, 0, 0);
+                step(0, true, cur, 3, 0, 0, 0);
                 // this wave's reads of the stage have arrived, and so has its part of the next one
                 __builtin_amdgcn_s_waitcnt(WAIT_LOADS_AND_LDS((RING - 2) * NL));
                 asm volatile("s_barrier" ::: "memory");
-                next();
                 last = cur;
                 cur = cur == (RING - 1) * STAGE ? 0 : cur + STAGE;
                 step(1, true, cur, 0, last, 0, L0);
