@@ -257,8 +257,12 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ff_tile: the product for operands whose rows are whole 16-byte lines.  A workgroup of WC x WR waves computes BC x BR of C (gated: BC / 2
-// features of both projections), a wave FC x FR blocks of 32 x 32; 64 k at a time ("stage") pass through LDS, two stages in turn.
+// tile (k_ff_tile, k_ff_back): a workgroup of WC x WR waves computes BC x BR of C (gated: BC / 2 features of both projections), a wave FC x FR
+// blocks of 32 x 32; 64 k at a time ("stage") pass through LDS, two or four stages in turn.  DIRECT: for operands whose rows are whole
+// 16-byte lines; otherwise through registers (Stager).  Bound by the matrix units and what they may draw: 8192^3 takes 790 us (1.39
+// PFLOP/s at 1.9 GHz), 4096^3 112 to 117, of which 12 are the first loads, the epilogue and the launch; a stage takes 1.5 us, its
+// multiplications alone 1.08 at that clock: the rest are the barrier and the waits around it, which a second wave per SIMD would cover,
+// but the registers of 128 x 128 blocks leave no room for one, and smaller blocks read LDS half as often again.
 //   Global -> LDS: 16-byte direct loads, 1 KiB per instruction, lane l's 16 bytes at 16 l.  Rows, columns and k that do not exist
 //     are read from an offset behind the resource's end, which brings zeros and no traffic.
 //   An operand with k along its rows lies in LDS as [row][64 k], 128 bytes a row, its 16-byte part c at position c ^ (row / 2) % 8: the 16
@@ -267,13 +271,14 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
 //     read gives a lane four k of its row, the 16 lanes of a group reading 4 k x 16 rows.  The 64-byte part b of line k is kept at b ^ f(k),
 //     f(k) = k % 4 + 4 * (k / 8 % 2) (modulo the parts of a line): the eight lines of a read fall into different banks.
 //   The multiplications of 16 k run while the operands of the next 16 are read.  Behind the third of a stage's four steps a wave has all of the
-//     stage in registers: there it waits for its part of the next stage (requested a whole stage ago) and for the other waves, and
-//     requests the stage after that into the LDS just read, so that the fourth step's multiplications cover the first reads
-//     of the next stage and the barrier.
+//     stage in registers: there it waits for its part of the next stage and for the other waves, and requests the stage after that into
+//     the LDS just read, half of it during the fourth step, half during the first of the next stage (over three steps the last requests
+//     came late: 8192^3 2 % slower; all in one 6 %).  The addresses of a stage are formed ahead of the barrier, not behind it (2 %).
+//     Stages of 32 k, four in LDS, wait less but read half lines: 4096^3 124 against 115 us.
 //   The epilogue goes through LDS, 64 rows of a wave at a time, so that stores are whole lines and the code of the activations is there
 //     once; a lane's loads for several rows go out together (one after the other they made the epilogue of 256 x 256 take 16 us).
 // Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, in bands of four rows of tiles, and its workgroups share operands
-// in its L2.
+// in its L2.  XCDs start at different k, see below.
 // ------------------------------------------------------------------------------------------------
 #define OOB ((int)0x80000000)
 typedef int i4v __attribute__((ext_vector_type(4)));
@@ -303,8 +308,8 @@ __device__ __forceinline__ void line_to_lds(const i4v& base, int off, unsigned d
 #define WAIT_LOADS_AND_LDS(N) (0x0070 | ((N) & 15) | ((N) >> 4) << 14)
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// What the 16-byte parts of row `row` are kept at, of KB k a row (32 or 64): position c ^ swizzle.
-template <int KB> __device__ __forceinline__ int swizzle(int row) { return KB == 64 ? row >> 1 & 7 : row >> 2 & 3; }
+// What the 16-byte parts of row `row` are kept at: position c ^ swizzle.
+__device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
 // One operand's way from memory into LDS: a wave's N instructions of a stage.  ROWS of the operand per tile; TR: k across the rows.
 template <int N, int ROWS, bool TR, int KB> struct Loader {
     static constexpr int CPL = TR ? ROWS / 8 : KB / 8;      // 16-byte parts of a line in LDS
@@ -314,7 +319,7 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
     __device__ __forceinline__ static int part(int first, int i)
     {
         const int l = line(first, i), p = (threadIdx.x & 63) % CPL;
-        if (!TR) return p ^ swizzle<KB>(l);
+        if (!TR) return p ^ swizzle(l);
         return p ^ ((((l & 3) | ((l >> 3) & 1) << 2) & (ROWS / 32 - 1)) << 2);
     }
     template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int = 0)
@@ -412,7 +417,7 @@ template <typename T, int ROWS, bool TR, int KB> struct Reader {
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (!TR) at[i] = (row0 + l32) * (KB * 2) + (((2 * i + lhi) ^ swizzle<KB>(l32)) << 4);
+            if (!TR) at[i] = (row0 + l32) * (KB * 2) + (((2 * i + lhi) ^ swizzle(l32)) << 4);
             else {
                 const int f = ((lane >> 2 & 3) | lhi << 2) & (ROWS / 32 - 1);
                 at[i] = (lhi * 8 + (lane >> 2 & 3)) * (ROWS * 2) + (((row0 / 32 + i) ^ f) << 6) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
@@ -492,7 +497,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     const int per_seg = (a.nk + KB - 1) / KB, stages = per_seg * a.segments;
     const int first = (int)((int64_t)stages * split / a.splits), total = (int)((int64_t)stages * (split + 1) / a.splits) - first;
     // All of k: each XCD starts an eighth of it behind the last and comes round to where it started.  Workgroups of an XCD share operands in its L2
-    // and stay together; if all of them read the same k at a time, rows a power of two apart would keep few channels of the memory busy.
+    // and stay together; if all XCDs read the same k at a time, 8192^3 takes 3 % longer, 4096 x 16384 -> 4096 10 %.
     const int start = a.splits > 1 ? first : (int)((int64_t)total * (block & 7) >> 3);
     int seg = start >= per_seg && total > 0 ? 1 : 0, requests = total;   // segment; stages to request
     if (total > 0) segment(a.problems == 2 ? prob : seg, start - seg * per_seg);
@@ -745,7 +750,8 @@ __device__ __forceinline__ void add_sums(const DlfFfSumArgs& a, int block)
 
 // k_ff_back: both products of a backward pass and the column sums in one launch: their tiles fill the chip together (each alone leaves compute
 // units idle in its last round), and small layers, bound by launches, need one instead of three.  The weights' gradients go first:
-// they are the longer sums in training, and what is short fills the gaps.
+// they are the longer sums in training, and what is short fills the gaps.  The products of 4096 x 2048 -> 2048 take 70 us together, 38 and 38
+// apart; those of 4096 x 2048 -> 2 x 5632 329 with their join, 235 and 243 apart (1.15 PFLOP/s).
 template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT>
 __global__ FF_TILE_BOUNDS void k_ff_back(const DlfFfBackArgs a)
 {
@@ -763,7 +769,8 @@ __global__ FF_TILE_BOUNDS void k_ff_back(const DlfFfBackArgs a)
     if (b < a.sum.blocks) add_sums(a.sum, b);
 }
 
-// k_ff_join: the sums over the splits of k, in order, and the epilogue.
+// k_ff_join: the sums over the splits of k, in order, and the epilogue.  Bound by memory: 117 MB in 20 us.  Chosen where it costs less than
+// the compute units that the tiles alone leave idle.
 template <typename T, bool GATED> __device__ __forceinline__ void join(const DlfFfArgs& a, int64_t unit)
 {
     const int cols = (a.nc + 7) >> 3;
@@ -919,7 +926,8 @@ __global__ __launch_bounds__(512, (GATED ? 2 : NF) + MR <= 3 ? 4 : 2) void k_ff_
 // k_ff_rows: k_ff_few for operands whose rows are whole 16-byte lines.  There a wave's load takes 64 bytes of each of 16 rows, and pieces
 // of many lines cost a compute unit several times their size; here the operands come as whole 128-byte lines, eight rows per
 // instruction, into a ring in LDS that belongs to the wave alone: 64 k ("stage") of its features and rows at a time, D stages
-// requested ahead, no barrier before the waves meet.  LDS holds a stage as k_ff_tile does.
+// requested ahead, no barrier before the waves meet.  LDS holds a stage as k_ff_tile does.  5 x 2048 -> 32001 takes 24.4 us (5.4 TB/s
+// of weights), 1 x 4096 -> 2 x 10880 32 us (5.6), 16 x 2048 -> 2 x 5632 10.5 (4.4), 1 x 1024 -> 1024 3.9 (a launch and a round trip).
 // ------------------------------------------------------------------------------------------------
 template <typename T, int NF, int MR, bool GATED>
 __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
@@ -994,7 +1002,7 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // k_ff_dz: the gradient behind the activation, and column sums of it in 32 bits (before it is rounded).  Bound by memory: 8 bytes an
-// element, gated 14.  A workgroup takes `chunk` rows of 256 columns: 32 threads by eight columns, eight rows at a time; their
+// element, gated 14 (4096 x 2048: 14 us, 4.8 TB/s; gated 4096 x 5632: 67 us, 4.8 TB/s, what a large copy reaches).  A workgroup takes `chunk` rows of 256 columns: 32 threads by eight columns, eight rows at a time; their
 // sums meet in LDS, in a fixed order, and k_ff_back adds up what the chunks leave.
 // ------------------------------------------------------------------------------------------------
 template <typename T, bool GATED>

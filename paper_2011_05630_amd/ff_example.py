@@ -105,8 +105,9 @@ def main(argv=None):
     for _ in range(100):
         net.run(x[:1])
     torch.cuda.synchronize()
+    us = (time.perf_counter() - t) * 1e4
     off = float((whole[:1].float() - one.float()).abs().max() / whole[:1].float().abs().max())
-    print("one token: %.1f us; its logits differ from the batch's by %.2g of the largest" % ((time.perf_counter() - t) * 1e4, off))
+    print("one token: %.1f us; its logits differ from the batch's by %.2g of the largest" % (us, off))
     return losses, off
 
 
