@@ -150,8 +150,8 @@ struct Rate {
 };
 const Rate& rate(int shape)
 {
-    static const Rate rates[DLF_FF_NUM_SHAPES] = {{1, {1450}, 7000}, {2, {900, 900}, 4000}, {2, {950, 1250}, 5000}, {1, {500}, 5000},
-                                                  {3, {530, 620, 760}, 4000}, {2, {640, 850}, 4000}};
+    static const Rate rates[DLF_FF_NUM_SHAPES] = {{1, {1450}, 7000}, {2, {900, 900}, 4000}, {2, {750, 1130}, 5000}, {1, {500}, 5000},
+                                                  {3, {380, 490, 640}, 4000}, {2, {550, 730}, 4000}};
     return rates[shape];
 }
 // Tiles of two lengths, the first kind's started first, as they fill the compute units.

@@ -322,7 +322,7 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
         if (!TR) return p ^ swizzle(l);
         return p ^ ((((l & 3) | ((l >> 3) & 1) << 2) & (ROWS / 32 - 1)) << 2);
     }
-    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int = 0)
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -349,25 +349,29 @@ template <int N, int ROWS, bool TR, int KB> struct Loader {
 // ... of rows that start anywhere: through registers, by a load and, a stage later, a write to LDS.  Rows and columns that do not exist
 // are read as others and not stored.  A part of eight that ends behind the operand's last k (or column) is read as the last eight there
 // are and shifted, zeros moving in: a 16-byte load never leaves the operand.  Only operands of less than eight are read one by one.
+// Which parts those are is the same for every stage that is not whole, so a load is one instruction without a branch: with branches the compiler
+// loses count of the loads on their way and waits for all of them.
 template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
     typedef Loader<N, ROWS, TR, KB> Map;
-    unsigned off[N];
+    static constexpr int BIAS = 128;        // bytes: what a part may begin in front of the stage's first
+    unsigned off[N], last[N];               // of a whole stage, of one that is not
     typename T::v8 v[N];
-    int64_t line_bytes;
     int edge;               // across: columns of a tile that ends inside a part of eight, else 0
     int tail;               // k of the stage in v if they are not whole, else 0
     bool tiny;              // less than eight k (along) or columns (across) in all
-    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int extent)
+    template <bool GATED> __device__ __forceinline__ void setup(int first, int avail, int64_t ld, int extent, int nk)
     {
-        line_bytes = ld * 2;
         tiny = extent < 8;
         tail = 0;
         edge = TR && avail < ROWS && (avail & 7) != 0 ? avail : 0;
+        const int left = nk % KB;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int l = Map::line(first, i), p = Map::part(first, i) * 8, row = GATED ? (l >> 6) * 32 + (l & 31) : l;
-            if (!TR) off[i] = (unsigned)(min(row, avail - 1) * ld + p) * 2;
-            else off[i] = (unsigned)(l * ld + (edge > 0 && !tiny ? min(p, avail - 8) + 8 : p < avail ? p : 0)) * 2;   // (+ 8: see load)
+            const int at = !TR ? p : edge > 0 && !tiny ? min(p, avail - 8) : p < avail ? p : 0;
+            off[i] = (unsigned)((!TR ? min(row, avail - 1) : l) * ld * 2 + at * 2 + BIAS);
+            if (!TR) last[i] = off[i] - (unsigned)(max(0, 8 - (left - p)) * 2);
+            else last[i] = off[i] - (unsigned)(max(0, l - (left - 1)) * ld * 2);
         }
     }
     // elements of part i that exist, in a stage of `left` k
@@ -376,23 +380,19 @@ template <typename T, int N, int ROWS, bool TR, int KB> struct Stager {
         const int p = Map::part(first, i) * 8;
         return !TR ? left - p : Map::line(first, i) >= left ? 0 : edge > 0 ? edge - p : 8;
     }
-    __device__ __forceinline__ void load(const char* base, int first, int k_left)
+    __device__ __forceinline__ void load(const char* base, int k_left)
+    {
+        const bool whole = k_left >= KB;
+        tail = whole ? 0 : k_left;
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base - BIAS + (whole ? off[i] : last[i]), 16);
+    }
+    // ... of an operand of less than eight
+    __device__ __forceinline__ void load_tiny(const char* base, int first, int k_left)
     {
         tail = k_left < KB ? k_left : 0;
-        if (edge > 0 && !tiny) base -= 16;                  // the last eight columns may begin in front of the tile
-        if (tiny) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = load8<T>(base + off[i], 0, count(first, i, k_left));
-        } else if (tail == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base + off[i], 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int64_t back = !TR ? max(0, 8 - count(first, i, k_left)) * 2 : max(0, Map::line(first, i) - (k_left - 1)) * line_bytes;
-                __builtin_memcpy(&v[i], base + ((int64_t)off[i] - back), 16);
-            }
-        }
+        for (int i = 0; i < N; ++i) v[i] = load8<T>(base - BIAS + off[i], 0, count(first, i, k_left));
     }
     __device__ __forceinline__ void put(unsigned dst, int first)
     {
@@ -481,8 +481,13 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     const char *pb, *qb, *ub = nullptr;
     int k_left;
     auto offsets = [&]() __attribute__((always_inline)) {
-        lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp, PT ? a.nc : a.nk);
-        lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq, QT ? a.nr : a.nk);
+        if constexpr (DIRECT) {
+            lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp);
+            lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq);
+        } else {
+            lp.template setup<GATED>(wave * LP, a.nc - c0, a.ldp, PT ? a.nc : a.nk, a.nk);
+            lq.template setup<false>(wave * LQ, a.nr - r0, a.ldq, QT ? a.nr : a.nk, a.nk);
+        }
     };
     if constexpr (!DIRECT) offsets();
     // Requests go on with stage `at` of segment w (operand pair) at the next call of next().
@@ -508,6 +513,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
     int limit = 0x7fffffff;
     int plain = 0;                                          // further stages that need nothing but the next address
     auto next = [&]() __attribute__((always_inline)) {
+        if (!DIRECT && requests == 0) return;               // the last stage's address stays: loads of it that nobody reads
         k_left -= KB;
         --requests;
         if (__builtin_expect(--plain < 0, 0)) {
@@ -612,47 +618,64 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, int block)
             }
             auto fetch = [&](int d) __attribute__((always_inline)) {
                 next();
-                ps[d].load(pb, wave * LP, k_left);
-                qs[d].load(qb, wave * LQ, k_left);
+                ps[d].load(pb, k_left);
+                qs[d].load(qb, k_left);
             };
             auto put = [&](unsigned stage, int d) __attribute__((always_inline)) {
                 ps[d].put(stage, wave * LP);
                 qs[d].put(stage + QOFF, wave * LQ);
             };
-            fetch(0);
-            put(0, 0);
+            if (lp.tiny || lq.tiny) {
+                // operands of less than eight, element by element: one stage at a time
+                for (int s = 0; s < total; ++s) {
+                    next();
+                    if (lp.tiny) ps[0].load_tiny(pb, wave * LP, k_left);
+                    else ps[0].load(pb, k_left);
+                    if (lq.tiny) qs[0].load_tiny(qb, wave * LQ, k_left);
+                    else qs[0].load(qb, k_left);
+                    __syncthreads();
+                    put(0, 0);
+                    __syncthreads();
 #pragma unroll
-            for (int d = 0; d < RING; ++d)
-                if (d + 1 < total) fetch(d);
-            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
-            asm volatile("s_barrier" ::: "memory");
+                    for (int r = 0; r < FC + FR; ++r) read(0, 0, 0, r);
 #pragma unroll
-            for (int r = 0; r < FC + FR; ++r) read(0, 0, 0, r);
-            auto turn = [&](int s, int d) __attribute__((always_inline)) {
-                const unsigned cur = (d & 1) * STAGE;
-                step(0, true, cur, 1, 0, 0, 0);
-                put(STAGE - cur, d);                        // everybody has read what was there before
-                if (s + 1 + RING < total) fetch(d);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int k = 0; k < KS; ++k) step(k & 1, k + 1 < KS, 0, k + 1, 0, 0, 0);
+                }
+            } else {
+                fetch(0);
+                put(0, 0);
 #pragma unroll
-                for (int k = 1; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+                for (int d = 0; d < RING; ++d) fetch(d);
                 __builtin_amdgcn_s_waitcnt(WAIT_LDS);
                 asm volatile("s_barrier" ::: "memory");
-                step(1, true, STAGE - cur, 0, 0, 0, 0);
-            };
-            static_assert(RING % 2 == 0, "two slots of LDS in turn");
-            int s = 0;
-            for (; s + RING < total; s += RING) static_for<0, RING>([&](auto d) __attribute__((always_inline)) { turn(s + decltype(d)::value, decltype(d)::value); });
-            unsigned cur = 0;
-            static_for<0, RING - 1>([&](auto d) __attribute__((always_inline)) {
-                if (s + decltype(d)::value + 1 < total) {
-                    turn(s + decltype(d)::value, decltype(d)::value);
-                    cur = STAGE - cur;
-                }
-            });
 #pragma unroll
-            for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
-            step(1, false, 0, 0, 0, 0, 0);
+                for (int r = 0; r < FC + FR; ++r) read(0, 0, 0, r);
+                auto turn = [&](int d, bool more) __attribute__((always_inline)) {
+                    const unsigned cur = (d & 1) * STAGE;
+                    step(0, true, cur, 1, 0, 0, 0);
+                    put(STAGE - cur, d);                        // everybody has read what was there before
+                    if (more) fetch(d);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int k = 1; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+                    __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+                    asm volatile("s_barrier" ::: "memory");
+                    step(1, true, STAGE - cur, 0, 0, 0, 0);
+                };
+                static_assert(RING % 2 == 0, "two slots of LDS in turn");
+                int s = 0;
+                for (; s + RING < total; s += RING) static_for<0, RING>([&](auto d) __attribute__((always_inline)) { turn(decltype(d)::value, true); });
+                unsigned cur = 0;
+                static_for<0, RING - 1>([&](auto d) __attribute__((always_inline)) {
+                    if (s + decltype(d)::value + 1 < total) {
+                        turn(decltype(d)::value, false);
+                        cur = STAGE - cur;
+                    }
+                });
+#pragma unroll
+                for (int k = 0; k < KS - 1; ++k) step(k & 1, true, cur, k + 1, 0, 0, 0);
+                step(1, false, 0, 0, 0, 0, 0);
+            }
         }
     }
     // ---- epilogue: JB * 32 rows at a time through an area of LDS that is the wave's own ----
