@@ -143,7 +143,8 @@ private:
     at::Tensor w_[2], b_[2];
 
     at::TensorOptions options(at::ScalarType t) const { return at::TensorOptions().dtype(t).device(device_); }
-    at::Tensor workspace(size_t need) const { return need > 0 ? at::empty({(int64_t)need}, options(at::kByte)) : at::Tensor(); }
+    // (SIZE_MAX: the call itself will refuse the description, and say why)
+    at::Tensor workspace(size_t need) const { return need > 0 && need != SIZE_MAX ? at::empty({(int64_t)need}, options(at::kByte)) : at::Tensor(); }
     static void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
     static float* floats(const at::Tensor& t) { return t.defined() ? t.data_ptr<float>() : nullptr; }
     static py::object wrap(const at::Tensor& t) { return t.defined() ? py::reinterpret_steal<py::object>(THPVariable_Wrap(t)) : py::none(); }
@@ -199,6 +200,10 @@ PYBIND11_MODULE(_dlf_torch, m)
 {
     py::class_<Op>(m, "Op")
         .def(py::init<bool, int, at::Tensor, std::optional<at::Tensor>, std::optional<at::Tensor>, std::optional<at::Tensor>, int64_t>())
-        .def("forward", &Op::forward)
-        .def("backward", &Op::backward);
+        // (wrapped: PyTorch's own errors, out of memory among them, keep their Python types)
+        .def("forward", torch::wrap_pybind_function([](const Op& op, py::handle x, py::handle residual, py::handle out, bool save, int64_t stream) {
+            return op.forward(x, residual, out, save, stream);
+        }))
+        .def("backward", torch::wrap_pybind_function([](const Op& op, py::handle dy, py::handle x, py::handle saved, bool want_x, bool want_w, bool want_b,
+                                                        int64_t stream) { return op.backward(dy, x, saved, want_x, want_w, want_b, stream); }));
 }
