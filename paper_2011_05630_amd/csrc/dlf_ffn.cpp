@@ -222,6 +222,7 @@ Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
 // The two products of a backward pass in one launch: both in tiles of one shape.
 struct BackCut {
     Cut w, x;
+    bool x_first = false;
 };
 // rows, in, out as of the layer; problems: 2 for the gated pair
 BackCut least_back(int64_t rows, int64_t in, int64_t out, int problems, bool any, bool want_w, bool want_x)
@@ -234,10 +235,12 @@ BackCut least_back(int64_t rows, int64_t in, int64_t out, int problems, bool any
             const Cut w = cut_as(shape, sw, out, in, problems, false);
             each_split(want_x ? stages_x : 1, [&](int sx) {
                 const Cut x = cut_as(shape, sx, rows, in, 1, false);
-                const double t = fill_ns(shape, want_w ? (int64_t)w.tiles_r * w.tiles_c * problems * sw : 0, (double)stages_w / sw,
-                                         want_x ? (int64_t)x.tiles_r * x.tiles_c * sx : 0, (double)stages_x / sx) +
+                const int64_t nw = want_w ? (int64_t)w.tiles_r * w.tiles_c * problems * sw : 0, nx = want_x ? (int64_t)x.tiles_r * x.tiles_c * sx : 0;
+                const double lw = (double)stages_w / sw, lx = (double)stages_x / sx;
+                const bool x_first = lx > lw;
+                const double t = (x_first ? fill_ns(shape, nx, lx, nw, lw) : fill_ns(shape, nw, lw, nx, lx)) +
                                  join_ns((want_w ? w.part_bytes : 0) + (want_x ? x.part_bytes : 0));
-                if (least == 0 || t < least) { least = t; best = {w, x}; }
+                if (least == 0 || t < least) { least = t; best = {w, x, x_first}; }
             });
         });
     });
@@ -417,6 +420,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         if (!cx) c.x.problems = 0;
         if (part == 1) c.sum.blocks = 0;
         const BackCut k = choose_back(std::max<int64_t>(1, f.d.rows), f.d.in_features, f.d.out_features, nz, cw || cx ? any : false, cw, cx);
+        c.x_first = k.x_first;
         set_cut(c.w, k.w, ws + l.join);
         set_cut(c.x, k.x, ws + l.join + align256(k.w.part_bytes));
         TRY(launched(f, dlf_ff_start_back(&c, k.w.shape, f.d.dtype, stream)));

@@ -51,7 +51,8 @@ struct DlfFfSumArgs {
 struct DlfFfBackArgs {
     DlfFfArgs w, x;
     DlfFfSumArgs sum;
-    int32_t blocks_w, blocks_x;  // workgroups: w's first, x's behind them, then the sums'
+    int32_t blocks_w, blocks_x;  // workgroups of either; the sums' come last
+    int32_t x_first;             // x's tiles are the longer ones and start first, else w's
 };
 
 // Partial column sums: of at most this many parts, of at least so many rows (those that a workgroup of k_ff_dz takes at a time).

@@ -772,13 +772,14 @@ __device__ __forceinline__ void add_sums(const DlfFfSumArgs& a, int block)
 }
 
 // k_ff_back: both products of a backward pass and the column sums in one launch: their tiles fill the chip together (each alone leaves compute
-// units idle in its last round), and small layers, bound by launches, need one instead of three.  The weights' gradients go first:
-// they are the longer sums in training, and what is short fills the gaps.  The products of 4096 x 2048 -> 2048 take 70 us together, 38 and 38
-// apart; those of 4096 x 2048 -> 2 x 5632 329 with their join, 235 and 243 apart (1.15 PFLOP/s).
+// units idle in its last round), and small layers, bound by launches, need one instead of three.  The product of the longer sums
+// goes first, and what is short fills the gaps.  The products of 4096 x 2048 -> 2048 take 70 us together, 38 and 38 apart; those of 4096 x 2048
+// -> 2 x 5632 351 (1.08 PFLOP/s; 372 with the other order), 235 and 243 apart.
 template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT>
 __global__ FF_TILE_BOUNDS void k_ff_back(const DlfFfBackArgs a)
 {
     int b = blockIdx.x;
+    if (a.x_first) b = b < a.blocks_x ? b + a.blocks_w : b < a.blocks_x + a.blocks_w ? b - a.blocks_x : b;   // (both multiples of eight)
     if (b < a.blocks_w) {
         tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, b);
         return;
