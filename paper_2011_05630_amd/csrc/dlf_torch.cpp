@@ -51,6 +51,7 @@ public:
     // -> (y or h, what backward needs or None)
     py::object forward(py::handle x, py::handle residual, py::handle out, bool save, int64_t stream) const
     {
+        weights();
         const at::Tensor& xt = tensor(x, in_, "x");
         const Rows xr = rows(xt, in_, "x");
         const c10::DeviceGuard guard(device_);
@@ -98,6 +99,7 @@ public:
     py::tuple backward(py::handle dy, py::handle x, py::handle saved, bool want_x, bool want_w, bool want_b, int64_t stream) const
     {
         const char* const name = gated_ ? "dh" : "dy";
+        weights();
         const at::Tensor& xt = tensor(x, in_, "x");
         const Rows xr = rows(xt, in_, "x");
         const at::Tensor& dt = tensor(dy, out_, name);
@@ -149,6 +151,22 @@ private:
     static float* floats(const at::Tensor& t) { return t.defined() ? t.data_ptr<float>() : nullptr; }
     static py::object wrap(const at::Tensor& t) { return t.defined() ? py::reinterpret_steal<py::object>(THPVariable_Wrap(t)) : py::none(); }
 
+    // The weights and biases are the caller's own tensors: an assignment to `.data`, a module's conversion among them, exchanges their
+    // sizes, distances, type and device under this object, so that their form is looked at in every call.  (Values and addresses may change.)
+    void weights() const
+    {
+        for (int i = 0; i < (gated_ ? 2 : 1); ++i) {
+            const at::Tensor &w = w_[i], &b = b_[i];
+            if (!(w.scalar_type() == type_ && w.device() == device_ && w.layout() == at::kStrided && w.dim() == 2 && w.size(0) == out_ && w.size(1) == in_ &&
+                  (in_ == 1 || w.stride(1) == 1) && (out_ == 1 || w.stride(0) == w_stride_)))
+                refuse(gated_ ? i ? "w_up" : "w_gate" : "weight", ": no longer the ", c10::toString(type_), " tensor [", out_, ", ", in_, "] with rows ", w_stride_,
+                       " apart on ", device_, " that the operator was made of: make another");
+            if (b.defined() && !(b.scalar_type() == at::kFloat && b.device() == device_ && b.layout() == at::kStrided && b.dim() == 1 && b.size(0) == out_ &&
+                                 b.is_contiguous()))
+                refuse(gated_ ? i ? "b_up" : "b_gate" : "bias", ": no longer the contiguous fp32 tensor of ", out_, " elements on ", device_,
+                       " that the operator was made of: make another");
+        }
+    }
     const at::Tensor& tensor(py::handle h, int64_t width, const char* name) const
     {
         if (THPVariable_Check(h.ptr())) {

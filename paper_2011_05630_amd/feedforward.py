@@ -1,10 +1,11 @@
 """The feed-forward half of a transformer block on libdlf: a linear layer with bias, activation and residual in one kernel,
 a gated pair of projections in one kernel, the block of the two, and their gradients.
 
-The objects hold the caller's weight tensors (no copies: change them in place and the next call sees it).  PyTorch provides
-device memory and streams only.  Every call runs on the current stream of the weights' device, asynchronously; outputs,
-saved tensors and workspaces come from PyTorch's allocator, so calls may be captured into a graph.  A tensor that another
-stream wrote or will overwrite is ordered by the caller, as for any kernel.
+The objects hold the caller's weight tensors (no copies: change their values and the next call sees it; a tensor whose shape,
+type, row distance or device has changed is refused).  PyTorch provides device memory and streams only.  Every call runs on
+the current stream of the weights' device, asynchronously; outputs, saved tensors and workspaces come from PyTorch's allocator,
+so calls may be captured into a graph.  A tensor that another stream wrote or will overwrite is ordered by the caller, as for
+any kernel.
 
 Tensors are fp16 or bf16, all of one type, with rows of consecutive elements at any distance and alignment; biases and
 their gradients fp32.  Inputs may have any number of leading dimensions that lie at one row distance.

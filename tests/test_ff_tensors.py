@@ -1,0 +1,87 @@
+"""What the feed-forward operators do with tensors that changed, on CPU tensors without rows: nothing is launched, and no GPU is needed."""
+import pytest
+import torch
+
+from paper_2011_05630_amd import binding as B
+from paper_2011_05630_amd import feedforward as F
+
+N, K = 24, 16
+X = torch.zeros(0, K, dtype=torch.bfloat16)
+DY = torch.zeros(0, N, dtype=torch.bfloat16)
+SAVED = {False: torch.zeros(0, N), True: torch.zeros(2, 0, N)}
+
+
+def operands(gated):
+    """Weights, then biases, under the names that refusals use."""
+    names = (("w_gate", "w_up"), ("b_gate", "b_up")) if gated else (("weight",), ("bias",))
+    return {n: torch.zeros(N, K, dtype=torch.bfloat16) for n in names[0]}, {n: torch.zeros(N) for n in names[1]}
+
+
+def native(gated, w, b):
+    pair = lambda d: tuple(d.values()) if gated else tuple(d.values()) + (None,)
+    return F._native().Op(gated, B.FF_ACT["silu"], *pair(w), *pair(b), K)
+
+
+def calls(op, gated, x=X, dy=DY):
+    return (lambda: op.forward(x, None, None, False, 0), lambda: op.forward(x, None, None, True, 0),
+            lambda: op.backward(dy, x, SAVED[gated], True, True, True, 0), lambda: op.backward(dy, x, SAVED[gated], False, False, False, 0))
+
+
+OTHER_WEIGHTS = {
+    "fewer rows": lambda: torch.zeros(2, K, dtype=torch.bfloat16), "fewer columns": lambda: torch.zeros(N, K - 1, dtype=torch.bfloat16),
+    "transposed": lambda: torch.zeros(K, N, dtype=torch.bfloat16).t(), "one dimension": lambda: torch.zeros(N * K, dtype=torch.bfloat16),
+    "farther rows": lambda: torch.zeros(N, K + 8, dtype=torch.bfloat16)[:, :K], "one row": lambda: torch.zeros(1, K, dtype=torch.bfloat16).expand(N, K),
+    "fp32": lambda: torch.zeros(N, K), "fp16": lambda: torch.zeros(N, K, dtype=torch.float16)}
+OTHER_BIASES = {
+    "shorter": lambda: torch.zeros(N - 1), "two dimensions": lambda: torch.zeros(1, N), "strided": lambda: torch.zeros(2 * N)[::2],
+    "bf16": lambda: torch.zeros(N, dtype=torch.bfloat16), "fp64": lambda: torch.zeros(N, dtype=torch.float64)}
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("other", sorted(OTHER_WEIGHTS))
+def test_weights_of_another_form_are_refused(gated, other):
+    """`.data = ` exchanges sizes, strides, type and device within the tensor that the operator holds; so do a module's conversions."""
+    for name in operands(gated)[0]:
+        w, b = operands(gated)
+        op = native(gated, w, b)
+        w[name].data = OTHER_WEIGHTS[other]()
+        for call in calls(op, gated):
+            with pytest.raises(ValueError, match="^%s: " % name):
+                call()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("other", sorted(OTHER_BIASES))
+def test_biases_of_another_form_are_refused(gated, other):
+    for name in operands(gated)[1]:
+        w, b = operands(gated)
+        op = native(gated, w, b)
+        b[name].data = OTHER_BIASES[other]()
+        for call in calls(op, gated):
+            with pytest.raises(ValueError, match="^%s: " % name):
+                call()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_values_of_the_same_form_are_followed(gated):
+    """New storage of the same form is a change that the next call sees; one row's distance to the next says nothing."""
+    w, b = operands(gated)
+    op = native(gated, w, b)
+    for t in list(w.values()) + list(b.values()):
+        t.data = torch.ones_like(t)
+    for call in calls(op, gated)[:2]:
+        call()
+    one = torch.zeros(1, K, dtype=torch.bfloat16)
+    op = F._native().Op(False, B.FF_ACT["none"], one, None, None, None, K)
+    one.data = torch.zeros(3, K + 5, dtype=torch.bfloat16)[1:2, :K]
+    assert op.forward(X, None, None, False, 0).shape == (0, 1)
+
+
+def test_a_module_that_converts_its_parameters():
+    m = torch.nn.Linear(K, N, bias=False, dtype=torch.bfloat16)
+    op = F._native().Op(False, B.FF_ACT["none"], m.weight.data, None, None, None, K)
+    held = F._native().Op(False, B.FF_ACT["none"], m.weight, None, None, None, K)
+    m.float()
+    op.forward(X, None, None, False, 0)                     # `.data` of before: a tensor of its own, unchanged
+    with torch.no_grad(), pytest.raises(ValueError, match="^weight: "):
+        held.forward(X, None, None, False, 0)

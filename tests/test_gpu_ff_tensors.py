@@ -1,0 +1,42 @@
+"""What the feed-forward operators do with tensors that changed, on the GPU."""
+import pytest
+import torch
+
+from ff_util import act, rows_of, same, whole
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+T = torch.bfloat16
+
+
+def F():
+    from paper_2011_05630_amd import feedforward
+    return feedforward
+
+
+def test_weights_that_changed():
+    """Values and addresses are followed; another device, type or shape under the operator is refused before a launch."""
+    announce("changed weights")
+    x, w, b = whole(40, 24, 1), whole(20, 24, 2), whole(1, 20, 3)[0]
+    xd, wd, bd = rows_of(x, T), rows_of(w, T), b.float().cuda()
+    op, pair = F().Linear(wd, bd), F().GatedLinear(wd, wd, bd, act="relu")
+    same(op.run(xd), x @ w.t() + b, "y")
+    w2, b2 = whole(20, 24, 4), whole(1, 20, 5)[0]
+    wd.copy_(w2.to(T))
+    bd.data = b2.float().cuda()
+    same(op.run(xd), x @ w2.t() + b2, "new values")
+    wd.data = rows_of(w, T)
+    same(op.run(xd), x @ w.t() + b2, "a new address")
+    same(pair.run(xd), act("relu", x @ w.t() + b2) * (x @ w.t()), "h")
+    kept = wd.data
+    for other in (kept.cpu(), kept.float(), kept[:3], rows_of(w, T, 8)):
+        wd.data = other
+        for o, dy in ((op, torch.zeros(40, 20, dtype=T, device="cuda")), (pair, torch.zeros(40, 20, dtype=T, device="cuda"))):
+            for call in (lambda: o.run(xd), lambda: o.run_saved(xd), lambda: o.backward(dy, xd, torch.zeros(2, 40, 20, device="cuda"))):
+                with pytest.raises(ValueError, match="^(weight|w_gate): "):
+                    call()
+    wd.data = kept
+    bd.data = b2.float()
+    with pytest.raises(ValueError, match="^bias: "):
+        op.run(xd)
