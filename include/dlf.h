@@ -303,7 +303,8 @@ dlf_status dlf_i8conv_run(const dlf_i8conv_t* layer, const void* in_dev, void* o
  * gradients are fp32 [out_features].  saved: fp32, [rows][out_features] (gated: [2][rows][out_features]), the
  * pre-activations z (g, then u) that the backward pass needs, 4-byte aligned; written by the forward call if not NULL.  The
  * gradients dx [rows][in_features] and dweight, dw_gate, dw_up [out_features][in_features] are written with rows next to each other.
- * y may be the residual itself (same address and stride); other outputs must not overlap anything.
+ * y (h) may be the residual itself (same address and stride); on any other operand it is refused, but columns of one matrix may lie
+ * beside each other.  Other outputs must not overlap anything.
  * rows = 0 is valid: nothing to compute forward, zero weight and bias gradients backward. */
 typedef enum { DLF_F16 = 0, DLF_BF16 = 1 } dlf_dtype;
 typedef struct {

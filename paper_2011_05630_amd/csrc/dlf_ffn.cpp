@@ -63,6 +63,48 @@ dlf_status check_ptr(const Ff& f, const void* p, const char* name, bool wanted, 
     return DLF_OK;
 }
 
+// Rows in memory, in bytes.
+struct Span {
+    uintptr_t p;
+    int64_t rows, row, stride;
+    Span(const void* at, int64_t rows_, int64_t row_, int64_t stride_) : p((uintptr_t)at), rows(rows_), row(row_), stride(rows_ > 1 ? stride_ : row_) {}
+    uintptr_t end() const { return p + (uintptr_t)((rows - 1) * stride + row); }
+    // whether a byte of [lo, hi), which meets [p, end()), lies in a row: the last row that starts in front of hi has the farthest end
+    bool meets(uintptr_t lo, uintptr_t hi) const
+    {
+        const int64_t last = std::min<int64_t>(rows - 1, (int64_t)((hi - 1 - p) / (uintptr_t)stride));
+        return p + (uintptr_t)(last * stride + row) > lo;
+    }
+};
+// Whether two sets of rows share a byte.  Columns of one matrix lie between each other's rows and share none.  (Rows at two different
+// distances, neither of them the row itself, are taken as apart.)
+bool share(const Span& a, const Span& b)
+{
+    if (a.rows <= 0 || b.rows <= 0 || a.end() <= b.p || b.end() <= a.p) return false;
+    if (a.stride == a.row) return b.meets(a.p, a.end());
+    if (b.stride == b.row) return a.meets(b.p, b.end());
+    if (a.stride != b.stride) return false;
+    const Span &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
+    const int64_t gap = (int64_t)(hi.p - lo.p), at = gap % lo.stride;        // hi's rows start here in lo's
+    return at < lo.row || (at + hi.row > lo.stride && gap / lo.stride + 1 < lo.rows);
+}
+// y is written while other workgroups read the operands: it may lie on the residual alone, element on element.
+dlf_status check_output(const Ff& f, const void* y, const void* x, const void* const w[2], const float* const bias[2], const void* res,
+                        const char* const (&names)[2][2])
+{
+    const int64_t in = (int64_t)f.d.in_features * 2, out = (int64_t)f.d.out_features * 2;
+    const char* const name = f.gated ? "h" : "y";
+    const Span s(y, f.d.rows, out, f.d.y_stride * 2);
+    if (share(s, Span(x, f.d.rows, in, f.d.x_stride * 2))) return fail(DLF_ERR_INVALID_ARG, "%s: %s overlaps x", f.call, name);
+    for (int i = 0; i < (f.gated ? 2 : 1); ++i) {
+        if (share(s, Span(w[i], f.d.out_features, in, f.d.w_stride * 2))) return fail(DLF_ERR_INVALID_ARG, "%s: %s overlaps %s", f.call, name, names[0][i]);
+        if (bias[i] && share(s, Span(bias[i], 1, out * 2, out * 2))) return fail(DLF_ERR_INVALID_ARG, "%s: %s overlaps %s", f.call, name, names[1][i]);
+    }
+    if (res && !(res == y && (f.d.rows == 1 || f.d.res_stride == f.d.y_stride)) && share(s, Span(res, f.d.rows, out, f.d.res_stride * 2)))
+        return fail(DLF_ERR_INVALID_ARG, "%s: %s overlaps the residual and is not the residual", f.call, name);
+    return DLF_OK;
+}
+
 dlf_status check_ws(const Ff& f, const void* ws, size_t have, size_t need)
 {
     if (need == 0) return DLF_OK;
@@ -466,9 +508,10 @@ dlf_status dlf_linear(const dlf_ff_desc* d, const void* x, const void* weight, c
     TRY(check_ptr(f, residual, "residual", false, 2));
     TRY(check_ptr(f, y, "y", some, 2));
     TRY(check_ptr(f, saved, "saved", false, 4));
-    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     const void* w[2] = {weight, nullptr};
     const float* b[2] = {bias, nullptr};
+    TRY(check_output(f, y, x, w, b, residual, {{"weight", ""}, {"bias", ""}}));
+    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     return forward(f, x, w, b, residual, y, saved, (char*)workspace, hip_stream);
 }
 
@@ -485,9 +528,10 @@ dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, co
     TRY(check_ptr(f, b_up, "b_up", false, 4));
     TRY(check_ptr(f, h, "h", some, 2));
     TRY(check_ptr(f, saved, "saved", false, 4));
-    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     const void* w[2] = {w_gate, w_up};
     const float* b[2] = {b_gate, b_up};
+    TRY(check_output(f, h, x, w, b, nullptr, {{"w_gate", "w_up"}, {"b_gate", "b_up"}}));
+    TRY(check_ws(f, workspace, workspace_bytes, forward_ws(f)));
     return forward(f, x, w, b, nullptr, h, saved, (char*)workspace, hip_stream);
 }
 

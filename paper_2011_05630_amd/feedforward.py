@@ -76,7 +76,7 @@ class Linear(_Operator):
         self._setup(False, act, (weight, None), (bias, None))
 
     def run(self, x, residual=None, out=None):
-        """-> y [..., out]; written to `out` if given (which may be the residual)."""
+        """-> y [..., out]; written to `out` if given (which may be the residual, and is refused on x or a weight)."""
         return self._forward(x, residual, out, False, _stream(self._index))
 
     def run_saved(self, x, residual=None, out=None):
@@ -101,7 +101,7 @@ class GatedLinear(_Operator):
         self._setup(True, act, (w_gate, w_up), (b_gate, b_up))
 
     def run(self, x, out=None):
-        """-> h [..., out]; written to `out` if given."""
+        """-> h [..., out]; written to `out` if given (which is refused on x or a weight)."""
         return self._forward(x, None, out, False, _stream(self._index))
 
     def run_saved(self, x, out=None):
@@ -128,7 +128,8 @@ class FeedForward:
         return self.down.run(self.gated.run(x), residual, out)
 
     def run_saved(self, x, residual=None, out=None):
-        """-> (y, saved): what `backward` needs."""
+        """-> (y, saved): what `backward` needs beside x.  `out` may be x itself where x is the residual, for a caller that
+        keeps x's values elsewhere for `backward`."""
         h, saved_g = self.gated.run_saved(x)
         y, saved_d = self.down.run_saved(h, residual, out)
         return y, (h, saved_g, saved_d)

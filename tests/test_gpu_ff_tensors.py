@@ -40,3 +40,20 @@ def test_weights_that_changed():
     bd.data = b2.float()
     with pytest.raises(ValueError, match="^bias: "):
         op.run(xd)
+
+
+@pytest.mark.parametrize("m", [5, 200])
+def test_outputs_beside_and_on_operands(m):
+    """An output beside its input in wider rows is right; one on its input, where other workgroups still read, is refused."""
+    announce("outputs on operands", m)
+    x, w = whole(m, 40, 1), whole(40, 40, 2)
+    buf = rows_of(torch.zeros(m, 80), T)
+    buf[:, 40:].copy_(x.to(T))
+    op = F().Linear(rows_of(w, T))
+    same(op.run(buf[:, 40:], out=buf[:, :40]), x @ w.t(), "y")
+    same(buf[:, 40:], x, "x")
+    from paper_2011_05630_amd.binding import DlfError
+    for kw in (dict(out=buf[:, 40:]), dict(out=buf[:, 39:79]), dict(out=buf[:, 40:], residual=buf[:, 40:])):
+        with pytest.raises(DlfError, match="overlaps"):
+            op.run(buf[:, 40:], **kw)
+    same(buf[:, 40:], x, "x")
