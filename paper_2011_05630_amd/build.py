@@ -53,6 +53,7 @@ def build(force=True, verbose=False):
            "-x", "hip",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Wno-unused-command-line-argument",
+           "-Wno-inline-asm",                   # (statements that write m0 name it as clobbered, which the compiler remarks on)
            "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-save-temps=obj")

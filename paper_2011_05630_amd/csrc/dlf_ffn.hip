@@ -301,7 +301,7 @@ __device__ __forceinline__ i4v resource(const void* p, int bytes = 0x7fffffff)
 // wherever it waits for an LDS read.
 __device__ __forceinline__ void line_to_lds(const i4v& base, int off, unsigned dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(base), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(base), "s"(dst) : "memory", "m0");
 }
 #define WAIT_LDS 0xc07f          // s_waitcnt lgkmcnt(0)
 // s_waitcnt vmcnt(N) lgkmcnt(0); known to the compiler, unlike an instruction in assembly
