@@ -2,6 +2,7 @@
 // (Small calls are bound by the host: a forward call takes 8.9 us with these steps in Python and ctypes, of which the launch is 3.4.)
 // PyTorch is used for its tensors and its allocator only.
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
@@ -111,6 +112,7 @@ public:
             if (st == nullptr || st->scalar_type() != at::kFloat || st->device() != device_ || !st->is_contiguous() ||
                 !(gated_ ? st->sizes().equals({2, xr.rows, out_}) : st->sizes().equals({xr.rows, out_})))
                 refuse("saved: the tensor that the forward call returned, fp32 [", gated_ ? "2, " : "", xr.rows, ", ", out_, "], expected");
+            undifferentiated(*st, "saved");
             sp = st->data_ptr<float>();
         }
         const c10::DeviceGuard guard(device_);
@@ -157,21 +159,35 @@ private:
     {
         for (int i = 0; i < (gated_ ? 2 : 1); ++i) {
             const at::Tensor &w = w_[i], &b = b_[i];
+            const char *const wn = gated_ ? i ? "w_up" : "w_gate" : "weight", *const bn = gated_ ? i ? "b_up" : "b_gate" : "bias";
             if (!(w.scalar_type() == type_ && w.device() == device_ && w.layout() == at::kStrided && w.dim() == 2 && w.size(0) == out_ && w.size(1) == in_ &&
                   (in_ == 1 || w.stride(1) == 1) && (out_ == 1 || w.stride(0) == w_stride_)))
-                refuse(gated_ ? i ? "w_up" : "w_gate" : "weight", ": no longer the ", c10::toString(type_), " tensor [", out_, ", ", in_, "] with rows ", w_stride_,
-                       " apart on ", device_, " that the operator was made of: make another");
+                refuse(wn, ": no longer the ", c10::toString(type_), " tensor [", out_, ", ", in_, "] with rows ", w_stride_, " apart on ", device_,
+                       " that the operator was made of: make another");
             if (b.defined() && !(b.scalar_type() == at::kFloat && b.device() == device_ && b.layout() == at::kStrided && b.dim() == 1 && b.size(0) == out_ &&
                                  b.is_contiguous()))
-                refuse(gated_ ? i ? "b_up" : "b_gate" : "bias", ": no longer the contiguous fp32 tensor of ", out_, " elements on ", device_,
-                       " that the operator was made of: make another");
+                refuse(bn, ": no longer the contiguous fp32 tensor of ", out_, " elements on ", device_, " that the operator was made of: make another");
+            undifferentiated(w, wn);
+            if (b.defined()) undifferentiated(b, bn);
         }
+    }
+    // Automatic differentiation does not see the calls: what it would have to follow is refused rather than dropped.
+    static void undifferentiated(const at::Tensor& t, const char* name)
+    {
+        if (t.requires_grad() && c10::AutogradState::get_tls_state().get_grad_mode())
+            refuse(name, ": requires a gradient, which automatic differentiation cannot take through this operator: call it under torch.no_grad(), "
+                         "gradients come from run_saved and backward");
+        if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+            refuse(name, ": carries a tangent, which this operator cannot pass on");
     }
     const at::Tensor& tensor(py::handle h, int64_t width, const char* name) const
     {
         if (THPVariable_Check(h.ptr())) {
             const at::Tensor& t = THPVariable_Unpack(h.ptr());
-            if (t.scalar_type() == type_ && t.device() == device_ && t.layout() == at::kStrided && t.dim() >= 1 && t.size(-1) == width) return t;
+            if (t.scalar_type() == type_ && t.device() == device_ && t.layout() == at::kStrided && t.dim() >= 1 && t.size(-1) == width) {
+                undifferentiated(t, name);
+                return t;
+            }
         }
         refuse(name, ": a ", c10::toString(type_), " tensor [..., ", width, "] on ", device_, " expected");
     }

@@ -7,6 +7,10 @@ the current stream of the weights' device, asynchronously; outputs, saved tensor
 so calls may be captured into a graph.  A tensor that another stream wrote or will overwrite is ordered by the caller, as for
 any kernel.
 
+Automatic differentiation does not see the calls, so an operand that requires a gradient (while gradients are recorded) or carries a
+tangent is refused: call under torch.no_grad(), or inside a torch.autograd.Function's forward and backward, and take the gradients from
+`run_saved` and `backward`.
+
 Tensors are fp16 or bf16, all of one type, with rows of consecutive elements at any distance and alignment; biases and
 their gradients fp32.  Inputs may have any number of leading dimensions that lie at one row distance.
 """

@@ -85,3 +85,70 @@ def test_a_module_that_converts_its_parameters():
     op.forward(X, None, None, False, 0)                     # `.data` of before: a tensor of its own, unchanged
     with torch.no_grad(), pytest.raises(ValueError, match="^weight: "):
         held.forward(X, None, None, False, 0)
+
+
+def forward_and_backward(gated, **kw):
+    """Each call, with the named operands in place of the usual ones: [(name, call)]."""
+    w, b = operands(gated)
+    w.update({k: v for k, v in kw.items() if k in w})
+    b.update({k: v for k, v in kw.items() if k in b})
+    op = native(gated, w, b)
+    x, saved, dy = kw.get("x", X), kw.get("saved", SAVED[gated]), kw.get("dh" if gated else "dy", DY)
+    forward = lambda save: op.forward(x, kw.get("residual"), kw.get("out"), save, 0)
+    backward = lambda: op.backward(dy, x, saved, False, False, False, 0)
+    out = []
+    if not {"saved", "dy", "dh"} & set(kw):
+        out += [lambda: forward(False), lambda: forward(True)]
+    if not {"residual", "out"} & set(kw):
+        out.append(backward)
+    return out
+
+
+NAMES = [(g, n) for g in (False, True) for n in (["x", "residual", "out", "saved"] + (["dh", "w_gate", "w_up", "b_gate", "b_up"] if g else ["dy", "weight", "bias"]))
+         if not (g and n == "residual")]
+
+
+def usual(gated, name):
+    w, b = operands(gated)
+    return dict(w, **b, x=X, residual=DY, out=DY, saved=SAVED[gated], dy=DY, dh=DY)[name].clone()
+
+
+@pytest.mark.parametrize("gated,name", NAMES)
+def test_operands_that_require_a_gradient_are_refused(gated, name):
+    """The operators stand outside automatic differentiation: a result without a graph would be a wrong gradient without a word."""
+    for t in (usual(gated, name).requires_grad_(), usual(gated, name).requires_grad_() * 1):
+        for call in forward_and_backward(gated, **{name: t}):
+            with pytest.raises(ValueError, match="^%s: .*no_grad" % name):
+                call()
+        with torch.no_grad():
+            for call in forward_and_backward(gated, **{name: t})[:1 if name in ("saved", "dy", "dh") else 2]:
+                try:
+                    call()
+                except B.DlfError as e:                     # (a backward call goes on to the GPU)
+                    assert e.status == B.DLF_ERR_HIP
+    with torch.inference_mode():
+        for call in forward_and_backward(gated, x=X)[:2]:
+            call()
+
+
+@pytest.mark.parametrize("gated,name", NAMES)
+def test_operands_with_a_tangent_are_refused(gated, name):
+    import torch.autograd.forward_ad as fw
+    t = usual(gated, name)
+    with fw.dual_level():
+        d = fw.make_dual(t, torch.ones_like(t))
+        for call in forward_and_backward(gated, **{name: d}):
+            with pytest.raises(ValueError, match="^%s: .*tangent" % name):
+                call()
+        with fw._set_fwd_grad_enabled(False):
+            for call in forward_and_backward(gated, x=X)[:2]:
+                call()
+
+
+def test_function_transforms_are_refused():
+    op = native(False, *operands(False))
+    x = torch.zeros(3, K, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="^x: "):
+        torch.func.grad(lambda v: op.forward(v, None, None, False, 0).sum())(x)
+    with pytest.raises(ValueError, match="^x: "):
+        torch.func.jvp(lambda v: op.forward(v, None, None, False, 0), (x,), (x,))

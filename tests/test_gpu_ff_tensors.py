@@ -57,3 +57,33 @@ def test_outputs_beside_and_on_operands(m):
         with pytest.raises(DlfError, match="overlaps"):
             op.run(buf[:, 40:], **kw)
     same(buf[:, 40:], x, "x")
+
+
+def test_inside_an_autograd_function():
+    """What differentiation can use: the calls within a Function, on operands that require gradients; outside one they are refused."""
+    announce("autograd function")
+    x, w, b, dy = whole(70, 40, 1), whole(24, 40, 2), whole(1, 24, 3)[0], whole(70, 24, 4)
+    xd, wd, bd = (v.requires_grad_() for v in (rows_of(x, T), rows_of(w, T), b.float().cuda()))
+    op = F().Linear(wd, bd, "relu")
+
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, b):
+            y, saved = op.run_saved(x)
+            ctx.save_for_backward(x, saved)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return op.backward(dy, *ctx.saved_tensors)
+
+    with pytest.raises(ValueError, match="no_grad"):
+        op.run(xd)
+    y = Layer.apply(xd, wd, bd)
+    z = x @ w.t() + b
+    same(y.detach(), act("relu", z), "y")
+    y.backward(rows_of(dy, T))
+    dz = dy * (z > 0)
+    same(xd.grad, dz @ w, "dx")
+    same(wd.grad, dz.t() @ x, "dw")
+    same(bd.grad, dz.sum(0), "db")
