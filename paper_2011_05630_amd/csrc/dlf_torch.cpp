@@ -91,6 +91,8 @@ public:
                        : dlf_linear(&d, xr.p, w_[0].data_ptr(), floats(b_[0]), rr.p, yr.p, sp, wp, need, (void*)stream);
         }
         check(s);
+        // (a tensor made in inference mode has no version)
+        if (!out.is_none() && !y.is_inference()) y.unsafeGetTensorImpl()->bump_version();
         py::object first = out.is_none() ? wrap(y) : py::reinterpret_borrow<py::object>(out);
         if (!save) return first;
         return py::make_tuple(first, wrap(saved));

@@ -152,3 +152,32 @@ def test_function_transforms_are_refused():
         torch.func.grad(lambda v: op.forward(v, None, None, False, 0).sum())(x)
     with pytest.raises(ValueError, match="^x: "):
         torch.func.jvp(lambda v: op.forward(v, None, None, False, 0), (x,), (x,))
+
+
+def test_outputs_raise_their_version():
+    """PyTorch tells by its version whether a tensor kept for a backward pass was written since."""
+    for gated in (False, True):
+        op = native(gated, *operands(gated))
+        out = DY.clone()
+        before = out._version
+        op.forward(X, None, out, False, 0)
+        assert out._version == before + 1
+        op.forward(X, None, out, True, 0)
+        assert out._version == before + 2
+    a = torch.zeros(0, N, requires_grad=True)
+    y = a.bfloat16()
+    loss = (y * y).sum()                                    # keeps y
+    with torch.no_grad():
+        op.forward(X, None, y, False, 0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        out = DY.clone()
+        op.forward(X, None, out, False, 0)                  # counts nothing
+    op.forward(X, None, out, False, 0)
+    big = F._native().Op(False, B.FF_ACT["none"], torch.empty(1, (1 << 20) + 1, dtype=torch.bfloat16), None, None, None, (1 << 20) + 1)
+    out = torch.zeros(0, 1, dtype=torch.bfloat16)
+    before = out._version
+    with pytest.raises(B.DlfError):
+        big.forward(torch.empty(0, (1 << 20) + 1, dtype=torch.bfloat16), None, out, False, 0)
+    assert out._version == before                           # refused, not written
