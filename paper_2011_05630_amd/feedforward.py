@@ -69,6 +69,20 @@ class _Operator:
         self._index = w.get_device()
         op = _native().Op(gated, B.FF_ACT[act], *weights, *biases, _stride(w, "weight"))
         self._forward, self._backward = op.forward, op.backward
+        self._fixed = frozenset(self.__dict__)
+
+    # The native operator holds what it was made of, and would not see another tensor in its place here.
+    def __setattr__(self, name, value):
+        self._refuse_fixed(name)
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        self._refuse_fixed(name)
+        object.__delattr__(self, name)
+
+    def _refuse_fixed(self, name):
+        if name in self.__dict__.get("_fixed", ()):
+            raise AttributeError("%s: fixed when the operator was made; change the tensor's values, or make another operator" % name)
 
 
 class Linear(_Operator):

@@ -181,3 +181,30 @@ def test_outputs_raise_their_version():
     with pytest.raises(B.DlfError):
         big.forward(torch.empty(0, (1 << 20) + 1, dtype=torch.bfloat16), None, out, False, 0)
     assert out._version == before                           # refused, not written
+
+
+def on_cpu(gated):
+    """The Python object around CPU tensors, which its constructor refuses."""
+    w, b = operands(gated)
+    op = object.__new__(F.GatedLinear if gated else F.Linear)
+    for name, t in dict(w, **b).items():
+        setattr(op, name, t)
+    pair = lambda d: tuple(d.values()) if gated else tuple(d.values()) + (None,)
+    op._setup(gated, "silu", pair(w), pair(b))
+    return op
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_what_an_operator_was_made_of_is_fixed(gated):
+    """The native operator would not see another tensor in a weight's place."""
+    op = on_cpu(gated)
+    for name in list(operands(gated)[0]) + list(operands(gated)[1]) + ["act", "dtype", "device", "in_features", "out_features"]:
+        have = getattr(op, name)
+        with pytest.raises(AttributeError, match="^%s: " % name):
+            setattr(op, name, torch.zeros(N, K, dtype=torch.bfloat16))
+        with pytest.raises(AttributeError, match="^%s: " % name):
+            delattr(op, name)
+        assert getattr(op, name) is have
+    op.label = "up"                                         # a caller's own
+    op.label = "down"
+    del op.label
