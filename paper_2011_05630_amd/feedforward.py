@@ -36,6 +36,17 @@ def _need(ok, msg, *a):
         raise ValueError(msg % a if a else msg)
 
 
+_GRADIENTS = ("x", "weight", "bias")
+
+
+def _wanted(need):
+    """Which of _GRADIENTS `need` names, which is some of them, or one."""
+    need = (need,) if isinstance(need, str) else tuple(need)
+    for n in need:
+        _need(n in _GRADIENTS, "need: some of %s expected, not %r", ", ".join(_GRADIENTS), n)
+    return tuple(g in need for g in _GRADIENTS)
+
+
 def _weight(t, name):
     _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES, "%s: a 2-dimensional fp16 or bf16 tensor on the GPU expected", name)
     _need(t.shape[0] > 0 and t.shape[1] > 0, "%s: empty", name)
@@ -101,10 +112,10 @@ class Linear(_Operator):
         """-> (y, saved): the pre-activations that `backward` needs, fp32 [rows, out]; None without an activation."""
         return self._forward(x, residual, out, True, _stream(self._index))
 
-    def backward(self, dy, x, saved, need=("x", "weight", "bias")):
+    def backward(self, dy, x, saved, need=_GRADIENTS):
         """Gradients for dy, the gradient of y: -> (dx, dweight, dbias), None for what `need` leaves out or the layer lacks.
         x and saved are those of the forward call.  The gradient of its residual is dy."""
-        return self._backward(dy, x, saved, "x" in need, "weight" in need, "bias" in need, _stream(self._index))
+        return self._backward(dy, x, saved, *_wanted(need), _stream(self._index))
 
 
 class GatedLinear(_Operator):
@@ -126,10 +137,10 @@ class GatedLinear(_Operator):
         """-> (h, saved): both projections' results, which `backward` needs, fp32 [2, rows, out]."""
         return self._forward(x, None, out, True, _stream(self._index))
 
-    def backward(self, dh, x, saved, need=("x", "weight", "bias")):
+    def backward(self, dh, x, saved, need=_GRADIENTS):
         """Gradients for dh, the gradient of h: -> (dx, dw_gate, dw_up, db_gate, db_up), None for what `need` leaves out or the
         layer lacks.  x and saved are those of the forward call."""
-        return self._backward(dh, x, saved, "x" in need, "weight" in need, "bias" in need, _stream(self._index))
+        return self._backward(dh, x, saved, *_wanted(need), _stream(self._index))
 
 
 class FeedForward:
@@ -152,10 +163,11 @@ class FeedForward:
         y, saved_d = self.down.run_saved(h, residual, out)
         return y, (h, saved_g, saved_d)
 
-    def backward(self, dy, x, saved, need=("x", "weight", "bias")):
+    def backward(self, dy, x, saved, need=_GRADIENTS):
         """-> (dx, (dw_gate, dw_up, db_gate, db_up), (dw_down, db_down)).  dx is the gradient through the products; where x
         was the residual too, dy is added to it by the caller."""
+        need = tuple(g for g, w in zip(_GRADIENTS, _wanted(need)) if w)
         h, saved_g, saved_d = saved
-        dh, dw, db = self.down.backward(dy, h, saved_d, tuple(set(need) | {"x"}))
+        dh, dw, db = self.down.backward(dy, h, saved_d, need + ("x",))
         g = self.gated.backward(dh, x, saved_g, need)
         return g[0], g[1:], (dw, db)

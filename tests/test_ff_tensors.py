@@ -208,3 +208,14 @@ def test_what_an_operator_was_made_of_is_fixed(gated):
     op.label = "up"                                         # a caller's own
     op.label = "down"
     del op.label
+
+
+def test_unknown_gradients_are_refused():
+    """A misspelled gradient would come back as None."""
+    for op in (on_cpu(False), on_cpu(True)):
+        for bad in (("weights",), ("x", "b"), "w", "bias, x", (1,)):
+            with pytest.raises(ValueError, match="^need: "):
+                op.backward(DY, X, SAVED[isinstance(op, F.GatedLinear)], need=bad)
+    block = object.__new__(F.FeedForward)
+    with pytest.raises(ValueError, match="^need: "):
+        block.backward(DY, X, (DY, SAVED[True], None), need=("weights",))
