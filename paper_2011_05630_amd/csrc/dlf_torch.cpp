@@ -111,7 +111,7 @@ public:
         const float* sp = nullptr;
         if (gated_ || act_ != DLF_ACT_NONE) {
             const at::Tensor* const st = THPVariable_Check(saved.ptr()) ? &THPVariable_Unpack(saved.ptr()) : nullptr;
-            if (st == nullptr || st->scalar_type() != at::kFloat || st->device() != device_ || !st->is_contiguous() ||
+            if (st == nullptr || st->scalar_type() != at::kFloat || st->device() != device_ || !readable(*st) || !st->is_contiguous() ||
                 !(gated_ ? st->sizes().equals({2, xr.rows, out_}) : st->sizes().equals({xr.rows, out_})))
                 refuse("saved: the tensor that the forward call returned, fp32 [", gated_ ? "2, " : "", xr.rows, ", ", out_, "], expected");
             undifferentiated(*st, "saved");
@@ -162,17 +162,19 @@ private:
         for (int i = 0; i < (gated_ ? 2 : 1); ++i) {
             const at::Tensor &w = w_[i], &b = b_[i];
             const char *const wn = gated_ ? i ? "w_up" : "w_gate" : "weight", *const bn = gated_ ? i ? "b_up" : "b_gate" : "bias";
-            if (!(w.scalar_type() == type_ && w.device() == device_ && w.layout() == at::kStrided && w.dim() == 2 && w.size(0) == out_ && w.size(1) == in_ &&
+            if (!(w.scalar_type() == type_ && w.device() == device_ && readable(w) && w.dim() == 2 && w.size(0) == out_ && w.size(1) == in_ &&
                   (in_ == 1 || w.stride(1) == 1) && (out_ == 1 || w.stride(0) == w_stride_)))
                 refuse(wn, ": no longer the ", c10::toString(type_), " tensor [", out_, ", ", in_, "] with rows ", w_stride_, " apart on ", device_,
                        " that the operator was made of: make another");
-            if (b.defined() && !(b.scalar_type() == at::kFloat && b.device() == device_ && b.layout() == at::kStrided && b.dim() == 1 && b.size(0) == out_ &&
+            if (b.defined() && !(b.scalar_type() == at::kFloat && b.device() == device_ && readable(b) && b.dim() == 1 && b.size(0) == out_ &&
                                  b.is_contiguous()))
                 refuse(bn, ": no longer the contiguous fp32 tensor of ", out_, " elements on ", device_, " that the operator was made of: make another");
             undifferentiated(w, wn);
             if (b.defined()) undifferentiated(b, bn);
         }
     }
+    // Memory that holds the elements as they are (a view may leave their negation to the reader).
+    static bool readable(const at::Tensor& t) { return t.layout() == at::kStrided && !t.is_neg(); }
     // Automatic differentiation does not see the calls: what it would have to follow is refused rather than dropped.
     static void undifferentiated(const at::Tensor& t, const char* name)
     {
@@ -186,12 +188,12 @@ private:
     {
         if (THPVariable_Check(h.ptr())) {
             const at::Tensor& t = THPVariable_Unpack(h.ptr());
-            if (t.scalar_type() == type_ && t.device() == device_ && t.layout() == at::kStrided && t.dim() >= 1 && t.size(-1) == width) {
+            if (t.scalar_type() == type_ && t.device() == device_ && readable(t) && t.dim() >= 1 && t.size(-1) == width) {
                 undifferentiated(t, name);
                 return t;
             }
         }
-        refuse(name, ": a ", c10::toString(type_), " tensor [..., ", width, "] on ", device_, " expected");
+        refuse(name, ": a ", c10::toString(type_), " tensor [..., ", width, "] on ", device_, " expected", pending(h));
     }
     void same_leading(const at::Tensor& t, const at::Tensor& x, const char* name) const
     {

@@ -48,14 +48,14 @@ def _wanted(need):
 
 
 def _weight(t, name):
-    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES, "%s: a 2-dimensional fp16 or bf16 tensor on the GPU expected", name)
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _TYPES and not t.is_neg(), "%s: a 2-dimensional fp16 or bf16 tensor on the GPU expected", name)
     _need(t.shape[0] > 0 and t.shape[1] > 0, "%s: empty", name)
     _stride(t, name)
     return t
 
 
 def _bias(t, n, w, name):
-    _need(t is None or (isinstance(t, torch.Tensor) and t.device == w.device and t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous()),
+    _need(t is None or (isinstance(t, torch.Tensor) and t.device == w.device and t.dtype == torch.float32 and tuple(t.shape) == (n,) and t.is_contiguous() and not t.is_neg()),
           "%s: a contiguous fp32 tensor of %d elements on the weight's device expected", name, n)
     return t
 

@@ -219,3 +219,18 @@ def test_unknown_gradients_are_refused():
     block = object.__new__(F.FeedForward)
     with pytest.raises(ValueError, match="^need: "):
         block.backward(DY, X, (DY, SAVED[True], None), need=("weights",))
+
+
+def test_pending_negations_are_refused():
+    """A view whose elements are the negated ones of its memory."""
+    neg = torch._neg_view
+    for gated, name in NAMES:
+        t = neg(usual(gated, name))
+        for call in forward_and_backward(gated, **{name: t}):
+            with pytest.raises(ValueError, match="^%s: " % name):
+                call()
+    column = torch.zeros(0, 1, dtype=torch.complex32).conj().imag
+    op = F._native().Op(False, B.FF_ACT["none"], torch.zeros(2, 1, dtype=torch.float16), None, None, None, 1)
+    with pytest.raises(ValueError, match="^x: "):
+        op.forward(column, None, None, False, 0)
+    op.forward(column.resolve_neg(), None, None, False, 0)
