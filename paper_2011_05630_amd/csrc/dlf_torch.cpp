@@ -193,7 +193,8 @@ private:
                 return t;
             }
         }
-        refuse(name, ": a ", c10::toString(type_), " tensor [..., ", width, "] on ", device_, " expected", pending(h));
+        refuse(name, ": a ", c10::toString(type_), " tensor [..., ", width, "] on ", device_, " expected",
+               THPVariable_Check(h.ptr()) && THPVariable_Unpack(h.ptr()).is_neg() ? ", its negation resolved" : "");
     }
     void same_leading(const at::Tensor& t, const at::Tensor& x, const char* name) const
     {
