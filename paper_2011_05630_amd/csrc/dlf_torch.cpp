@@ -237,6 +237,7 @@ private:
 
 PYBIND11_MODULE(_dlf_torch, m)
 {
+    m.attr("built_with") = DLF_BUILT_WITH;                  // "built with PyTorch <version>": what the build script looks for
     py::class_<Op>(m, "Op")
         .def(py::init<bool, int, at::Tensor, std::optional<at::Tensor>, std::optional<at::Tensor>, std::optional<at::Tensor>, int64_t>())
         // (wrapped: PyTorch's own errors, out of memory among them, keep their Python types)

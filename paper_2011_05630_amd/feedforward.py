@@ -23,7 +23,12 @@ _TYPES = (torch.float16, torch.bfloat16)
 
 def _native():
     B.lib()                     # a missing library says so itself
-    from . import _dlf_torch
+    try:
+        from . import _dlf_torch
+    except ImportError as e:
+        raise RuntimeError("_dlf_torch.so is not built, or not for this PyTorch: run `python -m paper_2011_05630_amd.build` first (%s)" % e) from e
+    if _dlf_torch.built_with != "built with PyTorch " + torch.__version__:
+        raise RuntimeError("_dlf_torch.so is %s, this is %s: run `python -m paper_2011_05630_amd.build` again" % (_dlf_torch.built_with, torch.__version__))
     return _dlf_torch
 
 
