@@ -22,6 +22,9 @@ dlf_status fail(dlf_status s, const char* fmt, ...)
     return dlf_set_error(s, buf);
 }
 
+// A launch holds fewer than 2^32 threads, 256 to a workgroup.
+constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;
+
 // A description with its strides filled in.
 struct Ff {
     dlf_ff_desc d;
@@ -48,9 +51,10 @@ dlf_status check_desc(const dlf_ff_desc* d, bool gated, const char* call, Ff& f)
         if (*q.s < q.row || *q.s >= (int64_t)1 << 24)
             return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %lld elements, %lld apart", call, q.name, (long long)q.row, (long long)*q.s);
     }
-    // the products of the forward pass and of the gradients, with the column sums, by the workgroups of their launches
+    // the products of the forward pass and of the gradients, with the column sums, by the workgroups of their launches, each product's a
+    // multiple of eight
     const int64_t t = 64, m = (d->rows + t - 1) / t, i = (d->in_features + t - 1) / t, o = (d->out_features + t - 1) / t;
-    if (std::max(m * o * 2, m * i + 2 * i * o + 2 * o) >= (int64_t)1 << 24)
+    if (std::max(m * o * 2, m * i + 2 * i * o + 2 * o) >= MOST_WORKGROUPS - 16)
         return fail(DLF_ERR_UNSUPPORTED, "%s: %lld rows, %d -> %d features are more tiles than a launch holds", call, (long long)d->rows,
                     d->in_features, d->out_features);
     return DLF_OK;
@@ -167,6 +171,7 @@ dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
 struct Cut {
     int shape = DLF_FF_SHAPE_128, splits = 1, tiles_r = 0, tiles_c = 0;
     size_t part_bytes = 0;
+    int64_t tiles() const { return (int64_t)tiles_r * tiles_c; }
 };
 int g_force_splits = 0;
 
@@ -224,12 +229,14 @@ double fill_ns(int shape, int64_t n0, double stages0, int64_t n1, double stages1
 }
 double join_ns(size_t part_bytes) { return part_bytes > 0 ? 3500 + (double)part_bytes * 2 / 4000 : 0; }
 
-// The splits that a product may have: at least four stages each.
-template <typename F> void each_split(int64_t stages, F&& f)
+// The splits that a product of nr x nc outputs in so many tiles may have: at least four stages each, and workgroups that the launches have room
+// for: `spare` of them beside its tiles, half for either of two products, and half of the launch that joins the sums, by eights of outputs.
+template <typename F> void each_split(int64_t stages, int64_t nr, int64_t nc, int64_t tiles, int64_t spare, F&& f)
 {
-    for (int splits = 1; splits <= 16; ++splits) {
-        if (splits > 1 && stages / splits < 4) break;
-        if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, std::max<int64_t>(1, stages / 4))) continue;
+    const bool joins = nr * ((nc + 7) / 8) / 256 < MOST_WORKGROUPS / 2 - 1;
+    const int64_t most = joins ? std::max<int64_t>(1, std::min<int64_t>({16, stages / 4, 1 + spare / (2 * tiles)})) : 1;
+    for (int splits = 1; splits <= most; ++splits) {
+        if (g_force_splits > 0 && splits != std::min<int64_t>(g_force_splits, most)) continue;
         f(splits);
     }
 }
@@ -252,9 +259,10 @@ Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
     Cut best;
     double least = 0;
     each_shape(gated, any, [&](int shape) {
-        each_split(ceil_div(nk, 64), [&](int splits) {
+        const int64_t tiles = cut_as(shape, 1, nr, nc, 1, gated).tiles();
+        each_split(ceil_div(nk, 64), nr, nc, tiles, MOST_WORKGROUPS - 16 - tiles, [&](int splits) {
             const Cut c = cut_as(shape, splits, nr, nc, 1, gated);
-            const double t = fill_ns(shape, (int64_t)c.tiles_r * c.tiles_c * splits, (double)ceil_div(nk, 64) / splits, 0, 0) + join_ns(c.part_bytes);
+            const double t = fill_ns(shape, c.tiles() * splits, (double)ceil_div(nk, 64) / splits, 0, 0) + join_ns(c.part_bytes);
             if (least == 0 || t < least) { least = t; best = c; }
         });
     });
@@ -273,11 +281,13 @@ BackCut least_back(int64_t rows, int64_t in, int64_t out, int problems, bool any
     double least = 0;
     const int64_t stages_w = ceil_div(rows, 64), stages_x = (int64_t)ceil_div(out, 64) * problems;
     each_shape(false, any, [&](int shape) {
-        each_split(want_w ? stages_w : 1, [&](int sw) {
+        const int64_t tiles_w = cut_as(shape, 1, out, in, 1, false).tiles() * problems, tiles_x = cut_as(shape, 1, rows, in, 1, false).tiles();
+        const int64_t spare = MOST_WORKGROUPS - 16 - 2 * (int64_t)ceil_div(out, 64) - tiles_w - tiles_x;
+        each_split(want_w ? stages_w : 1, out * problems, in, tiles_w, spare, [&](int sw) {
             const Cut w = cut_as(shape, sw, out, in, problems, false);
-            each_split(want_x ? stages_x : 1, [&](int sx) {
+            each_split(want_x ? stages_x : 1, rows, in, tiles_x, spare, [&](int sx) {
                 const Cut x = cut_as(shape, sx, rows, in, 1, false);
-                const int64_t nw = want_w ? (int64_t)w.tiles_r * w.tiles_c * problems * sw : 0, nx = want_x ? (int64_t)x.tiles_r * x.tiles_c * sx : 0;
+                const int64_t nw = want_w ? w.tiles() * problems * sw : 0, nx = want_x ? x.tiles() * sx : 0;
                 const double lw = (double)stages_w / sw, lx = (double)stages_x / sx;
                 const bool x_first = lx > lw;
                 const double t = (x_first ? fill_ns(shape, nx, lx, nw, lw) : fill_ns(shape, nw, lw, nx, lx)) +
