@@ -305,12 +305,14 @@ dlf_status dlf_i8conv_run(const dlf_i8conv_t* layer, const void* in_dev, void* o
  * gradients dx [rows][in_features] and dweight, dw_gate, dw_up [out_features][in_features] are written with rows next to each other.
  * y (h) may be the residual itself (same address and stride); on any other operand it is refused, but columns of one matrix may lie
  * beside each other.  Other outputs must not overlap anything.
- * rows = 0 is valid: nothing to compute forward, zero weight and bias gradients backward. */
+ * rows = 0 is valid: nothing to compute forward, zero weight and bias gradients backward.  How many there may be is bounded by what a
+ * launch holds: with m, i, o = rows, in_features, out_features in 64s, rounded up, 2 m o and m i + 2 i o + 2 o have to stay below
+ * 2^24 - 16 (4096 -> 4096: 8.39 million rows; one feature: 2^29 - 576), else DLF_ERR_UNSUPPORTED. */
 typedef enum { DLF_F16 = 0, DLF_BF16 = 1 } dlf_dtype;
 typedef struct {
     int32_t dtype;              /* dlf_dtype                                                              */
     int32_t act;                /* dlf_act                                                                */
-    int64_t rows;               /* 0 .. 2^30                                                              */
+    int64_t rows;               /* 0 and more, see above                                                  */
     int32_t in_features;        /* 1 .. 2^20                                                              */
     int32_t out_features;       /* 1 .. 2^20 (gated: of either projection)                                */
     int64_t x_stride;           /* elements from row to row, >= the row, < 2^24; 0: the row               */

@@ -11,8 +11,9 @@ Automatic differentiation does not see the calls, so an operand that requires a 
 tangent is refused: call under torch.no_grad(), or inside a torch.autograd.Function's forward and backward, and take the gradients from
 `run_saved` and `backward`.
 
-Tensors are fp16 or bf16, all of one type, with rows of consecutive elements at any distance and alignment; biases and
-their gradients fp32.  Inputs may have any number of leading dimensions that lie at one row distance.
+Tensors are fp16 or bf16, all of one type, with rows of consecutive elements at any alignment and any distance below
+2^24 elements (of a single row it says nothing); biases and their gradients fp32.  Inputs may have any number of leading dimensions
+that lie at one row distance.
 """
 import torch
 
