@@ -294,8 +294,11 @@ dlf_status dlf_i8conv_run(const dlf_i8conv_t* layer, const void* in_dev, void* o
  *
  * (The activation comes before the residual, as in a transformer block; a network layer applies its own after it.)
  * Products and sums are accumulated in 32 bits and rounded once, to the tensors' type; in the backward pass dz (dg,
- * du) is rounded to that type on its way into the products, the bias gradients are summed before that.  An activation
- * with a step has the derivative 0 on it.  Results do not depend on timing: equal calls give equal bits.
+ * du) is rounded to that type on its way into the products, the bias gradients are summed before that.  Between two calls
+ * stands a tensor of that type: a block's h in front of its second product, dh in front of the first one's backward pass.
+ * Each of these roundings has the type's range as well: in fp16 what exceeds 65504 becomes infinite and what is below
+ * 2^-25 zero, where a computation in 32 bits throughout would go on (bf16 keeps the range of fp32); fp16 training scales its
+ * loss.  An activation with a step has the derivative 0 on it.  Results do not depend on timing: equal calls give equal bits.
  *
  * Tensors are DEVICE and row-major: x [rows][in_features], weight, w_gate, w_up [out_features][in_features], residual,
  * y, h, dy, dh [rows][out_features], of type `dtype`, a row's elements next to each other, rows as far apart as the

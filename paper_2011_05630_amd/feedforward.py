@@ -47,6 +47,8 @@ _GRADIENTS = ("x", "weight", "bias")
 
 def _wanted(need):
     """Which of _GRADIENTS `need` names, which is some of them, or one."""
+    if need is _GRADIENTS:
+        return True, True, True
     need = (need,) if isinstance(need, str) else tuple(need)
     for n in need:
         _need(n in _GRADIENTS, "need: some of %s expected, not %r", ", ".join(_GRADIENTS), n)
@@ -150,7 +152,8 @@ class GatedLinear(_Operator):
 
 
 class FeedForward:
-    """The block y = down(gated(x)) + residual: two kernels forward."""
+    """The block y = down(gated(x)) + residual: two kernels forward.  h, between the two products, and its gradient, between the two backward
+    calls, are tensors of the weights' type, with its rounding and its range (fp16: infinite above 65504, zero below 2^-25)."""
 
     def __init__(self, gated, down):
         _need(isinstance(gated, GatedLinear) and isinstance(down, Linear), "a GatedLinear and a Linear expected")
