@@ -155,12 +155,13 @@ dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
 {
     DlfFfFew c;
     c.rows = g_force != 1 && lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
-    // Rows per workgroup: 32 rather than 64 of them even where 64 exist (gated 64 x 2048 -> 2 x 5632: 16.6 against 18.4 us), there with
-    // 32 features for the reads of x (64 x 4096 -> 4096: 12.1 against 14.8 us; fewer workgroups lose below 33 rows).
+    // Rows per workgroup: 32 rather than 16 (the kernel, 64 rows 2048 -> 2 x 5632: 13.0 against 15.7 us, 4096 -> 4096 11.8 against 14.0), above 32
+    // rows with 32 features for the reads of x (64 x 4096 -> 4096 10.9 against 11.8, 48 x 2048 -> 32001 38 against 45; 32 x 4096 -> 4096 would
+    // lose, 10.5 against 8.4: fewer workgroups).
     c.mr = a.nr <= 16 ? 1 : 2;
     c.nf = gated || a.nr <= 32 ? 1 : 2;
-    // Waves that share k: eight while every workgroup has a compute unit to itself, else four (2001 of them: 24.3 against 24.7 us, 680
-    // gated: 31.8 against 35.9), and no more than there are stages of 64 k.
+    // Waves that share k: eight while every workgroup has a compute unit to itself (128 of them: 7.6 us, with four 9.2), else four (2001: 24.7,
+    // with eight 25.6; 680 gated: 32.1, with eight 36.6), and no more than there are stages of 64 k.
     const int64_t groups = (int64_t)((a.nc + 16 * c.nf - 1) / (16 * c.nf)) * ((a.nr + 16 * c.mr - 1) / (16 * c.mr));
     c.waves = groups <= 256 ? 8 : 4;
     while (c.waves > 1 && c.waves * 64 >= 2 * a.nk) c.waves >>= 1;

@@ -35,7 +35,7 @@ struct DlfFfDzArgs {
     const void* dy;
     int64_t lddy;
     const float* saved;     // null: dz = dy, only the sums are wanted
-    void* dz[2];            // rows of lddz elements, zeros behind column n
+    void* dz[2];            // rows of lddz elements, a multiple of eight, zeros behind column n
     int64_t lddz;
     int32_t rows, n, act;
     int32_t chunk;          // rows of one partial sum
@@ -69,8 +69,9 @@ static constexpr DlfFfShape DLF_FF_SHAPES[DLF_FF_NUM_SHAPES] = {{256, 256, 2}, {
 // Forward products of few rows: on k_ff_rows (operands of whole lines) or k_ff_few, 16 nf features x 16 mr rows (each 1 or 2) per workgroup.
 #define DLF_FF_FEW_ROWS 64
 struct DlfFfFew { int rows, nf, mr, waves; };
-// k_ff_rows: stages of 64 k that a wave holds in LDS (2: 16 x 5632 -> 2048 takes 10.4 us with 2, 3 and 4, 1 x 4096 -> 2 x 10880 gated 31.8, 31.3 and
-// 34.8 us, 16 x 2048 -> 2 x 5632 gated 12.5, 12.6 and 15.1: with more, fewer workgroups share a compute unit); LDS of a workgroup.
+// k_ff_rows: stages of 64 k that a wave holds in LDS (the kernel with 2, 3 and 4 of them: 16 x 5632 -> 2048 takes 7.2, 7.1 and 7.5 us, 1 x 4096 ->
+// 2 x 10880 gated 32.1, 31.5 and 35.4, 16 x 2048 -> 2 x 5632 gated 10.1, 11.1 and 12.9: with more, fewer workgroups share a compute unit, and
+// eight waves of 32 features and 32 rows would pass its LDS); LDS of a workgroup.
 #define DLF_FF_ROWS_RING 2
 #define DLF_FF_ROWS_LDS(WAVES, NF, MR, GATED) ((WAVES) * DLF_FF_ROWS_RING * (((GATED) ? 2 : (NF)) + (MR)) * 2048)
 

@@ -275,6 +275,8 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, int prob, int r,
 //     the LDS just read, half of it during the fourth step, half during the first of the next stage (over three steps the last requests
 //     came late: 8192^3 2 % slower; all in one 6 %).  The addresses of a stage are formed ahead of the barrier, not behind it (2 %).
 //     Stages of 32 k, four in LDS, wait less but read half lines: 4096^3 124 against 115 us.
+//   Through registers, 4096 x 4099 -> 4101 takes 248 us (0.56 PFLOP/s), 4096 x 4099 -> 2 x 10881 gated 1071 (0.68), 128 x 128 tiles both: loads of
+//     rows off their lines, a write to LDS and a barrier a stage.
 //   The epilogue goes through LDS, 64 rows of a wave at a time, so that stores are whole lines and the code of the activations is there
 //     once; a lane's loads for several rows go out together (one after the other they made the epilogue of 256 x 256 take 16 us).
 // Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, in bands of four rows of tiles, and its workgroups share operands
@@ -867,7 +869,8 @@ __device__ __forceinline__ void few_finish(const DlfFfArgs& a, const f4v (&acc)[
 // launch and one round trip to memory: nothing is staged, every wave reads its operands from memory straight into the registers
 // that v_mfma_f32_16x16x32 takes them from.  A workgroup computes 16 NF features (gated: 16 of both projections) for 16 MR rows, its waves
 // share k in equal runs of 32-wide steps and meet in LDS, in a fixed order.  A wave keeps D steps requested.  Rows that do not exist are
-// read as the last that does and not stored; a last step that is not whole is the last wave's, requested first.
+// read as the last that does and not stored; a last step that is not whole is the last wave's, requested first.  On the operands of
+// k_ff_rows, whose figures are below: 5 x 2048 -> 32001 27.0 us, 1 x 4096 -> 2 x 10880 35.4, 16 x 2048 -> 2 x 5632 14.2, 64 x 4096 -> 4096 17.9.
 // ------------------------------------------------------------------------------------------------
 template <typename T, int NF, int MR, bool GATED>
 __global__ __launch_bounds__(512, (GATED ? 2 : NF) + MR <= 3 ? 4 : 2) void k_ff_few(const DlfFfArgs a)
@@ -950,8 +953,9 @@ __global__ __launch_bounds__(512, (GATED ? 2 : NF) + MR <= 3 ? 4 : 2) void k_ff_
 // k_ff_rows: k_ff_few for operands whose rows are whole 16-byte lines.  There a wave's load takes 64 bytes of each of 16 rows, and pieces
 // of many lines cost a compute unit several times their size; here the operands come as whole 128-byte lines, eight rows per
 // instruction, into a ring in LDS that belongs to the wave alone: 64 k ("stage") of its features and rows at a time, D stages
-// requested ahead, no barrier before the waves meet.  LDS holds a stage as k_ff_tile does.  5 x 2048 -> 32001 takes 24.4 us (5.4 TB/s
-// of weights), 1 x 4096 -> 2 x 10880 32 us (5.6), 16 x 2048 -> 2 x 5632 10.5 (4.4), 1 x 1024 -> 1024 3.9 (a launch and a round trip).
+// requested ahead, no barrier before the waves meet.  LDS holds a stage as k_ff_tile does.  5 x 2048 -> 32001 takes 24.6 us (5.3 TB/s
+// of weights), 1 x 4096 -> 2 x 10880 32 us (5.6), 16 x 2048 -> 2 x 5632 10.1 (4.6), 1 x 1024 -> 1024 3.8 (a launch and a round trip); more rows
+// read x oftener: 64 x 2048 -> 2 x 5632 13.0, 64 x 4096 -> 4096 10.9 (3.1).
 // ------------------------------------------------------------------------------------------------
 template <typename T, int NF, int MR, bool GATED>
 __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
@@ -1026,8 +1030,9 @@ __global__ __launch_bounds__(512) void k_ff_rows(const DlfFfArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // k_ff_dz: the gradient behind the activation, and column sums of it in 32 bits (before it is rounded).  Bound by memory: 8 bytes an
-// element, gated 14 (4096 x 2048: 14 us, 4.8 TB/s; gated 4096 x 5632: 67 us, 4.8 TB/s, what a large copy reaches).  A workgroup takes `chunk` rows of 256 columns: 32 threads by eight columns, eight rows at a time; their
-// sums meet in LDS, in a fixed order, and k_ff_back adds up what the chunks leave.
+// element, gated 14 (4096 x 2048: 14 us, 4.8 TB/s; gated 4096 x 5632: 67 us, 4.8 TB/s, what a large copy reaches).  A workgroup takes `chunk`
+// rows of 256 columns: 32 threads by eight columns, eight rows at a time; their sums meet in LDS, in a fixed order, and k_ff_back adds up
+// what the chunks leave.  (At most 64 chunks: up to 512 columns leave half the compute units idle.)
 // ------------------------------------------------------------------------------------------------
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
@@ -1066,7 +1071,9 @@ __global__ __launch_bounds__(256) void k_ff_dz(const DlfFfDzArgs a)
                         }
                     }
                 });
-                // rows of dz are whole eights: what lies behind column n is read as zeros by the products
+                // One rounding to the tensors' type, which the matrix units multiply: gradients are off by 0.0023 of their norm
+                // against 0.0017 with dz in 32 bits (bf16; fp16 0.00029 against 0.00021, and its range).  Rows of dz are whole eights, zeros behind
+                // column n, so that a thread's eight are one store.
 #pragma unroll
                 for (int z2 = 0; z2 < NZ; ++z2) {
                     if (n < 8) {
