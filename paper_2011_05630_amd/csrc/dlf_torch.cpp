@@ -114,7 +114,7 @@ public:
             if (st == nullptr || st->scalar_type() != at::kFloat || st->device() != device_ || !readable(*st) || !st->is_contiguous() ||
                 !(gated_ ? st->sizes().equals({2, xr.rows, out_}) : st->sizes().equals({xr.rows, out_})))
                 refuse("saved: the tensor that the forward call returned, fp32 [", gated_ ? "2, " : "", xr.rows, ", ", out_, "], expected");
-            undifferentiated(*st, "saved");
+            usable(*st, "saved");
             sp = st->data_ptr<float>();
         }
         const c10::DeviceGuard guard(device_);
@@ -169,27 +169,33 @@ private:
             if (b.defined() && !(b.scalar_type() == at::kFloat && b.device() == device_ && readable(b) && b.dim() == 1 && b.size(0) == out_ &&
                                  b.is_contiguous()))
                 refuse(bn, ": no longer the contiguous fp32 tensor of ", out_, " elements on ", device_, " that the operator was made of: make another");
-            undifferentiated(w, wn);
-            if (b.defined()) undifferentiated(b, bn);
+            usable(w, wn);
+            if (b.defined()) usable(b, bn);
         }
     }
     // Memory that holds the elements as they are (a view may leave their negation to the reader).
     static bool readable(const at::Tensor& t) { return t.layout() == at::kStrided && !t.is_neg(); }
-    // Automatic differentiation does not see the calls: what it would have to follow is refused rather than dropped.
-    static void undifferentiated(const at::Tensor& t, const char* name)
+    static void usable(const at::Tensor& t, const char* name)
     {
+        // Automatic differentiation does not see the calls: what it would have to follow is refused rather than dropped.
         if (t.requires_grad() && c10::AutogradState::get_tls_state().get_grad_mode())
             refuse(name, ": requires a gradient, which automatic differentiation cannot take through this operator: call it under torch.no_grad(), "
                          "gradients come from run_saved and backward");
         if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
             refuse(name, ": carries a tangent, which this operator cannot pass on");
+        // A storage may be freed or shortened under its tensors.
+        if (t.numel() > 0) {
+            int64_t last = t.storage_offset();
+            for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
+            if ((size_t)(last + 1) * t.itemsize() > t.storage().nbytes()) refuse(name, ": its storage no longer holds it");
+        }
     }
     const at::Tensor& tensor(py::handle h, int64_t width, const char* name) const
     {
         if (THPVariable_Check(h.ptr())) {
             const at::Tensor& t = THPVariable_Unpack(h.ptr());
             if (t.scalar_type() == type_ && t.device() == device_ && readable(t) && t.dim() >= 1 && t.size(-1) == width) {
-                undifferentiated(t, name);
+                usable(t, name);
                 return t;
             }
         }

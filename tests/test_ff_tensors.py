@@ -234,3 +234,25 @@ def test_pending_negations_are_refused():
     with pytest.raises(ValueError, match="^x: "):
         op.forward(column, None, None, False, 0)
     op.forward(column.resolve_neg(), None, None, False, 0)
+
+
+@pytest.mark.parametrize("gated,name", NAMES)
+def test_storage_that_was_taken_away_is_refused(gated, name):
+    """A freed or shortened storage leaves a tensor its sizes: behind an offset its address is not even null."""
+    w, b = operands(gated)
+    dy = "dh" if gated else "dy"
+    all_of = dict(w, **b, x=torch.zeros(5, K, dtype=torch.bfloat16), saved=torch.zeros(2, 5, N) if gated else torch.zeros(5, N),
+                  **{n: torch.zeros(5, N, dtype=torch.bfloat16) for n in ("residual", "out", "dy", "dh")})
+    usual = all_of[name]
+    for left in (0, 16, (2 * usual.numel() - 1) * usual.itemsize):
+        buf = torch.zeros(2 * usual.numel(), dtype=usual.dtype)
+        t = buf[usual.numel():].view(usual.shape)
+        kw = dict(all_of, **{name: t})
+        op = native(gated, {n: kw[n] for n in w}, {n: kw[n] for n in b})
+        buf.untyped_storage().resize_(left)
+        if name not in ("saved", dy):
+            with pytest.raises(ValueError, match="^%s: .*storage" % name):
+                op.forward(kw["x"], kw["residual"] if name == "residual" else None, kw["out"] if name == "out" else None, True, 0)
+        if name not in ("residual", "out"):
+            with pytest.raises(ValueError, match="^%s: .*storage" % name):
+                op.backward(kw[dy], kw["x"], kw["saved"], True, True, True, 0)
