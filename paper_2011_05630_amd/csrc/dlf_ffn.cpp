@@ -132,13 +132,19 @@ dlf_status launched(const Ff& f, int e)
 // Testing hook: 0 = by rule, 1 = k_ff_few wherever a few-rows kernel applies, 2 + shape = a tile kernel wherever it applies.
 int g_force = 0;
 
-std::once_flag g_once;
-int g_once_rc = 0;
+// A kernel's attributes belong to the device that it is set up on: once for each that calls run on.
+constexpr int MOST_DEVICES = 64;
+std::once_flag g_once[MOST_DEVICES];
+int g_once_rc[MOST_DEVICES];
 
 dlf_status kernels_ready()
 {
-    std::call_once(g_once, [] { g_once_rc = dlf_ff_kernels_init(); });
-    if (g_once_rc != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc));
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return fail(DLF_ERR_HIP, "no device: %s", hipGetErrorString(e));
+    if (device < 0 || device >= MOST_DEVICES) return fail(DLF_ERR_UNSUPPORTED, "device %d", device);
+    std::call_once(g_once[device], [device] { g_once_rc[device] = dlf_ff_kernels_init(); });
+    if (g_once_rc[device] != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc[device]));
     return DLF_OK;
 }
 

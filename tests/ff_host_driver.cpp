@@ -1,5 +1,8 @@
 // The host side of the feed-forward operators (csrc/dlf_ffn.cpp) with stand-ins for the launchers: random calls on addresses that nobody
-// reads, each launch checked against what its kernels assume.  Usage: ff_host_driver <seed> <calls>; prints what it saw, or the first fault.
+// reads, each launch checked against what its kernels assume.  Usage: ff_host_driver <seed> <calls> | devices;
+// prints what it saw, or the first fault.
+#include <hip/hip_runtime.h>
+
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -9,6 +12,14 @@
 
 #include "../include/dlf_debug.h"
 #include "../paper_2011_05630_amd/csrc/dlf_ffn.h"
+
+// The devices of a machine with eight; the library's kernels are set up once on each that it runs on.
+static int g_device = 0, g_setups[8], g_broken = -1;
+extern "C" hipError_t hipGetDevice(int* d)
+{
+    *d = g_device;
+    return hipSuccess;
+}
 
 static char g_error[512];
 dlf_status dlf_set_error(dlf_status s, const char* msg)
@@ -83,7 +94,11 @@ static int64_t tiles(const DlfFfArgs& a, int shape, bool gated, bool pt, bool qt
 }
 
 extern "C" {
-int dlf_ff_kernels_init(void) { return 0; }
+int dlf_ff_kernels_init(void)
+{
+    ++g_setups[g_device];
+    return g_device == g_broken ? hipErrorInvalidValue : 0;
+}
 int dlf_ff_start_tile(const DlfFfArgs* a, int shape, int, int gated, void*)
 {
     ++g.launches;
@@ -167,8 +182,26 @@ static void* place(double bytes)
     return (void*)p;
 }
 
+static int devices()
+{
+    dlf_ff_desc d;
+    memset(&d, 0, sizeof d);
+    d.rows = 3;
+    d.in_features = d.out_features = 16;
+    void *x = (void*)0x100000, *w = (void*)0x200000, *y = (void*)0x300000;
+    g_broken = 5;
+    for (int turn = 0; turn < 3; ++turn)
+        for (g_device = 0; g_device < 8; ++g_device)
+            if ((dlf_linear(&d, x, w, nullptr, nullptr, y, nullptr, nullptr, 0, nullptr) == DLF_OK) != (g_device != g_broken)) return 1;
+    printf("setups");
+    for (int n : g_setups) printf(" %d", n);
+    printf("\n");
+    return 0;
+}
+
 int main(int argc, char** argv)
 {
+    if (argc > 1 && strcmp(argv[1], "devices") == 0) return devices();
     rng.seed(argc > 1 ? strtoull(argv[1], nullptr, 10) : 1);
     const int calls = argc > 2 ? atoi(argv[2]) : 1000;
     int status[16] = {0}, most = 0;

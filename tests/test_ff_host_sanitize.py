@@ -42,3 +42,10 @@ def test_random_calls(driver, seed):
     m = re.match(r"calls 60000 ok (\d+) invalid (\d+) unsupported (\d+) split (\d+) seen ([\d ]+)$", r.stdout.strip())
     assert m and int(m.group(1)) > 50000 and int(m.group(3)) > 0 and int(m.group(4)) > 1000
     assert all(int(n) > 100 for n in m.group(5).split())          # every shape, both few-rows kernels, the pass before the products
+
+
+def test_kernels_are_set_up_on_every_device(driver):
+    """Once each, on the calls' first use of it; a device that fails stays refused, the others run."""
+    r = subprocess.run([driver, "devices"], stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout + r.stderr[-3000:]
+    assert r.stdout.strip() == "setups" + " 1" * 8
