@@ -254,7 +254,7 @@ def _to_8_bits(x, scale, noise, mantissa, low, kept):
     r = (noise << cut - 16) + (1 << cut - 17)
     code = (torch.where(small, y + 2.0 ** low, y).view(torch.int32).long() + r >> cut) - first + torch.where(small, 0, 1 << mantissa)
     if kept:
-        code = torch.where(y > 0, code.clamp_min(1), code)
+        code = torch.where(x > 0, code.clamp_min(1), code)
     code = torch.where(torch.isfinite(x), code, 0x7F)
     return torch.where(x.view(torch.int32) < 0, code + 128, code).to(torch.uint8)
 
