@@ -311,7 +311,7 @@ dlf_status dlf_i8conv_run(const dlf_i8conv_t* layer, const void* in_dev, void* o
  * rows = 0 is valid: nothing to compute forward, zero weight and bias gradients backward.  How many there may be is bounded by what a
  * launch holds: with m, i, o = rows, in_features, out_features in 64s, rounded up, 2 m o and m i + 2 i o + 2 o have to stay below
  * 2^24 - 16 (4096 -> 4096: 8.39 million rows; one feature: 2^29 - 576), else DLF_ERR_UNSUPPORTED. */
-typedef enum { DLF_F16 = 0, DLF_BF16 = 1 } dlf_dtype;
+typedef enum { DLF_F16 = 0, DLF_BF16 = 1, DLF_F32 = 2 /* the optimizer's operators only */ } dlf_dtype;
 typedef struct {
     int32_t dtype;              /* dlf_dtype                                                              */
     int32_t act;                /* dlf_act                                                                */
@@ -342,6 +342,113 @@ dlf_status dlf_gated(const dlf_ff_desc* d, const void* x, const void* w_gate, co
 dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* x, const void* w_gate, const void* w_up, const float* saved,
                               void* dx, void* dw_gate, void* dw_up, float* db_gate, float* db_up, void* workspace, size_t workspace_bytes,
                               void* hip_stream);
+
+/* ---- Cross entropy of a linear layer ----------------------------------------------------------
+ * The loss at the end of a stack of blocks over a large number of classes (a vocabulary), without its logits in memory:
+ *
+ *   z[r][c] = sum over i of x[r][i] * weight[c][i] + bias[c]      lse[r] = log sum over c of exp(z[r][c])
+ *   loss[r] = lse[r] - z[r][target[r]]                            0 where target[r] == ignore
+ *   dz[r][c] = (dloss[r] + dlse[r]) * exp(z[r][c] - lse[r]) - dloss[r] * (c == target[r])      dloss counts as 0 where target[r] == ignore
+ *   dx = dz weight;  dweight = dz^T x;  dbias[c] = sum over r of dz[r][c]
+ *
+ * dlf_cross_entropy            loss, and lse if wanted
+ * dlf_cross_entropy_backward   the gradients for those of loss and lse; the logits are computed again
+ * dlf_cross_entropy_gradients  loss and gradients in one call (dlse = 0), for a program that knows dloss beforehand (1 / rows, a loss scale):
+ *                              a quarter of the operations less than the other two
+ *
+ * A target that is neither a class nor `ignore` gives a loss and gradients of NaN.  A class whose bias is -infinity takes no part; if none does,
+ * lse is -infinity and the loss NaN.  All sums, exponentials and logarithms are held in 32 bits.  The gradients take rows in pieces: a
+ * piece's dz stays in the workspace, in at most `piece_bytes` (but for 256 rows at least), in the tensors' type, which the matrix units
+ * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14, so that a mean over many rows does not vanish,
+ * and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
+ * dlf_cross_entropy_gradients, where no dbias is wanted, keeps exp(z - a maximum) in 16 bits (fp16) in between rather than computing the logits again.
+ * Nothing depends on timing: equal calls give equal bits.
+ *
+ * Tensors are DEVICE and row-major: x [rows][in_features], weight [classes][in_features], of type `dtype`, a row's elements next to
+ * each other, rows as far apart as the strides say (0: next to each other), any 2-byte aligned address; bias, dbias fp32 [classes]; target
+ * int64 [rows]; loss, lse fp32 [rows]; dloss, dlse fp32, row r's at r * their stride (0: one for all rows), dloss NULL: dloss_value for
+ * all rows, dlse NULL: none.  dx [rows][in_features], dweight [classes][in_features] with rows next to each other.  Outputs must
+ * not overlap anything.  rows = 0 is valid: zero gradients of weight and bias.  With i, o = in_features, classes in 64s, rounded up, 2 i o + 2 o + 4 i
+ * has to stay below 2^24 - 16, else DLF_ERR_UNSUPPORTED. */
+typedef struct {
+    int32_t dtype;              /* DLF_F16 or DLF_BF16                                                    */
+    int32_t in_features;        /* 1 .. 2^20                                                              */
+    int64_t rows;               /* 0 .. 2^30                                                              */
+    int32_t classes;            /* 1 .. 2^20                                                              */
+    int32_t reserved;           /* 0                                                                      */
+    int64_t ignore;             /* the target of a row that counts for nothing                            */
+    int64_t x_stride;           /* elements from row to row, >= the row, < 2^24; 0: the row               */
+    int64_t w_stride;           /* ... of weight                                                          */
+    int64_t piece_bytes;        /* what dz may take, 0: 2^30                                              */
+} dlf_ce_desc;
+/* Bytes of workspace (DEVICE, 256-byte aligned, used by one call at a time); SIZE_MAX for a description that the calls refuse. */
+size_t dlf_cross_entropy_workspace_bytes(const dlf_ce_desc* d);
+size_t dlf_cross_entropy_backward_workspace_bytes(const dlf_ce_desc* d);
+size_t dlf_cross_entropy_gradients_workspace_bytes(const dlf_ce_desc* d);
+/* Asynchronous on hip_stream; they allocate nothing and record only kernel launches.  bias and lse (of the first) may be NULL; a gradient whose
+ * pointer is NULL is not computed. */
+dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target, float* loss,
+                             float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+dlf_status dlf_cross_entropy_backward(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target,
+                                      const float* lse, const float* dloss, int64_t dloss_stride, float dloss_value, const float* dlse,
+                                      int64_t dlse_stride, void* dx, void* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                                      void* hip_stream);
+dlf_status dlf_cross_entropy_gradients(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target,
+                                       const float* dloss, int64_t dloss_stride, float dloss_value, float* loss, void* dx, void* dweight,
+                                       float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Optimizer: many tensors at once ----------------------------------------------------------
+ * dlf_gradient_norm    norm = |scale| * sqrt(sum of g^2 over all elements of all tensors), summed in 64 bits in a fixed order;
+ *                      factor = scale, times most / norm where norm > most; NaN where norm is not finite (in 32 bits)
+ * dlf_adamw_step       t = steps done + 1, g = factor * gradient (factor: one fp32 on the device, or NULL: 1)
+ *                      m' = b1 m + (1 - b1) g;  v' = b2 v + (1 - b2) g g
+ *                      p' = p (1 - rate decay) - rate m' / (1 - b1^t) / (sqrt(v' / (1 - b2^t)) + eps);  copy = p' rounded to its type
+ *                      a factor that is not finite leaves everything as it is, the count of steps too
+ *
+ * Gradients, parameters fp16, bf16 or fp32, copies fp16 or bf16 beside fp32 parameters; any mixture, each tensor's elements next to each
+ * other, at any address its type is aligned to, of any number of elements, 0 among them.  All is computed in 32 bits; m' and v' by single roundings in
+ * the order written ((1 - b2) g first, then times g).  A parameter is rounded to its type once, a copy from the parameter in 32 bits.
+ *
+ * States lie in arrays over all tensors: tensor i's begin at the sum of the sizes in front of it, each rounded up to DLF_ADAMW_BLOCK.
+ * What lies behind a tensor's last element up to the next block has to be zero and stays so.  DLF_ADAMW_FP32: m, v fp32.  DLF_ADAMW_8BIT: a byte each, m as e4m3 (OCP, largest 448), v as
+ * e5m2 (largest 57344), times their block's scale, fp32: the least power of two from 2^-110 on by which the block's largest finite value comes to
+ * at most 448 (57344).  What is stored is rounded up as often as what is missing says, by 16 bits of a hash of seed, step and place in the
+ * array, down otherwise, to a multiple of the type's last place; a v above zero stays above zero; what is not finite becomes the NaN 0x7f, in its place alone.  The update itself uses m' and v' as
+ * they are before that.  All arrays 16-byte aligned.  counter: four doubles, 8-byte aligned: steps done, b1 and b2 to their power, 0: it starts as
+ * {0, 1, 1, 0}.  A step's launches may be captured; steps on the same arrays have to follow each other.
+ *
+ * dlf_adamw_table fills a HOST buffer that the caller copies to the device (16-byte aligned there) and keeps for all steps: it holds the tensors' addresses and sizes. */
+#define DLF_ADAMW_BLOCK 64
+typedef enum { DLF_ADAMW_FP32 = 0, DLF_ADAMW_8BIT = 1 } dlf_adamw_state;
+typedef struct {
+    void* param;
+    void* copy;                 /* or NULL                                                                */
+    int64_t count;              /* elements, 0 .. 2^40, of all tensors at most 2^42                       */
+    int32_t param_dtype;        /* dlf_dtype                                                              */
+    int32_t copy_dtype;         /* DLF_F16 or DLF_BF16                                                    */
+    float decay;
+    int32_t reserved;           /* 0                                                                      */
+} dlf_adamw_tensor;
+typedef struct {
+    double beta1, beta2;        /* 0 <= and < 1                                                           */
+    float eps;                  /* >= 0                                                                   */
+    uint32_t seed;
+    int32_t state;              /* dlf_adamw_state                                                        */
+    int32_t reserved;           /* 0                                                                      */
+} dlf_adamw_desc;
+/* Elements of the state arrays (scales: a DLF_ADAMW_BLOCK-th), bytes of the table; SIZE_MAX for tensors that the calls refuse. */
+size_t dlf_adamw_state_elements(const dlf_adamw_tensor* tensors, int32_t n);
+size_t dlf_adamw_table_bytes(const dlf_adamw_tensor* tensors, int32_t n);
+dlf_status dlf_adamw_table(const dlf_adamw_tensor* tensors, int32_t n, void* host_table, size_t bytes);
+/* gradients, gradient_dtypes: HOST arrays of n device addresses (NULL: that tensor is left as it is) and dlf_dtypes.  table: on the device, as dlf_adamw_table
+ * filled it for the same tensors.  rate_at: one fp32 on the device, or NULL: rate.  m_scale, v_scale: NULL with states in 32 bits. */
+dlf_status dlf_adamw_step(const dlf_adamw_desc* d, const dlf_adamw_tensor* tensors, int32_t n, const void* table, const void* const* gradients,
+                          const int32_t* gradient_dtypes, void* m, void* v, float* m_scale, float* v_scale, double* counter, float rate,
+                          const float* rate_at, const float* factor, void* hip_stream);
+/* counts, dtypes, gradients: HOST arrays of n.  norm, factor (may be NULL): one fp32 each on the device. */
+size_t dlf_gradient_norm_workspace_bytes(const int64_t* counts, int32_t n);
+dlf_status dlf_gradient_norm(const void* const* gradients, const int64_t* counts, const int32_t* dtypes, int32_t n, float most, float scale,
+                             float* norm, float* factor, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 const char* dlf_status_string(dlf_status s);
 const char* dlf_last_error(void);

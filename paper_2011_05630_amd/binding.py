@@ -17,6 +17,9 @@ ACT = {"none": 0, "relu": 1, "relu6": 2}
 # ... of the feed-forward operators
 FF_ACT = dict(ACT, gelu=3, gelu_tanh=4, silu=5, sigmoid=6)
 DTYPE = {"fp16": 0, "bf16": 1}
+# ... of the optimizer's operators, and what they keep their states in
+OPT_DTYPE = dict(DTYPE, fp32=2)
+ADAMW_STATE = {"fp32": 0, "8bit": 1}
 TUNER_DP, TUNER_GREEDY, TUNER_MANUAL, TUNER_LAYERWISE, TUNER_MAXFUSE = 0, 1, 2, 3, 4
 DLF_OK = 0
 DLF_ERR_INVALID_ARG = 1
@@ -58,6 +61,23 @@ class FfDesc(ctypes.Structure):
                 ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
                 ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
                 ("res_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
+
+
+class CeDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("in_features", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("classes", ctypes.c_int32), ("reserved", ctypes.c_int32), ("ignore", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("piece_bytes", ctypes.c_int64)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("param_dtype", ctypes.c_int32), ("copy_dtype", ctypes.c_int32), ("decay", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_float),
+                ("seed", ctypes.c_uint32), ("state", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -165,6 +185,26 @@ def lib():
         f = getattr(L, name + "_workspace_bytes")
         f.argtypes = [ffp]
         f.restype = sz
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    for name, args in (("", [vp] * 6), ("_backward", [vp] * 6 + [i64, f32, vp, i64, vp, vp, vp]), ("_gradients", [vp] * 5 + [i64, f32] + [vp] * 4)):
+        f = getattr(L, "dlf_cross_entropy" + name)
+        f.argtypes = [ctypes.POINTER(CeDesc)] + args + [vp, sz, vp]
+        f.restype = i32
+        f = getattr(L, "dlf_cross_entropy" + name + "_workspace_bytes")
+        f.argtypes = [ctypes.POINTER(CeDesc)]
+        f.restype = sz
+    atp, vpp = ctypes.POINTER(AdamwTensor), ctypes.POINTER(vp)
+    for name in ("dlf_adamw_state_elements", "dlf_adamw_table_bytes"):
+        getattr(L, name).argtypes = [atp, i32]
+        getattr(L, name).restype = sz
+    L.dlf_adamw_table.argtypes = [atp, i32, vp, sz]
+    L.dlf_adamw_table.restype = i32
+    L.dlf_adamw_step.argtypes = [ctypes.POINTER(AdamwDesc), atp, i32, vp, vpp, i32p] + [vp] * 5 + [f32, vp, vp, vp]
+    L.dlf_adamw_step.restype = i32
+    L.dlf_gradient_norm_workspace_bytes.argtypes = [ctypes.POINTER(i64), i32]
+    L.dlf_gradient_norm_workspace_bytes.restype = sz
+    L.dlf_gradient_norm.argtypes = [vpp, ctypes.POINTER(i64), i32p, i32, f32, f32, vp, vp, vp, sz, vp]
+    L.dlf_gradient_norm.restype = i32
     _lib = L
     return L
 
@@ -377,11 +417,14 @@ def dlf_ff_desc(dtype, act, rows, in_features, out_features, x_stride=0, w_strid
     return FfDesc(DTYPE[dtype], FF_ACT[act], rows, in_features, out_features, x_stride, w_stride, y_stride, res_stride, dy_stride)
 
 
-def _ff_workspace(name, desc):
-    n = getattr(lib(), name + "_workspace_bytes")(desc)
+def _size(n):
     if n == ctypes.c_size_t(-1).value:
         raise DlfError(DLF_ERR_INVALID_ARG, lib().dlf_last_error().decode())
     return n
+
+
+def _ff_workspace(name, desc):
+    return _size(getattr(lib(), name + "_workspace_bytes")(desc))
 
 
 def dlf_linear_workspace_bytes(desc):
@@ -417,6 +460,84 @@ def dlf_gated_backward(desc, dh, x, w_gate, w_up, saved, dx, dw_gate, dw_up, db_
                        stream=None):
     _check(lib().dlf_gated_backward(desc, dh, x, w_gate, w_up, saved, dx, dw_gate, dw_up, db_gate, db_up, workspace, workspace_bytes,
                                     stream))
+
+
+def dlf_ce_desc(dtype, rows, in_features, classes, ignore=-100, x_stride=0, w_stride=0, piece_bytes=0):
+    """The description of a cross entropy call; dtype: "fp16" or "bf16", strides in elements (0: rows next to each other)."""
+    return CeDesc(DTYPE[dtype], in_features, rows, classes, 0, ignore, x_stride, w_stride, piece_bytes)
+
+
+def dlf_cross_entropy_workspace_bytes(desc):
+    return _ff_workspace("dlf_cross_entropy", desc)
+
+
+def dlf_cross_entropy_backward_workspace_bytes(desc):
+    return _ff_workspace("dlf_cross_entropy_backward", desc)
+
+
+def dlf_cross_entropy_gradients_workspace_bytes(desc):
+    return _ff_workspace("dlf_cross_entropy_gradients", desc)
+
+
+def dlf_cross_entropy(desc, x, weight, bias, target, loss, lse=None, workspace=None, workspace_bytes=0, stream=None):
+    """Device addresses (int or None)."""
+    _check(lib().dlf_cross_entropy(desc, x, weight, bias, target, loss, lse, workspace, workspace_bytes, stream))
+
+
+def dlf_cross_entropy_backward(desc, x, weight, bias, target, lse, dloss, dloss_stride, dloss_value, dlse, dlse_stride, dx, dweight, dbias,
+                               workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().dlf_cross_entropy_backward(desc, x, weight, bias, target, lse, dloss, dloss_stride, dloss_value, dlse, dlse_stride, dx, dweight,
+                                            dbias, workspace, workspace_bytes, stream))
+
+
+def dlf_cross_entropy_gradients(desc, x, weight, bias, target, dloss, dloss_stride, dloss_value, loss, dx, dweight, dbias, workspace=None,
+                                workspace_bytes=0, stream=None):
+    _check(lib().dlf_cross_entropy_gradients(desc, x, weight, bias, target, dloss, dloss_stride, dloss_value, loss, dx, dweight, dbias,
+                                             workspace, workspace_bytes, stream))
+
+
+def dlf_adamw_tensors(tensors):
+    """tensors: (parameter's address, copy's address or None, elements, dtype, copy's dtype or None, decay) each, dtypes: keys of OPT_DTYPE."""
+    a = (AdamwTensor * max(1, len(tensors)))()
+    for i, (p, c, n, t, ct, decay) in enumerate(tensors):
+        a[i] = AdamwTensor(p, c, n, OPT_DTYPE[t], OPT_DTYPE[ct] if ct else 0, decay, 0)
+    return a
+
+
+def dlf_adamw_desc(betas=(0.9, 0.95), eps=1e-8, seed=0, state="fp32"):
+    return AdamwDesc(betas[0], betas[1], eps, seed, ADAMW_STATE[state], 0)
+
+
+def dlf_adamw_state_elements(tensors, n):
+    return _size(lib().dlf_adamw_state_elements(tensors, n))
+
+
+def dlf_adamw_table_bytes(tensors, n):
+    return _size(lib().dlf_adamw_table_bytes(tensors, n))
+
+
+def dlf_adamw_table(tensors, n, host_table, bytes):
+    """host_table: the address of host memory."""
+    _check(lib().dlf_adamw_table(tensors, n, host_table, bytes))
+
+
+def dlf_adamw_step(desc, tensors, n, table, gradients, gradient_dtypes, m, v, m_scale, v_scale, counter, rate, rate_at=None, factor=None,
+                   stream=None):
+    """gradients: device addresses (int or None), gradient_dtypes: keys of OPT_DTYPE."""
+    k = max(1, n)
+    _check(lib().dlf_adamw_step(desc, tensors, n, table, (ctypes.c_void_p * k)(*gradients), (ctypes.c_int32 * k)(*(OPT_DTYPE[t] for t in gradient_dtypes)),
+                                m, v, m_scale, v_scale, counter, rate, rate_at, factor, stream))
+
+
+def dlf_gradient_norm_workspace_bytes(counts):
+    return _size(lib().dlf_gradient_norm_workspace_bytes((ctypes.c_int64 * max(1, len(counts)))(*counts), len(counts)))
+
+
+def dlf_gradient_norm(gradients, counts, dtypes, most, scale, norm, factor=None, workspace=None, workspace_bytes=0, stream=None):
+    n = len(counts)
+    k = max(1, n)
+    _check(lib().dlf_gradient_norm((ctypes.c_void_p * k)(*gradients), (ctypes.c_int64 * k)(*counts), (ctypes.c_int32 * k)(*(OPT_DTYPE[t] for t in dtypes)), n,
+                                   most, scale, norm, factor, workspace, workspace_bytes, stream))
 
 
 def dlf_cost_model_version():

@@ -5,13 +5,14 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdlf.so")
-SOURCES = ["dlf_kernels.hip", "dlf_host.cpp", "dlf_ffn.hip", "dlf_ffn.cpp"]
-HEADERS = ["dlf_internal.h", "dlf_ffn.h", os.path.join("..", "..", "include", "dlf.h"),
+SOURCES = ["dlf_kernels.hip", "dlf_host.cpp", "dlf_ffn.hip", "dlf_ffn.cpp", "dlf_ce.hip", "dlf_ce.cpp", "dlf_opt.hip", "dlf_opt.cpp"]
+HEADERS = ["dlf_internal.h", "dlf_ffn.h", "dlf_ff_plan.h", "dlf_tile.h", "dlf_ce.h", "dlf_opt.h", os.path.join("..", "..", "include", "dlf.h"),
            os.path.join("..", "..", "include", "dlf_debug.h")]
 
 
-# The feed-forward operators on PyTorch's tensors; links against libdlf.so beside it and the libraries of the PyTorch it is built with.
+# The operators on PyTorch's tensors; they link against libdlf.so beside them and the libraries of the PyTorch they are built with.
 TORCH_SOURCE = "dlf_torch.cpp"
+TORCH_PARTS = ["dlf_torch_loss.cpp", "dlf_torch_opt.cpp"]
 TORCH_LIB = os.path.join(HERE, "_dlf_torch.so")
 
 
@@ -31,7 +32,7 @@ def _built_with():
 
 def needs_build_torch():
     """Missing, older than its sources, or built with another PyTorch than the one installed (it names its own)."""
-    if not os.path.exists(TORCH_LIB) or _older(TORCH_LIB, [TORCH_SOURCE, os.path.join("..", "..", "include", "dlf.h")]):
+    if not os.path.exists(TORCH_LIB) or _older(TORCH_LIB, [TORCH_SOURCE] + TORCH_PARTS + ["dlf_torch.h", os.path.join("..", "..", "include", "dlf.h")]):
         return True
     with open(TORCH_LIB, "rb") as f:
         return _built_with().encode() not in f.read()
@@ -55,7 +56,7 @@ def build_torch():
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            '-DDLF_BUILT_WITH="%s"' % _built_with(), "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
     cmd += ["-I" + p for p in ext.include_paths() + [sysconfig.get_paths()["include"]]]
-    cmd += ["-o", tmp, os.path.join(CSRC, TORCH_SOURCE), "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+    cmd += ["-o", tmp] + [os.path.join(CSRC, s) for s in [TORCH_SOURCE] + TORCH_PARTS] + ["-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
     for p in ext.library_paths():
         cmd += ["-L" + p, "-Wl,-rpath," + p]
     _run(cmd + ["-lc10", "-ltorch_cpu", "-ltorch_python"], TORCH_LIB, tmp)

@@ -1,0 +1,415 @@
+// Host side of the cross entropy of a linear layer: checks of the arguments, pieces of rows, workspace layout, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <mutex>
+
+#include "dlf_ce.h"
+#include "dlf_ff_plan.h"
+
+namespace {
+
+dlf_status fail(dlf_status s, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return dlf_set_error(s, buf);
+}
+#define TRY(X)                             \
+    do {                                   \
+        const dlf_status try_s = (X);      \
+        if (try_s != DLF_OK) return try_s; \
+    } while (0)
+
+constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;       // a launch holds fewer than 2^32 threads, 256 to a workgroup
+constexpr int64_t LEAST_PIECE = 256, MOST_PIECE = 1 << 16;  // rows
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+// A description with its strides filled in, and the rows of a piece.
+struct Ce {
+    dlf_ce_desc d;
+    const char* call;
+    int64_t ldz, piece;     // elements of a row of dz; rows
+    int64_t pieces() const { return std::max<int64_t>(1, ceil_div(d.rows, piece)); }
+    int64_t first(int64_t p) const { return p * piece; }
+    int64_t rows(int64_t p) const { return std::min(piece, d.rows - p * piece); }
+};
+
+// Whether a piece of so many rows fits the launches: its tiles of 64 x 64, those of the gradients' products with the column sums, and k_ce_dz.
+bool launches(int64_t rows, int64_t in, int64_t classes)
+{
+    const int64_t m = ceil_div(rows, 64), i = ceil_div(in, 64), o = ceil_div(classes, 64);
+    return 2 * m * o < MOST_WORKGROUPS - 16 && m * i + 2 * i * o + 2 * o < MOST_WORKGROUPS - 16 &&
+           rows * ceil_div(classes, DLF_CE_DZ_COLS) < MOST_WORKGROUPS - 16;
+}
+
+dlf_status check_desc(const dlf_ce_desc* d, const char* call, Ce& f)
+{
+    if (!d) return fail(DLF_ERR_INVALID_ARG, "%s: null description", call);
+    f.d = *d;
+    f.call = call;
+    if (d->dtype != DLF_F16 && d->dtype != DLF_BF16) return fail(DLF_ERR_INVALID_ARG, "%s: dtype %d", call, d->dtype);
+    if (d->reserved != 0) return fail(DLF_ERR_INVALID_ARG, "%s: reserved is not 0", call);
+    if (d->rows < 0 || d->rows > (int64_t)1 << 30) return fail(DLF_ERR_INVALID_ARG, "%s: %lld rows", call, (long long)d->rows);
+    if (d->in_features < 1 || d->in_features > 1 << 20 || d->classes < 1 || d->classes > 1 << 20)
+        return fail(DLF_ERR_INVALID_ARG, "%s: %d features, %d classes", call, d->in_features, d->classes);
+    struct { int64_t* s; const char* name; } strides[] = {{&f.d.x_stride, "x"}, {&f.d.w_stride, "weight"}};
+    for (auto& q : strides) {
+        if (*q.s == 0) *q.s = d->in_features;
+        if (*q.s < d->in_features || *q.s >= (int64_t)1 << 24)
+            return fail(DLF_ERR_INVALID_ARG, "%s: %s has rows of %d elements, %lld apart", call, q.name, d->in_features, (long long)*q.s);
+    }
+    if (d->piece_bytes < 0 || d->piece_bytes > (int64_t)1 << 50) return fail(DLF_ERR_INVALID_ARG, "%s: piece_bytes %lld", call, (long long)d->piece_bytes);
+    if (!launches(LEAST_PIECE, d->in_features, d->classes))
+        return fail(DLF_ERR_UNSUPPORTED, "%s: %d features, %d classes are more tiles than a launch holds", call, d->in_features, d->classes);
+    f.ldz = ceil_div(d->classes, 8) * 8;
+    const int64_t most = (d->piece_bytes == 0 ? (int64_t)1 << 30 : d->piece_bytes) / (2 * f.ldz);
+    f.piece = std::max(LEAST_PIECE, std::min(MOST_PIECE, most) / LEAST_PIECE * LEAST_PIECE);
+    while (f.piece > LEAST_PIECE && !launches(f.piece, d->in_features, d->classes)) f.piece = std::max(LEAST_PIECE, f.piece / 2 / LEAST_PIECE * LEAST_PIECE);
+    // pieces of about one size
+    const int64_t n = std::max<int64_t>(1, ceil_div(d->rows, f.piece));
+    f.piece = std::max(LEAST_PIECE, ceil_div(ceil_div(d->rows, n), LEAST_PIECE) * LEAST_PIECE);
+    return DLF_OK;
+}
+
+dlf_status check_ptr(const Ce& f, const void* p, const char* name, bool wanted, uintptr_t align)
+{
+    if (!p && wanted) return fail(DLF_ERR_INVALID_ARG, "%s: null %s", f.call, name);
+    if (((uintptr_t)p & (align - 1)) != 0) return fail(DLF_ERR_INVALID_ARG, "%s: %s is not aligned to %d bytes", f.call, name, (int)align);
+    return DLF_OK;
+}
+dlf_status check_ws(const Ce& f, const void* ws, size_t have, size_t need)
+{
+    if (need == 0) return DLF_OK;
+    if (have < need) return fail(DLF_ERR_OOM, "%s: workspace too small: %zu < %zu", f.call, have, need);
+    if (!ws || ((uintptr_t)ws & 255) != 0) return fail(DLF_ERR_INVALID_ARG, "%s: workspace must be a 256-byte aligned device pointer", f.call);
+    return DLF_OK;
+}
+dlf_status launched(const Ce& f, int e)
+{
+    if (e != 0) return fail(DLF_ERR_HIP, "%s: launch failed: %s", f.call, hipGetErrorString((hipError_t)e));
+    return DLF_OK;
+}
+
+// A kernel's attributes belong to the device that it is set up on: once for each that calls run on.
+constexpr int MOST_DEVICES = 64;
+std::once_flag g_once[MOST_DEVICES];
+int g_once_rc[MOST_DEVICES];
+
+dlf_status kernels_ready()
+{
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return fail(DLF_ERR_HIP, "no device: %s", hipGetErrorString(e));
+    if (device < 0 || device >= MOST_DEVICES) return fail(DLF_ERR_UNSUPPORTED, "device %d", device);
+    std::call_once(g_once[device], [device] { g_once_rc[device] = dlf_ce_kernels_init(); });
+    if (g_once_rc[device] != 0) return fail(DLF_ERR_HIP, "kernel setup failed: %s", hipGetErrorString((hipError_t)g_once_rc[device]));
+    return DLF_OK;
+}
+
+// The tiles of a piece's logits.  any: the operands' rows start anywhere.
+DlfFfCut cut_of(const Ce& f, int64_t rows, bool any) { return dlf_ff_whole_cut(rows, f.d.classes, f.d.in_features, any); }
+int64_t parts_of(const Ce& f, const DlfFfCut& c) { return ceil_div(f.d.classes, dlf_ce_width(c.shape)); }
+
+// What a call keeps in the workspace, for its largest piece (column sums: for all of them); addresses are not known where its size is asked for.
+struct Layout {
+    size_t part = 0, at = 0, lse = 0, unit = 0, dz = 0, sums = 0, sum = 0, join = 0, bytes = 0;
+    size_t take(size_t n)
+    {
+        const size_t here = bytes;
+        bytes += align256(n);
+        return here;
+    }
+};
+// logits: their parts are needed; gradients: what the gradients need
+Layout layout_of(const Ce& f, bool logits, bool gradients)
+{
+    Layout l;
+    const int64_t most = std::min(f.piece, f.d.rows), nc = f.d.classes;
+    if (most == 0) return l;
+    int64_t parts = dlf_ff_is_few(most) ? ceil_div(nc, 16) : 0, chunks = 0;
+    // the last piece may be cut otherwise than the others, and few rows are
+    for (const int64_t rows : {most, f.rows(f.pieces() - 1)})
+        for (const bool any : {false, true}) {
+            const DlfFfCut c = cut_of(f, rows, any);
+            parts = std::max(parts, ceil_div(parts_of(f, c) * rows, most));
+            if (dlf_ff_is_few(rows)) parts = std::max(parts, ceil_div(ceil_div(nc, 16) * rows, most));
+            chunks = std::max<int64_t>(chunks, (int64_t)c.tiles_r * 2);
+        }
+    if (logits) {
+        l.part = l.take((size_t)parts * most * 8);
+        l.at = l.take((size_t)most * 4);
+        l.lse = l.take((size_t)most * 4);
+    }
+    if (!gradients) return l;
+    l.unit = l.take(8);
+    l.dz = l.take((size_t)most * f.ldz * 2);
+    l.sums = l.take((size_t)chunks * f.pieces() * nc * 4);
+    if (f.pieces() > 1) l.sum = l.take((size_t)nc * f.d.in_features * 4);
+    size_t join = 0;
+    for (const int64_t rows : {most, f.rows(f.pieces() - 1)})
+        for (int k = 0; k < 8; ++k) {
+            if (!(k & 3)) continue;
+            const DlfFfBackCut c = dlf_ff_back_cut(rows, f.d.in_features, nc, k & 4, k & 1, k & 2);
+            join = std::max(join, align256(c.w.part_bytes) + align256(c.x.part_bytes));
+        }
+    l.join = l.take(join);
+    return l;
+}
+
+// A call's operands.
+struct In {
+    const void *x, *w;
+    const float* bias;
+    const int64_t* target;
+    const char* x_at(const Ce& f, int64_t row) const { return (const char*)x + row * f.d.x_stride * 2; }
+};
+bool whole_lines(const Ce& f, const In& in)
+{
+    return dlf_ff_lines(in.w, f.d.w_stride, f.d.in_features) && dlf_ff_lines(in.x, f.d.x_stride, f.d.in_features);
+}
+void product(const Ce& f, const In& in, int64_t first, int64_t rows, DlfCeArgs& a)
+{
+    memset(&a, 0, sizeof a);
+    a.t.p[0] = in.w; a.t.q[0] = in.x_at(f, first);
+    a.t.ldp = f.d.w_stride; a.t.ldq = f.d.x_stride;
+    a.t.nr = (int)rows; a.t.nc = f.d.classes; a.t.nk = f.d.in_features;
+    a.t.segments = a.t.problems = a.t.splits = 1;
+    a.t.bias[0] = in.bias;
+    a.target = in.target + first;
+    a.ignore = f.d.ignore;
+    a.ldz = f.ldz;
+}
+void set_cut(DlfFfArgs& a, const DlfFfCut& c)
+{
+    a.tiles_r = c.tiles_r;
+    a.tiles_c = c.tiles_c;
+}
+
+// Loss and lse of a piece (either may be null); keep: the exponentials too, in dz.  -> the classes of a part
+dlf_status logits(const Ce& f, const In& in, int64_t first, int64_t rows, bool keep, const Layout& l, char* ws, float* loss, float* lse, int& width,
+                  void* stream)
+{
+    DlfCeArgs a;
+    product(f, in, first, rows, a);
+    a.part = (float*)(ws + l.part);
+    a.at = (float*)(ws + l.at);
+    if (!keep && dlf_ff_is_few(rows)) {
+        const DlfFfFew c = dlf_ff_few_cut(a.t);
+        width = 16;
+        TRY(launched(f, dlf_ce_start_few(&a, &c, f.d.dtype, stream)));
+    } else {
+        const DlfFfCut c = cut_of(f, rows, !whole_lines(f, in));
+        set_cut(a.t, c);
+        if (keep) a.dz = ws + l.dz;
+        width = dlf_ce_width(c.shape);
+        TRY(launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : DLF_CE_STAT, stream)));
+    }
+    const DlfCeJoinArgs j = {a.part, a.at, a.target, a.ignore, (int)ceil_div(f.d.classes, width), (int)rows, f.d.classes, loss, lse};
+    return launched(f, dlf_ce_start_join(&j, stream));
+}
+
+struct Out {
+    void *dx, *dw;
+    float* db;
+};
+// The gradients of all rows: dz of a piece from the lse given, or with loss and lse computed on the way, then the products.
+dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven given, float* loss, const Out& out, char* ws, void* stream)
+{
+    const Layout l = layout_of(f, lse == nullptr, true);
+    const int64_t pieces = f.pieces(), nc = f.d.classes, k = f.d.in_features;
+    TRY(kernels_ready());
+    if (f.d.rows > 0 && f.d.dtype == DLF_F16 && (out.dx || out.dw || out.db)) {
+        const DlfCeUnitArgs u = {given, f.d.rows, (float*)(ws + l.unit)};
+        TRY(launched(f, dlf_ce_start_unit(&u, stream)));
+        given.unit = u.unit;
+    }
+    const bool whole = whole_lines(f, in);
+    int chunks = 0;
+    for (int64_t p = 0; p < pieces; ++p) {
+        const int64_t first = f.first(p), rows = f.rows(p);
+        DlfCeGiven g = given;
+        if (g.dloss) g.dloss += first * g.dloss_stride;
+        if (g.dlse) g.dlse += first * g.dlse_stride;
+        const float* piece_lse = lse ? lse + first : nullptr;
+        if (rows > 0) {
+            // the exponentials are kept where they need not say what the bias's gradient is, which has 32 bits
+            const bool wanted = out.dx || out.dw || out.db, keep = !lse && wanted && !out.db;
+            int width = 0;
+            if (!lse) {
+                float* const to = (float*)(ws + l.lse);
+                TRY(logits(f, in, first, rows, keep, l, ws, loss ? loss + first : nullptr, to, width, stream));
+                piece_lse = to;
+            }
+            if (!wanted) continue;
+            if (keep) {
+                const DlfCeDzArgs z = {ws + l.dz, f.ldz, (const float*)(ws + l.part), width, (int)rows, (int)nc, in.target + first, f.d.ignore, piece_lse, g};
+                TRY(launched(f, dlf_ce_start_dz(&z, f.d.dtype, stream)));
+            } else {
+                DlfCeArgs a;
+                product(f, in, first, rows, a);
+                const DlfFfCut c = cut_of(f, rows, !whole);
+                set_cut(a.t, c);
+                a.dz = ws + l.dz;
+                a.lse = piece_lse;
+                a.given = g;
+                if (out.db) a.sums = (float*)(ws + l.sums) + (size_t)chunks * nc;
+                chunks += c.tiles_r * 2;
+                TRY(launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, DLF_CE_DZ, stream)));
+            }
+        }
+        DlfCeBackArgs e;
+        memset(&e, 0, sizeof e);
+        DlfFfBackArgs& b = e.b;
+        b.w.splits = b.x.splits = 1;
+        const bool last = p == pieces - 1, want_x = out.dx && rows > 0, want_w = out.dw != nullptr;
+        const char* const dz = rows > 0 ? ws + l.dz : nullptr;
+        if (want_x) {
+            DlfFfArgs& a = b.x;
+            a.p[0] = in.w; a.q[0] = dz;
+            a.ldp = f.d.w_stride; a.ldq = f.ldz;
+            a.nr = (int)rows; a.nc = (int)k; a.nk = (int)nc;
+            a.segments = a.problems = 1;
+            a.out[0] = (char*)out.dx + first * k * 2; a.ldo = k;
+        }
+        if (want_w) {
+            DlfFfArgs& a = b.w;
+            a.p[0] = in.x_at(f, first); a.q[0] = dz;
+            a.ldp = f.d.x_stride; a.ldq = f.ldz;
+            a.nr = (int)nc; a.nc = (int)k; a.nk = (int)rows;
+            a.segments = a.problems = 1;
+            a.out[0] = out.dw; a.ldo = k;
+        }
+        if (out.db && last) {
+            b.sum.part[0] = chunks > 0 ? (const float*)(ws + l.sums) : out.db;    // (of no rows nothing is read: zeros)
+            b.sum.out[0] = out.db;
+            b.sum.n = (int)nc;
+            b.sum.chunks = chunks;
+            b.sum.blocks = (int)ceil_div(nc, 64);
+        }
+        if (!want_x && !want_w && b.sum.blocks == 0) continue;
+        // (dz has rows of whole lines, zeros behind the last class: only the other operands decide)
+        const DlfFfBackCut c = dlf_ff_back_cut(std::max<int64_t>(1, rows), k, nc, (want_x || want_w) && !whole, want_w, want_x);
+        b.x_first = c.x_first;
+        set_cut(b.w, c.w);
+        set_cut(b.x, c.x);
+        b.w.splits = c.w.splits;
+        b.x.splits = c.x.splits;
+        b.w.part = (float*)(ws + l.join);
+        b.x.part = (float*)(ws + l.join + align256(c.w.part_bytes));
+        if (!want_w) { b.w.problems = 0; b.w.splits = 1; }
+        if (!want_x) { b.x.problems = 0; b.x.splits = 1; }
+        e.inverse = given.unit ? given.unit + 1 : nullptr;
+        if (want_w && pieces > 1) {
+            e.sum = (float*)(ws + l.sum);
+            e.add = p > 0;
+            e.keep = !last;
+        }
+        TRY(launched(f, dlf_ce_start_back(&e, c.w.shape, f.d.dtype, stream)));
+    }
+    return DLF_OK;
+}
+
+size_t bytes_of(const dlf_ce_desc* d, bool logits, bool gradients, const char* call)
+{
+    Ce f;
+    return check_desc(d, call, f) == DLF_OK ? layout_of(f, logits, gradients).bytes : SIZE_MAX;
+}
+dlf_status check_in(const Ce& f, const In& in)
+{
+    const bool some = f.d.rows > 0;
+    TRY(check_ptr(f, in.x, "x", some, 2));
+    TRY(check_ptr(f, in.w, "weight", some, 2));
+    TRY(check_ptr(f, in.bias, "bias", false, 4));
+    return check_ptr(f, in.target, "target", some, 8);
+}
+dlf_status check_given(const Ce& f, const DlfCeGiven& g)
+{
+    TRY(check_ptr(f, g.dloss, "dloss", false, 4));
+    TRY(check_ptr(f, g.dlse, "dlse", false, 4));
+    if (g.dloss_stride < 0 || g.dlse_stride < 0 || g.dloss_stride > (int64_t)1 << 24 || g.dlse_stride > (int64_t)1 << 24)
+        return fail(DLF_ERR_INVALID_ARG, "%s: dloss and dlse lie %lld and %lld apart", f.call, (long long)g.dloss_stride, (long long)g.dlse_stride);
+    if (!g.dloss && !(std::fabs(g.dloss_value) <= 3e38f)) return fail(DLF_ERR_INVALID_ARG, "%s: dloss is not finite", f.call);
+    return DLF_OK;
+}
+dlf_status check_out(const Ce& f, const Out& o)
+{
+    TRY(check_ptr(f, o.dx, "dx", false, 2));
+    TRY(check_ptr(f, o.dw, "dweight", false, 2));
+    return check_ptr(f, o.db, "dbias", false, 4);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dlf_cross_entropy_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, false, "dlf_cross_entropy_workspace_bytes"); }
+size_t dlf_cross_entropy_backward_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, false, true, "dlf_cross_entropy_backward_workspace_bytes"); }
+size_t dlf_cross_entropy_gradients_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, true, "dlf_cross_entropy_gradients_workspace_bytes"); }
+
+dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target, float* loss,
+                             float* lse, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    Ce f;
+    TRY(check_desc(d, "dlf_cross_entropy", f));
+    const In in = {x, weight, bias, target};
+    TRY(check_in(f, in));
+    TRY(check_ptr(f, loss, "loss", f.d.rows > 0, 4));
+    TRY(check_ptr(f, lse, "lse", false, 4));
+    const Layout l = layout_of(f, true, false);
+    TRY(check_ws(f, workspace, workspace_bytes, l.bytes));
+    if (f.d.rows == 0) return DLF_OK;
+    TRY(kernels_ready());
+    for (int64_t p = 0; p < f.pieces(); ++p) {
+        int width;
+        TRY(logits(f, in, f.first(p), f.rows(p), false, l, (char*)workspace, loss + f.first(p), lse ? lse + f.first(p) : nullptr, width, hip_stream));
+    }
+    return DLF_OK;
+}
+
+dlf_status dlf_cross_entropy_backward(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target,
+                                      const float* lse, const float* dloss, int64_t dloss_stride, float dloss_value, const float* dlse,
+                                      int64_t dlse_stride, void* dx, void* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                                      void* hip_stream)
+{
+    Ce f;
+    TRY(check_desc(d, "dlf_cross_entropy_backward", f));
+    const In in = {x, weight, bias, target};
+    const DlfCeGiven given = {dloss, dlse, dloss_stride, dlse_stride, dloss_value, nullptr};
+    const Out out = {dx, dweight, dbias};
+    TRY(check_in(f, in));
+    TRY(check_ptr(f, lse, "lse", f.d.rows > 0, 4));
+    TRY(check_given(f, given));
+    TRY(check_out(f, out));
+    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, false, true).bytes));
+    static const float none = 0.0f;                         // (of no rows nothing is read)
+    return gradients(f, in, lse ? lse : &none, given, nullptr, out, (char*)workspace, hip_stream);
+}
+
+dlf_status dlf_cross_entropy_gradients(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target,
+                                       const float* dloss, int64_t dloss_stride, float dloss_value, float* loss, void* dx, void* dweight,
+                                       float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    Ce f;
+    TRY(check_desc(d, "dlf_cross_entropy_gradients", f));
+    const In in = {x, weight, bias, target};
+    const DlfCeGiven given = {dloss, nullptr, dloss_stride, 0, dloss_value, nullptr};
+    const Out out = {dx, dweight, dbias};
+    TRY(check_in(f, in));
+    TRY(check_given(f, given));
+    TRY(check_ptr(f, loss, "loss", f.d.rows > 0, 4));
+    TRY(check_out(f, out));
+    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, true, true).bytes));
+    return gradients(f, in, nullptr, given, loss, out, (char*)workspace, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,75 @@
+// Shared between the host side of the cross entropy of a linear layer (dlf_ce.cpp) and its kernels (dlf_ce.hip).
+#pragma once
+#include "dlf_ffn.h"
+
+// What a product's epilogue does with the logits of its tile.
+enum { DLF_CE_STAT = 0,         // a maximum and a sum of exponentials of each row over a part of the classes, the target's logit
+       DLF_CE_KEEP = 1,         // ... and the exponentials themselves, in fp16
+       DLF_CE_DZ = 2 };         // their gradient
+// A row's gradients of loss and lse as the caller gives them.
+struct DlfCeGiven {
+    const float *dloss, *dlse;  // null: dloss_value, none
+    int64_t dloss_stride, dlse_stride;
+    float dloss_value;
+    const float* unit;          // {a power of two that dz is scaled by, its inverse}, or null
+};
+struct DlfCeArgs {
+    DlfFfArgs t;                // p: weight, q: x, bias
+    const int64_t* target;
+    int64_t ignore;
+    float* part;                // [parts][nr] {maximum, sum of exp(z - maximum)}
+    float* at;                  // [nr] the target's logit, of rows whose target is a class
+    void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: 2^15 exp(z - its part's maximum)
+    int64_t ldz;                // a multiple of eight
+    const float* lse;
+    DlfCeGiven given;
+    float* sums;                // [chunks][nc] column sums of dz, in 32 bits, or null
+};
+struct DlfCeJoinArgs {
+    const float* part;
+    const float* at;
+    const int64_t* target;
+    int64_t ignore;
+    int32_t parts, nr, nc;
+    float *loss, *lse;          // either may be null
+};
+struct DlfCeDzArgs {
+    void* dz;                   // KEEP's in, dz out
+    int64_t ldz;
+    const float* part;
+    int32_t width;              // classes of a part
+    int32_t nr, nc;
+    const int64_t* target;
+    int64_t ignore;
+    const float* lse;
+    DlfCeGiven given;
+};
+struct DlfCeUnitArgs {
+    DlfCeGiven given;
+    int64_t rows;
+    float* unit;
+};
+struct DlfCeBackArgs {
+    DlfFfBackArgs b;
+    const float* inverse;       // the products are scaled by it; or null
+    float* sum;                 // [classes][in] the weight's gradient over the pieces in front, or null
+    int32_t add, keep;
+};
+// Classes of a part, by tile shape: what a wave's columns are.
+static inline int dlf_ce_width(int shape) { return DLF_FF_SHAPES[shape].bc / 2; }
+static inline int dlf_ce_chunk(int shape) { return DLF_FF_SHAPES[shape].br / 2; }
+// Rows of a workgroup of k_ce_join, and up to how many rows a workgroup has one.
+#define DLF_CE_JOIN_ROWS 32
+#define DLF_CE_JOIN_FEW 256
+// Columns of a workgroup of k_ce_dz.
+#define DLF_CE_DZ_COLS 2048
+
+extern "C" {
+int dlf_ce_kernels_init(void);
+int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int dtype, int mode, void* stream);
+int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int dtype, void* stream);
+int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream);
+int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream);
+int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream);
+int dlf_ce_start_back(const DlfCeBackArgs* a, int shape, int dtype, void* stream);
+}

@@ -1,0 +1,474 @@
+// gfx950 (CDNA4) kernels of the cross entropy of a linear layer over many classes, without its logits in memory.  The products are those of dlf_tile.h;
+// what is here are their epilogues, and what joins them.
+//
+//   lse = log sum_c exp z_c: every wave leaves, for each row and its 32 to 128 classes, the maximum m and s = sum exp(z - m), which
+//   k_ce_join adds up as sum s exp(m - M).  dz_c = (dloss + dlse) exp(z_c - lse) - dloss [c = target].
+#include "dlf_tile.h"
+#include "dlf_ce.h"
+
+#define LOG2_E 1.44269504f
+#define LN_2 0.693147181f
+#define MINUS_INF (-__builtin_inff())
+// exp(d).  d is rounded before it is multiplied: a maximum times log2(e), rounded, would shift all of a row's exponentials.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2_E); }
+
+// A row's part of the gradient: dz = total * exp(z - lse) - own at the target.
+struct RowGradient {
+    float total, own;
+};
+__device__ __forceinline__ RowGradient row_gradient(const DlfCeGiven& g, int64_t r, int64_t t, int64_t ignore, int nc)
+{
+    RowGradient q;
+    q.own = t == ignore ? 0.0f : g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value;
+    float l = g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f;
+    if (g.unit != nullptr) {
+        const float u = g.unit[0];
+        q.own *= u;
+        l *= u;
+    }
+    q.total = q.own + l;
+    if (t != ignore && (t < 0 || t >= nc)) q.total = __builtin_nanf("");        // no class: not silently anything
+    return q;
+}
+
+// ------------------------------------------------------------------------------------------------
+// The epilogues of a tile.  A lane holds, of one row of each block of 32, every other four of the wave's columns: a row's maximum and sum are its own
+// and one other lane's, without LDS.  The target's logit lies in one of the lane's registers, which is looked for only where a row of the
+// block has its target among the wave's columns.
+// ------------------------------------------------------------------------------------------------
+template <int MODE> struct Entropy {
+    static constexpr bool OWN = true, SUMS = false;
+    const DlfCeArgs& e;
+
+    template <typename T, int FC, int FR, int WC>
+    __device__ __forceinline__ void tile(const DlfFfArgs& a, f16v (&acc)[FC][FR], int row0, int col0, int wave) const
+    {
+        typedef typename std::conditional<MODE == DLF_CE_KEEP, F16, T>::type S;
+        constexpr int CW = FC * 32, CROW = CW + 4, LPR = CW / 8, RPU = 64 / LPR;   // columns of the wave, floats of an LDS row, lanes to a row, rows of a store
+        const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5, left = a.nc - col0;
+        // stores go through an area of LDS that is the wave's own, so that they are whole lines
+        float* const lf = (float*)ff_lds + wave * (32 * CROW);
+        const int cw = lane % LPR * 8, rw = lane / LPR;
+        float sum[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+        if (MODE != DLF_CE_STAT) __syncthreads();
+        if (left <= 0) return;                              // a wave behind the last class
+#pragma unroll
+        for (int j = 0; j < FR; ++j) {
+            // One block of 32 rows at a time: the accumulators leave few registers.  (Comparisons and loads of one block are not kept for the next.)
+            __builtin_amdgcn_sched_barrier(0);
+            int mine = lhi * 4;
+            asm volatile("" : "+v"(mine)::"memory");
+            float z[FC][16];
+#pragma unroll
+            for (int i = 0; i < FC; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    z[i][k] = acc[i][j][k];
+                    asm volatile("" : "+v"(z[i][k]));       // (read here, not where the product ends)
+                }
+            if (a.bias[0] != nullptr) {
+                const float* const b = a.bias[0] + col0 + mine;
+                if (left >= CW) {
+#pragma unroll
+                    for (int i = 0; i < FC; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float four[4];
+                            __builtin_memcpy(four, b + i * 32 + q * 8, 16);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) z[i][q * 4 + k] += four[k];
+                        }
+                } else {
+                    const int last = left - 1 - mine;       // (of columns that do not exist any: they are cut)
+#pragma unroll
+                    for (int i = 0; i < FC; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[i][k] += b[min(i * 32 + (k >> 2) * 8 + (k & 3), last)];
+                }
+            }
+            auto cut = [&](float v) __attribute__((always_inline)) {            // columns that do not exist
+                if (left >= CW) return;
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) z[i][k] = i * 32 + (k >> 2) * 8 + (k & 3) >= left - mine ? v : z[i][k];
+            };
+            const int r = row0 + j * 32 + l32, at = min(r, a.nr - 1);
+            const int64_t t = e.target[at];
+            const int rel = (t >= 0 && t < a.nc ? (int)t - col0 : -8) - mine;  // the target's place among the lane's columns
+            const bool near = r < a.nr && rel >= -4 && rel < CW;
+            // f on the target's logit, in the lane that holds it
+            auto target = [&](auto&& f) __attribute__((always_inline)) {
+                if (__builtin_amdgcn_ballot_w64(near) == 0) return;
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (near && rel == i * 32 + (k >> 2) * 8 + (k & 3)) z[i][k] = f(z[i][k]);
+            };
+            if constexpr (MODE == DLF_CE_DZ) {
+                RowGradient g = row_gradient(e.given, at, t, e.ignore, a.nc);
+                if (r >= a.nr) g.total = g.own = 0.0f;
+                const float lse = e.lse[at];
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float v = g.total * exp_of(z[i][k] - lse);
+                        z[i][k] = g.total == 0.0f ? 0.0f : v;
+                    }
+                target([&](float v) __attribute__((always_inline)) { return v - g.own; });
+                cut(0.0f);
+            } else {
+                float m = MINUS_INF, s = 0.0f;
+                cut(MINUS_INF);
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) m = fmaxf(m, z[i][k]);
+                m = fmaxf(m, __shfl_xor(m, 32, 64));
+                target([&](float v) __attribute__((always_inline)) { return e.at[r] = v; });
+                const float from = m == MINUS_INF ? 0.0f : m;
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        z[i][k] = exp_of(z[i][k] - from);
+                        s += z[i][k];
+                    }
+                s += __shfl_xor(s, 32, 64);
+                if (lhi == 0 && r < a.nr) {
+                    const float2 both = {m, s};
+                    *(float2*)(e.part + ((int64_t)(col0 / CW) * a.nr + r) * 2) = both;
+                }
+            }
+            if constexpr (MODE != DLF_CE_STAT) {
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *(f4v*)(lf + l32 * CROW + i * 32 + q * 8 + lhi * 4) = f4v{z[i][q * 4], z[i][q * 4 + 1], z[i][q * 4 + 2], z[i][q * 4 + 3]};
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+                for (int u = 0; u < 32; u += RPU) {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) *(f4v*)(v + k * 4) = *(const f4v*)(lf + (u + rw) * CROW + cw + k * 4);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (MODE == DLF_CE_DZ) sum[i] += v[i];                  // (zeros in rows that do not exist)
+                        else v[i] *= 32768.0f;
+                    }
+                    // One rounding to the type that the matrix units multiply.  KEEP: fp16, whatever the tensors' type, with 2^-40 of its part's
+                    // maximum as the least that is not lost; the maximum itself is exact, so that 1 - p of a sure target is.
+                    const int ru = row0 + j * 32 + u + rw;
+                    if (ru < a.nr && col0 + cw < e.ldz) store_some<S, 8>(e.dz, (int64_t)ru * e.ldz + col0 + cw, 8, v);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        if (MODE == DLF_CE_DZ && e.sums != nullptr) {
+#pragma unroll
+            for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor(sum[i], d, 64);
+            if (e.given.unit != nullptr) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] *= e.given.unit[1];
+            }
+            const int c = col0 + cw;
+            if (lane < LPR && c < a.nc) store_floats(e.sums + (int64_t)(row0 / (FR * 32)) * a.nc + c, a.nc - c, sum);
+        }
+    }
+
+    // Few rows: a block of 16 classes and 16 rows, a lane's four classes of row lane % 16.
+    __device__ __forceinline__ void few(const DlfFfArgs& a, f4v v, int r, int c) const
+    {
+        float z[4] = {v.x, v.y, v.z, v.w}, m = MINUS_INF, s = 0.0f;
+        if (a.bias[0] != nullptr) {
+            float b[4];
+            load_floats(a.bias[0] + c, a.nc - c, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] += b[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            z[i] = c + i < a.nc ? z[i] : MINUS_INF;
+            m = fmaxf(m, z[i]);
+        }
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float from = m == MINUS_INF ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += exp_of(z[i] - from);
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        const int first = c & ~15;
+        if (r >= a.nr || first >= a.nc) return;
+        const int64_t t = e.target[r];
+        if (t >= c && t < c + 4 && t < a.nc) e.at[r] = t == c ? z[0] : t == c + 1 ? z[1] : t == c + 2 ? z[2] : z[3];
+        if (c == first) {
+            const float2 both = {m, s};
+            *(float2*)(e.part + ((int64_t)(first >> 4) * a.nr + r) * 2) = both;
+        }
+    }
+};
+
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT, int MODE>
+__global__ FF_TILE_BOUNDS void k_ce_tile(const DlfCeArgs e)
+{
+    tile<T, BC, BR, WC, WR, KB, RING, DIRECT, false, false, false>(e.t, Entropy<MODE>{e}, blockIdx.x);
+}
+template <typename T, int NF, int MR>
+__global__ __launch_bounds__(512, NF + MR <= 3 ? 4 : 2) void k_ce_few(const DlfCeArgs e)
+{
+    few<T, NF, MR, false>(e.t, Entropy<DLF_CE_STAT>{e});
+}
+template <typename T, int NF, int MR>
+__global__ __launch_bounds__(512) void k_ce_rows(const DlfCeArgs e)
+{
+    rows_in_lds<T, NF, MR, false>(e.t, Entropy<DLF_CE_STAT>{e});
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_ce_join: a row's parts to its lse and loss.  ROWS of them to a workgroup, its other threads share the parts, in a fixed order.
+// ------------------------------------------------------------------------------------------------
+template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCeJoinArgs a)
+{
+    constexpr int GROUPS = 256 / ROWS;
+    __shared__ float2 shared[256];
+    const int r = blockIdx.x * ROWS + threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+    float m = MINUS_INF, s = 0.0f;
+    auto add = [&](float m2, float s2) __attribute__((always_inline)) {
+        const float top = fmaxf(m, m2), from = top == MINUS_INF ? 0.0f : top;
+        s = s * exp_of(m - from) + s2 * exp_of(m2 - from);
+        m = top;
+    };
+    if (r < a.nr) {
+        constexpr int AT = 8;                               // parts whose loads share a wait
+        int p = g;
+        for (; p + (AT - 1) * GROUPS < a.parts; p += AT * GROUPS) {
+            float2 v[AT];
+#pragma unroll
+            for (int k = 0; k < AT; ++k) v[k] = *(const float2*)(a.part + ((int64_t)(p + k * GROUPS) * a.nr + r) * 2);
+#pragma unroll
+            for (int k = 0; k < AT; ++k) add(v[k].x, v[k].y);
+        }
+        for (; p < a.parts; p += GROUPS) {
+            const float2 v = *(const float2*)(a.part + ((int64_t)p * a.nr + r) * 2);
+            add(v.x, v.y);
+        }
+    }
+    shared[threadIdx.x] = float2{m, s};
+#pragma unroll
+    for (int h = GROUPS / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        if (g < h) {
+            const float2 v = shared[threadIdx.x + h * ROWS];
+            add(v.x, v.y);
+            shared[threadIdx.x] = float2{m, s};
+        }
+    }
+    if (g != 0 || r >= a.nr) return;
+    const float lse = m == MINUS_INF ? (s == s ? MINUS_INF : s) : m + __builtin_amdgcn_logf(s) * LN_2;
+    if (a.lse != nullptr) a.lse[r] = lse;
+    if (a.loss != nullptr) {
+        const int64_t t = a.target[r];
+        a.loss[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.nc ? __builtin_nanf("") : lse - a.at[r];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_ce_dz: dz from the exponentials kept, in their place: each times (dloss + dlse) exp(its part's maximum - lse).  Bound by memory.
+// ------------------------------------------------------------------------------------------------
+template <typename T> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
+{
+    const int cols = (int)((a.ldz + DLF_CE_DZ_COLS - 1) / DLF_CE_DZ_COLS), r = blockIdx.x / cols;
+    const int c = (blockIdx.x - r * cols) * DLF_CE_DZ_COLS + threadIdx.x * 8;
+    if (c >= a.ldz) return;
+    const int64_t at = (int64_t)r * a.ldz + c, t = a.target[r];
+    const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
+    const F16::v8 q = load8<F16>(a.dz, at, 8);
+    const float m = a.part[((int64_t)(c / a.width) * a.nr + r) * 2];
+    const float by = g.total == 0.0f ? 0.0f : g.total * exp_of(m - a.lse[r]) * (1.0f / 32768.0f);
+    const int64_t rel = t - c;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = g.total == 0.0f ? 0.0f : (float)q[i] * by;
+        if (rel == i && t != a.ignore) v[i] -= g.own;
+        if (c + i >= a.nc) v[i] = 0.0f;
+    }
+    store_some<T, 8>(a.dz, at, 8, v);
+}
+
+// ------------------------------------------------------------------------------------------------
+// k_ce_unit: for fp16, the power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14: dz, at most twice that, stays below 2^15,
+// and classes of probability 2^-28 are numbers of full precision.
+// ------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void k_ce_unit(const DlfCeUnitArgs a)
+{
+    __shared__ float waves[16];
+    const DlfCeGiven& g = a.given;
+    float m = 0.0f;
+    const int64_t rows = (g.dloss != nullptr && g.dloss_stride != 0) || (g.dlse != nullptr && g.dlse_stride != 0) ? a.rows : min((int64_t)1, a.rows);
+    for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+        const float v = fabsf(g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value) + fabsf(g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f);
+        m = v <= 3.402823466e38f ? fmaxf(m, v) : m;         // (what is not finite makes its own row so)
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 16; ++w) m = fmaxf(m, waves[w]);
+    // 2^(13 - e) for m = 1.x * 2^e, as far as it and its inverse are normal numbers
+    int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23) - 127;
+    if (m == 0.0f) e = 13;
+    const int k = max(-126, min(126, 13 - e));
+    a.unit[0] = __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
+    a.unit[1] = __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
+}
+
+// k_ce_back: the products dx = dz weight and dweight = dz^T x with the column sums, as k_ff_back, scaled back and added up over pieces.
+template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT>
+__global__ FF_TILE_BOUNDS void k_ce_back(const DlfCeBackArgs e)
+{
+    const DlfFfBackArgs& a = e.b;
+    int b = blockIdx.x;
+    if (a.x_first) b = b < a.blocks_x ? b + a.blocks_w : b < a.blocks_x + a.blocks_w ? b - a.blocks_x : b;   // (both multiples of eight)
+    if (b < a.blocks_w) {
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, Sums{e.inverse, e.sum, e.add, e.keep}, b);
+        return;
+    }
+    b -= a.blocks_w;
+    if (b < a.blocks_x) {
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, Sums{e.inverse, nullptr, 0, 0}, b);
+        return;
+    }
+    b -= a.blocks_x;
+    if (b < a.sum.blocks) add_sums(a.sum, b);
+}
+template <typename T> __global__ __launch_bounds__(256) void k_ce_join_back(const DlfCeBackArgs e)
+{
+    const bool w = (int)blockIdx.x < e.b.blocks_w;
+    const int64_t unit = (int64_t)(w ? blockIdx.x : blockIdx.x - e.b.blocks_w) * 256 + threadIdx.x;
+    if (w) join<T, false>(e.b.w, Sums{e.inverse, e.sum, e.add, e.keep}, unit);
+    else join<T, false>(e.b.x, Sums{e.inverse, nullptr, 0, 0}, unit);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Launches
+// ------------------------------------------------------------------------------------------------
+typedef void (*CeKernel)(const DlfCeArgs);
+typedef void (*CeBackKernel)(const DlfCeBackArgs);
+template <typename T, int MODE> static CeKernel tile_kernel(int shape)
+{
+    switch (shape) {
+    case DLF_FF_SHAPE_256: return k_ce_tile<T, 256, 256, 2, 2, 64, 2, true, MODE>;
+    case DLF_FF_SHAPE_128: return k_ce_tile<T, 128, 128, 2, 2, 64, 2, true, MODE>;
+    case DLF_FF_SHAPE_128_DEEP: return k_ce_tile<T, 128, 128, 2, 2, 64, 4, true, MODE>;
+    case DLF_FF_SHAPE_ANY64: return k_ce_tile<T, 64, 64, 2, 2, 64, 4, false, MODE>;
+    case DLF_FF_SHAPE_ANY64G: return nullptr;
+    default: return k_ce_tile<T, 128, 128, 2, 2, 64, 2, false, MODE>;
+    }
+}
+template <typename T> static CeKernel tile_kernel(int shape, int mode)
+{
+    return mode == DLF_CE_STAT ? tile_kernel<T, DLF_CE_STAT>(shape) : mode == DLF_CE_KEEP ? tile_kernel<T, DLF_CE_KEEP>(shape) : tile_kernel<T, DLF_CE_DZ>(shape);
+}
+template <typename T> static CeBackKernel back_kernel(int shape)
+{
+    switch (shape) {
+    case DLF_FF_SHAPE_256: return k_ce_back<T, 256, 256, 2, 2, 64, 2, true>;
+    case DLF_FF_SHAPE_128: return k_ce_back<T, 128, 128, 2, 2, 64, 2, true>;
+    case DLF_FF_SHAPE_128_DEEP: return k_ce_back<T, 128, 128, 2, 2, 64, 4, true>;
+    case DLF_FF_SHAPE_ANY64: return k_ce_back<T, 64, 64, 2, 2, 64, 4, false>;
+    case DLF_FF_SHAPE_ANY64G: return nullptr;
+    default: return k_ce_back<T, 128, 128, 2, 2, 64, 2, false>;
+    }
+}
+template <typename T> static CeKernel few_kernel(int rows, int nf, int mr)
+{
+    if (rows) return nf == 1 ? mr == 1 ? k_ce_rows<T, 1, 1> : k_ce_rows<T, 1, 2> : k_ce_rows<T, 2, 2>;
+    return nf == 1 ? mr == 1 ? k_ce_few<T, 1, 1> : k_ce_few<T, 1, 2> : k_ce_few<T, 2, 2>;
+}
+static size_t tile_lds(int shape)
+{
+    const DlfFfShape& s = DLF_FF_SHAPES[shape];
+    const size_t ring = (size_t)s.stages * 64 * (s.bc + s.br) * 2, out = (size_t)4 * (s.br < 128 ? 32 : 64) * (s.bc / 2 + 4) * 4;
+    return ring > out ? ring : out;
+}
+extern "C" int dlf_ce_kernels_init(void)
+{
+    for (int k = 0; k < 6; ++k) {
+        const int nf = k / 2 == 2 ? 2 : 1, mr = k / 2 == 0 ? 1 : 2;
+        const CeKernel f = (k & 1) ? few_kernel<BF16>(1, nf, mr) : few_kernel<F16>(1, nf, mr);
+        const hipError_t e = hipFuncSetAttribute((const void*)f, hipFuncAttributeMaxDynamicSharedMemorySize, DLF_FF_ROWS_LDS(8, nf, mr, 0));
+        if (e != hipSuccess) return (int)e;
+    }
+    for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
+        for (int k = 0; k < 8; ++k) {
+            const void* const f = k < 6 ? (const void*)((k & 1) ? tile_kernel<BF16>(shape, k >> 1) : tile_kernel<F16>(shape, k >> 1))
+                                        : (const void*)((k & 1) ? back_kernel<BF16>(shape) : back_kernel<F16>(shape));
+            if (f == nullptr) continue;
+            const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
+            if (e != hipSuccess) return (int)e;
+        }
+    return 0;
+}
+static unsigned tile_blocks(const DlfFfArgs& a) { return (unsigned)((a.tiles_r * a.tiles_c * a.problems * a.splits + 7) / 8 * 8); }
+static unsigned join_blocks(const DlfFfArgs& a) { return (unsigned)(((int64_t)a.nr * a.problems * ((a.nc + 7) / 8) + 255) / 256); }
+extern "C" int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int dtype, int mode, void* stream)
+{
+    hipLaunchKernelGGL(dtype == DLF_F16 ? tile_kernel<F16>(shape, mode) : tile_kernel<BF16>(shape, mode), dim3(tile_blocks(a->t)), dim3(256), tile_lds(shape),
+                       (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int dtype, void* stream)
+{
+    DlfCeArgs b = *a;
+    b.t.tiles_r = (a->t.nr + 16 * c->mr - 1) / (16 * c->mr);
+    b.t.tiles_c = (a->t.nc + 16 * c->nf - 1) / (16 * c->nf);
+    const dim3 grid((unsigned)((b.t.tiles_c + 7) / 8 * 8 * b.t.tiles_r)), block((unsigned)c->waves * 64);
+    const size_t lds = c->rows ? (size_t)DLF_FF_ROWS_LDS(c->waves, c->nf, c->mr, 0) : (size_t)c->waves * c->nf * c->mr * 1024;
+    hipLaunchKernelGGL(dtype == DLF_F16 ? few_kernel<F16>(c->rows, c->nf, c->mr) : few_kernel<BF16>(c->rows, c->nf, c->mr), grid, block, lds,
+                       (hipStream_t)stream, b);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream)
+{
+    if (a->nr <= DLF_CE_JOIN_FEW) hipLaunchKernelGGL(k_ce_join<1>, dim3((unsigned)a->nr), dim3(256), 0, (hipStream_t)stream, *a);
+    else
+        hipLaunchKernelGGL(k_ce_join<DLF_CE_JOIN_ROWS>, dim3((unsigned)((a->nr + DLF_CE_JOIN_ROWS - 1) / DLF_CE_JOIN_ROWS)), dim3(256), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream)
+{
+    const dim3 grid((unsigned)((int64_t)a->nr * ((a->ldz + DLF_CE_DZ_COLS - 1) / DLF_CE_DZ_COLS)));
+    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz<F16>, grid, dim3(256), 0, (hipStream_t)stream, *a);
+    else hipLaunchKernelGGL(k_ce_dz<BF16>, grid, dim3(256), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream)
+{
+    hipLaunchKernelGGL(k_ce_unit, dim3(1), dim3(1024), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_back(const DlfCeBackArgs* a, int shape, int dtype, void* stream)
+{
+    DlfCeBackArgs e = *a;
+    DlfFfBackArgs& b = e.b;
+    b.blocks_w = (int)tile_blocks(b.w);
+    b.blocks_x = (int)tile_blocks(b.x);
+    hipLaunchKernelGGL(dtype == DLF_F16 ? back_kernel<F16>(shape) : back_kernel<BF16>(shape), dim3((unsigned)(b.blocks_w + b.blocks_x + b.sum.blocks)),
+                       dim3(256), tile_lds(shape), (hipStream_t)stream, e);
+    b.blocks_w = b.w.splits > 1 ? (int)join_blocks(b.w) : 0;
+    b.blocks_x = b.x.splits > 1 ? (int)join_blocks(b.x) : 0;
+    if (b.blocks_w + b.blocks_x > 0)
+        hipLaunchKernelGGL(dtype == DLF_F16 ? k_ce_join_back<F16> : k_ce_join_back<BF16>, dim3((unsigned)(b.blocks_w + b.blocks_x)), dim3(256), 0,
+                           (hipStream_t)stream, e);
+    return (int)hipGetLastError();
+}

@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "../../include/dlf_debug.h"
+#include "dlf_ff_plan.h"
 #include "dlf_ffn.h"
 
 namespace {
@@ -148,19 +149,11 @@ dlf_status kernels_ready()
     return DLF_OK;
 }
 
-// Whether the tile kernel takes an operand: rows in whole 16-byte lines, offsets inside a tile that fit 31 bits.
-bool lines(const void* p, int64_t ld, int64_t row)
-{
-    return ((uintptr_t)p & 15) == 0 && (ld & 7) == 0 && (row & 7) == 0 && ld < (int64_t)1 << 22;
-}
-
-
-
 // The forward product of few rows, straight from memory.
-dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
+DlfFfFew few_cut(const DlfFfArgs& a, bool gated)
 {
     DlfFfFew c;
-    c.rows = g_force != 1 && lines(a.p[0], a.ldp, a.nk) && (!gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+    c.rows = g_force != 1 && dlf_ff_lines(a.p[0], a.ldp, a.nk) && (!gated || dlf_ff_lines(a.p[1], a.ldp, a.nk)) && dlf_ff_lines(a.q[0], a.ldq, a.nk);
     // Rows per workgroup: 32 rather than 16 (the kernel, 64 rows 2048 -> 2 x 5632: 13.0 against 15.7 us, 4096 -> 4096 11.8 against 14.0), above 32
     // rows with 32 features for the reads of x (64 x 4096 -> 4096 10.9 against 11.8, 48 x 2048 -> 32001 38 against 45; 32 x 4096 -> 4096 would
     // lose, 10.5 against 8.4: fewer workgroups).
@@ -171,15 +164,11 @@ dlf_status few_rows(const Ff& f, DlfFfArgs& a, bool gated, void* stream)
     const int64_t groups = (int64_t)((a.nc + 16 * c.nf - 1) / (16 * c.nf)) * ((a.nr + 16 * c.mr - 1) / (16 * c.mr));
     c.waves = groups <= 256 ? 8 : 4;
     while (c.waves > 1 && c.waves * 64 >= 2 * a.nk) c.waves >>= 1;
-    return launched(f, dlf_ff_start_few(&a, &c, f.d.dtype, gated, stream));
+    return c;
 }
 
-// How a product of these sizes is cut: a tile shape and the workgroups that share a tile's k.
-struct Cut {
-    int shape = DLF_FF_SHAPE_128, splits = 1, tiles_r = 0, tiles_c = 0;
-    size_t part_bytes = 0;
-    int64_t tiles() const { return (int64_t)tiles_r * tiles_c; }
-};
+using Cut = DlfFfCut;
+using BackCut = DlfFfBackCut;
 int g_force_splits = 0;
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
@@ -261,13 +250,13 @@ template <typename F> void each_shape(bool gated, bool any, F&& f)
         if (takes(shape, gated, any) && (!forced || shape == g_force - 2)) f(shape);
 }
 
-Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
+Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any, bool shared = true)
 {
     Cut best;
     double least = 0;
     each_shape(gated, any, [&](int shape) {
         const int64_t tiles = cut_as(shape, 1, nr, nc, 1, gated).tiles();
-        each_split(ceil_div(nk, 64), nr, nc, tiles, MOST_WORKGROUPS - 16 - tiles, [&](int splits) {
+        each_split(shared ? ceil_div(nk, 64) : 1, nr, nc, tiles, MOST_WORKGROUPS - 16 - tiles, [&](int splits) {
             const Cut c = cut_as(shape, splits, nr, nc, 1, gated);
             const double t = fill_ns(shape, c.tiles() * splits, (double)ceil_div(nk, 64) / splits, 0, 0) + join_ns(c.part_bytes);
             if (least == 0 || t < least) { least = t; best = c; }
@@ -276,11 +265,6 @@ Cut least_forward(int64_t nr, int64_t nc, int64_t nk, bool gated, bool any)
     return best;
 }
 
-// The two products of a backward pass in one launch: both in tiles of one shape.
-struct BackCut {
-    Cut w, x;
-    bool x_first = false;
-};
 // rows, in, out as of the layer; problems: 2 for the gated pair
 BackCut least_back(int64_t rows, int64_t in, int64_t out, int problems, bool any, bool want_w, bool want_x)
 {
@@ -337,7 +321,7 @@ BackCut choose_back(int64_t rows, int64_t in, int64_t out, int problems, bool an
                              [&] { return least_back(rows, in, out, problems, any, want_w, want_x); });
 }
 
-bool is_few(int64_t rows) { return rows <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 1); }
+bool is_few_rows(int64_t rows) { return rows <= DLF_FF_FEW_ROWS && (g_force == 0 || g_force == 1); }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 // The workspace of a backward call: dz, partial column sums, partial sums of the products.  What the addresses are, and which gradients are
@@ -372,7 +356,7 @@ BackLayout back_layout(const Ff& f)
 
 size_t forward_ws(const Ff& f)
 {
-    if (f.d.rows == 0 || is_few(f.d.rows)) return 0;
+    if (f.d.rows == 0 || is_few_rows(f.d.rows)) return 0;
     const int64_t nr = f.d.rows, nc = f.d.out_features, nk = f.d.in_features;
     return align256(std::max(choose(nr, nc, nk, f.gated, false).part_bytes, choose(nr, nc, nk, f.gated, true).part_bytes));
 }
@@ -401,8 +385,11 @@ dlf_status forward(const Ff& f, const void* x, const void* const w[2], const flo
     a.out[0] = y; a.ldo = f.d.y_stride;
     a.saved = saved; a.act = f.d.act;
     TRY(kernels_ready());
-    if (is_few(a.nr)) return few_rows(f, a, f.gated, stream);
-    const bool whole = lines(a.p[0], a.ldp, a.nk) && (!f.gated || lines(a.p[1], a.ldp, a.nk)) && lines(a.q[0], a.ldq, a.nk);
+    if (is_few_rows(a.nr)) {
+        const DlfFfFew c = few_cut(a, f.gated);
+        return launched(f, dlf_ff_start_few(&a, &c, f.d.dtype, f.gated, stream));
+    }
+    const bool whole = dlf_ff_lines(a.p[0], a.ldp, a.nk) && (!f.gated || dlf_ff_lines(a.p[1], a.ldp, a.nk)) && dlf_ff_lines(a.q[0], a.ldq, a.nk);
     const Cut c = choose(a.nr, a.nc, a.nk, f.gated, !whole);
     set_cut(a, c, ws);
     return launched(f, dlf_ff_start_tile(&a, c.shape, f.d.dtype, f.gated, stream));
@@ -449,7 +436,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
         DlfFfArgs& a = b.x;
         for (int i = 0; i < nz; ++i) {
             a.p[i] = w[i]; a.q[i] = dz[i];
-            whole_x = whole_x && lines(w[i], f.d.w_stride, f.d.in_features) && lines(dz[i], lddz, f.d.out_features);
+            whole_x = whole_x && dlf_ff_lines(w[i], f.d.w_stride, f.d.in_features) && dlf_ff_lines(dz[i], lddz, f.d.out_features);
         }
         a.ldp = f.d.w_stride; a.ldq = lddz;
         a.nr = (int)f.d.rows; a.nc = f.d.in_features; a.nk = f.d.out_features;
@@ -463,7 +450,7 @@ dlf_status backward(const Ff& f, const void* dy, const void* x, const void* cons
             if (dw[i]) {
                 a.p[a.problems] = x; a.q[a.problems] = dz[i]; a.out[a.problems] = dw[i];
                 ++a.problems;
-                whole_w = whole_w && lines(x, f.d.x_stride, f.d.in_features) && lines(dz[i], lddz, f.d.out_features);
+                whole_w = whole_w && dlf_ff_lines(x, f.d.x_stride, f.d.in_features) && dlf_ff_lines(dz[i], lddz, f.d.out_features);
             }
         a.ldp = f.d.x_stride; a.ldq = lddz;
         a.nr = f.d.out_features; a.nc = f.d.in_features; a.nk = (int)f.d.rows;
@@ -499,6 +486,18 @@ size_t backward_bytes(const dlf_ff_desc* d, bool gated, const char* call)
 }
 
 }  // namespace
+
+// ---- for the products of other operators ----
+bool dlf_ff_is_few(int64_t rows) { return is_few_rows(rows); }
+DlfFfFew dlf_ff_few_cut(const DlfFfArgs& a) { return few_cut(a, false); }
+DlfFfCut dlf_ff_whole_cut(int64_t nr, int64_t nc, int64_t nk, bool any)
+{
+    return kept_cut<Cut>({nr, nc, nk, 4 + (any ? 1 : 0)}, [&] { return least_forward(nr, nc, nk, false, any, false); });
+}
+DlfFfBackCut dlf_ff_back_cut(int64_t rows, int64_t in, int64_t out, bool any, bool want_w, bool want_x)
+{
+    return choose_back(rows, in, out, 1, any, want_w, want_x);
+}
 
 extern "C" {
 

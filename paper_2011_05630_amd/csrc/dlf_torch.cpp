@@ -1,42 +1,11 @@
-// The feed-forward operators on PyTorch's tensors: checks of the operands, outputs, workspaces and the call of libdlf in one native step.
+// The feed-forward operators on PyTorch's tensors, and the module that holds them and the others: checks of the operands, outputs, workspaces and the call of libdlf in one native step.
 // (Small calls are bound by the host: a forward call takes 8.9 us with these steps in Python and ctypes, of which the launch is 3.4.)
 // PyTorch is used for its tensors and its allocator only.
-#include <ATen/ATen.h>
-#include <c10/core/AutogradState.h>
-#include <c10/core/DeviceGuard.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <torch/csrc/utils/pybind.h>
+#include "dlf_torch.h"
 
-#include <sstream>
-
-#include "../../include/dlf.h"
-
-namespace py = pybind11;
+using namespace dlf;
 
 namespace {
-
-template <typename... A> [[noreturn]] void refuse(const A&... a)
-{
-    std::ostringstream s;
-    (s << ... << a);
-    throw py::value_error(s.str());
-}
-
-// libdlf's refusal as the Python binding's exception.
-void check(dlf_status s)
-{
-    if (s == DLF_OK) return;
-    const py::object cls = py::module::import("paper_2011_05630_amd.binding").attr("DlfError");
-    const py::object e = cls((int)s, std::string(dlf_last_error()));
-    PyErr_SetObject(cls.ptr(), e.ptr());
-    throw py::error_already_set();
-}
-
-// An operand as rows: its address, how many, how far apart.
-struct Rows {
-    void* p;
-    int64_t rows, stride;
-};
 
 class Op {
 public:
@@ -91,8 +60,7 @@ public:
                        : dlf_linear(&d, xr.p, w_[0].data_ptr(), floats(b_[0]), rr.p, yr.p, sp, wp, need, (void*)stream);
         }
         check(s);
-        // (a tensor made in inference mode has no version)
-        if (!out.is_none() && !y.is_inference()) y.unsafeGetTensorImpl()->bump_version();
+        if (!out.is_none()) written(y);
         py::object first = out.is_none() ? wrap(y) : py::reinterpret_borrow<py::object>(out);
         if (!save) return first;
         return py::make_tuple(first, wrap(saved));
@@ -149,11 +117,7 @@ private:
     at::Tensor w_[2], b_[2];
 
     at::TensorOptions options(at::ScalarType t) const { return at::TensorOptions().dtype(t).device(device_); }
-    // (SIZE_MAX: the call itself will refuse the description, and say why)
-    at::Tensor workspace(size_t need) const { return need > 0 && need != SIZE_MAX ? at::empty({(int64_t)need}, options(at::kByte)) : at::Tensor(); }
-    static void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
-    static float* floats(const at::Tensor& t) { return t.defined() ? t.data_ptr<float>() : nullptr; }
-    static py::object wrap(const at::Tensor& t) { return t.defined() ? py::reinterpret_steal<py::object>(THPVariable_Wrap(t)) : py::none(); }
+    at::Tensor workspace(size_t need) const { return dlf::workspace(need, device_); }
 
     // The weights and biases are the caller's own tensors: an assignment to `.data`, a module's conversion among them, exchanges their
     // sizes, distances, type and device under this object, so that their form is looked at in every call.  (Values and addresses may change.)
@@ -173,23 +137,6 @@ private:
             if (b.defined()) usable(b, bn);
         }
     }
-    // Memory that holds the elements as they are (a view may leave their negation to the reader).
-    static bool readable(const at::Tensor& t) { return t.layout() == at::kStrided && !t.is_neg(); }
-    static void usable(const at::Tensor& t, const char* name)
-    {
-        // Automatic differentiation does not see the calls: what it would have to follow is refused rather than dropped.
-        if (t.requires_grad() && c10::AutogradState::get_tls_state().get_grad_mode())
-            refuse(name, ": requires a gradient, which automatic differentiation cannot take through this operator: call it under torch.no_grad(), "
-                         "gradients come from run_saved and backward");
-        if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
-            refuse(name, ": carries a tangent, which this operator cannot pass on");
-        // A storage may be freed or shortened under its tensors.
-        if (t.numel() > 0) {
-            int64_t last = t.storage_offset();
-            for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
-            if ((size_t)(last + 1) * t.itemsize() > t.storage().nbytes()) refuse(name, ": its storage no longer holds it");
-        }
-    }
     const at::Tensor& tensor(py::handle h, int64_t width, const char* name) const
     {
         if (THPVariable_Check(h.ptr())) {
@@ -207,25 +154,7 @@ private:
         if (!t.sizes().slice(0, t.dim() - 1).equals(x.sizes().slice(0, x.dim() - 1)))
             refuse(name, ": the leading dimensions of x expected, ", x.sizes().slice(0, x.dim() - 1));
     }
-    // The leading dimensions have to lie at one distance: each is its inner neighbour's size times its distance away.
-    static Rows rows(const at::Tensor& t, int64_t width, const char* name)
-    {
-        const auto sizes = t.sizes(), strides = t.strides();
-        const int64_t dims = t.dim();
-        Rows r = {t.data_ptr(), 1, width};
-        for (int64_t i = 0; i < dims - 1; ++i) r.rows *= sizes[i];
-        if (width != 1 && r.rows > 0 && strides[dims - 1] != 1) refuse(name, ": a row's elements have to lie next to each other");
-        if (r.rows <= 1) return r;
-        int64_t have = 1;                                   // rows of the dimensions passed, from the innermost
-        for (int64_t i = dims - 2; i >= 0; --i) {
-            if (sizes[i] == 1) continue;
-            if (have == 1) r.stride = strides[i];
-            else if (strides[i] != have * r.stride) refuse(name, ": its rows do not lie at one distance");
-            have *= sizes[i];
-        }
-        if (r.stride < width) refuse(name, ": rows overlap");
-        return r;
-    }
+    static Rows rows(const at::Tensor& t, int64_t width, const char* name) { return rows_of(t, width, name); }
     dlf_ff_desc desc(const Rows& x, int64_t ys, int64_t rs, int64_t ds) const
     {
         dlf_ff_desc d;
@@ -252,4 +181,6 @@ PYBIND11_MODULE(_dlf_torch, m)
         }))
         .def("backward", torch::wrap_pybind_function([](const Op& op, py::handle dy, py::handle x, py::handle saved, bool want_x, bool want_w, bool want_b,
                                                         int64_t stream) { return op.backward(dy, x, saved, want_x, want_w, want_b, stream); }));
+    bind_optimizer(m);
+    bind_loss(m);
 }
