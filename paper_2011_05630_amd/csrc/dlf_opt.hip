@@ -193,98 +193,190 @@ __device__ __forceinline__ uint32_t finite_bits(float x)
     return b < 0x7f800000u ? b : 0u;
 }
 
-struct Eight {
-    float g[8], p[8], m[8], v[8];
-    uint32_t m8[2], v8[2];
-    float ms, vs;
+// What a launch's threads share.
+struct Step {
+    float factor, by, root, rate;
+    uint32_t key;
 };
+// Eight consecutive elements on their way: of a type that the compiler knows they are loaded first and converted when they are used; loads and
+// conversions behind a branch on the type would wait for each other.
+template <int TYPE> struct Raw {
+    float f[8];
+    __device__ __forceinline__ void load(const void* base, int64_t at)
+    {
+        __builtin_memcpy(f, (const char*)base + at * (TYPE == DLF_F32 ? 4 : 2), TYPE == DLF_F32 ? 32 : 16);
+    }
+    __device__ __forceinline__ void to(float (&out)[8]) const
+    {
+        uint16_t h[8];
+        __builtin_memcpy(h, f, 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            out[i] = TYPE == DLF_F32 ? f[i] : TYPE == DLF_BF16 ? from_bf16(h[i]) : (float)__builtin_bit_cast(_Float16, h[i]);
+    }
+};
+// The square root by its instruction, off by a unit of the last place; numbers near the end of the range are brought up for it.  (Its result is none near the
+// end, so that the reciprocal's instruction takes it as it is.  Root and quotient correctly rounded: 2.5 times the instructions of the whole update.)
+__device__ __forceinline__ float root_of(float x)
+{
+    const bool small = x < 0x1p-96f;
+    const float r = __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x);
+    return small ? r * 0x1p-32f : r;
+}
+// m', v' of eight elements, and p'.
+__device__ __forceinline__ void update(const DlfStepArgs& a, const Step& w, float away, const float (&g)[8], float (&p)[8], float (&m)[8], float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma clang fp contract(off)
+        const float q = a.factor != nullptr ? g[i] * w.factor : g[i];
+        m[i] = a.b1 * m[i] + a.c1 * q;
+        v[i] = a.b2 * v[i] + a.c2 * q * q;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)                             // (a factor 1 - rate decay would be rounded by a good part of what it takes off)
+        p[i] -= __builtin_fmaf(p[i], away, w.by * m[i] * __builtin_amdgcn_rcpf(root_of(v[i] * w.root) + a.eps));
+}
+// The states of eight elements in 8 bits; the eight lanes of a block are here together.
+__device__ __forceinline__ void store_small(const DlfStepArgs& a, const Step& w, int64_t st, const float (&m)[8], const float (&v)[8])
+{
+    uint32_t bm = 0, bv = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t qm = finite_bits(m[i]), qv = finite_bits(v[i]);
+        bm = bm > qm ? bm : qm;
+        bv = bv > qv ? bv : qv;
+    }
+    const uint32_t sm = scale_of<8>(max_of_8(bm)), sv = scale_of<15>(max_of_8(bv));
+    const float im = __builtin_bit_cast(float, (254u << 23) - sm), iv = __builtin_bit_cast(float, (254u << 23) - sv);
+    const uint32_t mine = w.key ^ stir((uint32_t)((uint64_t)st >> 32));
+    uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t h = stir((uint32_t)(st + i) ^ mine);
+        wm[i >> 2] |= code_of<3, -6, false>(m[i], im, h >> 16) << (i & 3) * 8;
+        wv[i >> 2] |= code_of<2, -14, true>(v[i], iv, h & 0xffffu) << (i & 3) * 8;
+    }
+    __builtin_memcpy((char*)a.m + st, wm, 8);
+    __builtin_memcpy((char*)a.v + st, wv, 8);
+    if ((threadIdx.x & 7) == 0) {
+        a.m_scale[st >> 6] = __builtin_bit_cast(float, sm);
+        a.v_scale[st >> 6] = __builtin_bit_cast(float, sv);
+    }
+}
+// A whole chunk, of known types.
+template <bool SMALL, int G, int P, int C> __device__ __forceinline__ void whole_chunk(const DlfStepArgs& a, const Step& w, const DlfOptChunk& c, const void* g)
+{
+    // eight elements a thread at a time, or sixteen: with states in 8 bits more waves share a compute unit instead
+    constexpr int UNITS = SMALL ? 1 : DLF_OPT_CHUNK / 2048;
+    const float away = w.rate * c.decay;
+#pragma unroll 1
+    for (int from = (int)threadIdx.x * 8; from < DLF_OPT_CHUNK; from += UNITS * 2048) {
+        Raw<G> rg[UNITS];
+        Raw<P> rp[UNITS];
+        float m[UNITS][8], v[UNITS][8], ms[UNITS], vs[UNITS];
+        uint32_t m8[UNITS][2], v8[UNITS][2];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int e = from + u * 2048;
+            const int64_t st = c.state + e;
+            rg[u].load(g, c.at + e);
+            rp[u].load(c.p, e);
+            if (SMALL) {
+                __builtin_memcpy(m8[u], (const char*)a.m + st, 8);
+                __builtin_memcpy(v8[u], (const char*)a.v + st, 8);
+                ms[u] = a.m_scale[st >> 6];
+                vs[u] = a.v_scale[st >> 6];
+            } else {
+                __builtin_memcpy(m[u], (const float*)a.m + st, 32);
+                __builtin_memcpy(v[u], (const float*)a.v + st, 32);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int e = from + u * 2048;
+            const int64_t st = c.state + e;
+            float gf[8], pf[8];
+            rg[u].to(gf);
+            rp[u].to(pf);
+            if (SMALL) {
+                decode8<false>(m8[u], ms[u], m[u]);
+                decode8<true>(v8[u], vs[u], v[u]);
+            }
+            update(a, w, away, gf, pf, m[u], v[u]);
+            store8(c.p, e, 8, P, pf);
+            if (C >= 0) store8(c.c, e, 8, C, pf);
+            if (SMALL) {
+                store_small(a, w, st, m[u], v[u]);
+            } else {
+                store8(a.m, st, 8, DLF_F32, m[u]);
+                store8(a.v, st, 8, DLF_F32, v[u]);
+            }
+        }
+    }
+}
+// A tensor's last chunk, of any types.
+template <bool SMALL> __device__ __forceinline__ void last_chunk(const DlfStepArgs& a, const Step& w, const DlfOptChunk& c, const void* g, int g_type)
+{
+    const float away = w.rate * c.decay;
+    for (int e = (int)threadIdx.x * 8; SMALL ? (e & ~63) < c.n : e < c.n; e += 2048) {   // (the eight lanes of a block of 64 stay together)
+        const int n = c.n - e;
+        const int64_t st = c.state + e;
+        float gf[8], pf[8], m[8], v[8];
+        load8(g, c.at + e, n, g_type, gf);
+        load8(c.p, e, n, c.p_type, pf);
+        if (SMALL) {
+            uint32_t m8[2], v8[2];
+            __builtin_memcpy(m8, (const char*)a.m + st, 8);
+            __builtin_memcpy(v8, (const char*)a.v + st, 8);
+            decode8<false>(m8, a.m_scale[st >> 6], m);
+            decode8<true>(v8, a.v_scale[st >> 6], v);
+        } else {
+            load8(a.m, st, n, DLF_F32, m);
+            load8(a.v, st, n, DLF_F32, v);
+        }
+        update(a, w, away, gf, pf, m, v);
+        store8(c.p, e, n, c.p_type, pf);
+        if (c.c != nullptr) store8(c.c, e, n, c.c_type, pf);
+        if (SMALL) {
+            store_small(a, w, st, m, v);
+        } else {
+            store8(a.m, st, n, DLF_F32, m);
+            store8(a.v, st, n, DLF_F32, v);
+        }
+    }
+}
+template <bool SMALL, int G> __device__ __forceinline__ void whole_chunk_of(const DlfStepArgs& a, const Step& w, const DlfOptChunk& c, const void* g)
+{
+    if (c.p_type == DLF_F32) {
+        if (c.c == nullptr) whole_chunk<SMALL, G, DLF_F32, -1>(a, w, c, g);
+        else if (c.c_type == DLF_BF16) whole_chunk<SMALL, G, DLF_F32, DLF_BF16>(a, w, c, g);
+        else whole_chunk<SMALL, G, DLF_F32, DLF_F16>(a, w, c, g);
+    } else if (c.p_type == DLF_BF16) whole_chunk<SMALL, G, DLF_BF16, -1>(a, w, c, g);
+    else whole_chunk<SMALL, G, DLF_F16, -1>(a, w, c, g);
+}
 
 template <bool SMALL>
 __global__ __launch_bounds__(256) void k_step(const DlfStepArgs a)
 {
-    const float factor = a.factor != nullptr ? *a.factor : 1.0f;
-    if (!(fabsf(factor) <= 3.402823466e38f)) return;        // a step that is to be left out
+    Step w;
+    w.factor = a.factor != nullptr ? *a.factor : 1.0f;
+    if (!(fabsf(w.factor) <= 3.402823466e38f)) return;      // a step that is to be left out
     const double t0 = a.counter[0], p1 = a.counter[1] * a.beta1, p2 = a.counter[2] * a.beta2;
-    const float rate = a.rate_at != nullptr ? *a.rate_at : a.rate;
-    const float by = (float)((double)rate / (1.0 - p1)), root = (float)(1.0 / (1.0 - p2));
-    const uint32_t key = SMALL ? stir(stir(a.seed) + (uint32_t)(int64_t)t0) : 0u;
+    w.rate = a.rate_at != nullptr ? *a.rate_at : a.rate;
+    w.by = (float)((double)w.rate / (1.0 - p1));
+    w.root = (float)(1.0 / (1.0 - p2));
+    w.key = SMALL ? stir(stir(a.seed) + (uint32_t)(int64_t)t0) : 0u;
     for (int k = blockIdx.x; k < a.chunks; k += gridDim.x) {
         const DlfOptChunk c = a.table[k];
         const int tensor = c.tensor - a.first_tensor;
         const void* const g = a.g[tensor];
         if (g == nullptr) continue;
         const int g_type = a.type[tensor];
-        const float away = rate * c.decay;
-        constexpr int UNITS = DLF_OPT_CHUNK / 2048;
-        Eight x[UNITS];
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            const int e = u * 2048 + (int)threadIdx.x * 8, n = c.n - e;
-            const int64_t st = c.state + e;
-            if (SMALL ? (e & ~63) < c.n : n > 0) {          // the eight lanes of a block of 64 stay together
-                if (SMALL) {
-                    __builtin_memcpy(x[u].m8, (const char*)a.m + st, 8);
-                    __builtin_memcpy(x[u].v8, (const char*)a.v + st, 8);
-                    x[u].ms = a.m_scale[st >> 6];
-                    x[u].vs = a.v_scale[st >> 6];
-                } else {
-                    load8(a.m, st, n, DLF_F32, x[u].m);
-                    load8(a.v, st, n, DLF_F32, x[u].v);
-                }
-                load8(g, c.at + e, n, g_type, x[u].g);
-                load8(c.p, e, n, c.p_type, x[u].p);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            const int e = u * 2048 + (int)threadIdx.x * 8, n = c.n - e;
-            const int64_t st = c.state + e;
-            if (!(SMALL ? (e & ~63) < c.n : n > 0)) continue;
-            if (SMALL) {
-                decode8<false>(x[u].m8, x[u].ms, x[u].m);
-                decode8<true>(x[u].v8, x[u].vs, x[u].v);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma clang fp contract(off)
-                const float q = a.factor != nullptr ? x[u].g[i] * factor : x[u].g[i];
-                x[u].m[i] = a.b1 * x[u].m[i] + a.c1 * q;
-                x[u].v[i] = a.b2 * x[u].v[i] + a.c2 * q * q;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)                     // (a factor 1 - rate decay would be rounded by a good part of what it takes off)
-                x[u].p[i] -= __builtin_fmaf(x[u].p[i], away, by * x[u].m[i] / (sqrtf(x[u].v[i] * root) + a.eps));
-            store8(c.p, e, n, c.p_type, x[u].p);
-            if (c.c != nullptr) store8(c.c, e, n, c.c_type, x[u].p);
-            if (SMALL) {
-                uint32_t bm = 0, bv = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t qm = finite_bits(x[u].m[i]), qv = finite_bits(x[u].v[i]);
-                    bm = bm > qm ? bm : qm;
-                    bv = bv > qv ? bv : qv;
-                }
-                const uint32_t sm = scale_of<8>(max_of_8(bm)), sv = scale_of<15>(max_of_8(bv));
-                const float im = __builtin_bit_cast(float, (254u << 23) - sm), iv = __builtin_bit_cast(float, (254u << 23) - sv);
-                const uint32_t mine = key ^ stir((uint32_t)((uint64_t)st >> 32));
-                uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t h = stir((uint32_t)(st + i) ^ mine);
-                    wm[i >> 2] |= code_of<3, -6, false>(x[u].m[i], im, h >> 16) << (i & 3) * 8;
-                    wv[i >> 2] |= code_of<2, -14, true>(x[u].v[i], iv, h & 0xffffu) << (i & 3) * 8;
-                }
-                __builtin_memcpy((char*)a.m + st, wm, 8);
-                __builtin_memcpy((char*)a.v + st, wv, 8);
-                if ((threadIdx.x & 7) == 0) {
-                    a.m_scale[st >> 6] = __builtin_bit_cast(float, sm);
-                    a.v_scale[st >> 6] = __builtin_bit_cast(float, sv);
-                }
-            } else {
-                store8(a.m, st, n, DLF_F32, x[u].m);
-                store8(a.v, st, n, DLF_F32, x[u].v);
-            }
-        }
+        if (c.n < DLF_OPT_CHUNK) last_chunk<SMALL>(a, w, c, g, g_type);
+        else if (g_type == DLF_F32) whole_chunk_of<SMALL, DLF_F32>(a, w, c, g);
+        else if (g_type == DLF_BF16) whole_chunk_of<SMALL, DLF_BF16>(a, w, c, g);
+        else whole_chunk_of<SMALL, DLF_F16>(a, w, c, g);
     }
     if (a.last == 0) return;
     // every workgroup has read the counter when the last of them arrives here
