@@ -30,6 +30,8 @@ dlf_status fail(dlf_status s, const char* fmt, ...)
 
 constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;       // a launch holds fewer than 2^32 threads, 256 to a workgroup
 constexpr int64_t LEAST_PIECE = 256, MOST_PIECE = 1 << 16;  // rows
+// Operands whose rows start anywhere are copied to rows of whole lines from so many rows on, for the products of a loss and of gradients.
+constexpr int64_t PACK_LOSS = 512, PACK_GRADIENTS = 128;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -39,6 +41,8 @@ struct Ce {
     dlf_ce_desc d;
     const char* call;
     int64_t ldz, piece;     // elements of a row of dz; rows
+    int64_t lines;          // 16-byte parts of a row of x or weight
+    bool pack_x, pack_w;    // copied to rows of whole lines
     int64_t pieces() const { return std::max<int64_t>(1, ceil_div(d.rows, piece)); }
     int64_t first(int64_t p) const { return p * piece; }
     int64_t rows(int64_t p) const { return std::min(piece, d.rows - p * piece); }
@@ -52,7 +56,7 @@ bool launches(int64_t rows, int64_t in, int64_t classes)
            rows * ceil_div(classes, DLF_CE_DZ_COLS) < MOST_WORKGROUPS - 16;
 }
 
-dlf_status check_desc(const dlf_ce_desc* d, const char* call, Ce& f)
+dlf_status check_desc(const dlf_ce_desc* d, bool gradients, const char* call, Ce& f)
 {
     if (!d) return fail(DLF_ERR_INVALID_ARG, "%s: null description", call);
     f.d = *d;
@@ -78,6 +82,10 @@ dlf_status check_desc(const dlf_ce_desc* d, const char* call, Ce& f)
     // pieces of about one size
     const int64_t n = std::max<int64_t>(1, ceil_div(d->rows, f.piece));
     f.piece = std::max(LEAST_PIECE, ceil_div(ceil_div(d->rows, n), LEAST_PIECE) * LEAST_PIECE);
+    f.lines = ceil_div(d->in_features, 8);
+    const bool pays = d->rows >= (gradients ? PACK_GRADIENTS : PACK_LOSS) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
+    f.pack_x = pays && !dlf_ff_lines(nullptr, f.d.x_stride, d->in_features);
+    f.pack_w = pays && !dlf_ff_lines(nullptr, f.d.w_stride, d->in_features);
     return DLF_OK;
 }
 
@@ -122,7 +130,7 @@ int64_t parts_of(const Ce& f, const DlfFfCut& c) { return ceil_div(f.d.classes, 
 
 // What a call keeps in the workspace, for its largest piece (column sums: for all of them); addresses are not known where its size is asked for.
 struct Layout {
-    size_t part = 0, at = 0, lse = 0, unit = 0, dz = 0, sums = 0, sum = 0, join = 0, bytes = 0;
+    size_t x = 0, w = 0, part = 0, at = 0, lse = 0, unit = 0, dz = 0, sums = 0, sum = 0, join = 0, bytes = 0;
     size_t take(size_t n)
     {
         const size_t here = bytes;
@@ -145,6 +153,8 @@ Layout layout_of(const Ce& f, bool logits, bool gradients)
             if (dlf_ff_is_few(rows)) parts = std::max(parts, ceil_div(ceil_div(nc, 16) * rows, most));
             chunks = std::max<int64_t>(chunks, (int64_t)c.tiles_r * 2);
         }
+    if (f.pack_x) l.x = l.take((size_t)most * f.lines * 16);
+    if (f.pack_w) l.w = l.take((size_t)nc * f.lines * 16);
     if (logits) {
         l.part = l.take((size_t)parts * most * 8);
         l.at = l.take((size_t)most * 4);
@@ -171,21 +181,50 @@ struct In {
     const void *x, *w;
     const float* bias;
     const int64_t* target;
-    const char* x_at(const Ce& f, int64_t row) const { return (const char*)x + row * f.d.x_stride * 2; }
 };
-bool whole_lines(const Ce& f, const In& in)
+// ... those of a piece, as its products read them.
+struct Piece {
+    int64_t first, rows;
+    const void *x, *w;
+    int64_t ldx, ldw;
+    bool whole;             // rows of whole lines
+};
+dlf_status piece_of(const Ce& f, const In& in, int64_t p, const Layout& l, char* ws, Piece& q, void* stream)
 {
-    return dlf_ff_lines(in.w, f.d.w_stride, f.d.in_features) && dlf_ff_lines(in.x, f.d.x_stride, f.d.in_features);
+    q.first = f.first(p);
+    q.rows = f.rows(p);
+    q.x = (const char*)in.x + q.first * f.d.x_stride * 2;
+    q.w = in.w;
+    q.ldx = f.d.x_stride;
+    q.ldw = f.d.w_stride;
+    const bool x = dlf_ff_lines(in.x, q.ldx, f.d.in_features), w = dlf_ff_lines(in.w, q.ldw, f.d.in_features);
+    q.whole = (x || f.pack_x) && (w || f.pack_w);
+    if (!q.whole || (x && w) || q.rows == 0) return DLF_OK;
+    DlfCePackArgs a;
+    memset(&a, 0, sizeof a);
+    a.k = f.d.in_features;
+    a.parts = (int)f.lines;
+    if (f.pack_x) {
+        a.m[0] = {q.x, ws + l.x, q.ldx, q.rows};
+        q.x = ws + l.x;
+        q.ldx = f.lines * 8;
+    }
+    if (f.pack_w) {
+        if (p == 0) a.m[1] = {q.w, ws + l.w, q.ldw, f.d.classes};
+        q.w = ws + l.w;
+        q.ldw = f.lines * 8;
+    }
+    return a.m[0].rows + a.m[1].rows > 0 ? launched(f, dlf_ce_start_pack(&a, stream)) : DLF_OK;
 }
-void product(const Ce& f, const In& in, int64_t first, int64_t rows, DlfCeArgs& a)
+void product(const Ce& f, const In& in, const Piece& q, DlfCeArgs& a)
 {
     memset(&a, 0, sizeof a);
-    a.t.p[0] = in.w; a.t.q[0] = in.x_at(f, first);
-    a.t.ldp = f.d.w_stride; a.t.ldq = f.d.x_stride;
-    a.t.nr = (int)rows; a.t.nc = f.d.classes; a.t.nk = f.d.in_features;
+    a.t.p[0] = q.w; a.t.q[0] = q.x;
+    a.t.ldp = q.ldw; a.t.ldq = q.ldx;
+    a.t.nr = (int)q.rows; a.t.nc = f.d.classes; a.t.nk = f.d.in_features;
     a.t.segments = a.t.problems = a.t.splits = 1;
     a.t.bias[0] = in.bias;
-    a.target = in.target + first;
+    a.target = in.target + q.first;
     a.ignore = f.d.ignore;
     a.ldz = f.ldz;
 }
@@ -195,26 +234,29 @@ void set_cut(DlfFfArgs& a, const DlfFfCut& c)
     a.tiles_c = c.tiles_c;
 }
 
-// Loss and lse of a piece (either may be null); keep: the exponentials too, in dz.  -> the classes of a part
-dlf_status logits(const Ce& f, const In& in, int64_t first, int64_t rows, bool keep, const Layout& l, char* ws, float* loss, float* lse, int& width,
-                  void* stream)
+// The parts of a piece's rows; keep: the exponentials too, in dz.  -> the classes of a part
+dlf_status logits(const Ce& f, const In& in, const Piece& q, bool keep, const Layout& l, char* ws, int& width, void* stream)
 {
     DlfCeArgs a;
-    product(f, in, first, rows, a);
+    product(f, in, q, a);
     a.part = (float*)(ws + l.part);
     a.at = (float*)(ws + l.at);
-    if (!keep && dlf_ff_is_few(rows)) {
+    if (!keep && dlf_ff_is_few(q.rows)) {
         const DlfFfFew c = dlf_ff_few_cut(a.t);
         width = 16;
-        TRY(launched(f, dlf_ce_start_few(&a, &c, f.d.dtype, stream)));
-    } else {
-        const DlfFfCut c = cut_of(f, rows, !whole_lines(f, in));
-        set_cut(a.t, c);
-        if (keep) a.dz = ws + l.dz;
-        width = dlf_ce_width(c.shape);
-        TRY(launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : DLF_CE_STAT, stream)));
+        return launched(f, dlf_ce_start_few(&a, &c, f.d.dtype, stream));
     }
-    const DlfCeJoinArgs j = {a.part, a.at, a.target, a.ignore, (int)ceil_div(f.d.classes, width), (int)rows, f.d.classes, loss, lse};
+    const DlfFfCut c = cut_of(f, q.rows, !q.whole);
+    set_cut(a.t, c);
+    if (keep) a.dz = ws + l.dz;
+    width = dlf_ce_width(c.shape);
+    return launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : DLF_CE_STAT, stream));
+}
+// ... and from them loss and lse, either of which may be null.
+dlf_status join(const Ce& f, const In& in, const Piece& q, const Layout& l, char* ws, int width, float* loss, float* lse, void* stream)
+{
+    const DlfCeJoinArgs j = {(const float*)(ws + l.part), (const float*)(ws + l.at), in.target + q.first, f.d.ignore, (int)ceil_div(f.d.classes, width),
+                             (int)q.rows, f.d.classes, loss, lse};
     return launched(f, dlf_ce_start_join(&j, stream));
 }
 
@@ -227,41 +269,55 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
 {
     const Layout l = layout_of(f, lse == nullptr, true);
     const int64_t pieces = f.pieces(), nc = f.d.classes, k = f.d.in_features;
+    const bool wanted = out.dx || out.dw || out.db;
     TRY(kernels_ready());
-    if (f.d.rows > 0 && f.d.dtype == DLF_F16 && (out.dx || out.dw || out.db)) {
+    if (!given.dlse && (!given.dloss || given.dloss_stride == 0)) {
+        given.one = f.d.dtype == DLF_F16 ? 16384.0f : 1.0f;
+    } else if (f.d.rows > 0 && f.d.dtype == DLF_F16 && wanted) {
         const DlfCeUnitArgs u = {given, f.d.rows, (float*)(ws + l.unit)};
         TRY(launched(f, dlf_ce_start_unit(&u, stream)));
         given.unit = u.unit;
     }
-    const bool whole = whole_lines(f, in);
+    float* const back = given.one > 0.0f && f.d.rows > 0 && wanted ? (float*)(ws + l.unit) : nullptr;
+    // The exponentials are kept where they need not say what the bias's gradient is, which has 32 bits.
+    const bool keep = !lse && wanted && !out.db;
     int chunks = 0;
     for (int64_t p = 0; p < pieces; ++p) {
-        const int64_t first = f.first(p), rows = f.rows(p);
+        Piece q;
+        TRY(piece_of(f, in, p, l, ws, q, stream));
         DlfCeGiven g = given;
-        if (g.dloss) g.dloss += first * g.dloss_stride;
-        if (g.dlse) g.dlse += first * g.dlse_stride;
-        const float* piece_lse = lse ? lse + first : nullptr;
-        if (rows > 0) {
-            // the exponentials are kept where they need not say what the bias's gradient is, which has 32 bits
-            const bool wanted = out.dx || out.dw || out.db, keep = !lse && wanted && !out.db;
+        if (g.dloss) g.dloss += q.first * g.dloss_stride;
+        if (g.dlse) g.dlse += q.first * g.dlse_stride;
+        if (q.rows > 0) {
+            const float* piece_lse = lse ? lse + q.first : nullptr;
+            float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
-            if (!lse) {
+            if (!lse) TRY(logits(f, in, q, keep, l, ws, width, stream));
+            if (!lse && !keep) {
                 float* const to = (float*)(ws + l.lse);
-                TRY(logits(f, in, first, rows, keep, l, ws, loss ? loss + first : nullptr, to, width, stream));
+                TRY(join(f, in, q, l, ws, width, piece_loss, to, stream));
                 piece_lse = to;
             }
             if (!wanted) continue;
             if (keep) {
-                const DlfCeDzArgs z = {ws + l.dz, f.ldz, (const float*)(ws + l.part), width, (int)rows, (int)nc, in.target + first, f.d.ignore, piece_lse, g};
+                const int64_t slices = ceil_div(f.ldz, DLF_CE_DZ_COLS);
+                float* to = nullptr;                        // (workgroups that do not run at once do not form their rows' lse)
+                if (q.rows * slices > 2048) {
+                    to = (float*)(ws + l.lse);
+                    TRY(join(f, in, q, l, ws, width, piece_loss, to, stream));
+                }
+                const DlfCeDzArgs z = {ws + l.dz, f.ldz, (const float*)(ws + l.part), (const float*)(ws + l.at), (int)ceil_div(nc, width), width, (int)q.rows,
+                                       (int)nc, (int)slices, in.target + q.first, f.d.ignore, to, piece_loss, g, back};
                 TRY(launched(f, dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else {
                 DlfCeArgs a;
-                product(f, in, first, rows, a);
-                const DlfFfCut c = cut_of(f, rows, !whole);
+                product(f, in, q, a);
+                const DlfFfCut c = cut_of(f, q.rows, !q.whole);
                 set_cut(a.t, c);
                 a.dz = ws + l.dz;
                 a.lse = piece_lse;
                 a.given = g;
+                a.back = back;
                 if (out.db) a.sums = (float*)(ws + l.sums) + (size_t)chunks * nc;
                 chunks += c.tiles_r * 2;
                 TRY(launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, DLF_CE_DZ, stream)));
@@ -271,21 +327,21 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         memset(&e, 0, sizeof e);
         DlfFfBackArgs& b = e.b;
         b.w.splits = b.x.splits = 1;
-        const bool last = p == pieces - 1, want_x = out.dx && rows > 0, want_w = out.dw != nullptr;
-        const char* const dz = rows > 0 ? ws + l.dz : nullptr;
+        const bool last = p == pieces - 1, want_x = out.dx && q.rows > 0, want_w = out.dw != nullptr;
+        const char* const dz = q.rows > 0 ? ws + l.dz : nullptr;
         if (want_x) {
             DlfFfArgs& a = b.x;
-            a.p[0] = in.w; a.q[0] = dz;
-            a.ldp = f.d.w_stride; a.ldq = f.ldz;
-            a.nr = (int)rows; a.nc = (int)k; a.nk = (int)nc;
+            a.p[0] = q.w; a.q[0] = dz;
+            a.ldp = q.ldw; a.ldq = f.ldz;
+            a.nr = (int)q.rows; a.nc = (int)k; a.nk = (int)nc;
             a.segments = a.problems = 1;
-            a.out[0] = (char*)out.dx + first * k * 2; a.ldo = k;
+            a.out[0] = (char*)out.dx + q.first * k * 2; a.ldo = k;
         }
         if (want_w) {
             DlfFfArgs& a = b.w;
-            a.p[0] = in.x_at(f, first); a.q[0] = dz;
-            a.ldp = f.d.x_stride; a.ldq = f.ldz;
-            a.nr = (int)nc; a.nc = (int)k; a.nk = (int)rows;
+            a.p[0] = q.x; a.q[0] = dz;
+            a.ldp = q.ldx; a.ldq = f.ldz;
+            a.nr = (int)nc; a.nc = (int)k; a.nk = (int)q.rows;
             a.segments = a.problems = 1;
             a.out[0] = out.dw; a.ldo = k;
         }
@@ -298,7 +354,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         }
         if (!want_x && !want_w && b.sum.blocks == 0) continue;
         // (dz has rows of whole lines, zeros behind the last class: only the other operands decide)
-        const DlfFfBackCut c = dlf_ff_back_cut(std::max<int64_t>(1, rows), k, nc, (want_x || want_w) && !whole, want_w, want_x);
+        const DlfFfBackCut c = dlf_ff_back_cut(std::max<int64_t>(1, q.rows), k, nc, (want_x || want_w) && !q.whole, want_w, want_x);
         b.x_first = c.x_first;
         set_cut(b.w, c.w);
         set_cut(b.x, c.x);
@@ -308,7 +364,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         b.x.part = (float*)(ws + l.join + align256(c.w.part_bytes));
         if (!want_w) { b.w.problems = 0; b.w.splits = 1; }
         if (!want_x) { b.x.problems = 0; b.x.splits = 1; }
-        e.inverse = given.unit ? given.unit + 1 : nullptr;
+        e.back = back ? back : given.unit ? given.unit + 1 : nullptr;
         if (want_w && pieces > 1) {
             e.sum = (float*)(ws + l.sum);
             e.add = p > 0;
@@ -322,7 +378,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
 size_t bytes_of(const dlf_ce_desc* d, bool logits, bool gradients, const char* call)
 {
     Ce f;
-    return check_desc(d, call, f) == DLF_OK ? layout_of(f, logits, gradients).bytes : SIZE_MAX;
+    return check_desc(d, gradients, call, f) == DLF_OK ? layout_of(f, logits, gradients).bytes : SIZE_MAX;
 }
 dlf_status check_in(const Ce& f, const In& in)
 {
@@ -360,7 +416,7 @@ dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* we
                              float* lse, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     Ce f;
-    TRY(check_desc(d, "dlf_cross_entropy", f));
+    TRY(check_desc(d, false, "dlf_cross_entropy", f));
     const In in = {x, weight, bias, target};
     TRY(check_in(f, in));
     TRY(check_ptr(f, loss, "loss", f.d.rows > 0, 4));
@@ -370,8 +426,11 @@ dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* we
     if (f.d.rows == 0) return DLF_OK;
     TRY(kernels_ready());
     for (int64_t p = 0; p < f.pieces(); ++p) {
+        Piece q;
         int width;
-        TRY(logits(f, in, f.first(p), f.rows(p), false, l, (char*)workspace, loss + f.first(p), lse ? lse + f.first(p) : nullptr, width, hip_stream));
+        TRY(piece_of(f, in, p, l, (char*)workspace, q, hip_stream));
+        TRY(logits(f, in, q, false, l, (char*)workspace, width, hip_stream));
+        TRY(join(f, in, q, l, (char*)workspace, width, loss + q.first, lse ? lse + q.first : nullptr, hip_stream));
     }
     return DLF_OK;
 }
@@ -382,9 +441,9 @@ dlf_status dlf_cross_entropy_backward(const dlf_ce_desc* d, const void* x, const
                                       void* hip_stream)
 {
     Ce f;
-    TRY(check_desc(d, "dlf_cross_entropy_backward", f));
+    TRY(check_desc(d, true, "dlf_cross_entropy_backward", f));
     const In in = {x, weight, bias, target};
-    const DlfCeGiven given = {dloss, dlse, dloss_stride, dlse_stride, dloss_value, nullptr};
+    const DlfCeGiven given = {dloss, dlse, dloss_stride, dlse_stride, dloss_value, nullptr, 0.0f};
     const Out out = {dx, dweight, dbias};
     TRY(check_in(f, in));
     TRY(check_ptr(f, lse, "lse", f.d.rows > 0, 4));
@@ -400,9 +459,9 @@ dlf_status dlf_cross_entropy_gradients(const dlf_ce_desc* d, const void* x, cons
                                        float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     Ce f;
-    TRY(check_desc(d, "dlf_cross_entropy_gradients", f));
+    TRY(check_desc(d, true, "dlf_cross_entropy_gradients", f));
     const In in = {x, weight, bias, target};
-    const DlfCeGiven given = {dloss, nullptr, dloss_stride, 0, dloss_value, nullptr};
+    const DlfCeGiven given = {dloss, nullptr, dloss_stride, 0, dloss_value, nullptr, 0.0f};
     const Out out = {dx, dweight, dbias};
     TRY(check_in(f, in));
     TRY(check_given(f, given));

@@ -12,6 +12,17 @@ struct DlfCeGiven {
     int64_t dloss_stride, dlse_stride;
     float dloss_value;
     const float* unit;          // {a power of two that dz is scaled by, its inverse}, or null
+    float one;                  // > 0: dloss is the same for all rows and there is no dlse: dz is formed for a dloss of so much, see k_ce_back
+};
+// A matrix copied to rows of whole 16-byte lines, zeros behind column k.
+struct DlfCePack {
+    const void* from;
+    void* to;
+    int64_t stride, rows;       // no rows: nothing
+};
+struct DlfCePackArgs {
+    DlfCePack m[2];
+    int32_t k, parts;           // columns; lines of a row
 };
 struct DlfCeArgs {
     DlfFfArgs t;                // p: weight, q: x, bias
@@ -24,6 +35,7 @@ struct DlfCeArgs {
     const float* lse;
     DlfCeGiven given;
     float* sums;                // [chunks][nc] column sums of dz, in 32 bits, or null
+    float* back;                // what the products of dz are to be scaled by goes here, or null
 };
 struct DlfCeJoinArgs {
     const float* part;
@@ -37,12 +49,16 @@ struct DlfCeDzArgs {
     void* dz;                   // KEEP's in, dz out
     int64_t ldz;
     const float* part;
-    int32_t width;              // classes of a part
+    const float* at;
+    int32_t parts, width;       // classes of a part
     int32_t nr, nc;
+    int32_t slices;             // workgroups of a row, DLF_CE_DZ_COLS columns each
     const int64_t* target;
     int64_t ignore;
-    const float* lse;
+    const float* lse;           // or null: lse and loss are formed here
+    float* loss;
     DlfCeGiven given;
+    float* back;                // as in DlfCeArgs
 };
 struct DlfCeUnitArgs {
     DlfCeGiven given;
@@ -51,7 +67,7 @@ struct DlfCeUnitArgs {
 };
 struct DlfCeBackArgs {
     DlfFfBackArgs b;
-    const float* inverse;       // the products are scaled by it; or null
+    const float* back;          // the products are scaled by it; or null
     float* sum;                 // [classes][in] the weight's gradient over the pieces in front, or null
     int32_t add, keep;
 };
@@ -59,7 +75,7 @@ struct DlfCeBackArgs {
 static inline int dlf_ce_width(int shape) { return DLF_FF_SHAPES[shape].bc / 2; }
 static inline int dlf_ce_chunk(int shape) { return DLF_FF_SHAPES[shape].br / 2; }
 // Rows of a workgroup of k_ce_join, and up to how many rows a workgroup has one.
-#define DLF_CE_JOIN_ROWS 32
+#define DLF_CE_JOIN_ROWS 16
 #define DLF_CE_JOIN_FEW 256
 // Columns of a workgroup of k_ce_dz.
 #define DLF_CE_DZ_COLS 2048
@@ -70,6 +86,7 @@ int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int dtype, int mode, void* 
 int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int dtype, void* stream);
 int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream);
 int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream);
+int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream);
 int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream);
 int dlf_ce_start_back(const DlfCeBackArgs* a, int shape, int dtype, void* stream);
 }

@@ -12,6 +12,18 @@
 // exp(d).  d is rounded before it is multiplied: a maximum times log2(e), rounded, would shift all of a row's exponentials.
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2_E); }
 
+// How dz is scaled: products of it are undone by scale_back.  One dloss for all rows is left out of dz but for its sign and comes back as a factor in 32
+// bits: rounded with every element, it would bring its own rounding into all of them.  fp16: see k_ce_unit.
+__device__ __forceinline__ float the_dloss(const DlfCeGiven& g) { return g.dloss != nullptr ? g.dloss[0] : g.dloss_value; }
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+__device__ __forceinline__ float scale_back(const DlfCeGiven& g)
+{
+    if (g.one > 0.0f) {
+        const float d = fabsf(the_dloss(g));
+        return is_finite(d) ? d / g.one : 1.0f;
+    }
+    return g.unit != nullptr ? g.unit[1] : 1.0f;
+}
 // A row's part of the gradient: dz = total * exp(z - lse) - own at the target.
 struct RowGradient {
     float total, own;
@@ -19,14 +31,20 @@ struct RowGradient {
 __device__ __forceinline__ RowGradient row_gradient(const DlfCeGiven& g, int64_t r, int64_t t, int64_t ignore, int nc)
 {
     RowGradient q;
-    q.own = t == ignore ? 0.0f : g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value;
-    float l = g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f;
-    if (g.unit != nullptr) {
-        const float u = g.unit[0];
-        q.own *= u;
-        l *= u;
+    if (g.one > 0.0f) {
+        const float d = the_dloss(g);
+        q.own = t == ignore || d == 0.0f ? 0.0f : is_finite(d) ? copysignf(g.one, d) : __builtin_nanf("");
+        q.total = q.own;
+    } else {
+        q.own = t == ignore ? 0.0f : g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value;
+        float l = g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f;
+        if (g.unit != nullptr) {
+            const float u = g.unit[0];
+            q.own *= u;
+            l *= u;
+        }
+        q.total = q.own + l;
     }
-    q.total = q.own + l;
     if (t != ignore && (t < 0 || t >= nc)) q.total = __builtin_nanf("");        // no class: not silently anything
     return q;
 }
@@ -39,6 +57,7 @@ __device__ __forceinline__ RowGradient row_gradient(const DlfCeGiven& g, int64_t
 template <int MODE> struct Entropy {
     static constexpr bool OWN = true, SUMS = false;
     const DlfCeArgs& e;
+    __device__ __forceinline__ const Entropy& ready() const { return *this; }
 
     template <typename T, int FC, int FR, int WC>
     __device__ __forceinline__ void tile(const DlfFfArgs& a, f16v (&acc)[FC][FR], int row0, int col0, int wave) const
@@ -46,6 +65,7 @@ template <int MODE> struct Entropy {
         typedef typename std::conditional<MODE == DLF_CE_KEEP, F16, T>::type S;
         constexpr int CW = FC * 32, CROW = CW + 4, LPR = CW / 8, RPU = 64 / LPR;   // columns of the wave, floats of an LDS row, lanes to a row, rows of a store
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5, left = a.nc - col0;
+        if (MODE == DLF_CE_DZ && e.back != nullptr && row0 == 0 && col0 == 0 && lane == 0) *e.back = scale_back(e.given);
         // stores go through an area of LDS that is the wave's own, so that they are whole lines
         float* const lf = (float*)ff_lds + wave * (32 * CROW);
         const int cw = lane % LPR * 8, rw = lane / LPR;
@@ -174,10 +194,9 @@ template <int MODE> struct Entropy {
             for (int d = LPR; d < 64; d <<= 1)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor(sum[i], d, 64);
-            if (e.given.unit != nullptr) {
+            const float back = scale_back(e.given);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] *= e.given.unit[1];
-            }
+            for (int i = 0; i < 8; ++i) sum[i] *= back;
             const int c = col0 + cw;
             if (lane < LPR && c < a.nc) store_floats(e.sums + (int64_t)(row0 / (FR * 32)) * a.nc + c, a.nc - c, sum);
         }
@@ -235,64 +254,126 @@ __global__ __launch_bounds__(512) void k_ce_rows(const DlfCeArgs e)
 // ------------------------------------------------------------------------------------------------
 // k_ce_join: a row's parts to its lse and loss.  ROWS of them to a workgroup, its other threads share the parts, in a fixed order.
 // ------------------------------------------------------------------------------------------------
-template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCeJoinArgs a)
-{
-    constexpr int GROUPS = 256 / ROWS;
-    __shared__ float2 shared[256];
-    const int r = blockIdx.x * ROWS + threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+// Sums s of exp(z - m) over parts of the classes, brought together.
+struct Parts {
     float m = MINUS_INF, s = 0.0f;
-    auto add = [&](float m2, float s2) __attribute__((always_inline)) {
+    __device__ __forceinline__ void add(float m2, float s2)
+    {
         const float top = fmaxf(m, m2), from = top == MINUS_INF ? 0.0f : top;
         s = s * exp_of(m - from) + s2 * exp_of(m2 - from);
         m = top;
-    };
-    if (r < a.nr) {
+    }
+    // ... those of parts first, first + step, ... of row r
+    __device__ __forceinline__ void take(const float* part, int parts, int nr, int r, int first, int step)
+    {
         constexpr int AT = 8;                               // parts whose loads share a wait
-        int p = g;
-        for (; p + (AT - 1) * GROUPS < a.parts; p += AT * GROUPS) {
+        for (int p = first; p < parts; p += AT * step) {
             float2 v[AT];
 #pragma unroll
-            for (int k = 0; k < AT; ++k) v[k] = *(const float2*)(a.part + ((int64_t)(p + k * GROUPS) * a.nr + r) * 2);
+            for (int k = 0; k < AT; ++k) v[k] = *(const float2*)(part + ((int64_t)min(p + k * step, parts - 1) * nr + r) * 2);
+            float top = m;
 #pragma unroll
-            for (int k = 0; k < AT; ++k) add(v[k].x, v[k].y);
-        }
-        for (; p < a.parts; p += GROUPS) {
-            const float2 v = *(const float2*)(a.part + ((int64_t)p * a.nr + r) * 2);
-            add(v.x, v.y);
+            for (int k = 0; k < AT; ++k) {
+                if (p + k * step >= parts) v[k] = float2{MINUS_INF, 0.0f};
+                top = fmaxf(top, v[k].x);
+            }
+            const float from = top == MINUS_INF ? 0.0f : top;
+            s *= exp_of(m - from);
+#pragma unroll
+            for (int k = 0; k < AT; ++k) s += v[k].y * exp_of(v[k].x - from);
+            m = top;
         }
     }
-    shared[threadIdx.x] = float2{m, s};
+    __device__ __forceinline__ float lse() const { return m == MINUS_INF ? (s == s ? MINUS_INF : s) : m + __builtin_amdgcn_logf(s) * LN_2; }
+};
+__device__ __forceinline__ float loss_of(float lse, int64_t t, int64_t ignore, int nc, const float* at)
+{
+    return t == ignore ? 0.0f : t < 0 || t >= nc ? __builtin_nanf("") : lse - *at;
+}
+// A row's parts in all of a workgroup's 256 threads, in a fixed order.
+__device__ __forceinline__ Parts all_parts(const float* part, int parts, int nr, int r)
+{
+    __shared__ float2 waves[4];
+    Parts q;
+    q.take(part, parts, nr, r, threadIdx.x, 256);
 #pragma unroll
-    for (int h = GROUPS / 2; h > 0; h >>= 1) {
-        __syncthreads();
-        if (g < h) {
-            const float2 v = shared[threadIdx.x + h * ROWS];
-            add(v.x, v.y);
-            shared[threadIdx.x] = float2{m, s};
-        }
+    for (int d = 1; d < 64; d <<= 1) {
+        const float m = __shfl_xor(q.m, d, 64), s = __shfl_xor(q.s, d, 64);
+        // (the same two in the same order in either lane)
+        Parts u;
+        const bool low = (threadIdx.x & d) == 0;
+        u.m = low ? q.m : m;
+        u.s = low ? q.s : s;
+        u.add(low ? m : q.m, low ? s : q.s);
+        q = u;
     }
-    if (g != 0 || r >= a.nr) return;
-    const float lse = m == MINUS_INF ? (s == s ? MINUS_INF : s) : m + __builtin_amdgcn_logf(s) * LN_2;
-    if (a.lse != nullptr) a.lse[r] = lse;
-    if (a.loss != nullptr) {
-        const int64_t t = a.target[r];
-        a.loss[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.nc ? __builtin_nanf("") : lse - a.at[r];
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = float2{q.m, q.s};
+    __syncthreads();
+    Parts all;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) all.add(waves[w].x, waves[w].y);
+    return all;
+}
+
+template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCeJoinArgs a)
+{
+    if constexpr (ROWS == 1) {
+        const int r = blockIdx.x;
+        const Parts q = all_parts(a.part, a.parts, a.nr, r);
+        if (threadIdx.x != 0) return;
+        const float lse = q.lse();
+        if (a.lse != nullptr) a.lse[r] = lse;
+        if (a.loss != nullptr) a.loss[r] = loss_of(lse, a.target[r], a.ignore, a.nc, a.at + r);
+    } else {
+        constexpr int GROUPS = 256 / ROWS;
+        __shared__ float2 shared[256];
+        const int r = blockIdx.x * ROWS + threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+        Parts q;
+        if (r < a.nr) q.take(a.part, a.parts, a.nr, r, g, GROUPS);
+        shared[threadIdx.x] = float2{q.m, q.s};
+#pragma unroll
+        for (int h = GROUPS / 2; h > 0; h >>= 1) {
+            __syncthreads();
+            if (g < h) {
+                const float2 v = shared[threadIdx.x + h * ROWS];
+                q.add(v.x, v.y);
+                shared[threadIdx.x] = float2{q.m, q.s};
+            }
+        }
+        if (g != 0 || r >= a.nr) return;
+        const float lse = q.lse();
+        if (a.lse != nullptr) a.lse[r] = lse;
+        if (a.loss != nullptr) a.loss[r] = loss_of(lse, a.target[r], a.ignore, a.nc, a.at + r);
     }
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ce_dz: dz from the exponentials kept, in their place: each times (dloss + dlse) exp(its part's maximum - lse).  Bound by memory.
+// k_ce_dz: dz from the exponentials kept, in their place: each times (dloss + dlse) exp(its part's maximum - lse).  A workgroup takes a slice of a row.  Where
+// all of them run at once, each forms its row's lse by itself: a launch for that costs more.  Bound by memory: 4096 rows of 32000 classes 86 us (6.1 TB/s, some of
+// it from the last-level cache); with the lse formed by each workgroup 105 to 110 against 86 and 8.6 for k_ce_join.
 // ------------------------------------------------------------------------------------------------
-template <typename T> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
+template <typename T, bool FORM> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
 {
-    const int cols = (int)((a.ldz + DLF_CE_DZ_COLS - 1) / DLF_CE_DZ_COLS), r = blockIdx.x / cols;
-    const int c = (blockIdx.x - r * cols) * DLF_CE_DZ_COLS + threadIdx.x * 8;
-    if (c >= a.ldz) return;
+    const int r = blockIdx.x / a.slices, c = (blockIdx.x - r * a.slices) * DLF_CE_DZ_COLS + threadIdx.x * 8;
+    // the loads first: what follows branches
+    const bool in = c < a.ldz;
     const int64_t at = (int64_t)r * a.ldz + c, t = a.target[r];
+    F16::v8 q;
+    float m = 0.0f, lse;
+    if (in) {
+        q = load8<F16>(a.dz, at, 8);
+        m = a.part[((int64_t)(c >> __builtin_ctz(a.width)) * a.nr + r) * 2];
+    }
+    if constexpr (FORM) {
+        lse = all_parts(a.part, a.parts, a.nr, r).lse();
+        if (c == 0) a.loss[r] = loss_of(lse, t, a.ignore, a.nc, a.at + r);
+    } else {
+        lse = a.lse[r];
+    }
+    if (a.back != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.back = scale_back(a.given);
+    if (!in) return;
     const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
-    const F16::v8 q = load8<F16>(a.dz, at, 8);
-    const float m = a.part[((int64_t)(c / a.width) * a.nr + r) * 2];
-    const float by = g.total == 0.0f ? 0.0f : g.total * exp_of(m - a.lse[r]) * (1.0f / 32768.0f);
+    const float by = g.total * exp_of(m - lse) * (1.0f / 32768.0f);
     const int64_t rel = t - c;
     float v[8];
 #pragma unroll
@@ -304,9 +385,24 @@ template <typename T> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCe
     store_some<T, 8>(a.dz, at, 8, v);
 }
 
+// k_ce_pack: up to two matrices whose rows start anywhere, copied to rows of whole lines, for the tiles that are loaded directly.
+__global__ __launch_bounds__(256) void k_ce_pack(const DlfCePackArgs a)
+{
+    int64_t line = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t of_first = a.m[0].rows * a.parts;
+    const int which = line >= of_first ? 1 : 0;
+    const DlfCePack& m = a.m[which];
+    if (which) line -= of_first;
+    const int64_t r = line / a.parts;
+    if (r >= m.rows) return;
+    const int c = (int)(line - r * a.parts) * 8;
+    const F16::v8 v = load8<F16>(m.from, r * m.stride + c, a.k - c);
+    __builtin_memcpy((char*)m.to + line * 16, &v, 16);
+}
+
 // ------------------------------------------------------------------------------------------------
-// k_ce_unit: for fp16, the power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14: dz, at most twice that, stays below 2^15,
-// and classes of probability 2^-28 are numbers of full precision.
+// k_ce_unit: for fp16 and gradients of each row's own, the power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14: dz, at most
+// twice that, stays below 2^15, and classes of probability 2^-28 are numbers of full precision.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void k_ce_unit(const DlfCeUnitArgs a)
 {
@@ -332,6 +428,53 @@ __global__ __launch_bounds__(1024) void k_ce_unit(const DlfCeUnitArgs a)
     a.unit[1] = __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
 }
 
+// The epilogue of the gradients' products: scaled by one value in memory, added to sums of 32 bits or left there.
+struct Sums {
+    static constexpr bool OWN = false, SUMS = true;
+    const float* scale;     // or null
+    float* sum;             // [nr][nc] or null
+    int add, keep;          // what is there is added; the sum goes there and nowhere else
+    float by = 1.0f;
+    // Where the epilogue begins.  As an instruction, waited for at once: with a load that the compiler knows it waits for all loads in every turn of the main
+    // loop, whose registers it takes for the load's (4096 x 4096 over 32000 classes 1745 -> 1913 us).
+    __device__ __forceinline__ Sums ready() const
+    {
+        Sums s = *this;
+        if (scale != nullptr) asm volatile("s_load_dword %0, %1, 0x0\n\ts_waitcnt lgkmcnt(0)" : "=s"(s.by) : "s"(scale) : "memory");
+        return s;
+    }
+    // whether the outputs are to be stored
+    template <int V> __device__ __forceinline__ bool take(const DlfFfArgs& a, int r, int c, int n, float (&v)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] *= by;
+        if (sum == nullptr) return true;
+        float* const at = sum + (int64_t)r * a.nc + c;
+        if (add != 0) {
+            float before[V];
+            __builtin_memset(before, 0, sizeof before);
+            if (n >= V) {
+                __builtin_memcpy(before, at, 4 * V);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i < n) before[i] = at[i];
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += before[i];
+        }
+        if (keep == 0) return true;
+        if (n >= V) {
+            __builtin_memcpy(at, v, 4 * V);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < n) at[i] = v[i];
+        }
+        return false;
+    }
+};
+
 // k_ce_back: the products dx = dz weight and dweight = dz^T x with the column sums, as k_ff_back, scaled back and added up over pieces.
 template <typename T, int BC, int BR, int WC, int WR, int KB, int RING, bool DIRECT>
 __global__ FF_TILE_BOUNDS void k_ce_back(const DlfCeBackArgs e)
@@ -340,12 +483,12 @@ __global__ FF_TILE_BOUNDS void k_ce_back(const DlfCeBackArgs e)
     int b = blockIdx.x;
     if (a.x_first) b = b < a.blocks_x ? b + a.blocks_w : b < a.blocks_x + a.blocks_w ? b - a.blocks_x : b;   // (both multiples of eight)
     if (b < a.blocks_w) {
-        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, Sums{e.inverse, e.sum, e.add, e.keep}, b);
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, Sums{e.back, e.sum, e.add, e.keep}, b);
         return;
     }
     b -= a.blocks_w;
     if (b < a.blocks_x) {
-        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, Sums{e.inverse, nullptr, 0, 0}, b);
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, Sums{e.back, nullptr, 0, 0}, b);
         return;
     }
     b -= a.blocks_x;
@@ -355,8 +498,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_ce_join_back(cons
 {
     const bool w = (int)blockIdx.x < e.b.blocks_w;
     const int64_t unit = (int64_t)(w ? blockIdx.x : blockIdx.x - e.b.blocks_w) * 256 + threadIdx.x;
-    if (w) join<T, false>(e.b.w, Sums{e.inverse, e.sum, e.add, e.keep}, unit);
-    else join<T, false>(e.b.x, Sums{e.inverse, nullptr, 0, 0}, unit);
+    if (w) join<T, false>(e.b.w, Sums{e.back, e.sum, e.add, e.keep}, unit);
+    else join<T, false>(e.b.x, Sums{e.back, nullptr, 0, 0}, unit);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -447,9 +590,15 @@ extern "C" int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream)
 }
 extern "C" int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream)
 {
-    const dim3 grid((unsigned)((int64_t)a->nr * ((a->ldz + DLF_CE_DZ_COLS - 1) / DLF_CE_DZ_COLS)));
-    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz<F16>, grid, dim3(256), 0, (hipStream_t)stream, *a);
-    else hipLaunchKernelGGL(k_ce_dz<BF16>, grid, dim3(256), 0, (hipStream_t)stream, *a);
+    const dim3 grid((unsigned)(a->nr * a->slices));
+    void (*const f)(const DlfCeDzArgs) = dtype == DLF_F16 ? (a->lse != nullptr ? k_ce_dz<F16, false> : k_ce_dz<F16, true>)
+                                                          : (a->lse != nullptr ? k_ce_dz<BF16, false> : k_ce_dz<BF16, true>);
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream)
+{
+    hipLaunchKernelGGL(k_ce_pack, dim3((unsigned)(((a->m[0].rows + a->m[1].rows) * a->parts + 255) / 256)), dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream)

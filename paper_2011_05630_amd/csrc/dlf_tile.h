@@ -165,51 +165,12 @@ template <int V> __device__ __forceinline__ void store_floats(float* p, int n, c
     }
 }
 
-// What a kernel adds to the epilogue.  OWN: it has one of its own, see tile(); SUMS: the product is scaled, by one value in memory, and added
-// to sums of 32 bits or left there.
+// What a kernel adds to the epilogue.  OWN: it has one of its own, see tile(); SUMS: take() changes the outputs before they are stored, and says
+// whether they are.  ready(): what of it is used where the epilogue begins.
 struct Plain {
     static constexpr bool OWN = false, SUMS = false;
+    __device__ __forceinline__ const Plain& ready() const { return *this; }
 };
-struct Sums {
-    static constexpr bool OWN = false, SUMS = true;
-    const float* scale;     // or null
-    float* sum;             // [nr][nc] or null
-    int add, keep;          // what is there is added; the sum goes there and nowhere else
-    // whether the outputs are to be stored
-    template <int V> __device__ __forceinline__ bool take(const DlfFfArgs& a, int r, int c, int n, float (&v)[V]) const
-    {
-        if (scale != nullptr) {
-            const float f = *scale;
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] *= f;
-        }
-        if (sum == nullptr) return true;
-        float* const at = sum + (int64_t)r * a.nc + c;
-        if (add != 0) {
-            float before[V];
-            __builtin_memset(before, 0, sizeof before);
-            if (n >= V) {
-                __builtin_memcpy(before, at, 4 * V);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (i < n) before[i] = at[i];
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += before[i];
-        }
-        if (keep == 0) return true;
-        if (n >= V) {
-            __builtin_memcpy(at, v, 4 * V);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < n) at[i] = v[i];
-        }
-        return false;
-    }
-};
-
 // The epilogue of V outputs C[r][c .. c + n): bias, pre-activations kept, activation, product with the second projection,
 // residual, one rounding.
 template <typename T, bool GATED, int V, typename E>
@@ -746,6 +707,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, const E& extra, int blo
     const float* const src = lf + rw * CROW + (GATED ? (cw >> 5) * 64 + (cw & 31) : cw);
     float* const part = a.part + (int64_t)(split * (GATED ? 2 : a.problems) + prob) * a.nr * a.nc;
     __syncthreads();
+    const auto last = extra.ready();
 #pragma unroll
     for (int j = 0; j < FR; j += JB) {
 #pragma unroll
@@ -779,7 +741,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, const E& extra, int blo
                         if (GATED) store_floats(part + ((int64_t)a.nr + ru) * a.nc + c, 8, w[k]);
                     }
                 } else {
-                    finish_many<T, GATED, AT>(a, extra, prob, r + u * RPU, RPU, c, v, w);
+                    finish_many<T, GATED, AT>(a, last, prob, r + u * RPU, RPU, c, v, w);
                 }
             }
         }
@@ -798,7 +760,7 @@ __device__ __forceinline__ void tile(const DlfFfArgs& a, const E& extra, int blo
                 store_floats(part + (int64_t)rt * a.nc + ca, n, v);
                 if (GATED) store_floats(part + ((int64_t)a.nr + rt) * a.nc + ca, n, w);
             } else {
-                finish<T, GATED, 8>(a, extra, prob, rt, ca, n, v, w);
+                finish<T, GATED, 8>(a, last, prob, rt, ca, n, v, w);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -848,7 +810,7 @@ template <typename T, bool GATED, typename E> __device__ __forceinline__ void jo
             if (GATED) u[i] += y[i];
         }
     }
-    finish<T, GATED, 8>(a, extra, prob, r, c, n, v, u);
+    finish<T, GATED, 8>(a, extra.ready(), prob, r, c, n, v, u);
 }
 
 // The waves' partial sums of a workgroup's 16 NF features x 16 MR rows meet in LDS, in the order of the waves.
