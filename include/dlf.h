@@ -361,7 +361,7 @@ dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* 
  * piece's dz stays in the workspace, in at most `piece_bytes` (but for 256 rows at least), in the tensors' type, which the matrix units
  * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14, so that a mean over many rows does not vanish,
  * and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
- * dlf_cross_entropy_gradients, where no dbias is wanted, keeps exp(z - a maximum) in 16 bits (fp16) in between rather than computing the logits again.
+ * dlf_cross_entropy_gradients, where no dbias is wanted, keeps exp(z - a maximum) in 16 bits (eleven behind the point) in between rather than computing the logits again.
  * Nothing depends on timing: equal calls give equal bits.
  *
  * Tensors are DEVICE and row-major: x [rows][in_features], weight [classes][in_features], of type `dtype`, a row's elements next to

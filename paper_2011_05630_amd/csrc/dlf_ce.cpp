@@ -128,9 +128,14 @@ dlf_status kernels_ready()
 DlfFfCut cut_of(const Ce& f, int64_t rows, bool any) { return dlf_ff_whole_cut(rows, f.d.classes, f.d.in_features, any); }
 int64_t parts_of(const Ce& f, const DlfFfCut& c) { return ceil_div(f.d.classes, dlf_ce_width(c.shape)); }
 
+// Few rows: the weight's gradient, each row of which is the product of one or two elements of dz and their rows of x, would be off by those elements'
+// roundings (0.0027 of its norm rather than 0.0017, bf16).  It is multiplied from dz and what its rounding took, as a sum of twice as many rows, which costs
+// next to nothing beside the bytes of the result.
+bool twice(const Ce& f) { return f.d.rows <= DLF_FF_FEW_ROWS; }
+
 // What a call keeps in the workspace, for its largest piece (column sums: for all of them); addresses are not known where its size is asked for.
 struct Layout {
-    size_t x = 0, w = 0, part = 0, at = 0, lse = 0, unit = 0, dz = 0, sums = 0, sum = 0, join = 0, bytes = 0;
+    size_t x = 0, w = 0, part = 0, at = 0, lse = 0, inverse = 0, unit = 0, rest = 0, dz = 0, low = 0, sums = 0, sum = 0, join = 0, bytes = 0;
     size_t take(size_t n)
     {
         const size_t here = bytes;
@@ -161,8 +166,11 @@ Layout layout_of(const Ce& f, bool logits, bool gradients)
         l.lse = l.take((size_t)most * 4);
     }
     if (!gradients) return l;
+    l.inverse = l.take((size_t)most * 4);
     l.unit = l.take(8);
+    l.rest = l.take((size_t)most * 4);
     l.dz = l.take((size_t)most * f.ldz * 2);
+    if (twice(f)) l.low = l.take((size_t)most * f.ldz * 2);
     l.sums = l.take((size_t)chunks * f.pieces() * nc * 4);
     if (f.pieces() > 1) l.sum = l.take((size_t)nc * f.d.in_features * 4);
     size_t join = 0;
@@ -234,14 +242,15 @@ void set_cut(DlfFfArgs& a, const DlfFfCut& c)
     a.tiles_c = c.tiles_c;
 }
 
-// The parts of a piece's rows; keep: the exponentials too, in dz.  -> the classes of a part
-dlf_status logits(const Ce& f, const In& in, const Piece& q, bool keep, const Layout& l, char* ws, int& width, void* stream)
+// The parts of a piece's rows; keep: the exponentials too, in dz.  tiles: by the kernel that forms dz, whose logits have the same bits: where a
+// target is nearly sure, 1 - p is what is left of them.  -> the classes of a part
+dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool keep, const Layout& l, char* ws, int& width, void* stream)
 {
     DlfCeArgs a;
     product(f, in, q, a);
     a.part = (float*)(ws + l.part);
     a.at = (float*)(ws + l.at);
-    if (!keep && dlf_ff_is_few(q.rows)) {
+    if (!tiles && dlf_ff_is_few(q.rows)) {
         const DlfFfFew c = dlf_ff_few_cut(a.t);
         width = 16;
         return launched(f, dlf_ce_start_few(&a, &c, f.d.dtype, stream));
@@ -253,10 +262,10 @@ dlf_status logits(const Ce& f, const In& in, const Piece& q, bool keep, const La
     return launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : DLF_CE_STAT, stream));
 }
 // ... and from them loss and lse, either of which may be null.
-dlf_status join(const Ce& f, const In& in, const Piece& q, const Layout& l, char* ws, int width, float* loss, float* lse, void* stream)
+dlf_status join(const Ce& f, const In& in, const Piece& q, const Layout& l, char* ws, int width, float* loss, float* lse, float* inverse, void* stream)
 {
     const DlfCeJoinArgs j = {(const float*)(ws + l.part), (const float*)(ws + l.at), in.target + q.first, f.d.ignore, (int)ceil_div(f.d.classes, width),
-                             (int)q.rows, f.d.classes, loss, lse};
+                             (int)q.rows, f.d.classes, loss, lse, inverse};
     return launched(f, dlf_ce_start_join(&j, stream));
 }
 
@@ -289,13 +298,15 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         if (g.dloss) g.dloss += q.first * g.dloss_stride;
         if (g.dlse) g.dlse += q.first * g.dlse_stride;
         if (q.rows > 0) {
+            float* inverse = nullptr;
             const float* piece_lse = lse ? lse + q.first : nullptr;
             float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
-            if (!lse) TRY(logits(f, in, q, keep, l, ws, width, stream));
+            if (!lse) TRY(logits(f, in, q, wanted, keep, l, ws, width, stream));
             if (!lse && !keep) {
                 float* const to = (float*)(ws + l.lse);
-                TRY(join(f, in, q, l, ws, width, piece_loss, to, stream));
+                inverse = (float*)(ws + l.inverse);
+                TRY(join(f, in, q, l, ws, width, piece_loss, to, inverse, stream));
                 piece_lse = to;
             }
             if (!wanted) continue;
@@ -304,10 +315,10 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 float* to = nullptr;                        // (workgroups that do not run at once do not form their rows' lse)
                 if (q.rows * slices > 2048) {
                     to = (float*)(ws + l.lse);
-                    TRY(join(f, in, q, l, ws, width, piece_loss, to, stream));
+                    TRY(join(f, in, q, l, ws, width, piece_loss, to, nullptr, stream));
                 }
                 const DlfCeDzArgs z = {ws + l.dz, f.ldz, (const float*)(ws + l.part), (const float*)(ws + l.at), (int)ceil_div(nc, width), width, (int)q.rows,
-                                       (int)nc, (int)slices, in.target + q.first, f.d.ignore, to, piece_loss, g, back};
+                                       (int)nc, (int)slices, in.target + q.first, f.d.ignore, to, piece_loss, g, (float*)(ws + l.rest), back, twice(f) ? ws + l.low : nullptr};
                 TRY(launched(f, dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else {
                 DlfCeArgs a;
@@ -316,6 +327,9 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 set_cut(a.t, c);
                 a.dz = ws + l.dz;
                 a.lse = piece_lse;
+                a.inverse = inverse;
+                a.rest = (float*)(ws + l.rest);
+                a.low = twice(f) ? ws + l.low : nullptr;
                 a.given = g;
                 a.back = back;
                 if (out.db) a.sums = (float*)(ws + l.sums) + (size_t)chunks * nc;
@@ -343,6 +357,10 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             a.ldp = q.ldx; a.ldq = f.ldz;
             a.nr = (int)nc; a.nc = (int)k; a.nk = (int)q.rows;
             a.segments = a.problems = 1;
+            if (twice(f) && q.rows > 0) {
+                a.segments = 2;
+                a.p[1] = a.p[0]; a.q[1] = ws + l.low;
+            }
             a.out[0] = out.dw; a.ldo = k;
         }
         if (out.db && last) {
@@ -364,6 +382,10 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         b.x.part = (float*)(ws + l.join + align256(c.w.part_bytes));
         if (!want_w) { b.w.problems = 0; b.w.splits = 1; }
         if (!want_x) { b.x.problems = 0; b.x.splits = 1; }
+        if (want_x) {
+            e.rest = (const float*)(ws + l.rest);
+            e.target = in.target + q.first;
+        }
         e.back = back ? back : given.unit ? given.unit + 1 : nullptr;
         if (want_w && pieces > 1) {
             e.sum = (float*)(ws + l.sum);
@@ -429,8 +451,8 @@ dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* we
         Piece q;
         int width;
         TRY(piece_of(f, in, p, l, (char*)workspace, q, hip_stream));
-        TRY(logits(f, in, q, false, l, (char*)workspace, width, hip_stream));
-        TRY(join(f, in, q, l, (char*)workspace, width, loss + q.first, lse ? lse + q.first : nullptr, hip_stream));
+        TRY(logits(f, in, q, false, false, l, (char*)workspace, width, hip_stream));
+        TRY(join(f, in, q, l, (char*)workspace, width, loss + q.first, lse ? lse + q.first : nullptr, nullptr, hip_stream));
     }
     return DLF_OK;
 }

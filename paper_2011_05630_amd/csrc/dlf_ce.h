@@ -4,7 +4,7 @@
 
 // What a product's epilogue does with the logits of its tile.
 enum { DLF_CE_STAT = 0,         // a maximum and a sum of exponentials of each row over a part of the classes, the target's logit
-       DLF_CE_KEEP = 1,         // ... and the exponentials themselves, in fp16
+       DLF_CE_KEEP = 1,         // ... and the exponentials themselves, in 16 bits
        DLF_CE_DZ = 2 };         // their gradient
 // A row's gradients of loss and lse as the caller gives them.
 struct DlfCeGiven {
@@ -30,12 +30,14 @@ struct DlfCeArgs {
     int64_t ignore;
     float* part;                // [parts][nr] {maximum, sum of exp(z - maximum)}
     float* at;                  // [nr] the target's logit, of rows whose target is a class
-    void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: 2^15 exp(z - its part's maximum)
+    void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: exp(z - its part's maximum) in 16 bits
     int64_t ldz;                // a multiple of eight
-    const float* lse;
+    const float *lse, *inverse; // DZ: p = exp(z - lse) * inverse (null: 1)
     DlfCeGiven given;
+    float* rest;                // [nr] what dz's rounding takes from a row's target, or null
     float* sums;                // [chunks][nc] column sums of dz, in 32 bits, or null
     float* back;                // what the products of dz are to be scaled by goes here, or null
+    void* low;                  // what the rounding of dz takes from it, laid out as it, or null
 };
 struct DlfCeJoinArgs {
     const float* part;
@@ -44,6 +46,7 @@ struct DlfCeJoinArgs {
     int64_t ignore;
     int32_t parts, nr, nc;
     float *loss, *lse;          // either may be null
+    float* inverse;             // null, or: the maximum goes to lse, 1 / the sum of exp(z - maximum) here
 };
 struct DlfCeDzArgs {
     void* dz;                   // KEEP's in, dz out
@@ -58,7 +61,8 @@ struct DlfCeDzArgs {
     const float* lse;           // or null: lse and loss are formed here
     float* loss;
     DlfCeGiven given;
-    float* back;                // as in DlfCeArgs
+    float *rest, *back;         // as in DlfCeArgs
+    void* low;
 };
 struct DlfCeUnitArgs {
     DlfCeGiven given;
@@ -70,6 +74,8 @@ struct DlfCeBackArgs {
     const float* back;          // the products are scaled by it; or null
     float* sum;                 // [classes][in] the weight's gradient over the pieces in front, or null
     int32_t add, keep;
+    const float* rest;          // of dz, see DlfCeArgs; or null
+    const int64_t* target;
 };
 // Classes of a part, by tile shape: what a wave's columns are.
 static inline int dlf_ce_width(int shape) { return DLF_FF_SHAPES[shape].bc / 2; }

@@ -12,6 +12,27 @@
 // exp(d).  d is rounded before it is multiplied: a maximum times log2(e), rounded, would shift all of a row's exponentials.
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2_E); }
 
+// ... to the last place: with what the product with log2(e) rounds off.  (-infinity: the difference of two of them would be none.)
+__device__ __forceinline__ float exp_of_all(float d)
+{
+    d = d < -200.0f ? -200.0f : d;
+    const float t = d * LOG2_E, off = __builtin_fmaf(d, 1.925963e-8f, __builtin_fmaf(d, LOG2_E, -t)), v = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(v, off * LN_2, v);
+}
+
+// Exponentials kept in 16 bits, two to a word: from 0 to 1, an exponent of five bits and eleven bits behind the point, a bit more than fp16, whose sign
+// they do not need.  They are bits 12 to 27 of the number times 2^-96 in 32 bits, so that reading one back is a shift, what follows times 2^96.  What is
+// below 2^-42 is lost; 1 is exact, so that 1 - p of a sure target is.  (NaN is not kept: such a row's sum says so.)
+__device__ __forceinline__ uint32_t kept_of(float x0, float x1)
+{
+    const uint32_t b0 = __builtin_bit_cast(uint32_t, x0 * 0x1p-96f) + 0x800u, b1 = __builtin_bit_cast(uint32_t, x1 * 0x1p-96f) + 0x800u;
+    return (b1 & 0x0ffff000u) << 4 | (b0 >> 12 & 0xffffu);
+}
+__device__ __forceinline__ float from_kept(uint32_t w, int i)
+{
+    return __builtin_bit_cast(float, (i ? w >> 4 : w << 12) & 0x0ffff000u);
+}
+
 // How dz is scaled: products of it are undone by scale_back.  One dloss for all rows is left out of dz but for its sign and comes back as a factor in 32
 // bits: rounded with every element, it would bring its own rounding into all of them.  fp16: see k_ce_unit.
 __device__ __forceinline__ float the_dloss(const DlfCeGiven& g) { return g.dloss != nullptr ? g.dloss[0] : g.dloss_value; }
@@ -49,6 +70,15 @@ __device__ __forceinline__ RowGradient row_gradient(const DlfCeGiven& g, int64_t
     return q;
 }
 
+// What the rounding of eight elements to type T takes from them.
+template <typename T> __device__ __forceinline__ void store_low(void* low, int64_t at, const float (&v)[8])
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[i] - (float)(typename T::e)v[i];
+    store_some<T, 8>(low, at, 8, f);
+}
+
 // ------------------------------------------------------------------------------------------------
 // The epilogues of a tile.  A lane holds, of one row of each block of 32, every other four of the wave's columns: a row's maximum and sum are its own
 // and one other lane's, without LDS.  The target's logit lies in one of the lane's registers, which is looked for only where a row of the
@@ -62,7 +92,6 @@ template <int MODE> struct Entropy {
     template <typename T, int FC, int FR, int WC>
     __device__ __forceinline__ void tile(const DlfFfArgs& a, f16v (&acc)[FC][FR], int row0, int col0, int wave) const
     {
-        typedef typename std::conditional<MODE == DLF_CE_KEEP, F16, T>::type S;
         constexpr int CW = FC * 32, CROW = CW + 4, LPR = CW / 8, RPU = 64 / LPR;   // columns of the wave, floats of an LDS row, lanes to a row, rows of a store
         const int lane = threadIdx.x & 63, l32 = lane & 31, lhi = lane >> 5, left = a.nc - col0;
         if (MODE == DLF_CE_DZ && e.back != nullptr && row0 == 0 && col0 == 0 && lane == 0) *e.back = scale_back(e.given);
@@ -131,15 +160,20 @@ template <int MODE> struct Entropy {
             if constexpr (MODE == DLF_CE_DZ) {
                 RowGradient g = row_gradient(e.given, at, t, e.ignore, a.nc);
                 if (r >= a.nr) g.total = g.own = 0.0f;
-                const float lse = e.lse[at];
+                const float lse = e.lse[at], total = e.inverse != nullptr ? g.total * e.inverse[at] : g.total;
 #pragma unroll
                 for (int i = 0; i < FC; ++i)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const float v = g.total * exp_of(z[i][k] - lse);
+                        const float v = total * exp_of_all(z[i][k] - lse);
                         z[i][k] = g.total == 0.0f ? 0.0f : v;
                     }
-                target([&](float v) __attribute__((always_inline)) { return v - g.own; });
+                if (e.rest != nullptr && col0 == 0 && lhi == 0 && r < a.nr && (t < 0 || t >= a.nc)) e.rest[r] = 0.0f;
+                target([&](float v) __attribute__((always_inline)) {
+                    v -= g.own;
+                    if (e.rest != nullptr) e.rest[r] = v - (float)(typename T::e)v;
+                    return v;
+                });
                 cut(0.0f);
             } else {
                 float m = MINUS_INF, s = 0.0f;
@@ -176,15 +210,21 @@ template <int MODE> struct Entropy {
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) *(f4v*)(v + k * 4) = *(const f4v*)(lf + (u + rw) * CROW + cw + k * 4);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (MODE == DLF_CE_DZ) sum[i] += v[i];                  // (zeros in rows that do not exist)
-                        else v[i] *= 32768.0f;
-                    }
-                    // One rounding to the type that the matrix units multiply.  KEEP: fp16, whatever the tensors' type, with 2^-40 of its part's
-                    // maximum as the least that is not lost; the maximum itself is exact, so that 1 - p of a sure target is.
                     const int ru = row0 + j * 32 + u + rw;
-                    if (ru < a.nr && col0 + cw < e.ldz) store_some<S, 8>(e.dz, (int64_t)ru * e.ldz + col0 + cw, 8, v);
+                    const bool in = ru < a.nr && col0 + cw < e.ldz;
+                    const int64_t to = (int64_t)ru * e.ldz + col0 + cw;
+                    if (MODE == DLF_CE_DZ) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] += v[i];             // (zeros in rows that do not exist)
+                        // one rounding to the type that the matrix units multiply
+                        if (in) store_some<T, 8>(e.dz, to, 8, v);
+                        if (in && e.low != nullptr) store_low<T>(e.low, to, v);
+                    } else {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = kept_of(v[i * 2], v[i * 2 + 1]);
+                        if (in) __builtin_memcpy((uint16_t*)e.dz + to, w, 16);
+                    }
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -322,7 +362,8 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCe
         const Parts q = all_parts(a.part, a.parts, a.nr, r);
         if (threadIdx.x != 0) return;
         const float lse = q.lse();
-        if (a.lse != nullptr) a.lse[r] = lse;
+        if (a.lse != nullptr) a.lse[r] = a.inverse != nullptr ? q.m : lse;
+        if (a.inverse != nullptr) a.inverse[r] = 1.0f / q.s;
         if (a.loss != nullptr) a.loss[r] = loss_of(lse, a.target[r], a.ignore, a.nc, a.at + r);
     } else {
         constexpr int GROUPS = 256 / ROWS;
@@ -342,7 +383,8 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCe
         }
         if (g != 0 || r >= a.nr) return;
         const float lse = q.lse();
-        if (a.lse != nullptr) a.lse[r] = lse;
+        if (a.lse != nullptr) a.lse[r] = a.inverse != nullptr ? q.m : lse;
+        if (a.inverse != nullptr) a.inverse[r] = 1.0f / q.s;
         if (a.loss != nullptr) a.loss[r] = loss_of(lse, a.target[r], a.ignore, a.nc, a.at + r);
     }
 }
@@ -358,10 +400,10 @@ template <typename T, bool FORM> __global__ __launch_bounds__(256) void k_ce_dz(
     // the loads first: what follows branches
     const bool in = c < a.ldz;
     const int64_t at = (int64_t)r * a.ldz + c, t = a.target[r];
-    F16::v8 q;
+    uint32_t q[4];
     float m = 0.0f, lse;
     if (in) {
-        q = load8<F16>(a.dz, at, 8);
+        __builtin_memcpy(q, (const uint16_t*)a.dz + at, 16);
         m = a.part[((int64_t)(c >> __builtin_ctz(a.width)) * a.nr + r) * 2];
     }
     if constexpr (FORM) {
@@ -373,16 +415,21 @@ template <typename T, bool FORM> __global__ __launch_bounds__(256) void k_ce_dz(
     if (a.back != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.back = scale_back(a.given);
     if (!in) return;
     const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
-    const float by = g.total * exp_of(m - lse) * (1.0f / 32768.0f);
+    const float by = g.total * exp_of(m - lse) * 0x1p96f;
     const int64_t rel = t - c;
     float v[8];
+    if (c == 0 && (t < 0 || t >= a.nc)) a.rest[r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        v[i] = g.total == 0.0f ? 0.0f : (float)q[i] * by;
-        if (rel == i && t != a.ignore) v[i] -= g.own;
+        v[i] = g.total == 0.0f ? 0.0f : from_kept(q[i >> 1], i & 1) * by;
         if (c + i >= a.nc) v[i] = 0.0f;
+        if (rel == i && c + i < a.nc) {
+            if (t != a.ignore) v[i] -= g.own;
+            a.rest[r] = v[i] - (float)(typename T::e)v[i];
+        }
     }
     store_some<T, 8>(a.dz, at, 8, v);
+    if (a.low != nullptr) store_low<T>(a.low, at, v);
 }
 
 // k_ce_pack: up to two matrices whose rows start anywhere, copied to rows of whole lines, for the tiles that are loaded directly.
@@ -434,7 +481,33 @@ struct Sums {
     const float* scale;     // or null
     float* sum;             // [nr][nc] or null
     int add, keep;          // what is there is added; the sum goes there and nowhere else
+    // What the rounding of dz has taken from a row's target, rest[r], times its class's weights: the largest element of dz by far, whose rounding would be the
+    // result's.
+    const float* rest;      // [nr] or null
+    const int64_t* target;
+    const void* w;
+    int64_t ldw;
     float by = 1.0f;
+    template <typename T, int N, int V> __device__ __forceinline__ void correct(const DlfFfArgs& a, int r, int step, int c, int n, float (*v)[V]) const
+    {
+        if (rest == nullptr) return;
+        float by[N];
+        int64_t at[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int row = min(r + k * step, a.nr - 1);
+            by[k] = rest[row];
+            at[k] = target[row];
+        }
+        typename Some<T, V>::v q[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k)                         // (without a class there is no rest)
+            q[k] = load_some<T, V>(w, (by[k] != 0.0f ? at[k] : 0) * ldw + c, n);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] = by[k] != 0.0f ? __builtin_fmaf(by[k], (float)q[k][i], v[k][i]) : v[k][i];
+    }
     // Where the epilogue begins.  As an instruction, waited for at once: with a load that the compiler knows it waits for all loads in every turn of the main
     // loop, whose registers it takes for the load's (4096 x 4096 over 32000 classes 1745 -> 1913 us).
     __device__ __forceinline__ Sums ready() const
@@ -483,12 +556,12 @@ __global__ FF_TILE_BOUNDS void k_ce_back(const DlfCeBackArgs e)
     int b = blockIdx.x;
     if (a.x_first) b = b < a.blocks_x ? b + a.blocks_w : b < a.blocks_x + a.blocks_w ? b - a.blocks_x : b;   // (both multiples of eight)
     if (b < a.blocks_w) {
-        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, Sums{e.back, e.sum, e.add, e.keep}, b);
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, true, false>(a.w, Sums{e.back, e.sum, e.add, e.keep, nullptr, nullptr, nullptr, 0}, b);
         return;
     }
     b -= a.blocks_w;
     if (b < a.blocks_x) {
-        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, Sums{e.back, nullptr, 0, 0}, b);
+        tile<T, BC, BR, WC, WR, KB, RING, DIRECT, true, false, false>(a.x, Sums{e.back, nullptr, 0, 0, e.rest, e.target, e.b.x.p[0], e.b.x.ldp}, b);
         return;
     }
     b -= a.blocks_x;
@@ -498,8 +571,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_ce_join_back(cons
 {
     const bool w = (int)blockIdx.x < e.b.blocks_w;
     const int64_t unit = (int64_t)(w ? blockIdx.x : blockIdx.x - e.b.blocks_w) * 256 + threadIdx.x;
-    if (w) join<T, false>(e.b.w, Sums{e.back, e.sum, e.add, e.keep}, unit);
-    else join<T, false>(e.b.x, Sums{e.back, nullptr, 0, 0}, unit);
+    if (w) join<T, false>(e.b.w, Sums{e.back, e.sum, e.add, e.keep, nullptr, nullptr, nullptr, 0}, unit);
+    else join<T, false>(e.b.x, Sums{e.back, nullptr, 0, 0, e.rest, e.target, e.b.x.p[0], e.b.x.ldp}, unit);
 }
 
 // ------------------------------------------------------------------------------------------------

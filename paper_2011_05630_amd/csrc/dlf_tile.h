@@ -165,8 +165,8 @@ template <int V> __device__ __forceinline__ void store_floats(float* p, int n, c
     }
 }
 
-// What a kernel adds to the epilogue.  OWN: it has one of its own, see tile(); SUMS: take() changes the outputs before they are stored, and says
-// whether they are.  ready(): what of it is used where the epilogue begins.
+// What a kernel adds to the epilogue.  OWN: it has one of its own, see tile(); SUMS: correct() and take() change the outputs before they
+// are stored, and the latter says whether they are.  ready(): what of it is used where the epilogue begins.
 struct Plain {
     static constexpr bool OWN = false, SUMS = false;
     __device__ __forceinline__ const Plain& ready() const { return *this; }
@@ -207,6 +207,7 @@ __device__ __forceinline__ void finish(const DlfFfArgs& a, const E& extra, int p
         for (int i = 0; i < V; ++i) v[i] += (float)q[i];
     }
     if constexpr (E::SUMS) {
+        extra.template correct<T, 1, V>(a, r, 0, c, n, &v);
         if (!extra.take(a, r, c, n, v)) return;
     }
     store_some<T, V>(a.out[prob], (int64_t)r * a.ldo + c, n, v);
@@ -252,6 +253,7 @@ __device__ __forceinline__ void finish_many(const DlfFfArgs& a, const E& extra, 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[k][i] = act_of<decltype(act)::value>(v[k][i]);
         });
+    if constexpr (E::SUMS) extra.template correct<T, N, 8>(a, r, step, c, 8, v);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         if (GATED) {
