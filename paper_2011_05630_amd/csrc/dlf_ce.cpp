@@ -171,7 +171,7 @@ Layout layout_of(const Ce& f, bool logits, bool gradients)
     l.rest = l.take((size_t)most * 4);
     l.dz = l.take((size_t)most * f.ldz * 2);
     if (twice(f)) l.low = l.take((size_t)most * f.ldz * 2);
-    l.sums = l.take((size_t)chunks * f.pieces() * nc * 4);
+    l.sums = l.take((size_t)(1 + chunks) * nc * 4);         // the pieces' in front, the piece's chunks
     if (f.pieces() > 1) l.sum = l.take((size_t)nc * f.d.in_features * 4);
     size_t join = 0;
     for (const int64_t rows : {most, f.rows(f.pieces() - 1)})
@@ -290,8 +290,8 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
     float* const back = given.one > 0.0f && f.d.rows > 0 && wanted ? (float*)(ws + l.unit) : nullptr;
     // The exponentials are kept where they need not say what the bias's gradient is, which has 32 bits.
     const bool keep = !lse && wanted && !out.db;
-    int chunks = 0;
     for (int64_t p = 0; p < pieces; ++p) {
+        int chunks = 0;
         Piece q;
         TRY(piece_of(f, in, p, l, ws, q, stream));
         DlfCeGiven g = given;
@@ -332,8 +332,8 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 a.low = twice(f) ? ws + l.low : nullptr;
                 a.given = g;
                 a.back = back;
-                if (out.db) a.sums = (float*)(ws + l.sums) + (size_t)chunks * nc;
-                chunks += c.tiles_r * 2;
+                if (out.db) a.sums = (float*)(ws + l.sums) + nc;
+                chunks = c.tiles_r * 2;
                 TRY(launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, DLF_CE_DZ, stream)));
             }
         }
@@ -363,11 +363,13 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             }
             a.out[0] = out.dw; a.ldo = k;
         }
-        if (out.db && last) {
-            b.sum.part[0] = chunks > 0 ? (const float*)(ws + l.sums) : out.db;    // (of no rows nothing is read: zeros)
-            b.sum.out[0] = out.db;
+        if (out.db) {
+            // (of no rows nothing is read: zeros)
+            float* const sums = chunks > 0 ? (float*)(ws + l.sums) : out.db;
+            b.sum.part[0] = p > 0 ? sums : chunks > 0 ? sums + nc : sums;
+            b.sum.out[0] = last ? out.db : sums;
             b.sum.n = (int)nc;
-            b.sum.chunks = chunks;
+            b.sum.chunks = chunks + (p > 0 ? 1 : 0);
             b.sum.blocks = (int)ceil_div(nc, 64);
         }
         if (!want_x && !want_w && b.sum.blocks == 0) continue;
