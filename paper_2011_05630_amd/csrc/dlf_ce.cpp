@@ -30,8 +30,13 @@ dlf_status fail(dlf_status s, const char* fmt, ...)
 
 constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;       // a launch holds fewer than 2^32 threads, 256 to a workgroup
 constexpr int64_t LEAST_PIECE = 256, MOST_PIECE = 1 << 16;  // rows
-// Operands whose rows start anywhere are copied to rows of whole lines from so many rows on, for the products of a loss and of gradients.
-constexpr int64_t PACK_LOSS = 512, PACK_GRADIENTS = 128;
+// Whether operands whose rows start anywhere are copied to rows of whole lines first: modelled in ns, a launch and the copy against what `products` products
+// take longer on tiles through registers.  Bf16, us with the copy and without: loss of 1024 x 2051 over 32001 classes 178 and 205, of 768 rows 184 and 158;
+// with gradients 2048 rows 942 and 1325, 512 339 and 363, 256 245 and 212; 1024 x 770 over 5003 classes 69 and 72, 512 rows 52 and 51.
+bool copy_pays(int64_t rows, int64_t in, int64_t classes, int products)
+{
+    return rows > DLF_FF_FEW_ROWS && products * 1.2e-6 * (double)rows * in * classes > 5000 + 4.0 * (double)(rows + classes) * in / 3800;
+}
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -83,7 +88,7 @@ dlf_status check_desc(const dlf_ce_desc* d, bool gradients, const char* call, Ce
     const int64_t n = std::max<int64_t>(1, ceil_div(d->rows, f.piece));
     f.piece = std::max(LEAST_PIECE, ceil_div(ceil_div(d->rows, n), LEAST_PIECE) * LEAST_PIECE);
     f.lines = ceil_div(d->in_features, 8);
-    const bool pays = d->rows >= (gradients ? PACK_GRADIENTS : PACK_LOSS) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
+    const bool pays = copy_pays(d->rows, d->in_features, d->classes, gradients ? 3 : 1) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
     f.pack_x = pays && !dlf_ff_lines(nullptr, f.d.x_stride, d->in_features);
     f.pack_w = pays && !dlf_ff_lines(nullptr, f.d.w_stride, d->in_features);
     return DLF_OK;

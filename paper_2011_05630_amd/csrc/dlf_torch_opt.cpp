@@ -70,7 +70,7 @@ py::tuple gradient_norm(py::handle gradients, double most, double scale, int64_t
     const c10::DeviceGuard guard(*device);
     const int32_t n = (int32_t)p.size();
     const auto options = at::TensorOptions().dtype(at::kFloat).device(*device);
-    const at::Tensor both = at::empty({2}, options), norm = both.select(0, 0), factor = both.select(0, 1);
+    const at::Tensor norm = at::empty({}, options), factor = at::empty({}, options);
     const size_t need = dlf_gradient_norm_workspace_bytes(counts.data(), n);
     const at::Tensor ws = workspace(need, *device);
     dlf_status s;

@@ -12,6 +12,7 @@ from .feedforward import _native, _need, _stream
 
 _STATES = {"fp32": 0, "8bit": 1}
 BLOCK = 64          # elements of the states that share a scale
+_norm = None        # the native step, looked for once
 
 
 def _list(x, name):
@@ -23,10 +24,17 @@ def gradient_norm(gradients, most=float("inf"), scale=1.0):
     """-> (norm, factor), an fp32 element each on the gradients' device: norm = |scale| * sqrt(sum of all their squares), factor = scale, brought
     down by most / norm where the norm is above `most`, and NaN where it is not finite (`AdamW.step` leaves a step with such a factor out).
     scale: what the gradients are to be multiplied by, 1 / (loss scale) among others.  None among the gradients is passed over."""
+    global _norm
     gradients = _list(gradients, "gradients")
-    device = next((g.device for g in gradients if isinstance(g, torch.Tensor)), None)
-    _need(device is not None and device.type == "cuda", "gradients: tensors on the GPU expected")
-    return _native().gradient_norm(gradients, most, scale, _stream(device.index))
+    index = -1
+    for g in gradients:
+        if g is not None:
+            index = g.get_device() if isinstance(g, torch.Tensor) else -1
+            break
+    _need(index >= 0, "gradients: tensors on the GPU expected")
+    if _norm is None:
+        _norm = _native().gradient_norm
+    return _norm(gradients, most, scale, _stream(index))
 
 
 class AdamW:
