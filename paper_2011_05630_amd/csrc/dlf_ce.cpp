@@ -140,7 +140,7 @@ bool twice(const Ce& f) { return f.d.rows <= DLF_FF_FEW_ROWS; }
 
 // What a call keeps in the workspace, for its largest piece (column sums: for all of them); addresses are not known where its size is asked for.
 struct Layout {
-    size_t x = 0, w = 0, part = 0, at = 0, lse = 0, inverse = 0, unit = 0, rest = 0, dz = 0, low = 0, sums = 0, sum = 0, join = 0, bytes = 0;
+    size_t x = 0, w = 0, z = 0, part = 0, at = 0, lse = 0, inverse = 0, unit = 0, rest = 0, dz = 0, low = 0, sums = 0, sum = 0, join = 0, bytes = 0;
     size_t take(size_t n)
     {
         const size_t here = bytes;
@@ -171,6 +171,7 @@ Layout layout_of(const Ce& f, bool logits, bool gradients)
         l.lse = l.take((size_t)most * 4);
     }
     if (!gradients) return l;
+    if (dlf_ff_is_few(most)) l.z = l.take((size_t)most * f.ldz * 4);
     l.inverse = l.take((size_t)most * 4);
     l.unit = l.take(8);
     l.rest = l.take((size_t)most * 4);
@@ -247,14 +248,15 @@ void set_cut(DlfFfArgs& a, const DlfFfCut& c)
     a.tiles_c = c.tiles_c;
 }
 
-// The parts of a piece's rows; keep: the exponentials too, in dz.  tiles: by the kernel that forms dz, whose logits have the same bits: where a
-// target is nearly sure, 1 - p is what is left of them.  -> the classes of a part
-dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool keep, const Layout& l, char* ws, int& width, void* stream)
+// The parts of a piece's rows; keep: the exponentials too, in dz; z: of few rows the logits, there.  tiles: by the kernel that forms dz, whose logits
+// have the same bits: where a target is nearly sure, 1 - p is what is left of them.  -> the classes of a part
+dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool keep, float* z, const Layout& l, char* ws, int& width, void* stream)
 {
     DlfCeArgs a;
     product(f, in, q, a);
     a.part = (float*)(ws + l.part);
     a.at = (float*)(ws + l.at);
+    a.z = z;
     if (!tiles && dlf_ff_is_few(q.rows)) {
         const DlfFfFew c = dlf_ff_few_cut(a.t);
         width = 16;
@@ -281,7 +283,9 @@ struct Out {
 // The gradients of all rows: dz of a piece from the lse given, or with loss and lse computed on the way, then the products.
 dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven given, float* loss, const Out& out, char* ws, void* stream)
 {
-    const Layout l = layout_of(f, lse == nullptr, true);
+    // Few rows: their logits are kept in 32 bits, which costs less than to form them again.
+    const bool few = dlf_ff_is_few(f.d.rows);
+    const Layout l = layout_of(f, lse == nullptr || few, true);
     const int64_t pieces = f.pieces(), nc = f.d.classes, k = f.d.in_features;
     const bool wanted = out.dx || out.dw || out.db;
     TRY(kernels_ready());
@@ -294,7 +298,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
     }
     float* const back = given.one > 0.0f && f.d.rows > 0 && wanted ? (float*)(ws + l.unit) : nullptr;
     // The exponentials are kept where they need not say what the bias's gradient is, which has 32 bits.
-    const bool keep = !lse && wanted && !out.db;
+    const bool keep = !lse && wanted && !out.db && !few;
     for (int64_t p = 0; p < pieces; ++p) {
         int chunks = 0;
         Piece q;
@@ -307,23 +311,36 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             const float* piece_lse = lse ? lse + q.first : nullptr;
             float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
-            if (!lse) TRY(logits(f, in, q, wanted, keep, l, ws, width, stream));
-            if (!lse && !keep) {
+            if (!lse || (few && wanted)) TRY(logits(f, in, q, wanted && !few, keep, few && wanted ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
+            if (!lse && !keep && !(few && wanted && !out.db)) {
                 float* const to = (float*)(ws + l.lse);
                 inverse = (float*)(ws + l.inverse);
                 TRY(join(f, in, q, l, ws, width, piece_loss, to, inverse, stream));
                 piece_lse = to;
             }
             if (!wanted) continue;
-            if (keep) {
-                const int64_t slices = ceil_div(f.ldz, DLF_CE_DZ_COLS);
-                float* to = nullptr;                        // (workgroups that do not run at once do not form their rows' lse)
-                if (q.rows * slices > 2048) {
-                    to = (float*)(ws + l.lse);
+            DlfCeDzArgs z;
+            memset(&z, 0, sizeof z);
+            z.dz = ws + l.dz; z.ldz = f.ldz;
+            z.part = (const float*)(ws + l.part); z.at = (const float*)(ws + l.at);
+            z.nr = (int)q.rows; z.nc = (int)nc;
+            z.slices = (int)ceil_div(f.ldz, DLF_CE_DZ_COLS);
+            z.target = in.target + q.first; z.ignore = f.d.ignore;
+            z.lse = piece_lse; z.inverse = inverse; z.loss = piece_loss;
+            z.given = g; z.rest = (float*)(ws + l.rest); z.back = back;
+            z.low = twice(f) ? ws + l.low : nullptr;
+            if (width > 0) { z.width = width; z.parts = (int)ceil_div(nc, width); }
+            if (few) {
+                z.z = (const float*)(ws + l.z);
+                z.sums = out.db;
+                TRY(launched(f, piece_lse ? dlf_ce_start_dz_few(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
+            } else if (keep) {
+                // (workgroups that do not run at once do not form their rows' lse)
+                if (q.rows * z.slices > 2048) {
+                    float* const to = (float*)(ws + l.lse);
                     TRY(join(f, in, q, l, ws, width, piece_loss, to, nullptr, stream));
+                    z.lse = to;
                 }
-                const DlfCeDzArgs z = {ws + l.dz, f.ldz, (const float*)(ws + l.part), (const float*)(ws + l.at), (int)ceil_div(nc, width), width, (int)q.rows,
-                                       (int)nc, (int)slices, in.target + q.first, f.d.ignore, to, piece_loss, g, (float*)(ws + l.rest), back, twice(f) ? ws + l.low : nullptr};
                 TRY(launched(f, dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else {
                 DlfCeArgs a;
@@ -368,7 +385,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             }
             a.out[0] = out.dw; a.ldo = k;
         }
-        if (out.db) {
+        if (out.db && !(few && q.rows > 0)) {
             // (of no rows nothing is read: zeros)
             float* const sums = chunks > 0 ? (float*)(ws + l.sums) : out.db;
             b.sum.part[0] = p > 0 ? sums : chunks > 0 ? sums + nc : sums;
@@ -438,7 +455,10 @@ dlf_status check_out(const Ce& f, const Out& o)
 extern "C" {
 
 size_t dlf_cross_entropy_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, false, "dlf_cross_entropy_workspace_bytes"); }
-size_t dlf_cross_entropy_backward_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, false, true, "dlf_cross_entropy_backward_workspace_bytes"); }
+size_t dlf_cross_entropy_backward_workspace_bytes(const dlf_ce_desc* d)
+{
+    return bytes_of(d, d && dlf_ff_is_few(d->rows), true, "dlf_cross_entropy_backward_workspace_bytes");
+}
 size_t dlf_cross_entropy_gradients_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, true, "dlf_cross_entropy_gradients_workspace_bytes"); }
 
 dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target, float* loss,
@@ -458,7 +478,7 @@ dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* we
         Piece q;
         int width;
         TRY(piece_of(f, in, p, l, (char*)workspace, q, hip_stream));
-        TRY(logits(f, in, q, false, false, l, (char*)workspace, width, hip_stream));
+        TRY(logits(f, in, q, false, false, nullptr, l, (char*)workspace, width, hip_stream));
         TRY(join(f, in, q, l, (char*)workspace, width, loss + q.first, lse ? lse + q.first : nullptr, nullptr, hip_stream));
     }
     return DLF_OK;
@@ -478,7 +498,7 @@ dlf_status dlf_cross_entropy_backward(const dlf_ce_desc* d, const void* x, const
     TRY(check_ptr(f, lse, "lse", f.d.rows > 0, 4));
     TRY(check_given(f, given));
     TRY(check_out(f, out));
-    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, false, true).bytes));
+    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, dlf_ff_is_few(f.d.rows), true).bytes));
     static const float none = 0.0f;                         // (of no rows nothing is read)
     return gradients(f, in, lse ? lse : &none, given, nullptr, out, (char*)workspace, hip_stream);
 }

@@ -30,6 +30,7 @@ struct DlfCeArgs {
     int64_t ignore;
     float* part;                // [parts][nr] {maximum, sum of exp(z - maximum)}
     float* at;                  // [nr] the target's logit, of rows whose target is a class
+    float* z;                   // few rows: [nr][ldz] their logits, or null
     void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: exp(z - its part's maximum) in 16 bits
     int64_t ldz;                // a multiple of eight
     const float *lse, *inverse; // DZ: p = exp(z - lse) * inverse (null: 1)
@@ -50,6 +51,7 @@ struct DlfCeJoinArgs {
 };
 struct DlfCeDzArgs {
     void* dz;                   // KEEP's in, dz out
+    const float* z;             // ... or the logits of few rows in, and nothing in dz
     int64_t ldz;
     const float* part;
     const float* at;
@@ -59,10 +61,12 @@ struct DlfCeDzArgs {
     const int64_t* target;
     int64_t ignore;
     const float* lse;           // or null: lse and loss are formed here
+    const float* inverse;       // of few rows, as in DlfCeArgs
     float* loss;
     DlfCeGiven given;
     float *rest, *back;         // as in DlfCeArgs
     void* low;
+    float* sums;                // of few rows: [nc] column sums of dz, scaled back, or null
 };
 struct DlfCeUnitArgs {
     DlfCeGiven given;
@@ -92,6 +96,7 @@ int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int dtype, int mode, void* 
 int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int dtype, void* stream);
 int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream);
 int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream);
+int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int dtype, void* stream);
 int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream);
 int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream);
 int dlf_ce_start_back(const DlfCeBackArgs* a, int shape, int dtype, void* stream);

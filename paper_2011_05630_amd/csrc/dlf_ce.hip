@@ -161,13 +161,24 @@ template <int MODE> struct Entropy {
                 RowGradient g = row_gradient(e.given, at, t, e.ignore, a.nc);
                 if (r >= a.nr) g.total = g.own = 0.0f;
                 const float lse = e.lse[at], total = e.inverse != nullptr ? g.total * e.inverse[at] : g.total;
+                // (to the last place for the bias's gradient only: it is half of this epilogue, which a tile of few stages shows)
+                if (e.sums != nullptr) {
 #pragma unroll
-                for (int i = 0; i < FC; ++i)
+                    for (int i = 0; i < FC; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float v = total * exp_of_all(z[i][k] - lse);
-                        z[i][k] = g.total == 0.0f ? 0.0f : v;
-                    }
+                        for (int k = 0; k < 16; ++k) z[i][k] = total * exp_of_all(z[i][k] - lse);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < FC; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[i][k] = total * exp_of(z[i][k] - lse);
+                }
+                if (__builtin_amdgcn_ballot_w64(g.total == 0.0f) != 0) {        // rows without a gradient, whatever their logits are
+#pragma unroll
+                    for (int i = 0; i < FC; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[i][k] = g.total == 0.0f ? 0.0f : z[i][k];
+                }
                 if (e.rest != nullptr && col0 == 0 && lhi == 0 && r < a.nr && (t < 0 || t >= a.nc)) e.rest[r] = 0.0f;
                 target([&](float v) __attribute__((always_inline)) {
                     v -= g.own;
@@ -266,6 +277,7 @@ template <int MODE> struct Entropy {
         s += __shfl_xor(s, 32, 64);
         const int first = c & ~15;
         if (r >= a.nr || first >= a.nc) return;
+        if (e.z != nullptr && c < e.ldz) *(f4v*)(e.z + (int64_t)r * e.ldz + c) = f4v{z[0], z[1], z[2], z[3]};
         const int64_t t = e.target[r];
         if (t >= c && t < c + 4 && t < a.nc) e.at[r] = t == c ? z[0] : t == c + 1 ? z[1] : t == c + 2 ? z[2] : z[3];
         if (c == first) {
@@ -394,34 +406,43 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCe
 // all of them run at once, each forms its row's lse by itself: a launch for that costs more.  Bound by memory: 4096 rows of 32000 classes 86 us (6.1 TB/s, some of
 // it from the last-level cache); with the lse formed by each workgroup 105 to 110 against 86 and 8.6 for k_ce_join.
 // ------------------------------------------------------------------------------------------------
-template <typename T, bool FORM> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
+// LOGITS: from the logits of few rows, which have been kept in 32 bits.
+template <typename T, bool FORM, bool LOGITS> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
 {
+    static_assert(FORM || !LOGITS, "");
     const int r = blockIdx.x / a.slices, c = (blockIdx.x - r * a.slices) * DLF_CE_DZ_COLS + threadIdx.x * 8;
     // the loads first: what follows branches
     const bool in = c < a.ldz;
     const int64_t at = (int64_t)r * a.ldz + c, t = a.target[r];
     uint32_t q[4];
-    float m = 0.0f, lse;
+    float z[8], m = 0.0f, by;
     if (in) {
-        __builtin_memcpy(q, (const uint16_t*)a.dz + at, 16);
-        m = a.part[((int64_t)(c >> __builtin_ctz(a.width)) * a.nr + r) * 2];
+        if (LOGITS) {
+            __builtin_memcpy(z, a.z + at, 32);
+        } else {
+            __builtin_memcpy(q, (const uint16_t*)a.dz + at, 16);
+            m = a.part[((int64_t)(c >> __builtin_ctz(a.width)) * a.nr + r) * 2];
+        }
     }
     if constexpr (FORM) {
-        lse = all_parts(a.part, a.parts, a.nr, r).lse();
+        const Parts all = all_parts(a.part, a.parts, a.nr, r);
+        const float lse = all.lse();
         if (c == 0) a.loss[r] = loss_of(lse, t, a.ignore, a.nc, a.at + r);
+        if (LOGITS) m = all.m;
+        by = LOGITS ? 1.0f / all.s : exp_of(m - lse) * 0x1p96f;
     } else {
-        lse = a.lse[r];
+        by = exp_of(m - a.lse[r]) * 0x1p96f;
     }
     if (a.back != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.back = scale_back(a.given);
     if (!in) return;
     const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
-    const float by = g.total * exp_of(m - lse) * 0x1p96f;
+    by *= g.total;
     const int64_t rel = t - c;
     float v[8];
     if (c == 0 && (t < 0 || t >= a.nc)) a.rest[r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        v[i] = g.total == 0.0f ? 0.0f : from_kept(q[i >> 1], i & 1) * by;
+        v[i] = g.total == 0.0f ? 0.0f : (LOGITS ? exp_of(z[i] - m) : from_kept(q[i >> 1], i & 1)) * by;
         if (c + i >= a.nc) v[i] = 0.0f;
         if (rel == i && c + i < a.nc) {
             if (t != a.ignore) v[i] -= g.own;
@@ -430,6 +451,69 @@ template <typename T, bool FORM> __global__ __launch_bounds__(256) void k_ce_dz(
     }
     store_some<T, 8>(a.dz, at, 8, v);
     if (a.low != nullptr) store_low<T>(a.low, at, v);
+}
+
+// k_ce_dz_few: dz of few rows from their logits, kept in 32 bits, and its column sums.  p = exp(z - lse) * inverse.  A workgroup takes 256 classes, four to a
+// lane, its waves every eighth row; their sums meet in LDS, in a fixed order.  Bound by latency: a wave to all rows took 28 us for 60 of them.
+template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_few(const DlfCeDzArgs a)
+{
+    constexpr int WAVES = 8;
+    static_assert(DLF_FF_FEW_ROWS <= WAVES * 64, "a thread for each row");
+    struct Row {
+        float total, own, lse, zero;
+        int t;              // the target's class, or -1
+    };
+    __shared__ Row rows[DLF_FF_FEW_ROWS];
+    __shared__ f4v sums[WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if ((int)threadIdx.x < a.nr) {
+        const int r = threadIdx.x;
+        const int64_t t = a.target[r];
+        const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
+        const bool is_class = t >= 0 && t < a.nc;
+        rows[r] = Row{a.inverse != nullptr ? g.total * a.inverse[r] : g.total, g.own, a.lse[r], g.total, is_class ? (int)t : -1};
+        if (blockIdx.x == 0 && !is_class) a.rest[r] = 0.0f;
+        if (blockIdx.x == 0 && r == 0 && a.back != nullptr) *a.back = scale_back(a.given);
+    }
+    __syncthreads();
+    const int c = (blockIdx.x * 64 + lane) * 4;
+    f4v sum = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int AT = 4;                                   // rows whose loads share a wait
+    for (int r0 = wave; c < a.ldz && r0 < a.nr; r0 += AT * WAVES) {
+        f4v z[AT];
+#pragma unroll
+        for (int k = 0; k < AT; ++k) z[k] = *(const f4v*)(a.z + (int64_t)min(r0 + k * WAVES, a.nr - 1) * a.ldz + c);
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            const int r = r0 + k * WAVES;
+            if (r >= a.nr) break;
+            const Row q = rows[r];
+            const int64_t at = (int64_t)r * a.ldz + c;
+            float v[4], low[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = q.zero == 0.0f ? 0.0f : q.total * exp_of_all(z[k][i] - q.lse);
+                if (c + i >= a.nc) v[i] = 0.0f;
+                if (q.t == c + i) v[i] -= q.own;
+                sum[i] += v[i];
+                low[i] = v[i] - (float)(typename T::e)v[i];
+                if (q.t == c + i) a.rest[r] = low[i];
+            }
+            store_some<T, 4>(a.dz, at, 4, v);
+            store_some<T, 4>(a.low, at, 4, low);
+        }
+    }
+    if (a.sums == nullptr) return;
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= a.nc) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += sums[w][lane];
+    const float back = scale_back(a.given);
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = sum[i] * back;
+    store_floats(a.sums + c, a.nc - c, f);
 }
 
 // k_ce_pack: up to two matrices whose rows start anywhere, copied to rows of whole lines, for the tiles that are loaded directly.
@@ -664,9 +748,18 @@ extern "C" int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream)
 extern "C" int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream)
 {
     const dim3 grid((unsigned)(a->nr * a->slices));
-    void (*const f)(const DlfCeDzArgs) = dtype == DLF_F16 ? (a->lse != nullptr ? k_ce_dz<F16, false> : k_ce_dz<F16, true>)
-                                                          : (a->lse != nullptr ? k_ce_dz<BF16, false> : k_ce_dz<BF16, true>);
+    const bool h = dtype == DLF_F16;
+    void (*const f)(const DlfCeDzArgs) = a->z != nullptr     ? h ? k_ce_dz<F16, true, true> : k_ce_dz<BF16, true, true>
+                                         : a->lse != nullptr ? h ? k_ce_dz<F16, false, false> : k_ce_dz<BF16, false, false>
+                                                             : h ? k_ce_dz<F16, true, false> : k_ce_dz<BF16, true, false>;
     hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)stream, *a);
+    return (int)hipGetLastError();
+}
+extern "C" int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int dtype, void* stream)
+{
+    const dim3 grid((unsigned)((a->ldz + 255) / 256));
+    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz_few<F16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
+    else hipLaunchKernelGGL(k_ce_dz_few<BF16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream)

@@ -196,8 +196,31 @@ int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int, void*)
     NEED(DLF_FF_ROWS_LDS(c->waves, c->nf, c->mr, 0) <= 160 * 1024);
     use("part", a->part, (double)up(a->t.nc, 16) * a->t.nr * 8);
     use("at", a->at, (double)a->t.nr * 4);
-    g.kept = false;
+    if (a->z) use("z", a->z, (double)a->t.nr * a->ldz * 4);
+    g.kept = a->z != nullptr;
     g.parts = up(a->t.nc, 16);
+    return 0;
+}
+int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int, void*)
+{
+    ++g.launches;
+    ++g_seen["dz few"];
+    NEED(g.kept && a->nr == g.d->rows && a->nr <= DLF_FF_FEW_ROWS && a->nc == g.d->classes && a->ldz % 8 == 0);
+    given(a->given);
+    use("z", a->z, (double)a->nr * a->ldz * 4);
+    use("dz", a->dz, (double)a->nr * a->ldz * 2);
+    if (in_ws(a->lse)) {
+        use("lse", a->lse, (double)a->nr * 4);
+        use("inverse", a->inverse, (double)a->nr * 4);
+    } else {
+        NEED(a->lse == g.lse && !a->inverse);
+    }
+    rest_low(a->rest, a->low, a->nr, a->ldz);
+    NEED(a->low && a->sums == g.db);
+    if (a->sums) ++g.sums_out;
+    if (a->given.one > 0) use("unit", a->back, 4);
+    g.rows_done += a->nr;
+    g.kept = false;
     return 0;
 }
 int dlf_ce_start_join(const DlfCeJoinArgs* a, void*)
@@ -216,7 +239,11 @@ int dlf_ce_start_join(const DlfCeJoinArgs* a, void*)
 int dlf_ce_start_dz(const DlfCeDzArgs* a, int, void*)
 {
     ++g.launches;
-    ++g_seen[a->lse ? "dz" : "dz with lse"];
+    ++g_seen[a->z ? "dz of logits" : a->lse ? "dz" : "dz with lse"];
+    if (a->z) {
+        NEED(!a->lse && g.d->rows <= DLF_FF_FEW_ROWS);
+        use("z", a->z, (double)a->nr * a->ldz * 4);
+    }
     NEED(g.kept && a->parts == g.parts && a->parts == up(a->nc, a->width) && (a->width & (a->width - 1)) == 0 && a->nc == g.d->classes);
     NEED(a->slices == up(a->ldz, DLF_CE_DZ_COLS) && (int64_t)a->nr * a->slices * 256 < (int64_t)1 << 32);
     given(a->given);
