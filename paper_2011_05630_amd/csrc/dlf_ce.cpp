@@ -32,7 +32,9 @@ constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;       // a launch holds fe
 constexpr int64_t LEAST_PIECE = 256, MOST_PIECE = 1 << 16;  // rows
 // Whether operands whose rows start anywhere are copied to rows of whole lines first: modelled in ns, a launch and the copy against what `products` products
 // take longer on tiles through registers.  Bf16, us with the copy and without: loss of 1024 x 2051 over 32001 classes 178 and 205, of 768 rows 184 and 158;
-// with gradients 2048 rows 942 and 1325, 512 339 and 363, 256 245 and 212; 1024 x 770 over 5003 classes 69 and 72, 512 rows 52 and 51.
+// with gradients 2048 rows 942 and 1325, 512 339 and 363, 256 245 and 212; 1024 x 770 over 5003 classes 69 and 72, 512 rows 52 and 51.  With the bias's
+// gradient the logits are formed twice: 515 x 770 over 5003 classes, fp16, 62 and 71.
+constexpr int PRODUCTS_LOSS = 1, PRODUCTS_GRADIENTS = 3, PRODUCTS_BIAS = 5;
 bool copy_pays(int64_t rows, int64_t in, int64_t classes, int products)
 {
     return rows > DLF_FF_FEW_ROWS && products * 1.2e-6 * (double)rows * in * classes > 5000 + 4.0 * (double)(rows + classes) * in / 3800;
@@ -47,7 +49,7 @@ struct Ce {
     const char* call;
     int64_t ldz, piece;     // elements of a row of dz; rows
     int64_t lines;          // 16-byte parts of a row of x or weight
-    bool pack_x, pack_w;    // copied to rows of whole lines
+    bool pack_x, pack_w;    // copied to rows of whole lines, or room for it
     int64_t pieces() const { return std::max<int64_t>(1, ceil_div(d.rows, piece)); }
     int64_t first(int64_t p) const { return p * piece; }
     int64_t rows(int64_t p) const { return std::min(piece, d.rows - p * piece); }
@@ -88,7 +90,7 @@ dlf_status check_desc(const dlf_ce_desc* d, bool gradients, const char* call, Ce
     const int64_t n = std::max<int64_t>(1, ceil_div(d->rows, f.piece));
     f.piece = std::max(LEAST_PIECE, ceil_div(ceil_div(d->rows, n), LEAST_PIECE) * LEAST_PIECE);
     f.lines = ceil_div(d->in_features, 8);
-    const bool pays = copy_pays(d->rows, d->in_features, d->classes, gradients ? 3 : 1) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
+    const bool pays = copy_pays(d->rows, d->in_features, d->classes, gradients ? PRODUCTS_BIAS : PRODUCTS_LOSS) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
     f.pack_x = pays && !dlf_ff_lines(nullptr, f.d.x_stride, d->in_features);
     f.pack_w = pays && !dlf_ff_lines(nullptr, f.d.w_stride, d->in_features);
     return DLF_OK;
@@ -203,7 +205,7 @@ struct Piece {
     int64_t ldx, ldw;
     bool whole;             // rows of whole lines
 };
-dlf_status piece_of(const Ce& f, const In& in, int64_t p, const Layout& l, char* ws, Piece& q, void* stream)
+dlf_status piece_of(const Ce& f, const In& in, int64_t p, int products, const Layout& l, char* ws, Piece& q, void* stream)
 {
     q.first = f.first(p);
     q.rows = f.rows(p);
@@ -212,18 +214,19 @@ dlf_status piece_of(const Ce& f, const In& in, int64_t p, const Layout& l, char*
     q.ldx = f.d.x_stride;
     q.ldw = f.d.w_stride;
     const bool x = dlf_ff_lines(in.x, q.ldx, f.d.in_features), w = dlf_ff_lines(in.w, q.ldw, f.d.in_features);
-    q.whole = (x || f.pack_x) && (w || f.pack_w);
+    const bool pays = copy_pays(f.d.rows, f.d.in_features, f.d.classes, products);
+    q.whole = (x || (f.pack_x && pays)) && (w || (f.pack_w && pays));
     if (!q.whole || (x && w) || q.rows == 0) return DLF_OK;
     DlfCePackArgs a;
     memset(&a, 0, sizeof a);
     a.k = f.d.in_features;
     a.parts = (int)f.lines;
-    if (f.pack_x) {
+    if (f.pack_x && !x) {
         a.m[0] = {q.x, ws + l.x, q.ldx, q.rows};
         q.x = ws + l.x;
         q.ldx = f.lines * 8;
     }
-    if (f.pack_w) {
+    if (f.pack_w && !w) {
         if (p == 0) a.m[1] = {q.w, ws + l.w, q.ldw, f.d.classes};
         q.w = ws + l.w;
         q.ldw = f.lines * 8;
@@ -302,7 +305,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
     for (int64_t p = 0; p < pieces; ++p) {
         int chunks = 0;
         Piece q;
-        TRY(piece_of(f, in, p, l, ws, q, stream));
+        TRY(piece_of(f, in, p, out.db && !lse ? PRODUCTS_BIAS : PRODUCTS_GRADIENTS, l, ws, q, stream));
         DlfCeGiven g = given;
         if (g.dloss) g.dloss += q.first * g.dloss_stride;
         if (g.dlse) g.dlse += q.first * g.dlse_stride;
@@ -312,7 +315,9 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
             if (!lse || (few && wanted)) TRY(logits(f, in, q, wanted && !few, keep, few && wanted ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
-            if (!lse && !keep && !(few && wanted && !out.db)) {
+            // (a row's lse formed by each of its workgroups, of so many parts, takes longer than a launch: 15 rows of 103104 classes 23 us)
+            const bool forms = few && wanted && !out.db && ceil_div(nc, 16) <= 3000;
+            if (!lse && !keep && !forms) {
                 float* const to = (float*)(ws + l.lse);
                 inverse = (float*)(ws + l.inverse);
                 TRY(join(f, in, q, l, ws, width, piece_loss, to, inverse, stream));
@@ -477,7 +482,7 @@ dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* we
     for (int64_t p = 0; p < f.pieces(); ++p) {
         Piece q;
         int width;
-        TRY(piece_of(f, in, p, l, (char*)workspace, q, hip_stream));
+        TRY(piece_of(f, in, p, PRODUCTS_LOSS, l, (char*)workspace, q, hip_stream));
         TRY(logits(f, in, q, false, false, nullptr, l, (char*)workspace, width, hip_stream));
         TRY(join(f, in, q, l, (char*)workspace, width, loss + q.first, lse ? lse + q.first : nullptr, nullptr, hip_stream));
     }

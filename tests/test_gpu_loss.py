@@ -87,6 +87,20 @@ def test_pieces(dtype, bias):
     check_all(513, 41, 130, dtype, 4, bias, 0.0, gap=5, offset=1, piece_bytes=1)
 
 
+@pytest.mark.parametrize("m,k,v,gap,offset,bias,piece_bytes", [(1500, 520, 3000, 5, 3, False, 1 << 30), (1500, 521, 3000, 0, 0, True, 1 << 30),
+                                                               (1300, 521, 3000, 8, 1, False, 1), (1300, 523, 2999, 3, 0, True, 1), (4000, 1001, 3000, 0, 0, False, 1 << 30)])
+def test_operands_copied_to_whole_lines(m, k, v, gap, offset, bias, piece_bytes):
+    """Sizes at which rows that start anywhere are copied first: x alone, both, the weight once for several pieces, and for a loss alone."""
+    check_all(m, k, v, "bf16", 61, bias, 0.2, gap=gap, offset=offset, piece_bytes=piece_bytes)
+
+
+@pytest.mark.parametrize("m", [1, 3, 64, 65, 130])
+@pytest.mark.parametrize("bias", [False, True])
+def test_many_classes(m, bias):
+    """So many that a row's parts are joined by a launch of their own."""
+    check_all(m, 16, 60001, "bf16", 62, bias, 0.0)
+
+
 def test_leading_dimensions_and_gradients_of_one_element():
     from paper_2011_05630_amd import loss
     x, w, b, target, on = inputs(24, 40, 100, torch.bfloat16, 11, bias=True, ignored=0.3)
