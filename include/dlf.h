@@ -361,7 +361,8 @@ dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* 
  * piece's dz stays in the workspace, in at most `piece_bytes` (but for 256 rows at least), in the tensors' type, which the matrix units
  * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14, so that a mean over many rows does not vanish,
  * and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
- * dlf_cross_entropy_gradients, where no dbias is wanted, keeps exp(z - a maximum) in 16 bits (eleven behind the point) in between rather than computing the logits again.
+ * dlf_cross_entropy_gradients does not compute the logits again: where dbias is wanted, it keeps them in 32 bits, in twice what dz takes, beside it, else
+ * exp(z - a maximum) in 16 bits (eleven behind the point) in dz's place.
  * Nothing depends on timing: equal calls give equal bits.
  *
  * Tensors are DEVICE and row-major: x [rows][in_features], weight [classes][in_features], of type `dtype`, a row's elements next to
@@ -375,7 +376,7 @@ typedef struct {
     int32_t in_features;        /* 1 .. 2^20                                                              */
     int64_t rows;               /* 0 .. 2^30                                                              */
     int32_t classes;            /* 1 .. 2^20                                                              */
-    int32_t reserved;           /* 0                                                                      */
+    int32_t dbias;              /* dlf_cross_entropy_gradients: 1 if dbias may be wanted, else 0          */
     int64_t ignore;             /* the target of a row that counts for nothing                            */
     int64_t x_stride;           /* elements from row to row, >= the row, < 2^24; 0: the row               */
     int64_t w_stride;           /* ... of weight                                                          */

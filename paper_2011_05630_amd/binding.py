@@ -65,7 +65,7 @@ class FfDesc(ctypes.Structure):
 
 class CeDesc(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("in_features", ctypes.c_int32), ("rows", ctypes.c_int64),
-                ("classes", ctypes.c_int32), ("reserved", ctypes.c_int32), ("ignore", ctypes.c_int64),
+                ("classes", ctypes.c_int32), ("dbias", ctypes.c_int32), ("ignore", ctypes.c_int64),
                 ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("piece_bytes", ctypes.c_int64)]
 
 
@@ -462,9 +462,10 @@ def dlf_gated_backward(desc, dh, x, w_gate, w_up, saved, dx, dw_gate, dw_up, db_
                                     stream))
 
 
-def dlf_ce_desc(dtype, rows, in_features, classes, ignore=-100, x_stride=0, w_stride=0, piece_bytes=0):
-    """The description of a cross entropy call; dtype: "fp16" or "bf16", strides in elements (0: rows next to each other)."""
-    return CeDesc(DTYPE[dtype], in_features, rows, classes, 0, ignore, x_stride, w_stride, piece_bytes)
+def dlf_ce_desc(dtype, rows, in_features, classes, ignore=-100, x_stride=0, w_stride=0, piece_bytes=0, dbias=0):
+    """The description of a cross entropy call; dtype: "fp16" or "bf16", strides in elements (0: rows next to each other), dbias: 1 where
+    dlf_cross_entropy_gradients is to give it."""
+    return CeDesc(DTYPE[dtype], in_features, rows, classes, dbias, ignore, x_stride, w_stride, piece_bytes)
 
 
 def dlf_cross_entropy_workspace_bytes(desc):

@@ -32,12 +32,12 @@ constexpr int64_t MOST_WORKGROUPS = (int64_t)1 << 24;       // a launch holds fe
 constexpr int64_t LEAST_PIECE = 256, MOST_PIECE = 1 << 16;  // rows
 // Whether operands whose rows start anywhere are copied to rows of whole lines first: modelled in ns, a launch and the copy against what `products` products
 // take longer on tiles through registers.  Bf16, us with the copy and without: loss of 1024 x 2051 over 32001 classes 178 and 205, of 768 rows 184 and 158;
-// with gradients 2048 rows 942 and 1325, 512 339 and 363, 256 245 and 212; 1024 x 770 over 5003 classes 69 and 72, 512 rows 52 and 51.  With the bias's
-// gradient the logits are formed twice: 515 x 770 over 5003 classes, fp16, 62 and 71.
-constexpr int PRODUCTS_LOSS = 1, PRODUCTS_GRADIENTS = 3, PRODUCTS_BIAS = 5;
+// with gradients 2048 rows 942 and 1325, 512 339 and 363, 256 255 and 209; 1300 x 523 over 2999 classes, fp16, 56 and 71, 515 x 770 over 5003 55 and 56,
+// 300 rows 48 and 45; with a bias 62 and 77, 61 and 62, 54 and 51.
+constexpr int PRODUCTS_LOSS = 1, PRODUCTS_GRADIENTS = 3;
 bool copy_pays(int64_t rows, int64_t in, int64_t classes, int products)
 {
-    return rows > DLF_FF_FEW_ROWS && products * 1.2e-6 * (double)rows * in * classes > 5000 + 4.0 * (double)(rows + classes) * in / 3800;
+    return rows > DLF_FF_FEW_ROWS && products * 1.2e-6 * (double)rows * in * classes > 4400 + 4.0 * (double)(rows + classes) * in / 3800;
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -69,7 +69,7 @@ dlf_status check_desc(const dlf_ce_desc* d, bool gradients, const char* call, Ce
     f.d = *d;
     f.call = call;
     if (d->dtype != DLF_F16 && d->dtype != DLF_BF16) return fail(DLF_ERR_INVALID_ARG, "%s: dtype %d", call, d->dtype);
-    if (d->reserved != 0) return fail(DLF_ERR_INVALID_ARG, "%s: reserved is not 0", call);
+    if (d->dbias != 0 && d->dbias != 1) return fail(DLF_ERR_INVALID_ARG, "%s: dbias %d, 0 or 1 expected", call, d->dbias);
     if (d->rows < 0 || d->rows > (int64_t)1 << 30) return fail(DLF_ERR_INVALID_ARG, "%s: %lld rows", call, (long long)d->rows);
     if (d->in_features < 1 || d->in_features > 1 << 20 || d->classes < 1 || d->classes > 1 << 20)
         return fail(DLF_ERR_INVALID_ARG, "%s: %d features, %d classes", call, d->in_features, d->classes);
@@ -90,7 +90,7 @@ dlf_status check_desc(const dlf_ce_desc* d, bool gradients, const char* call, Ce
     const int64_t n = std::max<int64_t>(1, ceil_div(d->rows, f.piece));
     f.piece = std::max(LEAST_PIECE, ceil_div(ceil_div(d->rows, n), LEAST_PIECE) * LEAST_PIECE);
     f.lines = ceil_div(d->in_features, 8);
-    const bool pays = copy_pays(d->rows, d->in_features, d->classes, gradients ? PRODUCTS_BIAS : PRODUCTS_LOSS) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
+    const bool pays = copy_pays(d->rows, d->in_features, d->classes, gradients ? PRODUCTS_GRADIENTS : PRODUCTS_LOSS) && (f.piece + d->classes) * f.lines / 256 < MOST_WORKGROUPS - 16;
     f.pack_x = pays && !dlf_ff_lines(nullptr, f.d.x_stride, d->in_features);
     f.pack_w = pays && !dlf_ff_lines(nullptr, f.d.w_stride, d->in_features);
     return DLF_OK;
@@ -150,8 +150,8 @@ struct Layout {
         return here;
     }
 };
-// logits: their parts are needed; gradients: what the gradients need
-Layout layout_of(const Ce& f, bool logits, bool gradients)
+// logits: their parts are needed; gradients: what the gradients need; kept: the logits in 32 bits
+Layout layout_of(const Ce& f, bool logits, bool gradients, bool kept = false)
 {
     Layout l;
     const int64_t most = std::min(f.piece, f.d.rows), nc = f.d.classes;
@@ -173,12 +173,13 @@ Layout layout_of(const Ce& f, bool logits, bool gradients)
         l.lse = l.take((size_t)most * 4);
     }
     if (!gradients) return l;
-    if (dlf_ff_is_few(most)) l.z = l.take((size_t)most * f.ldz * 4);
+    if (kept || dlf_ff_is_few(most)) l.z = l.take((size_t)most * f.ldz * 4);
     l.inverse = l.take((size_t)most * 4);
     l.unit = l.take(8);
     l.rest = l.take((size_t)most * 4);
     l.dz = l.take((size_t)most * f.ldz * 2);
     if (twice(f)) l.low = l.take((size_t)most * f.ldz * 2);
+    chunks = std::max(chunks, ceil_div(most, DLF_CE_DZ_ROWS));
     l.sums = l.take((size_t)(1 + chunks) * nc * 4);         // the pieces' in front, the piece's chunks
     if (f.pieces() > 1) l.sum = l.take((size_t)nc * f.d.in_features * 4);
     size_t join = 0;
@@ -251,7 +252,7 @@ void set_cut(DlfFfArgs& a, const DlfFfCut& c)
     a.tiles_c = c.tiles_c;
 }
 
-// The parts of a piece's rows; keep: the exponentials too, in dz; z: of few rows the logits, there.  tiles: by the kernel that forms dz, whose logits
+// The parts of a piece's rows; keep: the exponentials too, in dz; z: the logits too, there.  tiles: by the kernel that forms dz, whose logits
 // have the same bits: where a target is nearly sure, 1 - p is what is left of them.  -> the classes of a part
 dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool keep, float* z, const Layout& l, char* ws, int& width, void* stream)
 {
@@ -269,7 +270,7 @@ dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool ke
     set_cut(a.t, c);
     if (keep) a.dz = ws + l.dz;
     width = dlf_ce_width(c.shape);
-    return launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : DLF_CE_STAT, stream));
+    return launched(f, dlf_ce_start_tile(&a, c.shape, f.d.dtype, keep ? DLF_CE_KEEP : z ? DLF_CE_LOGITS : DLF_CE_STAT, stream));
 }
 // ... and from them loss and lse, either of which may be null.
 dlf_status join(const Ce& f, const In& in, const Piece& q, const Layout& l, char* ws, int width, float* loss, float* lse, float* inverse, void* stream)
@@ -288,7 +289,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
 {
     // Few rows: their logits are kept in 32 bits, which costs less than to form them again.
     const bool few = dlf_ff_is_few(f.d.rows);
-    const Layout l = layout_of(f, lse == nullptr || few, true);
+    const Layout l = layout_of(f, lse == nullptr || few, true, lse == nullptr && f.d.dbias);
     const int64_t pieces = f.pieces(), nc = f.d.classes, k = f.d.in_features;
     const bool wanted = out.dx || out.dw || out.db;
     TRY(kernels_ready());
@@ -300,12 +301,12 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
         given.unit = u.unit;
     }
     float* const back = given.one > 0.0f && f.d.rows > 0 && wanted ? (float*)(ws + l.unit) : nullptr;
-    // The exponentials are kept where they need not say what the bias's gradient is, which has 32 bits.
-    const bool keep = !lse && wanted && !out.db && !few;
+    // The exponentials are kept where they need not say what the bias's gradient is, which has 32 bits; where they do, the logits are.
+    const bool keep = !lse && wanted && !out.db && !few, keep_logits = (few && wanted) || (!lse && out.db);
     for (int64_t p = 0; p < pieces; ++p) {
         int chunks = 0;
         Piece q;
-        TRY(piece_of(f, in, p, out.db && !lse ? PRODUCTS_BIAS : PRODUCTS_GRADIENTS, l, ws, q, stream));
+        TRY(piece_of(f, in, p, PRODUCTS_GRADIENTS, l, ws, q, stream));
         DlfCeGiven g = given;
         if (g.dloss) g.dloss += q.first * g.dloss_stride;
         if (g.dlse) g.dlse += q.first * g.dlse_stride;
@@ -314,7 +315,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             const float* piece_lse = lse ? lse + q.first : nullptr;
             float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
-            if (!lse || (few && wanted)) TRY(logits(f, in, q, wanted && !few, keep, few && wanted ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
+            if (!lse || keep_logits) TRY(logits(f, in, q, wanted && !few, keep, keep_logits ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
             // (a row's lse formed by each of its workgroups, of so many parts, takes longer than a launch: 15 rows of 103104 classes 23 us)
             const bool forms = few && wanted && !out.db && ceil_div(nc, 16) <= 3000;
             if (!lse && !keep && !forms) {
@@ -335,10 +336,11 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             z.given = g; z.rest = (float*)(ws + l.rest); z.back = back;
             z.low = twice(f) ? ws + l.low : nullptr;
             if (width > 0) { z.width = width; z.parts = (int)ceil_div(nc, width); }
-            if (few) {
+            if (keep_logits) {
                 z.z = (const float*)(ws + l.z);
-                z.sums = out.db;
-                TRY(launched(f, piece_lse ? dlf_ce_start_dz_few(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
+                if (out.db) z.sums = few ? out.db : (float*)(ws + l.sums) + nc;
+                if (!few) chunks = (int)ceil_div(q.rows, DLF_CE_DZ_ROWS);
+                TRY(launched(f, piece_lse ? dlf_ce_start_dz_sums(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else if (keep) {
                 // (workgroups that do not run at once do not form their rows' lse)
                 if (q.rows * z.slices > 2048) {
@@ -426,10 +428,10 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
     return DLF_OK;
 }
 
-size_t bytes_of(const dlf_ce_desc* d, bool logits, bool gradients, const char* call)
+size_t bytes_of(const dlf_ce_desc* d, bool logits, bool gradients, bool kept, const char* call)
 {
     Ce f;
-    return check_desc(d, gradients, call, f) == DLF_OK ? layout_of(f, logits, gradients).bytes : SIZE_MAX;
+    return check_desc(d, gradients, call, f) == DLF_OK ? layout_of(f, logits, gradients, kept && d->dbias).bytes : SIZE_MAX;
 }
 dlf_status check_in(const Ce& f, const In& in)
 {
@@ -459,12 +461,12 @@ dlf_status check_out(const Ce& f, const Out& o)
 
 extern "C" {
 
-size_t dlf_cross_entropy_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, false, "dlf_cross_entropy_workspace_bytes"); }
+size_t dlf_cross_entropy_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, false, false, "dlf_cross_entropy_workspace_bytes"); }
 size_t dlf_cross_entropy_backward_workspace_bytes(const dlf_ce_desc* d)
 {
-    return bytes_of(d, d && dlf_ff_is_few(d->rows), true, "dlf_cross_entropy_backward_workspace_bytes");
+    return bytes_of(d, d && dlf_ff_is_few(d->rows), true, false, "dlf_cross_entropy_backward_workspace_bytes");
 }
-size_t dlf_cross_entropy_gradients_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, true, "dlf_cross_entropy_gradients_workspace_bytes"); }
+size_t dlf_cross_entropy_gradients_workspace_bytes(const dlf_ce_desc* d) { return bytes_of(d, true, true, true, "dlf_cross_entropy_gradients_workspace_bytes"); }
 
 dlf_status dlf_cross_entropy(const dlf_ce_desc* d, const void* x, const void* weight, const float* bias, const int64_t* target, float* loss,
                              float* lse, void* workspace, size_t workspace_bytes, void* hip_stream)
@@ -521,7 +523,8 @@ dlf_status dlf_cross_entropy_gradients(const dlf_ce_desc* d, const void* x, cons
     TRY(check_given(f, given));
     TRY(check_ptr(f, loss, "loss", f.d.rows > 0, 4));
     TRY(check_out(f, out));
-    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, true, true).bytes));
+    if (dbias && !f.d.dbias) return fail(DLF_ERR_INVALID_ARG, "%s: dbias is not in the description", f.call);
+    TRY(check_ws(f, workspace, workspace_bytes, layout_of(f, true, true, f.d.dbias).bytes));
     return gradients(f, in, nullptr, given, loss, out, (char*)workspace, hip_stream);
 }
 

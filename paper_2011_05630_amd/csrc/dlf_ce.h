@@ -5,7 +5,8 @@
 // What a product's epilogue does with the logits of its tile.
 enum { DLF_CE_STAT = 0,         // a maximum and a sum of exponentials of each row over a part of the classes, the target's logit
        DLF_CE_KEEP = 1,         // ... and the exponentials themselves, in 16 bits
-       DLF_CE_DZ = 2 };         // their gradient
+       DLF_CE_DZ = 2,           // their gradient
+       DLF_CE_LOGITS = 3 };     // STAT, and the logits themselves, in 32 bits
 // A row's gradients of loss and lse as the caller gives them.
 struct DlfCeGiven {
     const float *dloss, *dlse;  // null: dloss_value, none
@@ -30,7 +31,7 @@ struct DlfCeArgs {
     int64_t ignore;
     float* part;                // [parts][nr] {maximum, sum of exp(z - maximum)}
     float* at;                  // [nr] the target's logit, of rows whose target is a class
-    float* z;                   // few rows: [nr][ldz] their logits, or null
+    float* z;                   // few rows (where not null), LOGITS: [nr][ldz] the logits
     void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: exp(z - its part's maximum) in 16 bits
     int64_t ldz;                // a multiple of eight
     const float *lse, *inverse; // DZ: p = exp(z - lse) * inverse (null: 1)
@@ -51,7 +52,7 @@ struct DlfCeJoinArgs {
 };
 struct DlfCeDzArgs {
     void* dz;                   // KEEP's in, dz out
-    const float* z;             // ... or the logits of few rows in, and nothing in dz
+    const float* z;             // ... or the logits in, and nothing in dz
     int64_t ldz;
     const float* part;
     const float* at;
@@ -61,12 +62,12 @@ struct DlfCeDzArgs {
     const int64_t* target;
     int64_t ignore;
     const float* lse;           // or null: lse and loss are formed here
-    const float* inverse;       // of few rows, as in DlfCeArgs
+    const float* inverse;       // of logits, as in DlfCeArgs
     float* loss;
     DlfCeGiven given;
     float *rest, *back;         // as in DlfCeArgs
     void* low;
-    float* sums;                // of few rows: [nc] column sums of dz, scaled back, or null
+    float* sums;                // of logits: [chunks of DLF_CE_DZ_ROWS][nc] column sums of dz, scaled back, or null
 };
 struct DlfCeUnitArgs {
     DlfCeGiven given;
@@ -89,6 +90,8 @@ static inline int dlf_ce_chunk(int shape) { return DLF_FF_SHAPES[shape].br / 2; 
 #define DLF_CE_JOIN_FEW 256
 // Columns of a workgroup of k_ce_dz.
 #define DLF_CE_DZ_COLS 2048
+// Rows of a workgroup of k_ce_dz_sums, which has 256 columns.
+#define DLF_CE_DZ_ROWS 64
 
 extern "C" {
 int dlf_ce_kernels_init(void);
@@ -96,7 +99,7 @@ int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int dtype, int mode, void* 
 int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int dtype, void* stream);
 int dlf_ce_start_join(const DlfCeJoinArgs* a, void* stream);
 int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream);
-int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int dtype, void* stream);
+int dlf_ce_start_dz_sums(const DlfCeDzArgs* a, int dtype, void* stream);
 int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream);
 int dlf_ce_start_unit(const DlfCeUnitArgs* a, void* stream);
 int dlf_ce_start_back(const DlfCeBackArgs* a, int shape, int dtype, void* stream);

@@ -157,6 +157,13 @@ template <int MODE> struct Entropy {
                     for (int k = 0; k < 16; ++k)
                         if (near && rel == i * 32 + (k >> 2) * 8 + (k & 3)) z[i][k] = f(z[i][k]);
             };
+            auto to_lds = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < FC; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *(f4v*)(lf + l32 * CROW + i * 32 + q * 8 + lhi * 4) = f4v{z[i][q * 4], z[i][q * 4 + 1], z[i][q * 4 + 2], z[i][q * 4 + 3]};
+            };
             if constexpr (MODE == DLF_CE_DZ) {
                 RowGradient g = row_gradient(e.given, at, t, e.ignore, a.nc);
                 if (r >= a.nr) g.total = g.own = 0.0f;
@@ -189,6 +196,7 @@ template <int MODE> struct Entropy {
             } else {
                 float m = MINUS_INF, s = 0.0f;
                 cut(MINUS_INF);
+                if (MODE == DLF_CE_LOGITS) to_lds();
 #pragma unroll
                 for (int i = 0; i < FC; ++i)
 #pragma unroll
@@ -210,11 +218,7 @@ template <int MODE> struct Entropy {
                 }
             }
             if constexpr (MODE != DLF_CE_STAT) {
-#pragma unroll
-                for (int i = 0; i < FC; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        *(f4v*)(lf + l32 * CROW + i * 32 + q * 8 + lhi * 4) = f4v{z[i][q * 4], z[i][q * 4 + 1], z[i][q * 4 + 2], z[i][q * 4 + 3]};
+                if (MODE != DLF_CE_LOGITS) to_lds();
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll 2
                 for (int u = 0; u < 32; u += RPU) {
@@ -230,6 +234,8 @@ template <int MODE> struct Entropy {
                         // one rounding to the type that the matrix units multiply
                         if (in) store_some<T, 8>(e.dz, to, 8, v);
                         if (in && e.low != nullptr) store_low<T>(e.low, to, v);
+                    } else if (MODE == DLF_CE_LOGITS) {
+                        if (in) __builtin_memcpy(e.z + to, v, 32);
                     } else {
                         uint32_t w[4];
 #pragma unroll
@@ -453,25 +459,26 @@ template <typename T, bool FORM, bool LOGITS> __global__ __launch_bounds__(256) 
     if (a.low != nullptr) store_low<T>(a.low, at, v);
 }
 
-// k_ce_dz_few: dz of few rows from their logits, kept in 32 bits, and its column sums.  p = exp(z - lse) * inverse.  A workgroup takes 256 classes, four to a
-// lane, its waves every eighth row; their sums meet in LDS, in a fixed order.  Bound by latency: a wave to all rows took 28 us for 60 of them.
-template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_few(const DlfCeDzArgs a)
+// k_ce_dz_sums: dz from the logits, kept in 32 bits, and its column sums.  p = exp(z - lse) * inverse.  A workgroup takes 256 classes, four to a
+// lane, of 64 rows, its waves every eighth row; their sums meet in LDS, in a fixed order.  Few rows are bound by latency (a wave to all rows took 28 us for 60 of them),
+// many by memory: 4096 rows of 32000 classes 155 us (5.1 TB/s).
+template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_sums(const DlfCeDzArgs a)
 {
     constexpr int WAVES = 8;
-    static_assert(DLF_FF_FEW_ROWS <= WAVES * 64, "a thread for each row");
+    static_assert(DLF_CE_DZ_ROWS <= WAVES * 64 && DLF_FF_FEW_ROWS <= DLF_CE_DZ_ROWS, "a thread for each row, one workgroup for few rows");
     struct Row {
         float total, own, lse, zero;
         int t;              // the target's class, or -1
     };
-    __shared__ Row rows[DLF_FF_FEW_ROWS];
+    __shared__ Row rows[DLF_CE_DZ_ROWS];
     __shared__ f4v sums[WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if ((int)threadIdx.x < a.nr) {
-        const int r = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.y * DLF_CE_DZ_ROWS, nr = min(a.nr - first, DLF_CE_DZ_ROWS);
+    if ((int)threadIdx.x < nr) {
+        const int r = first + threadIdx.x;
         const int64_t t = a.target[r];
         const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
         const bool is_class = t >= 0 && t < a.nc;
-        rows[r] = Row{a.inverse != nullptr ? g.total * a.inverse[r] : g.total, g.own, a.lse[r], g.total, is_class ? (int)t : -1};
+        rows[threadIdx.x] = Row{a.inverse != nullptr ? g.total * a.inverse[r] : g.total, g.own, a.lse[r], g.total, is_class ? (int)t : -1};
         if (blockIdx.x == 0 && !is_class) a.rest[r] = 0.0f;
         if (blockIdx.x == 0 && r == 0 && a.back != nullptr) *a.back = scale_back(a.given);
     }
@@ -479,15 +486,15 @@ template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_few(const D
     const int c = (blockIdx.x * 64 + lane) * 4;
     f4v sum = f4v{0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int AT = 4;                                   // rows whose loads share a wait
-    for (int r0 = wave; c < a.ldz && r0 < a.nr; r0 += AT * WAVES) {
+    for (int r0 = wave; c < a.ldz && r0 < nr; r0 += AT * WAVES) {
         f4v z[AT];
 #pragma unroll
-        for (int k = 0; k < AT; ++k) z[k] = *(const f4v*)(a.z + (int64_t)min(r0 + k * WAVES, a.nr - 1) * a.ldz + c);
+        for (int k = 0; k < AT; ++k) z[k] = *(const f4v*)(a.z + (int64_t)(first + min(r0 + k * WAVES, nr - 1)) * a.ldz + c);
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            const int r = r0 + k * WAVES;
-            if (r >= a.nr) break;
-            const Row q = rows[r];
+            if (r0 + k * WAVES >= nr) break;
+            const Row q = rows[r0 + k * WAVES];
+            const int r = first + r0 + k * WAVES;
             const int64_t at = (int64_t)r * a.ldz + c;
             float v[4], low[4];
 #pragma unroll
@@ -500,7 +507,7 @@ template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_few(const D
                 if (q.t == c + i) a.rest[r] = low[i];
             }
             store_some<T, 4>(a.dz, at, 4, v);
-            store_some<T, 4>(a.low, at, 4, low);
+            if (a.low != nullptr) store_some<T, 4>(a.low, at, 4, low);
         }
     }
     if (a.sums == nullptr) return;
@@ -513,7 +520,7 @@ template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_few(const D
     float f[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = sum[i] * back;
-    store_floats(a.sums + c, a.nc - c, f);
+    store_floats(a.sums + (int64_t)blockIdx.y * a.nc + c, a.nc - c, f);
 }
 
 // k_ce_pack: up to two matrices whose rows start anywhere, copied to rows of whole lines, for the tiles that are loaded directly.
@@ -677,7 +684,8 @@ template <typename T, int MODE> static CeKernel tile_kernel(int shape)
 }
 template <typename T> static CeKernel tile_kernel(int shape, int mode)
 {
-    return mode == DLF_CE_STAT ? tile_kernel<T, DLF_CE_STAT>(shape) : mode == DLF_CE_KEEP ? tile_kernel<T, DLF_CE_KEEP>(shape) : tile_kernel<T, DLF_CE_DZ>(shape);
+    return mode == DLF_CE_STAT ? tile_kernel<T, DLF_CE_STAT>(shape) : mode == DLF_CE_KEEP ? tile_kernel<T, DLF_CE_KEEP>(shape)
+                                : mode == DLF_CE_DZ ? tile_kernel<T, DLF_CE_DZ>(shape) : tile_kernel<T, DLF_CE_LOGITS>(shape);
 }
 template <typename T> static CeBackKernel back_kernel(int shape)
 {
@@ -710,8 +718,8 @@ extern "C" int dlf_ce_kernels_init(void)
         if (e != hipSuccess) return (int)e;
     }
     for (int shape = 0; shape < DLF_FF_NUM_SHAPES; ++shape)
-        for (int k = 0; k < 8; ++k) {
-            const void* const f = k < 6 ? (const void*)((k & 1) ? tile_kernel<BF16>(shape, k >> 1) : tile_kernel<F16>(shape, k >> 1))
+        for (int k = 0; k < 10; ++k) {
+            const void* const f = k < 8 ? (const void*)((k & 1) ? tile_kernel<BF16>(shape, k >> 1) : tile_kernel<F16>(shape, k >> 1))
                                         : (const void*)((k & 1) ? back_kernel<BF16>(shape) : back_kernel<F16>(shape));
             if (f == nullptr) continue;
             const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds(shape));
@@ -755,11 +763,11 @@ extern "C" int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream)
     hipLaunchKernelGGL(f, grid, dim3(256), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
-extern "C" int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int dtype, void* stream)
+extern "C" int dlf_ce_start_dz_sums(const DlfCeDzArgs* a, int dtype, void* stream)
 {
-    const dim3 grid((unsigned)((a->ldz + 255) / 256));
-    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz_few<F16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
-    else hipLaunchKernelGGL(k_ce_dz_few<BF16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
+    const dim3 grid((unsigned)((a->ldz + 255) / 256), (unsigned)((a->nr + DLF_CE_DZ_ROWS - 1) / DLF_CE_DZ_ROWS));
+    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz_sums<F16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
+    else hipLaunchKernelGGL(k_ce_dz_sums<BF16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream)

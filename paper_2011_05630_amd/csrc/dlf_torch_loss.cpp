@@ -63,7 +63,8 @@ public:
     // -> (loss, dx, dweight, dbias)
     py::tuple gradients(py::handle x, py::handle target, py::handle dloss, bool want_x, bool want_w, bool want_b, int64_t stream) const
     {
-        const Call c = call(x, target);
+        Call c = call(x, target);
+        c.d.dbias = want_b && b_.defined();
         const Given g = given(dloss, "dloss", c, true);
         const c10::DeviceGuard guard(device_);
         const at::Tensor loss = at::empty(c.leading, options(at::kFloat));

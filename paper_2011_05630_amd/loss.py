@@ -13,7 +13,8 @@ class CrossEntropy(_Operator):
     """loss[r] = log sum_c exp(z[r][c]) - z[r][target[r]], z = x weight^T + bias.  weight [classes, in], bias fp32 [classes] or None (a class
     whose bias is -inf takes no part).  A row whose target is `ignore_index` has loss 0 and no gradient; any other target that is no class gives NaN.
 
-    piece_bytes: what the gradients' intermediate results of a piece of the rows may take (256 rows at least)."""
+    piece_bytes: what dz of a piece of the rows may take (256 rows at least).  `gradients` with the bias's among them keeps the piece's logits beside it, twice
+    that much."""
 
     def __init__(self, weight, bias=None, ignore_index=-100, piece_bytes=1 << 30):
         self.weight = _weight(weight, "weight")

@@ -51,12 +51,19 @@ def test_bad_descriptions(kw):
         status(f, d)
 
 
-@pytest.mark.parametrize("field,value", [("dtype", 2), ("dtype", -1), ("reserved", 1)])
+@pytest.mark.parametrize("field,value", [("dtype", 2), ("dtype", -1), ("dbias", 2), ("dbias", -1)])
 def test_bad_fields(field, value):
     d = desc()
     setattr(d, field, value)
     for call in CALLS:
         assert status(call(d)) == B.DLF_ERR_INVALID_ARG
+
+
+def test_a_bias_gradient_that_the_description_does_not_name():
+    d, e = desc(), desc(dbias=1)
+    assert status(gradients(d, db=Q)) == B.DLF_ERR_INVALID_ARG
+    # backward keeps nothing for it
+    assert SIZES[0](d) == SIZES[0](e) and SIZES[1](d) == SIZES[1](e)
 
 
 def test_null_description():
@@ -120,6 +127,9 @@ def test_workspaces_are_bounded_by_the_piece():
     for piece in (1 << 28, 1 << 30):
         got = B.dlf_cross_entropy_gradients_workspace_bytes(desc(rows=65536, in_features=64, classes=131072, piece_bytes=piece))
         assert piece * 0.7 < got < 1.3 * piece + (64 << 20)
+        # ... and the logits, where the bias's gradient is wanted, twice that
+        got = B.dlf_cross_entropy_gradients_workspace_bytes(desc(rows=65536, in_features=64, classes=131072, piece_bytes=piece, dbias=1))
+        assert piece * 2.1 < got < 3.9 * piece + (64 << 20)
     assert B.dlf_cross_entropy_workspace_bytes(desc(rows=65536, in_features=64, classes=131072)) < 1 << 30
 
 

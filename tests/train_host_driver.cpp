@@ -42,7 +42,7 @@ static struct Call {
     const void *x, *w, *dx, *dw;
     const float *lse, *loss, *db, *dloss;
     const int64_t* target;
-    bool kept = false;
+    bool kept = false, lse_given = false;
     std::vector<double> chunks;                              // of an optimizer's call: elements seen of each tensor
     int64_t parts = 0;
 } g;
@@ -179,7 +179,9 @@ int dlf_ce_start_tile(const DlfCeArgs* a, int shape, int, int mode, void*)
         use("part", a->part, (double)up(a->t.nc, dlf_ce_width(shape)) * nr * 8);
         use("at", a->at, nr * 4);
         if (mode == DLF_CE_KEEP) use("dz", a->dz, nr * a->ldz * 2);
-        g.kept = mode == DLF_CE_KEEP;
+        if (mode == DLF_CE_LOGITS) use("z", a->z, nr * a->ldz * 4);
+        NEED((mode == DLF_CE_LOGITS) == (a->z != nullptr));
+        g.kept = mode == DLF_CE_KEEP || mode == DLF_CE_LOGITS;
         g.parts = up(a->t.nc, dlf_ce_width(shape));
     }
     return 0;
@@ -201,11 +203,13 @@ int dlf_ce_start_few(const DlfCeArgs* a, const DlfFfFew* c, int, void*)
     g.parts = up(a->t.nc, 16);
     return 0;
 }
-int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int, void*)
+int dlf_ce_start_dz_sums(const DlfCeDzArgs* a, int, void*)
 {
     ++g.launches;
-    ++g_seen["dz few"];
-    NEED(g.kept && a->nr == g.d->rows && a->nr <= DLF_FF_FEW_ROWS && a->nc == g.d->classes && a->ldz % 8 == 0);
+    const bool few = !a->sums || !in_ws(a->sums);            // (a forced kernel: few rows on tiles)
+    ++g_seen[few ? "dz few" : "dz sums"];
+    NEED(g.kept && a->nr >= 1 && a->nr <= 65536 && a->target - g.target + a->nr <= g.d->rows && a->nc == g.d->classes && a->ldz == up(a->nc, 8) * 8);
+    NEED(up(a->ldz, 256) * up(a->nr, DLF_CE_DZ_ROWS) * 512 < (int64_t)1 << 32);
     given(a->given);
     use("z", a->z, (double)a->nr * a->ldz * 4);
     use("dz", a->dz, (double)a->nr * a->ldz * 2);
@@ -216,8 +220,13 @@ int dlf_ce_start_dz_few(const DlfCeDzArgs* a, int, void*)
         NEED(a->lse == g.lse && !a->inverse);
     }
     rest_low(a->rest, a->low, a->nr, a->ldz);
-    NEED(a->low && a->sums == g.db);
-    if (a->sums) ++g.sums_out;
+    if (few) {
+        NEED(a->low && a->nr == g.d->rows && a->sums == g.db);
+        if (a->sums) ++g.sums_out;
+    } else {
+        NEED(g.db && !g.lse_given);
+        use("sums", a->sums, (double)up(a->nr, DLF_CE_DZ_ROWS) * a->nc * 4);
+    }
     if (a->given.one > 0) use("unit", a->back, 4);
     g.rows_done += a->nr;
     g.kept = false;
@@ -389,6 +398,7 @@ static dlf_status entropy(int c)
     d.rows = rng() % 40 == 0 ? 0 : pick(1, rng() % 3 ? 8192 : 1 << 20);
     d.in_features = (int)pick(1, rng() % 4 ? 12000 : 1 << 20);
     d.classes = (int)pick(1, rng() % 4 ? 140000 : 1 << 20);
+    d.dbias = (int)(rng() % 2);
     d.ignore = -100;
     d.x_stride = stride(d.in_features);
     d.w_stride = stride(d.in_features);
@@ -412,7 +422,8 @@ static dlf_status entropy(int c)
     g.x = x; g.w = w; g.lse = lse; g.loss = loss; g.target = target;
     g.dx = some & 1 ? dx : nullptr;
     g.dw = some & 2 ? dw : nullptr;
-    g.db = some & 4 ? db : nullptr;
+    g.db = some & 4 && (what == 1 || d.dbias) ? db : nullptr;
+    g.lse_given = what == 1;
     g.dloss = some & 8 ? dloss : nullptr;
     const int64_t ls = some & 16 ? 1 : 0;
     const float* const b = some & 32 ? bias : nullptr;
