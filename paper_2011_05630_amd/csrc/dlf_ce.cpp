@@ -43,6 +43,11 @@ bool copy_pays(int64_t rows, int64_t in, int64_t classes, int products)
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+// Up to how many parts a thread takes, and workgroups there are, where the workgroups of k_ce_dz_sums form their rows' lse.  Whole calls, bf16, us with a launch for
+// it and without: 515 x 770 over 5003 classes (10 parts a thread) 59.8 and 57.9, 2000 x 256 over 5000 (10; 640 workgroups) 69.9 and 68.2, 16 x 256 over
+// 16000 (32) 31.8 and 31.1; 60 rows (125) 40.8 and 45.5, 16 x 256 over 60000 (118) 58.9 and 61.5.
+constexpr int64_t MOST_PARTS_OF_A_THREAD = 32, MOST_FORMING = 768;
+
 // A description with its strides filled in, and the rows of a piece.
 struct Ce {
     dlf_ce_desc d;
@@ -318,7 +323,11 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             if (!lse || keep_logits) TRY(logits(f, in, q, wanted && !few, keep, keep_logits ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
             // (a row's lse formed by each of its workgroups, of so many parts, takes longer than a launch: 15 rows of 103104 classes 23 us)
             const bool forms = few && wanted && !out.db && ceil_div(nc, 16) <= 3000;
-            if (!lse && !keep && !forms) {
+            // ... and so do the workgroups of k_ce_dz_sums, while a thread has few parts and all of them run at once.
+            const int64_t chunk = std::min<int64_t>(q.rows, DLF_CE_DZ_ROWS);
+            const bool sums_form = !lse && out.db && ceil_div(ceil_div(nc, width), dlf_ce_dz_groups((int)chunk)) <= MOST_PARTS_OF_A_THREAD &&
+                                   ceil_div(f.ldz, 256) * ceil_div(q.rows, DLF_CE_DZ_ROWS) <= MOST_FORMING;
+            if (!lse && !keep && !forms && !sums_form) {
                 float* const to = (float*)(ws + l.lse);
                 inverse = (float*)(ws + l.inverse);
                 TRY(join(f, in, q, l, ws, width, piece_loss, to, inverse, stream));
@@ -340,7 +349,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 z.z = (const float*)(ws + l.z);
                 if (out.db) z.sums = few ? out.db : (float*)(ws + l.sums) + nc;
                 if (!few) chunks = (int)ceil_div(q.rows, DLF_CE_DZ_ROWS);
-                TRY(launched(f, piece_lse ? dlf_ce_start_dz_sums(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
+                TRY(launched(f, piece_lse || sums_form ? dlf_ce_start_dz_sums(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else if (keep) {
                 // (workgroups that do not run at once do not form their rows' lse)
                 if (q.rows * z.slices > 2048) {

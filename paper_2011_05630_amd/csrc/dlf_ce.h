@@ -1,5 +1,7 @@
 // Shared between the host side of the cross entropy of a linear layer (dlf_ce.cpp) and its kernels (dlf_ce.hip).
 #pragma once
+#include <hip/hip_runtime.h>
+
 #include "dlf_ffn.h"
 
 // What a product's epilogue does with the logits of its tile.
@@ -61,7 +63,7 @@ struct DlfCeDzArgs {
     int32_t slices;             // workgroups of a row, DLF_CE_DZ_COLS columns each
     const int64_t* target;
     int64_t ignore;
-    const float* lse;           // or null: lse and loss are formed here
+    const float* lse;           // or null: lse and loss are formed here, from the parts
     const float* inverse;       // of logits, as in DlfCeArgs
     float* loss;
     DlfCeGiven given;
@@ -90,8 +92,16 @@ static inline int dlf_ce_chunk(int shape) { return DLF_FF_SHAPES[shape].br / 2; 
 #define DLF_CE_JOIN_FEW 256
 // Columns of a workgroup of k_ce_dz.
 #define DLF_CE_DZ_COLS 2048
-// Rows of a workgroup of k_ce_dz_sums, which has 256 columns.
+// Rows of a workgroup of k_ce_dz_sums, which has 256 columns, and threads.
 #define DLF_CE_DZ_ROWS 64
+#define DLF_CE_DZ_THREADS 512
+// How many of its threads share a row's parts where it forms their lse: those left when the next power of two of them take the rows.
+__host__ __device__ static inline int dlf_ce_dz_groups(int rows)
+{
+    int n = DLF_CE_DZ_THREADS;
+    for (int span = 1; span < rows; span *= 2) n /= 2;
+    return n;
+}
 
 extern "C" {
 int dlf_ce_kernels_init(void);

@@ -461,10 +461,10 @@ template <typename T, bool FORM, bool LOGITS> __global__ __launch_bounds__(256) 
 
 // k_ce_dz_sums: dz from the logits, kept in 32 bits, and its column sums.  p = exp(z - lse) * inverse.  A workgroup takes 256 classes, four to a
 // lane, of 64 rows, its waves every eighth row; their sums meet in LDS, in a fixed order.  Few rows are bound by latency (a wave to all rows took 28 us for 60 of them),
-// many by memory: 4096 rows of 32000 classes 155 us (5.1 TB/s).
-template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_sums(const DlfCeDzArgs a)
+// many by memory: 4096 rows of 32000 classes 155 us (5.1 TB/s).  FORM: a workgroup forms its rows' lse by itself, in a fixed order.
+template <typename T, bool FORM> __global__ __launch_bounds__(DLF_CE_DZ_THREADS) void k_ce_dz_sums(const DlfCeDzArgs a)
 {
-    constexpr int WAVES = 8;
+    constexpr int WAVES = DLF_CE_DZ_THREADS / 64;
     static_assert(DLF_CE_DZ_ROWS <= WAVES * 64 && DLF_FF_FEW_ROWS <= DLF_CE_DZ_ROWS, "a thread for each row, one workgroup for few rows");
     struct Row {
         float total, own, lse, zero;
@@ -473,12 +473,29 @@ template <typename T> __global__ __launch_bounds__(512) void k_ce_dz_sums(const 
     __shared__ Row rows[DLF_CE_DZ_ROWS];
     __shared__ f4v sums[WAVES][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.y * DLF_CE_DZ_ROWS, nr = min(a.nr - first, DLF_CE_DZ_ROWS);
+    Parts all;                                              // of row threadIdx.x
+    if constexpr (FORM) {
+        __shared__ float2 shared[DLF_CE_DZ_THREADS];
+        const int groups = dlf_ce_dz_groups(nr), span = DLF_CE_DZ_THREADS / groups, mine = threadIdx.x & (span - 1), group = threadIdx.x / span;
+        if (mine < nr) all.take(a.part, a.parts, a.nr, first + mine, group, groups);
+        shared[threadIdx.x] = float2{all.m, all.s};
+        for (int h = groups / 2; h > 0; h >>= 1) {
+            __syncthreads();
+            if (group < h) {
+                const float2 v = shared[threadIdx.x + h * span];
+                all.add(v.x, v.y);
+                shared[threadIdx.x] = float2{all.m, all.s};
+            }
+        }
+    }
     if ((int)threadIdx.x < nr) {
         const int r = first + threadIdx.x;
         const int64_t t = a.target[r];
         const RowGradient g = row_gradient(a.given, r, t, a.ignore, a.nc);
         const bool is_class = t >= 0 && t < a.nc;
-        rows[threadIdx.x] = Row{a.inverse != nullptr ? g.total * a.inverse[r] : g.total, g.own, a.lse[r], g.total, is_class ? (int)t : -1};
+        const float inverse = FORM ? 1.0f / all.s : a.inverse != nullptr ? a.inverse[r] : 1.0f;
+        rows[threadIdx.x] = Row{g.total * inverse, g.own, FORM ? all.m : a.lse[r], g.total, is_class ? (int)t : -1};
+        if (FORM && blockIdx.x == 0) a.loss[r] = loss_of(all.lse(), t, a.ignore, a.nc, a.at + r);
         if (blockIdx.x == 0 && !is_class) a.rest[r] = 0.0f;
         if (blockIdx.x == 0 && r == 0 && a.back != nullptr) *a.back = scale_back(a.given);
     }
@@ -766,8 +783,10 @@ extern "C" int dlf_ce_start_dz(const DlfCeDzArgs* a, int dtype, void* stream)
 extern "C" int dlf_ce_start_dz_sums(const DlfCeDzArgs* a, int dtype, void* stream)
 {
     const dim3 grid((unsigned)((a->ldz + 255) / 256), (unsigned)((a->nr + DLF_CE_DZ_ROWS - 1) / DLF_CE_DZ_ROWS));
-    if (dtype == DLF_F16) hipLaunchKernelGGL(k_ce_dz_sums<F16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
-    else hipLaunchKernelGGL(k_ce_dz_sums<BF16>, grid, dim3(512), 0, (hipStream_t)stream, *a);
+    const bool h = dtype == DLF_F16;
+    void (*const f)(const DlfCeDzArgs) = a->lse != nullptr ? h ? k_ce_dz_sums<F16, false> : k_ce_dz_sums<BF16, false>
+                                                           : h ? k_ce_dz_sums<F16, true> : k_ce_dz_sums<BF16, true>;
+    hipLaunchKernelGGL(f, grid, dim3(DLF_CE_DZ_THREADS), 0, (hipStream_t)stream, *a);
     return (int)hipGetLastError();
 }
 extern "C" int dlf_ce_start_pack(const DlfCePackArgs* a, void* stream)

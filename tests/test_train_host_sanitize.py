@@ -47,5 +47,5 @@ def test_random_calls(driver, seed):
     seen = dict((k, int(v)) for k, v in re.findall(r"\[([^\]]+)\] (\d+)", m.group(4)))
     shapes = (0, 1, 2, 3, 4)
     want = {"mode%d shape%d" % (a, s) for a in (0, 1, 2, 3) for s in shapes} | {"back shape%d" % s for s in shapes}
-    want |= {"pack", "few", "few lines", "join", "dz", "dz with lse", "dz few", "dz sums", "dz of logits", "unit", "split", "norm", "step", "step small"}
+    want |= {"pack", "few", "few lines", "join", "dz", "dz with lse", "dz few", "dz sums", "dz few with lse", "dz sums with lse", "dz of logits", "unit", "split", "norm", "step", "step small"}
     assert want == set(seen) and all(n >= 10 for n in seen.values()), seen

@@ -213,7 +213,12 @@ int dlf_ce_start_dz_sums(const DlfCeDzArgs* a, int, void*)
     given(a->given);
     use("z", a->z, (double)a->nr * a->ldz * 4);
     use("dz", a->dz, (double)a->nr * a->ldz * 2);
-    if (in_ws(a->lse)) {
+    if (!a->lse) {
+        ++g_seen[few ? "dz few with lse" : "dz sums with lse"];
+        NEED(!g.lse_given && !a->inverse && a->parts == g.parts && a->loss - g.loss == a->target - g.target);
+        use("part", a->part, (double)a->parts * a->nr * 8);
+        use("at", a->at, (double)a->nr * 4);
+    } else if (in_ws(a->lse)) {
         use("lse", a->lse, (double)a->nr * 4);
         use("inverse", a->inverse, (double)a->nr * 4);
     } else {
