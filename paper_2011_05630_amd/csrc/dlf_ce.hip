@@ -21,8 +21,9 @@ __device__ __forceinline__ float exp_of_all(float d)
 }
 
 // Exponentials kept in 16 bits, two to a word: from 0 to 1, an exponent of five bits and eleven bits behind the point, a bit more than fp16, whose sign
-// they do not need.  They are bits 12 to 27 of the number times 2^-96 in 32 bits, so that reading one back is a shift, what follows times 2^96.  What is
-// below 2^-42 is lost; 1 is exact, so that 1 - p of a sure target is.  (NaN is not kept: such a row's sum says so.)
+// they do not need.  They are bits 12 to 27 of the number times 2^-96 in 32 bits, so that reading one back is a shift and a product with 2^96, both exact
+// (as a part of its row's factor 2^96 would make that infinite beside a large gradient, and a lost exponential NaN).  What is below 2^-42 is lost;
+// 1 is exact, so that 1 - p of a sure target is.  (NaN is not kept: such a row's sum says so.)
 __device__ __forceinline__ uint32_t kept_of(float x0, float x1)
 {
     const uint32_t b0 = __builtin_bit_cast(uint32_t, x0 * 0x1p-96f) + 0x800u, b1 = __builtin_bit_cast(uint32_t, x1 * 0x1p-96f) + 0x800u;
@@ -30,7 +31,7 @@ __device__ __forceinline__ uint32_t kept_of(float x0, float x1)
 }
 __device__ __forceinline__ float from_kept(uint32_t w, int i)
 {
-    return __builtin_bit_cast(float, (i ? w >> 4 : w << 12) & 0x0ffff000u);
+    return __builtin_bit_cast(float, (i ? w >> 4 : w << 12) & 0x0ffff000u) * 0x1p96f;
 }
 
 // How dz is scaled: products of it are undone by scale_back.  One dloss for all rows is left out of dz but for its sign and comes back as a factor in 32
@@ -435,9 +436,9 @@ template <typename T, bool FORM, bool LOGITS> __global__ __launch_bounds__(256) 
         const float lse = all.lse();
         if (c == 0) a.loss[r] = loss_of(lse, t, a.ignore, a.nc, a.at + r);
         if (LOGITS) m = all.m;
-        by = LOGITS ? 1.0f / all.s : exp_of(m - lse) * 0x1p96f;
+        by = LOGITS ? 1.0f / all.s : exp_of(m - lse);
     } else {
-        by = exp_of(m - a.lse[r]) * 0x1p96f;
+        by = exp_of(m - a.lse[r]);
     }
     if (a.back != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.back = scale_back(a.given);
     if (!in) return;

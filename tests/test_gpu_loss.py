@@ -279,6 +279,28 @@ def test_fp16_gradients_of_any_size(scale):
             assert (g[value.abs() - bound > 65520].isinf()).all()
 
 
+@pytest.mark.parametrize("scale", [2.0 ** 20, 2.0 ** 40, 1e30])
+@pytest.mark.parametrize("m", [130, 2100])
+def test_bf16_gradients_of_any_size(m, scale):
+    """Gradients of each row's own, far above 1, without the bias's: exponentials lost beside their part's largest, and classes that take no part, stay
+    zeros."""
+    from paper_2011_05630_amd import loss
+    announce(m, scale)
+    t, v = torch.bfloat16, 210
+    x, w, b, target, on = inputs(m, 40, v, t, 24, bias=True, ignored=0.1, sure=60.0)
+    off = torch.arange(v) % 5 == 3
+    target = torch.where(off[target.clamp_min(0)] & (target >= 0), target + 1, target)
+    dloss = (0.5 + torch.rand(m, generator=gen(25))) * scale
+    for bias in (None, torch.where(off, float("-inf"), b).float()):
+        ref = reference(x, w, None if bias is None else bias.double(), target)
+        want = gradients(ref, x, w, dloss.double(), torch.zeros(m).double(), t, kept=True)
+        op = loss.CrossEntropy(on["w"], None if bias is None else bias.cuda())
+        got, dx, dw, _ = op.gradients(on["x"], target.cuda(), dloss.cuda(), need=("x", "weight"))
+        within(got, ref["loss"], ref["e_loss"], "loss")
+        within(dx, *want["dx"], "dx")
+        within(dw, *want["dw"], "dw")
+
+
 def test_differences():
     """The gradients against differences of the losses themselves: steps of 2^-6 that the type holds exactly.  A row's loss along such a step has a third derivative of at most R^3,
     R the range of the step's logits, which costs a difference R^3 / 6; each loss is off by its bound."""
