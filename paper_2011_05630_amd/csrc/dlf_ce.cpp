@@ -353,9 +353,10 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             } else if (keep) {
                 // (workgroups that do not run at once do not form their rows' lse)
                 if (q.rows * z.slices > 2048) {
-                    float* const to = (float*)(ws + l.lse);
-                    TRY(join(f, in, q, l, ws, width, piece_loss, to, nullptr, stream));
+                    float *const to = (float*)(ws + l.lse), *const of = (float*)(ws + l.inverse);
+                    TRY(join(f, in, q, l, ws, width, piece_loss, to, of, stream));
                     z.lse = to;
+                    z.inverse = of;
                 }
                 TRY(launched(f, dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else {

@@ -64,7 +64,7 @@ struct DlfCeDzArgs {
     const int64_t* target;
     int64_t ignore;
     const float* lse;           // or null: lse and loss are formed here, from the parts
-    const float* inverse;       // of logits, as in DlfCeArgs
+    const float* inverse;       // p = exp(z - lse) * inverse (null: 1): a row's maximum is in lse then, 1 / its sum here; never null with exponentials kept
     float* loss;
     DlfCeGiven given;
     float *rest, *back;         // as in DlfCeArgs

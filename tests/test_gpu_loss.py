@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from ce_util import IGNORE, gradients, reference
-from ff_util import TYPES, gen, half_eps, rows_of, within
+from ff_util import TYPES, U, gen, half_eps, rows_of, within
 from gpu_util import announce
 
 pytestmark = pytest.mark.gpu
@@ -255,6 +255,46 @@ def test_large_logits(m):
     _, dx, dw, _ = op.gradients(on["x"], on["target"], 1.0)
     within(dx, *want["dx"], "dx")
     within(dw, *want["dw"], "dw")
+
+
+def sure_rows(m, v, t, seed):
+    """Logits of 4000 to 17000 that are the same in any order of their sums, whole numbers of quarters: a feature that all classes share, and fifteen of +-1 that tell them
+    apart, a row's being 2 to 2.5 times its target's."""
+    g = gen(seed)
+    w = torch.randint(0, 2, (v, 16), generator=g).double() * 2 - 1
+    w[:, 0] = 64
+    target = torch.randint(v, (m,), generator=g)
+    x = w[target] * (2.0 + 0.25 * torch.randint(0, 3, (m, 1), generator=g))
+    x[:, 0] = torch.randint(64, 257, (m,), generator=g).double()
+    return x, w, target, dict(x=x.to(t).cuda(), w=w.to(t).cuda(), target=target.cuda())
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("m", [40, 300, 2100])
+def test_sure_targets_of_large_logits(m, bias, dtype):
+    """In one call 1 - p of a sure target does not see how large its logit is.  Bounds: the logits are exact, so p is off by its row's sum
+    (ce_util's e_sum), its own exponential and quotient, where exponentials are kept by 2^-12 of it and 2^-31 of the row's, but not the largest, which is 1."""
+    from paper_2011_05630_amd import loss
+    announce(m, bias, dtype)
+    t, v = TYPES[dtype], 500
+    x, w, target, on = sure_rows(m, v, t, 26)
+    b = torch.zeros(v) if bias else None
+    ref = reference(x, w, b, target)
+    assert float(ref["lse"].min()) > 4000 and float((1 - ref["p"].gather(1, target[:, None])).median()) < 2e-3
+    far = ref["z"].max(1, keepdim=True).values - ref["z"]
+    e_sum = (64 + v / 16 + 32 + 4 * (ref["p"] * far).sum(1)) * U
+    kept = torch.where((far > 0) & (ref["p"] > 0), 2.0 ** -12 + 2.0 ** -31 / ref["p"], 0.0) if not bias else torch.zeros_like(far)
+    own = dict(ref, e_lse=e_sum, ez=kept)
+    op = loss.CrossEntropy(on["w"], None if b is None else b.cuda())
+    for dloss in (1.0, (0.5 + torch.rand(m, generator=gen(27))).cuda()):
+        each = torch.full((m,), dloss) if isinstance(dloss, float) else dloss.cpu()
+        want = gradients(own, x, w, each.double(), torch.zeros(m).double(), t)
+        _, dx, dw, db = op.gradients(on["x"], on["target"], dloss)
+        within(dx, *want["dx"], "dx")
+        within(dw, *want["dw"], "dw")
+        if bias:
+            within(db, *want["db"], "db")
 
 
 @pytest.mark.parametrize("scale", [1e-20, 1e-6, 1.0, 3e4, 1e20])
