@@ -359,8 +359,8 @@ dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* 
  * A target that is neither a class nor `ignore` gives a loss and gradients of NaN.  A class whose bias is -infinity takes no part; if none does,
  * lse is -infinity and the loss NaN.  All sums, exponentials and logarithms are held in 32 bits.  The gradients take rows in pieces: a
  * piece's dz stays in the workspace, in at most `piece_bytes` (but for 256 rows at least), in the tensors' type, which the matrix units
- * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14, so that a mean over many rows does not vanish,
- * and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
+ * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| (of rows that are
+ * ignored |dlse|) to between 2^13 and 2^14, so that a mean over many rows does not vanish, and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
  * dlf_cross_entropy_gradients does not compute the logits again: where dbias is wanted, it keeps them in 32 bits, in twice what dz takes, beside it, else
  * exp(z - a maximum) in 16 bits (eleven behind the point) in dz's place.
  * Nothing depends on timing: equal calls give equal bits.

@@ -301,7 +301,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
     if (!given.dlse && (!given.dloss || given.dloss_stride == 0)) {
         given.one = f.d.dtype == DLF_F16 ? 16384.0f : 1.0f;
     } else if (f.d.rows > 0 && f.d.dtype == DLF_F16 && wanted) {
-        const DlfCeUnitArgs u = {given, f.d.rows, (float*)(ws + l.unit)};
+        const DlfCeUnitArgs u = {given, in.target, f.d.ignore, f.d.rows, (float*)(ws + l.unit)};
         TRY(launched(f, dlf_ce_start_unit(&u, stream)));
         given.unit = u.unit;
     }

@@ -73,7 +73,8 @@ struct DlfCeDzArgs {
 };
 struct DlfCeUnitArgs {
     DlfCeGiven given;
-    int64_t rows;
+    const int64_t* target;
+    int64_t ignore, rows;
     float* unit;
 };
 struct DlfCeBackArgs {

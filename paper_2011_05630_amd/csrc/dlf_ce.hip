@@ -558,17 +558,20 @@ __global__ __launch_bounds__(256) void k_ce_pack(const DlfCePackArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // k_ce_unit: for fp16 and gradients of each row's own, the power of two that brings the largest |dloss| + |dlse| to between 2^13 and 2^14: dz, at most
-// twice that, stays below 2^15, and classes of probability 2^-28 are numbers of full precision.
+// twice that, stays below 2^15, and classes of probability 2^-28 are numbers of full precision.  dloss is 0 where a row has no target, whatever is there.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void k_ce_unit(const DlfCeUnitArgs a)
 {
     __shared__ float waves[16];
     const DlfCeGiven& g = a.given;
     float m = 0.0f;
-    const int64_t rows = (g.dloss != nullptr && g.dloss_stride != 0) || (g.dlse != nullptr && g.dlse_stride != 0) ? a.rows : min((int64_t)1, a.rows);
-    for (int64_t r = threadIdx.x; r < rows; r += 1024) {
-        const float v = fabsf(g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value) + fabsf(g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f);
+    const bool one = (g.dloss == nullptr || g.dloss_stride == 0) && (g.dlse == nullptr || g.dlse_stride == 0);
+    for (int64_t r = threadIdx.x; r < a.rows; r += 1024) {
+        const bool counts = a.target[r] != a.ignore;
+        const float l = fabsf(g.dloss != nullptr ? g.dloss[r * g.dloss_stride] : g.dloss_value), e = fabsf(g.dlse != nullptr ? g.dlse[r * g.dlse_stride] : 0.0f);
+        const float v = counts ? l + e : e;
         m = v <= 3.402823466e38f ? fmaxf(m, v) : m;         // (what is not finite makes its own row so)
+        if (one && counts) break;                           // (all others are the same)
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));

@@ -341,6 +341,43 @@ def test_bf16_gradients_of_any_size(m, scale):
         within(dw, *want["dw"], "dw")
 
 
+@pytest.mark.parametrize("m", [8, 130, 700])
+@pytest.mark.parametrize("bias", [False, True])
+def test_gradients_given_for_ignored_rows_scale_nothing(m, bias):
+    """fp16: the power of two that dz is scaled by comes from what counts."""
+    from paper_2011_05630_amd import loss
+    announce(m, bias)
+    t = torch.float16
+    x, w, b, target, on = inputs(m, 40, 210, t, 28, bias=bias, ignored=0.3)
+    target[m // 2] = IGNORE
+    on["target"].copy_(target)
+    ref = reference(x, w, b, target)
+    dloss, dlse = given(m, 29)
+    op = loss.CrossEntropy(on["w"], on["b"], piece_bytes=1)
+    _, lse = op.run_saved(on["x"], on["target"])
+    for away in (1e9, 1e30):
+        away = torch.where(target == IGNORE, away, dloss)
+        names = ("dx", "dw", "db")
+        want = gradients(ref, x, w, dloss.double(), torch.zeros(m).double(), t, kept=not bias)
+        for grads in (op.backward(away.cuda(), on["x"], on["target"], lse), op.gradients(on["x"], on["target"], away.cuda())[1:]):
+            for name, value in zip(names, grads):
+                if value is not None:
+                    within(value, *want[name], name)
+        want = gradients(ref, x, w, dloss.double(), dlse.double(), t)
+        for name, value in zip(names, op.backward(away.cuda(), on["x"], on["target"], lse, dlse=dlse.cuda())):
+            if value is not None:
+                within(value, *want[name], name + " with dlse")
+    # no row counts: dlse alone
+    none = torch.full((m,), IGNORE)
+    ref = reference(x, w, b, none)
+    for e in (dlse, torch.full((1,), 0.125)):
+        want = gradients(ref, x, w, torch.zeros(m).double(), e.double().expand(m), t)
+        for d in (1e30, torch.full((m,), 1e30).cuda()):
+            for name, value in zip(names, op.backward(d, on["x"], none.cuda(), lse, dlse=e.cuda())):
+                if value is not None:
+                    within(value, *want[name], name + " of dlse alone")
+
+
 def test_differences():
     """The gradients against differences of the losses themselves: steps of 2^-6 that the type holds exactly.  A row's loss along such a step has a third derivative of at most R^3,
     R the range of the step's logits, which costs a difference R^3 / 6; each loss is off by its bound."""
