@@ -14,13 +14,14 @@ int dtype_of(const at::Tensor& t)
     return t.scalar_type() == at::kFloat ? DLF_F32 : t.scalar_type() == at::kHalf ? DLF_F16 : t.scalar_type() == at::kBFloat16 ? DLF_BF16 : -1;
 }
 // Distances that name the same order of elements in memory (of a dimension of one element they say nothing).
-bool same_order(const at::Tensor& a, const at::Tensor& b)
+bool same_order(const at::Tensor& a, at::IntArrayRef sizes, at::IntArrayRef strides)
 {
-    if (!a.sizes().equals(b.sizes())) return false;
+    if (!a.sizes().equals(sizes)) return false;
     for (int64_t i = 0; i < a.dim(); ++i)
-        if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+        if (a.size(i) > 1 && a.stride(i) != strides[i]) return false;
     return true;
 }
+bool same_order(const at::Tensor& a, const at::Tensor& b) { return same_order(a, b.sizes(), b.strides()); }
 const at::Tensor* tensor_of(py::handle h) { return THPVariable_Check(h.ptr()) ? &THPVariable_Unpack(h.ptr()) : nullptr; }
 py::sequence list_of(py::handle h, const char* name)
 {
@@ -108,6 +109,7 @@ public:
             dlf_adamw_tensor q = {t->data_ptr(), nullptr, t->numel(), dtype_of(*t), 0, (float)decay[i], 0};
             own(*t, name);
             params_.push_back(*t);
+            forms_.push_back({t->sizes().vec(), t->strides().vec()});
             at::Tensor copy;
             const py::object c = second ? py::object((*second)[i]) : py::object(py::none());
             if (!c.is_none()) {
@@ -161,9 +163,9 @@ public:
         const int64_t n = (int64_t)tensors_.size();
         if ((int64_t)list.size() != n) refuse("gradients: one for each of ", n, " parameters expected");
         for (int64_t i = 0; i < n; ++i) {
-            unchanged(params_[i], Name("parameter", i), tensors_[i].param, tensors_[i].count, tensors_[i].param_dtype);
+            unchanged(params_[i], Name("parameter", i), i, tensors_[i].param, tensors_[i].param_dtype);
             if (copies_[i].defined()) {
-                unchanged(copies_[i], Name("copy", i), tensors_[i].copy, tensors_[i].count, tensors_[i].copy_dtype);
+                unchanged(copies_[i], Name("copy", i), i, tensors_[i].copy, tensors_[i].copy_dtype);
                 if (copies_[i].requires_grad() && !copies_[i].is_leaf()) refuse(Name("copy", i), ": automatic differentiation has computed it");
             }
             if (params_[i].requires_grad() && !params_[i].is_leaf()) refuse(Name("parameter", i), ": automatic differentiation has computed it");
@@ -221,9 +223,13 @@ private:
         uintptr_t lo, hi;
         Name name;
     };
+    struct Form {
+        std::vector<int64_t> sizes, strides;
+    };
     dlf_adamw_desc d_;
     at::Device device_ = at::kCPU;
     std::vector<at::Tensor> params_, copies_;
+    std::vector<Form> forms_;               // of the parameters, as they were
     std::vector<dlf_adamw_tensor> tensors_;
     std::vector<Range> ranges_;             // what a step writes, by address
     at::Tensor table_, m_, v_, m_scale_, v_scale_, counter_;
@@ -234,10 +240,11 @@ private:
         const uintptr_t at = (uintptr_t)t.data_ptr();
         if (t.numel() > 0) ranges_.push_back({at, at + (uintptr_t)t.numel() * t.itemsize(), name});
     }
-    // The table on the device holds addresses and sizes: `.data = ` exchanges them under this object.
-    void unchanged(const at::Tensor& t, const Name& name, const void* p, int64_t count, int dtype) const
+    // The table on the device holds addresses and sizes, and the states lie in the order of memory: `.data = ` exchanges them under this object.  (A
+    // parameter and its copy have one form.)
+    void unchanged(const at::Tensor& t, const Name& name, int64_t i, const void* p, int dtype) const
     {
-        if (t.data_ptr() != p || t.numel() != count || dtype_of(t) != dtype || t.device() != device_ || !readable(t) || !t.is_non_overlapping_and_dense())
+        if (t.data_ptr() != p || !same_order(t, forms_[i].sizes, forms_[i].strides) || dtype_of(t) != dtype || t.device() != device_ || !readable(t))
             refuse(name, ": no longer the tensor, or the memory, that the optimizer was made of: make another");
         held(t, name);
     }

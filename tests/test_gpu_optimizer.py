@@ -173,6 +173,17 @@ def test_strided_parameters_and_gradients():
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
 
 
+def test_strides_of_single_elements_say_nothing():
+    """The stride of a dimension of one element may change: no element is elsewhere."""
+    from paper_2011_05630_amd import optimizer
+    p, c = torch.zeros(1, 300).cuda(), torch.zeros(1, 300).cuda().bfloat16()
+    op = optimizer.AdamW([p], [c])
+    p.data = p.data.as_strided((1, 300), (7, 1))
+    c.data = c.data.as_strided((1, 300), (5, 1))
+    op.step([torch.ones(1, 300).cuda()], 0.5)
+    assert (p == -0.5).all() and (c == -0.5).all()
+
+
 @pytest.mark.parametrize("factor", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("state", ["fp32", "8bit"])
 def test_a_factor_that_is_not_finite_leaves_everything(state, factor):

@@ -201,6 +201,29 @@ def test_tensors_that_changed():
             o.step([torch.zeros(100), None], 0.1, None, 0)
 
 
+CHANGED = {"transposed": lambda t: t.t(), "reshaped": lambda t: t.reshape(20, 15), "flat": lambda t: t.reshape(300), "another dimension": lambda t: t[None]}
+
+
+@pytest.mark.parametrize("what", sorted(CHANGED))
+def test_tensors_whose_form_changed(what):
+    """The same memory with other sizes or strides: the gradient's order would be the new one, the copy's the old one."""
+    change = CHANGED[what]
+    for which in ("parameter", "copy", "both"):
+        p, c = pair(), [None, torch.zeros(30, 10).bfloat16()]
+        o = make(p, c)
+        if which != "copy":
+            p[1].data = change(p[1].data)
+        if which != "parameter":
+            c[1].data = change(c[1].data)
+        with pytest.raises(ValueError, match="^copy 1: no longer" if which == "copy" else "^parameter 1: no longer"):
+            o.step([None, torch.empty_like(p[1])], 0.1, None, 0)
+    square = [torch.zeros(10, 10)]
+    o = make(square)
+    square[0].data = square[0].data.t()
+    with pytest.raises(ValueError, match="^parameter 0: no longer"):
+        o.step([torch.empty_like(square[0])], 0.1, None, 0)
+
+
 def test_a_parameter_that_automatic_differentiation_computed():
     leaf = torch.zeros(100, requires_grad=True)
     o = make([leaf * 2])
