@@ -432,7 +432,7 @@ typedef struct {
 } dlf_adamw_tensor;
 typedef struct {
     double beta1, beta2;        /* 0 <= and < 1                                                           */
-    float eps;                  /* >= 0                                                                   */
+    float eps;                  /* 0, or 2^-126 .. 2^126                                                  */
     uint32_t seed;
     int32_t state;              /* dlf_adamw_state                                                        */
     int32_t reserved;           /* 0                                                                      */

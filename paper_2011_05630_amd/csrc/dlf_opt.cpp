@@ -192,7 +192,8 @@ dlf_status dlf_adamw_step(const dlf_adamw_desc* d, const dlf_adamw_tensor* tenso
     const char* const call = "dlf_adamw_step";
     if (!d) return fail(DLF_ERR_INVALID_ARG, "%s: null description", call);
     if (!(d->beta1 >= 0 && d->beta1 < 1 && d->beta2 >= 0 && d->beta2 < 1)) return fail(DLF_ERR_INVALID_ARG, "%s: betas %g, %g", call, d->beta1, d->beta2);
-    if (!(d->eps >= 0 && d->eps <= 3e38f)) return fail(DLF_ERR_INVALID_ARG, "%s: eps %g", call, (double)d->eps);
+    // (the reciprocal's instruction takes numbers from 2^-126 on, and gives none below)
+    if (!(d->eps == 0 || (d->eps >= 0x1p-126f && d->eps <= 0x1p126f))) return fail(DLF_ERR_INVALID_ARG, "%s: eps %g", call, (double)d->eps);
     if (d->state != DLF_ADAMW_FP32 && d->state != DLF_ADAMW_8BIT) return fail(DLF_ERR_INVALID_ARG, "%s: state %d", call, d->state);
     if (d->reserved != 0) return fail(DLF_ERR_INVALID_ARG, "%s: reserved is not 0", call);
     TRY(check_tensors(call, tensors, n));

@@ -216,7 +216,7 @@ template <int TYPE> struct Raw {
     }
 };
 // The square root by its instruction, off by a unit of the last place; numbers near the end of the range are brought up for it.  (Its result is none near the
-// end, so that the reciprocal's instruction takes it as it is.  Root and quotient correctly rounded: 2.5 times the instructions of the whole update.)
+// end, nor is eps, so that the reciprocal's instruction takes their sum as it is.  Root and quotient correctly rounded: 2.5 times the instructions of the whole update.)
 __device__ __forceinline__ float root_of(float x)
 {
     const bool small = x < 0x1p-96f;

@@ -56,7 +56,7 @@ class AdamW:
         _need(all(isinstance(p, torch.Tensor) and p.is_cuda for p in params), "params: tensors on the GPU expected")
         b1, b2 = betas
         _need(0 <= b1 < 1 and 0 <= b2 < 1, "betas: numbers from 0 to below 1 expected")
-        _need(0 <= eps <= 3e38, "eps: a number from 0 on expected")
+        _need(eps == 0 or 2.0 ** -126 <= eps <= 2.0 ** 126, "eps: 0, or a number from 2^-126 to 2^126, expected")
         _need(isinstance(seed, int) and 0 <= seed < 1 << 32, "seed: a whole number below 2^32 expected")
         decays = [float(d) for d in decay] if isinstance(decay, (list, tuple)) else [float(decay)] * len(params)
         self._make(params, None if copies is None else _list(copies, "copies"), decays, b1, b2, eps, state, seed)

@@ -123,6 +123,19 @@ def test_values_of_any_size(state):
     run_steps([3000, 200], "fp32", "fp32", None, state, 6, steps=4, grads=grads, eps=1e-3)
 
 
+@pytest.mark.parametrize("eps", [2.0 ** -126, 2.0 ** 126])
+@pytest.mark.parametrize("state", ["fp32", "8bit"])
+def test_eps_at_the_ends_of_its_range(eps, state):
+    """Beside second moments of zero, whose gradients were zero or had no square."""
+    def grads(s):
+        g = gen(95 + s)
+        v = torch.randn(300, generator=g) * 10.0 ** (torch.rand(300, generator=g) * 12 - 12)
+        v[::3] = 0.0
+        v[1::9] = 1e-25
+        return [v.cuda()]
+    run_steps([300], "fp32", "fp32", None, state, 8, grads=grads, eps=eps)
+
+
 def test_a_second_moment_above_zero_stays_above_zero():
     """Elements far below their block's largest would get a root of zero under their first moment."""
     from paper_2011_05630_amd import optimizer

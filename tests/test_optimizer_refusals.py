@@ -45,6 +45,18 @@ def test_descriptions(kw):
     assert step(d=B.dlf_adamw_desc(**kw)) == B.DLF_ERR_INVALID_ARG
 
 
+# (a reciprocal of less than 2^-126, or that is less, is none on the device: m = 0 times infinity would be NaN)
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 2.0 ** -127, 2.0 ** 126 * 1.001, 3e38])
+def test_eps_outside_the_range_of_reciprocals(eps):
+    from paper_2011_05630_amd import optimizer
+    assert step(d=B.dlf_adamw_desc(eps=eps)) == B.DLF_ERR_INVALID_ARG
+    with pytest.raises(ValueError, match="^eps: "):
+        optimizer.AdamW([], eps=eps)
+    if eps < 1:
+        with pytest.raises(ValueError, match="^eps: "):
+            optimizer.AdamW([], eps=1e-60)                  # (0 in 32 bits)
+
+
 @pytest.mark.parametrize("field,value", [("state", 2), ("state", -1), ("reserved", 1)])
 def test_bad_fields(field, value):
     d = B.dlf_adamw_desc()
