@@ -82,17 +82,24 @@ class AdamW:
         """Steps done, an int64 element on the device."""
         return self._counter[0].long()
 
+    @property
+    def powers(self):
+        """{steps done, b1, b2, b1^steps, b2^steps} in 64 bits, on the device: the powers as the steps multiplied them."""
+        return torch.cat([self._counter[:1], torch.full((1,), self.betas[0], dtype=torch.float64, device=self.device),
+                          torch.full((1,), self.betas[1], dtype=torch.float64, device=self.device), self._counter[1:3]])
+
     def _states(self):
         return {n: getattr(self, n) for n in ("m", "v", "m_scale", "v_scale") if getattr(self, n) is not None}
 
     def save_state(self):
-        """-> copies of the states and the count, for `load_state` of an object over parameters of the same sizes."""
-        return dict({n: t.clone() for n, t in self._states().items()}, count=self.count)
+        """-> copies of the states, the count and `powers`, for `load_state` of an object over parameters of the same sizes."""
+        return dict({n: t.clone() for n, t in self._states().items()}, count=self.count, powers=self.powers)
 
     def load_state(self, state):
-        """Takes over the values of `state`, as save_state returns it (the count may be a number)."""
+        """Takes over the values of `state`, as save_state returns it (the count may be a number).  Without `powers`, or with those of another count or
+        other betas, the powers are formed from the count, which may differ in the last places of 64 bits."""
         mine = self._states()
-        _need(set(state) == set(mine) | {"count"}, "state: %s expected", ", ".join(sorted(set(mine) | {"count"})))
+        _need(set(state) - {"powers"} == set(mine) | {"count"}, "state: %s expected", ", ".join(sorted(set(mine) | {"count", "powers"})))
         for n, t in mine.items():
             s = state[n]
             _need(isinstance(s, torch.Tensor) and s.shape == t.shape and s.dtype == t.dtype, "%s: a %s tensor %s expected", n, t.dtype, list(t.shape))
@@ -103,8 +110,16 @@ class AdamW:
         else:
             _need(isinstance(count, int) and count >= 0, "count: a whole number expected")
             count = torch.full((), count, dtype=torch.int64, device=self.device)
+        powers = state.get("powers")
+        if powers is not None:
+            _need(isinstance(powers, torch.Tensor) and powers.shape == (5,) and powers.dtype == torch.float64, "powers: an fp64 tensor [5] expected")
+            powers = powers.to(self.device)
         with torch.no_grad():
             for n, t in mine.items():
                 t.copy_(state[n])
             c = count.double()
-            self._counter.copy_(torch.stack([c, self.betas[0] ** c, self.betas[1] ** c, torch.zeros_like(c)]))
+            now = torch.stack([c, self.betas[0] ** c, self.betas[1] ** c, torch.zeros_like(c)])
+            if powers is not None:
+                same = (powers[:3] == torch.cat([now[:1], self.powers[1:3]])).all()
+                now[1:3] = torch.where(same, powers[3:], now[1:3])
+            self._counter.copy_(now)

@@ -238,6 +238,38 @@ def test_states_are_saved_and_loaded(state):
             second.load_state(bad)
 
 
+@pytest.mark.parametrize("state", ["fp32", "8bit"])
+def test_a_run_of_many_steps_goes_on_with_its_powers(state):
+    """The betas' powers are a product of as many factors as steps were done, which one power of the count is not bit for bit."""
+    from paper_2011_05630_amd import optimizer
+    params = tensors([300], torch.float32, 17)
+    op = optimizer.AdamW(params, betas=(0.9, 0.999), state=state)
+    for s in range(70):
+        op.step(tensors([300], torch.bfloat16, 18 + s % 3), 0.01)
+    saved = op.save_state()
+    assert saved["powers"].tolist()[:3] == [70.0, 0.9, 0.999] and torch.equal(saved["powers"], op.powers)
+    second = optimizer.AdamW([p.clone() for p in params], betas=(0.9, 0.999), state=state)
+    second.load_state(saved)
+    assert torch.equal(second.powers, op.powers)
+    # where they are not there, or belong to another count or other betas, they are formed anew
+    other = optimizer.AdamW([p.clone() for p in params], betas=(0.8, 0.99), state=state)
+    other.load_state(saved)
+    first = {n: t for n, t in saved.items() if n != "powers"}
+    for o, given, want in ((other, saved, (70, 0.8, 0.99)), (other, first, (70, 0.8, 0.99)), (other, dict(saved, count=3), (3, 0.8, 0.99)),
+                           (second, first, (70, 0.9, 0.999)), (second, dict(saved, count=5), (5, 0.9, 0.999))):
+        o.load_state(given)
+        n, b1, b2 = want
+        got = o.powers.tolist()
+        assert got[:3] == [n, b1, b2] and int(o.count) == n
+        for a, b in zip(got[3:], (b1 ** n, b2 ** n)):
+            assert abs(a - b) <= 4 * 2.0 ** -52 * b
+    for bad in (saved["powers"][:4], saved["powers"].float(), 1.0):
+        with pytest.raises(ValueError, match="^powers: "):
+            second.load_state(dict(saved, powers=bad))
+    with pytest.raises(ValueError, match="^state: "):
+        second.load_state(dict(saved, power=1.0))
+
+
 def bits_of(t):
     return t.view(torch.uint8)
 
