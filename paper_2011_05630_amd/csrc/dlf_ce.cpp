@@ -257,8 +257,8 @@ void set_cut(DlfFfArgs& a, const DlfFfCut& c)
     a.tiles_c = c.tiles_c;
 }
 
-// The parts of a piece's rows; keep: the exponentials too, in dz; z: the logits too, there.  tiles: by the kernel that forms dz, whose logits
-// have the same bits: where a target is nearly sure, 1 - p is what is left of them.  -> the classes of a part
+// The parts of a piece's rows; keep: the exponentials too, in dz; z: the logits too, there.  tiles: by tiles also where the piece, a last one, has few
+// rows: the kernels for few rows keep no exponentials.  -> the classes of a part
 dlf_status logits(const Ce& f, const In& in, const Piece& q, bool tiles, bool keep, float* z, const Layout& l, char* ws, int& width, void* stream)
 {
     DlfCeArgs a;
@@ -366,7 +366,6 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 set_cut(a.t, c);
                 a.dz = ws + l.dz;
                 a.lse = piece_lse;
-                a.inverse = inverse;
                 a.rest = (float*)(ws + l.rest);
                 a.low = twice(f) ? ws + l.low : nullptr;
                 a.given = g;

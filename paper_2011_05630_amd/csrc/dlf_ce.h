@@ -36,7 +36,7 @@ struct DlfCeArgs {
     float* z;                   // few rows (where not null), LOGITS: [nr][ldz] the logits
     void* dz;                   // [nr][ldz], zeros behind column nc; KEEP: exp(z - its part's maximum) in 16 bits
     int64_t ldz;                // a multiple of eight
-    const float *lse, *inverse; // DZ: p = exp(z - lse) * inverse (null: 1)
+    const float *lse, *inverse; // DZ: p = exp(z - lse), lse as the caller gives it; inverse is null
     DlfCeGiven given;
     float* rest;                // [nr] what dz's rounding takes from a row's target, or null
     float* sums;                // [chunks][nc] column sums of dz, in 32 bits, or null
@@ -87,7 +87,6 @@ struct DlfCeBackArgs {
 };
 // Classes of a part, by tile shape: what a wave's columns are.
 static inline int dlf_ce_width(int shape) { return DLF_FF_SHAPES[shape].bc / 2; }
-static inline int dlf_ce_chunk(int shape) { return DLF_FF_SHAPES[shape].br / 2; }
 // Rows of a workgroup of k_ce_join, and up to how many rows a workgroup has one.
 #define DLF_CE_JOIN_ROWS 16
 #define DLF_CE_JOIN_FEW 256

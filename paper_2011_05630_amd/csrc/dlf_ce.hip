@@ -168,7 +168,7 @@ template <int MODE> struct Entropy {
             if constexpr (MODE == DLF_CE_DZ) {
                 RowGradient g = row_gradient(e.given, at, t, e.ignore, a.nc);
                 if (r >= a.nr) g.total = g.own = 0.0f;
-                const float lse = e.lse[at], total = e.inverse != nullptr ? g.total * e.inverse[at] : g.total;
+                const float lse = e.lse[at], total = g.total;
                 // (to the last place for the bias's gradient only: it is half of this epilogue, which a tile of few stages shows)
                 if (e.sums != nullptr) {
 #pragma unroll
