@@ -43,10 +43,22 @@ bool copy_pays(int64_t rows, int64_t in, int64_t classes, int products)
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// Up to how many parts a thread takes, and workgroups there are, where the workgroups of k_ce_dz_sums form their rows' lse.  Whole calls, bf16, us with a launch for
-// it and without: 515 x 770 over 5003 classes (10 parts a thread) 59.8 and 57.9, 2000 x 256 over 5000 (10; 640 workgroups) 69.9 and 68.2, 16 x 256 over
-// 16000 (32) 31.8 and 31.1; 60 rows (125) 40.8 and 45.5, 16 x 256 over 60000 (118) 58.9 and 61.5.
+// Where the workgroups of dz form their rows' lse themselves instead of reading what a launch of k_ce_join leaves.  Whole calls of gradients, replayed, 256
+// features, bf16, us with that launch and without it.
+//
+// k_ce_dz_sums (a bias's gradient): while a thread has few parts to add up, and not many workgroups repeat it.  16 parts or fewer: 4096 rows over 2000
+// classes 56.7 and 54.8, 2048 over 5000 (640 workgroups) 70.7 and 69.2, over 6000 (768) 72.5 and 72.0, 100 over 8000 31.7 and 31.2; 20 of 1024 over 10000
+// 70.2 and 70.7; 32 of 60 over 4000 26.5 and 26.2, of 16 over 16000 30.8 and 30.1, of 4 over 64000 56.1 and 55.1, but of 100 over 16000 40.8 and 42.0;
+// 47 to 118 of 60 over 6000 27.7 and 28.2, 16000 40.7 and 45.9, 16 over 24000 36.5 and 36.2, 60000 59.4 and 62.2.  More workgroups: 1000 of 55 to 62 parts
+// (512 over 32000) 94.5 and 98.4; with 8 parts they would still gain (4096 over 4096, 1024 workgroups: 87.5 and 85.5), which is left.
 constexpr int64_t MOST_PARTS_OF_A_THREAD = 32, MOST_FORMING = 768;
+// k_ce_dz of few rows' logits, a workgroup of 2048 classes to a row, each reading all of the row's parts: by rows times parts.  1 x 103104 (6444) 75.1 and
+// 72.6, 15 x 48000 (45000) 50.1 and 48.3, 15 x 64000 (60000) 59.2 and 58.8, 60 x 16000 (60000) 40.0 and 34.6, 33 x 32000 (66000) 49.3 and 48.0; 15 x 80000 (75000)
+// 68.4 and 71.5, 33 x 48000 (99000) 61.7 and 64.3, 60 x 48000 (180000) 65.2 and 72.4, 60 x 103104 111 and 172.
+constexpr int64_t MOST_PARTS_OF_FEW_ROWS = 66000;
+// k_ce_dz of kept exponentials: up to as many workgroups as run at once.  2000 x 2000 (2000 workgroups) 41.2 and 39.7, 512 x 8000 (2048) 42.3 and 41.9, 128 x
+// 32000 (2048) 46.3 and 47.8; 4096 x 2000 (4096) 51.5 and 51.4, 1024 x 8000 (4096) 48.8 and 51.7, 256 x 32000 (4096) 55.0 and 58.7, 4096 x 32000 405 and 486.
+constexpr int64_t MOST_FORMING_KEPT = 2048;
 
 // A description with its strides filled in, and the rows of a piece.
 struct Ce {
@@ -321,9 +333,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
             float* const piece_loss = loss ? loss + q.first : nullptr;
             int width = 0;
             if (!lse || keep_logits) TRY(logits(f, in, q, wanted && !few, keep, keep_logits ? (float*)(ws + l.z) : nullptr, l, ws, width, stream));
-            // (a row's lse formed by each of its workgroups, of so many parts, takes longer than a launch: 15 rows of 103104 classes 23 us)
-            const bool forms = few && wanted && !out.db && ceil_div(nc, 16) <= 3000;
-            // ... and so do the workgroups of k_ce_dz_sums, while a thread has few parts and all of them run at once.
+            const bool forms = few && wanted && !out.db && q.rows * ceil_div(nc, 16) <= MOST_PARTS_OF_FEW_ROWS;
             const int64_t chunk = std::min<int64_t>(q.rows, DLF_CE_DZ_ROWS);
             const bool sums_form = !lse && out.db && ceil_div(ceil_div(nc, width), dlf_ce_dz_groups((int)chunk)) <= MOST_PARTS_OF_A_THREAD &&
                                    ceil_div(f.ldz, 256) * ceil_div(q.rows, DLF_CE_DZ_ROWS) <= MOST_FORMING;
@@ -351,8 +361,7 @@ dlf_status gradients(const Ce& f, const In& in, const float* lse, DlfCeGiven giv
                 if (!few) chunks = (int)ceil_div(q.rows, DLF_CE_DZ_ROWS);
                 TRY(launched(f, piece_lse || sums_form ? dlf_ce_start_dz_sums(&z, f.d.dtype, stream) : dlf_ce_start_dz(&z, f.d.dtype, stream)));
             } else if (keep) {
-                // (workgroups that do not run at once do not form their rows' lse)
-                if (q.rows * z.slices > 2048) {
+                if (q.rows * z.slices > MOST_FORMING_KEPT) {
                     float *const to = (float*)(ws + l.lse), *const of = (float*)(ws + l.inverse);
                     TRY(join(f, in, q, l, ws, width, piece_loss, to, of, stream));
                     z.lse = to;
