@@ -344,7 +344,8 @@ dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* 
                               void* hip_stream);
 
 /* ---- Cross entropy of a linear layer ----------------------------------------------------------
- * The loss at the end of a stack of blocks over a large number of classes (a vocabulary), without its logits in memory:
+ * The loss at the end of a stack of blocks over a large number of classes (a vocabulary): the loss without its logits in memory, the gradients with
+ * those of a piece of the rows at a time:
  *
  *   z[r][c] = sum over i of x[r][i] * weight[c][i] + bias[c]      lse[r] = log sum over c of exp(z[r][c])
  *   loss[r] = lse[r] - z[r][target[r]]                            0 where target[r] == ignore
@@ -352,17 +353,18 @@ dlf_status dlf_gated_backward(const dlf_ff_desc* d, const void* dh, const void* 
  *   dx = dz weight;  dweight = dz^T x;  dbias[c] = sum over r of dz[r][c]
  *
  * dlf_cross_entropy            loss, and lse if wanted
- * dlf_cross_entropy_backward   the gradients for those of loss and lse; the logits are computed again
+ * dlf_cross_entropy_backward   the gradients for those of loss and lse; the logits are computed again, in places by other kernels than those that
+ *                              formed lse (another order of the sums); lse in 32 bits leaves each probability off by up to 2^-24 |lse| of itself
  * dlf_cross_entropy_gradients  loss and gradients in one call (dlse = 0), for a program that knows dloss beforehand (1 / rows, a loss scale):
- *                              a quarter of the operations less than the other two
+ *                              a quarter of the operations less than the other two; probabilities come from a row's maximum and sum, not from lse
  *
  * A target that is neither a class nor `ignore` gives a loss and gradients of NaN.  A class whose bias is -infinity takes no part; if none does,
- * lse is -infinity and the loss NaN.  All sums, exponentials and logarithms are held in 32 bits.  The gradients take rows in pieces: a
+ * lse is -infinity and the loss NaN.  All sums, exponentials and logarithms are formed in 32 bits.  The gradients take rows in pieces: a
  * piece's dz stays in the workspace, in at most `piece_bytes` (but for 256 rows at least), in the tensors' type, which the matrix units
- * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| (of rows that are
- * ignored |dlse|) to between 2^13 and 2^14, so that a mean over many rows does not vanish, and the products are scaled back before they are rounded.  dbias is summed from 32 bits.  dweight is summed over the pieces in 32 bits.
- * dlf_cross_entropy_gradients does not compute the logits again: where dbias is wanted, it keeps them in 32 bits, in twice what dz takes, beside it, else
- * exp(z - a maximum) in 16 bits (eleven behind the point) in dz's place.
+ * multiply; in fp16 it is scaled by a power of two that brings the largest |dloss| + |dlse| (of rows that are ignored |dlse|) to between 2^13
+ * and 2^14, so that a mean over many rows does not vanish, and the products are scaled back before they are rounded.  dbias is summed from
+ * 32 bits.  dweight is summed over the pieces in 32 bits.  dlf_cross_entropy_gradients does not compute the logits again: where dbias is wanted, it
+ * keeps a piece's in 32 bits, in twice what dz takes, beside it, else exp(z - a maximum) in 16 bits (eleven behind the point) in dz's place.
  * Nothing depends on timing: equal calls give equal bits.
  *
  * Tensors are DEVICE and row-major: x [rows][in_features], weight [classes][in_features], of type `dtype`, a row's elements next to

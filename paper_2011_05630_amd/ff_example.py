@@ -4,7 +4,7 @@ tokens with hand-written gradients, then answering single tokens.
     python -m paper_2011_05630_amd.ff_example [--blocks 2] [--width 512] [--hidden 1408] [--classes 1000] [--tokens 2048] [--steps 30]
                                               [--optimizer sgd|adamw|adamw8] [--rate 1.0]
 
-sgd: the loss written out in PyTorch, a plain update.  adamw, adamw8: the cross entropy without its logits, the gradients' norm brought down to 1 and
+sgd: the loss written out in PyTorch, a plain update.  adamw, adamw8: the cross entropy and its gradients in one call, the gradients' norm brought down to 1 and
 AdamW with states in 32 or in 8 bits, by the library.  Prints the loss as it trains, the time of a step and of a single token, and how far the single token's logits are from the same row of
 a whole batch.
 """
