@@ -145,13 +145,13 @@ public:
             v_scale_ = at::ones({e / DLF_ADAMW_BLOCK}, here.dtype(at::kFloat));
         }
         counter_ = at::tensor({0.0, 1.0, 1.0, 0.0}, at::TensorOptions().dtype(at::kDouble)).to(device_);
-        own(m_, "m");
-        own(v_, "v");
+        made(m_, "m");
+        made(v_, "v");
         if (small) {
-            own(m_scale_, "m_scale");
-            own(v_scale_, "v_scale");
+            made(m_scale_, "m_scale");
+            made(v_scale_, "v_scale");
         }
-        own(counter_, "counter");
+        made(counter_, "counter");
         std::sort(ranges_.begin(), ranges_.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
         for (size_t i = 1; i < ranges_.size(); ++i)
             if (ranges_[i].lo < ranges_[i - 1].hi) refuse(ranges_[i - 1].name, " and ", ranges_[i].name, " overlap");
@@ -169,6 +169,11 @@ public:
                 if (copies_[i].requires_grad() && !copies_[i].is_leaf()) refuse(Name("copy", i), ": automatic differentiation has computed it");
             }
             if (params_[i].requires_grad() && !params_[i].is_leaf()) refuse(Name("parameter", i), ": automatic differentiation has computed it");
+        }
+        for (const State& s : states_) {
+            if (s.t.data_ptr() != s.p || s.t.numel() != s.count || s.t.scalar_type() != s.type || s.t.device() != device_ || !readable(s.t) || !s.t.is_contiguous())
+                refuse(s.name, ": no longer the tensor, or the memory, that the optimizer made");
+            held(s.t, s.name);
         }
         std::vector<const void*> p((size_t)n, nullptr);
         std::vector<int32_t> types((size_t)n, 0);
@@ -208,8 +213,7 @@ public:
             written(params_[i]);
             if (copies_[i].defined()) written(copies_[i]);
         }
-        for (const at::Tensor* t : {&m_, &v_, &m_scale_, &v_scale_, &counter_})
-            if (t->defined()) written(*t);
+        for (const State& s : states_) written(s.t);
     }
 
     py::object m() const { return wrap(m_); }
@@ -226,10 +230,19 @@ private:
     struct Form {
         std::vector<int64_t> sizes, strides;
     };
+    // The states are handed out, and `.data = ` exchanges them too.
+    struct State {
+        at::Tensor t;
+        const void* p;
+        int64_t count;
+        at::ScalarType type;
+        const char* name;
+    };
     dlf_adamw_desc d_;
     at::Device device_ = at::kCPU;
     std::vector<at::Tensor> params_, copies_;
     std::vector<Form> forms_;               // of the parameters, as they were
+    std::vector<State> states_;             // as they were made
     std::vector<dlf_adamw_tensor> tensors_;
     std::vector<Range> ranges_;             // what a step writes, by address
     at::Tensor table_, m_, v_, m_scale_, v_scale_, counter_;
@@ -239,6 +252,11 @@ private:
         held(t, name);
         const uintptr_t at = (uintptr_t)t.data_ptr();
         if (t.numel() > 0) ranges_.push_back({at, at + (uintptr_t)t.numel() * t.itemsize(), name});
+    }
+    void made(const at::Tensor& t, const char* name)
+    {
+        own(t, name);
+        states_.push_back({t, t.data_ptr(), t.numel(), t.scalar_type(), name});
     }
     // The table on the device holds addresses and sizes, and the states lie in the order of memory: `.data = ` exchanges them under this object.  (A
     // parameter and its copy have one form.)

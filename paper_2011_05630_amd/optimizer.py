@@ -48,7 +48,8 @@ class AdamW:
 
     The states are one tensor each over all parameters, `m` and `v` (and `m_scale`, `v_scale`): parameter i's begin at `offsets[i]`, in the order in which
     its elements lie in memory, zeros between its end and the next block.  Two steps of one object follow each other on one stream, or are ordered by the caller.
-    A parameter whose memory, type or form has changed is refused: make another object."""
+    A parameter whose memory, type or form has changed is refused: make another object.  The states' values may be read and written, their tensors
+    not exchanged."""
 
     def __init__(self, params, copies=None, betas=(0.9, 0.95), eps=1e-8, decay=0.0, state="fp32", seed=0):
         params = _list(params, "params")

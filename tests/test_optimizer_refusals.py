@@ -236,6 +236,24 @@ def test_tensors_whose_form_changed(what):
         o.step([torch.empty_like(square[0])], 0.1, None, 0)
 
 
+@pytest.mark.parametrize("name", ["m", "v", "m_scale", "v_scale", "counter"])
+def test_states_that_changed(name):
+    """The states are the object's own tensors, which a program may read and write, but not exchange: a step writes as many elements as there were."""
+    for change in ("memory", "size", "type", "storage"):
+        o = make(pair(), state="8bit")
+        t = getattr(o, name)
+        if change == "memory":
+            t.data = t.data.clone()
+        elif change == "size":
+            t.data = t.data[:-1]
+        elif change == "type":
+            t.data = t.data.view(torch.uint8)
+        else:
+            t.untyped_storage().resize_(0)
+        with pytest.raises(ValueError, match="^%s: no longer the tensor, or the memory" % name if change != "storage" else "^%s: " % name):
+            o.step([torch.zeros(100), None], 0.1, None, 0)
+
+
 def test_a_parameter_that_automatic_differentiation_computed():
     leaf = torch.zeros(100, requires_grad=True)
     o = make([leaf * 2])
