@@ -409,9 +409,9 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_ce_join(const DlfCe
 }
 
 // ------------------------------------------------------------------------------------------------
-// k_ce_dz: dz from the exponentials kept, in their place: each times dloss exp(its part's maximum - the row's) / the row's sum.  A workgroup takes a slice of a row.  Where
-// all of them run at once, each forms its row's lse by itself: a launch for that costs more.  Bound by memory: 4096 rows of 32000 classes 86 us (6.1 TB/s, some of
-// it from the last-level cache); with the lse formed by each workgroup 105 to 110 against 86 and 8.6 for k_ce_join.
+// k_ce_dz: dz from the exponentials kept, in their place: each times dloss exp(its part's maximum - the row's) / the row's sum.  A workgroup takes
+// a slice of a row.  Where all of them run at once, each forms its row's lse by itself: a launch for that costs more.  Bound by memory: 4096 rows of
+// 32000 classes 91 us (5.8 TB/s, some of it from the last-level cache; with 2^96 in `by` and lse alone 87); formed by each workgroup, the call takes 81 longer.
 // ------------------------------------------------------------------------------------------------
 // LOGITS: from the logits of few rows, which have been kept in 32 bits.
 template <typename T, bool FORM, bool LOGITS> __global__ __launch_bounds__(256) void k_ce_dz(const DlfCeDzArgs a)
