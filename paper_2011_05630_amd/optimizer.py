@@ -47,7 +47,8 @@ class AdamW:
     and a sixteenth an element instead of four.
 
     The states are one tensor each over all parameters, `m` and `v` (and `m_scale`, `v_scale`): parameter i's begin at `offsets[i]`, in the order in which
-    its elements lie in memory, zeros between its end and the next block.  Two steps of one object follow each other on one stream, or are ordered by the caller.
+    its elements lie in memory, zeros between its end and the next block.  The object is made on the
+    stream that is current then; what follows, its steps one after the other, is on the same stream, or ordered by the caller.
     A parameter whose memory, type or form has changed is refused: make another object.  The states' values may be read and written, their tensors
     not exchanged."""
 
